@@ -481,6 +481,105 @@ int dep_copy_chain(const depsync_copy_chain_desc* d, sync_policy_t* pol, depsync
 int depsync_copy_chain_plan(const depsync_copy_chain_desc* d, const sync_policy_t* pol, int n_cu,
                             depsync_plan_info* out);
 
+/* ---- the cache of token generation: attention of drafted tokens, append, weights, eviction --------------
+ *
+ * The loop of a serving program around the chains above, for caches whose sequences differ in length, whose key and value
+ * heads may be shared by several query heads, and whose new tokens may be a TREE of drafts of which only one path is kept:
+ *   1. dep_tree_attn       the drafted tokens attend to the cache and to one another;
+ *   2. dep_cache_append    the keys and values of the accepted ones go behind the cached rows;
+ *   3. dep_cache_weights   the attention weight every cached row received from them is added up;
+ *   4. dep_cache_evict     where the cache is over its budget, the rows of least weight make room.
+ * These are plain launches on one stream, in order; they use no policy object.  Conventions beside those at the top:
+ *  - head_dim 64 or 128 (other values: DEPSYNC_ENOTIMPL).  Tensors are [batch][token][head][head_dim] with a stride in
+ *    elements for each of the first three (multiples of 8, not negative; strides of dimensions of size 1 are not read); the innermost is contiguous,
+ *    bases are 16-byte aligned.  Query head h reads key and value head h / (heads / kv_heads).  A cache's token stride is at most 2^24.
+ *  - `cached` holds the valid rows of each sequence, in device memory; values outside 0..capacity are taken as the nearer end.
+ *    Rows at and behind it are never read.  Rows that a call does not name are left as they were.
+ *  - All memory is the current device's.  A workspace belongs to one call at a time: calls that may run at once, graphs that may be
+ *    replayed at once among them, need one each.  Nothing in it has to be set before a call or is kept for the next, and its address
+ *    is 16-byte aligned.  No call allocates or synchronises; all may be captured into a graph.
+ *  - Outputs overlap neither inputs nor one another, but where said.
+ */
+
+/* out = softmax(scale q k^T) v over, for drafted token t of a sequence, all cached rows and those drafted tokens j whose bit is set
+ * in row t of `tree`: bit j % 64 of word j / 64.  Masked keys count for nothing, whatever bits (infinities, NaN) they and their values
+ * hold.  A token that sees no key gets out = 0 and lse = -infinity.                                                                */
+typedef struct {
+    int32_t batch, tokens, heads, kv_heads, head_dim;   /* tokens: drafted ones per sequence, at least 1, at most 65536           */
+    int32_t dtype;                                      /* depsync_dtype                                                          */
+    int32_t capacity;                                   /* rows of each sequence's cache; 0: no cache (its pointers are not read)  */
+    int32_t max_cached;                                 /* what the work is divided by: the most rows that a sequence has now,
+                                                           as far as the host knows; 0 = capacity.  A wrong value costs time only  */
+    const void* q;     int64_t q_batch, q_token, q_head;
+    const void* k_new; const void* v_new; int64_t new_batch, new_token, new_head;     /* both alike                                */
+    const void* k_cache; const void* v_cache; int64_t cache_batch, cache_token, cache_head;
+    const int32_t* cached;                              /* [batch]                                                                */
+    const int32_t* drafted;                             /* [batch] drafted tokens that each sequence has, clamped to 0..tokens; the rows of
+                                                           out and lse behind them are left alone.  NULL: all                       */
+    const uint64_t* tree;  int64_t tree_batch;          /* [batch][tokens][ceil(tokens / 64)], tree_batch words from one sequence to the
+                                                           next (0: one tree for all).  NULL: token t sees 0..t                      */
+    float scale;                                        /* 0 = 1 / sqrt(head_dim)                                                  */
+    void* out;         int64_t out_batch, out_token, out_head;
+    float* lse;                                         /* [batch][tokens][heads], natural logarithm of the sum of exp(score); may be NULL */
+} depsync_tree_attn_desc;
+
+int dep_tree_attn(const depsync_tree_attn_desc* d, void* workspace, size_t workspace_bytes, void* stream);
+/* Bytes of workspace that dep_tree_attn needs (0: none; the pointer may then be NULL).  Only sizes are read; n_cu as for the planners. */
+int depsync_tree_attn_workspace(const depsync_tree_attn_desc* d, int n_cu, size_t* bytes);
+
+/* Cache row cached[b] + i of sequence b becomes the key and value of its drafted token accepted[b][i], for i < n_accepted[b]; the row's
+ * weight becomes 0 and its position start[b] + i, in every head, and cached_out[b] = cached[b] + n.  Rows that would lie behind the
+ * capacity are dropped, and do not count.                                                                                         */
+typedef struct {
+    int32_t batch, tokens, kv_heads, head_dim, dtype, capacity;
+    int32_t n_max;                                      /* entries of `accepted` per sequence (without it: 0..tokens, the first n are taken) */
+    const void* k_new; const void* v_new; int64_t new_batch, new_token, new_head;
+    void* k_cache; void* v_cache; int64_t cache_batch, cache_token, cache_head;
+    const int32_t* cached;  int32_t* cached_out;        /* [batch]; not the same array                                             */
+    const int32_t* accepted;                            /* [batch][n_max], clamped to 0..tokens-1; NULL: token i                    */
+    const int32_t* n_accepted;                          /* [batch], clamped to 0..n_max; NULL: n_max                                */
+    float* weights; int32_t* pos;                       /* [batch][kv_heads][capacity]; either may be NULL                          */
+    const int32_t* start;                               /* [batch]; with pos only                                                   */
+} depsync_cache_append_desc;
+int dep_cache_append(const depsync_cache_append_desc* d, void* stream);
+
+/* weights[b][h][k] += sum of exp(scale q.k - lse) over the query heads of head h and the accepted tokens i < n that see row k.  `cached`
+ * counts the accepted tokens' own rows, the last n: token i sees rows 0..cached - n + i (its path and all before).  q and lse are
+ * dep_tree_attn's.  The sum is taken in 32 bits in an order that depends on sizes alone.                                            */
+typedef struct {
+    int32_t batch, tokens, heads, kv_heads, head_dim, dtype, capacity;
+    int32_t max_cached;                                 /* 0 = capacity.  Rows behind it get no weight                              */
+    int32_t n_max;                                      /* as for dep_cache_append                                                 */
+    const void* q;     int64_t q_batch, q_token, q_head;
+    const float* lse;                                   /* [batch][tokens][heads]                                                  */
+    const void* k_cache; int64_t cache_batch, cache_token, cache_head;
+    const int32_t* cached;
+    const int32_t* accepted; const int32_t* n_accepted; /* as for dep_cache_append                                                 */
+    float scale;                                        /* 0 = 1 / sqrt(head_dim)                                                  */
+    float* weights;                                     /* [batch][kv_heads][capacity]                                             */
+} depsync_cache_weights_desc;
+int dep_cache_weights(const depsync_cache_weights_desc* d, void* stream);
+
+/* Keeps, of every sequence and head with more than `budget` rows, `budget` of them: first those whose position is one of the `recent`
+ * newest (greater than the head's largest - recent), then by weight; among equals the lowest row.  A weight that is NaN counts as the least.
+ * In place (k_out NULL): kept rows behind the budget move, in ascending order, to the rows before it that are not kept; all others stay, so
+ * a step that appended few moves few.  The order of rows means nothing to attention, and `pos` moves with them.
+ * Into other buffers (all four given): the kept rows in their order, also where a sequence is not over the budget.
+ * cached_out[b] = min(cached[b], budget).                                                                                         */
+typedef struct {
+    int32_t batch, kv_heads, head_dim, dtype, capacity;
+    int32_t max_cached;                                 /* as for dep_tree_attn                                                    */
+    int32_t budget, recent;                             /* 1 <= budget, 0 <= recent <= budget                                       */
+    void* k_cache; void* v_cache; int64_t cache_batch, cache_token, cache_head;
+    float* weights; int32_t* pos;                       /* [batch][kv_heads][capacity]                                             */
+    const int32_t* cached;  int32_t* cached_out;        /* [batch]; not the same array                                             */
+    int32_t capacity_out;                               /* rows of the other buffers, at least budget                              */
+    void* k_out; void* v_out; int64_t out_batch, out_token, out_head;
+    float* weights_out; int32_t* pos_out;               /* [batch][kv_heads][capacity_out]                                         */
+} depsync_cache_evict_desc;
+int dep_cache_evict(const depsync_cache_evict_desc* d, void* workspace, size_t workspace_bytes, void* stream);
+int depsync_cache_evict_workspace(const depsync_cache_evict_desc* d, size_t* bytes);
+
 /* ---- host mirrors of the device index arithmetic (Fig. 4b; Section II-A) -------------- */
 
 /* Linear position of tile (x,y) in row-major order: y*grid_x + x.                         */

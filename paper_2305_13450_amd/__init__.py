@@ -38,6 +38,8 @@ EXPORTS = [
     "depsync_gemm_chain_check_waits", "depsync_conv_chain_n_check_waits", "dep_gemm_chain_static",
     "depsync_gemm_chain_autotune_policy", "depsync_conv_chain_n_autotune_policy", "depsync_gemm_chain_policy",
     "depsync_conv_chain_n_policy", "depsync_gemm_chain_launch_form", "depsync_conv_chain_n_launch_form",
+    "dep_tree_attn", "depsync_tree_attn_workspace", "dep_cache_append", "dep_cache_weights", "dep_cache_evict",
+    "depsync_cache_evict_workspace",
 ]
 
 
@@ -117,6 +119,42 @@ class CopyChainDesc(ctypes.Structure):
                 ("bytes", ctypes.c_uint64), ("tile_bytes", ctypes.c_uint32)]
 
 
+def _fields(**groups):
+    """ctypes fields in the header's order: name -> "i" (int32), "l" (int64), "p" (pointer), "f" (float)."""
+    kinds = {"i": ctypes.c_int32, "l": ctypes.c_int64, "p": ctypes.c_void_p, "f": ctypes.c_float}
+    return [(n, kinds[k]) for n, k in groups.items()]
+
+
+class TreeAttnDesc(ctypes.Structure):
+    _fields_ = _fields(batch="i", tokens="i", heads="i", kv_heads="i", head_dim="i", dtype="i", capacity="i", max_cached="i",
+                       q="p", q_batch="l", q_token="l", q_head="l",
+                       k_new="p", v_new="p", new_batch="l", new_token="l", new_head="l",
+                       k_cache="p", v_cache="p", cache_batch="l", cache_token="l", cache_head="l",
+                       cached="p", drafted="p", tree="p", tree_batch="l", scale="f",
+                       out="p", out_batch="l", out_token="l", out_head="l", lse="p")
+
+
+class CacheAppendDesc(ctypes.Structure):
+    _fields_ = _fields(batch="i", tokens="i", kv_heads="i", head_dim="i", dtype="i", capacity="i", n_max="i",
+                       k_new="p", v_new="p", new_batch="l", new_token="l", new_head="l",
+                       k_cache="p", v_cache="p", cache_batch="l", cache_token="l", cache_head="l",
+                       cached="p", cached_out="p", accepted="p", n_accepted="p", weights="p", pos="p", start="p")
+
+
+class CacheWeightsDesc(ctypes.Structure):
+    _fields_ = _fields(batch="i", tokens="i", heads="i", kv_heads="i", head_dim="i", dtype="i", capacity="i", max_cached="i", n_max="i",
+                       q="p", q_batch="l", q_token="l", q_head="l", lse="p",
+                       k_cache="p", cache_batch="l", cache_token="l", cache_head="l",
+                       cached="p", accepted="p", n_accepted="p", scale="f", weights="p")
+
+
+class CacheEvictDesc(ctypes.Structure):
+    _fields_ = _fields(batch="i", kv_heads="i", head_dim="i", dtype="i", capacity="i", max_cached="i", budget="i", recent="i",
+                       k_cache="p", v_cache="p", cache_batch="l", cache_token="l", cache_head="l",
+                       weights="p", pos="p", cached="p", cached_out="p", capacity_out="i",
+                       k_out="p", v_out="p", out_batch="l", out_token="l", out_head="l", weights_out="p", pos_out="p")
+
+
 _LIB = None
 
 
@@ -162,6 +200,13 @@ def _lib() -> ctypes.CDLL:
         L.depsync_gemm_chain_policy.argtypes = [ctypes.POINTER(GemmChainDesc), vp, ctypes.POINTER(i32)]
         L.depsync_conv_chain_n_policy.argtypes = [ctypes.POINTER(ConvChainNDesc), vp, ctypes.POINTER(i32)]
         L.dep_gemm_chain_static.argtypes = [ctypes.POINTER(GemmChainDesc), i32, ctypes.POINTER(PolicyParams), vp]
+        szp = ctypes.POINTER(ctypes.c_size_t)
+        L.dep_tree_attn.argtypes = [ctypes.POINTER(TreeAttnDesc), vp, ctypes.c_size_t, vp]
+        L.depsync_tree_attn_workspace.argtypes = [ctypes.POINTER(TreeAttnDesc), i32, szp]
+        L.dep_cache_append.argtypes = [ctypes.POINTER(CacheAppendDesc), vp]
+        L.dep_cache_weights.argtypes = [ctypes.POINTER(CacheWeightsDesc), vp]
+        L.dep_cache_evict.argtypes = [ctypes.POINTER(CacheEvictDesc), vp, ctypes.c_size_t, vp]
+        L.depsync_cache_evict_workspace.argtypes = [ctypes.POINTER(CacheEvictDesc), szp]
         L.depsync_row_major.argtypes = [i32] * 4
         L.depsync_policy_sem.argtypes = [i32] * 6
         L.depsync_policy_value.argtypes = [i32] * 4
@@ -564,6 +609,259 @@ def conv_chain_n_check_waits(desc: ConvChainNDesc, kind: int, n_cu: int = 0, **p
     _check(_lib().depsync_conv_chain_n_check_waits(ctypes.byref(desc), kind, ctypes.byref(pp), n_cu, ctypes.byref(n)),
            "depsync_conv_chain_n_check_waits")
     return n.value
+
+
+# ---- the cache of token generation ----------------------------------------------------------
+
+def _dev4(t, name: str, shape, dtype):
+    """A [batch, token, head, head_dim] device tensor of this shape (None: any size) with contiguous rows -> its pointer."""
+    if not t.is_cuda or t.dim() != 4 or t.stride(3) != 1:
+        raise ValueError(f"{name} must be a 4-D device tensor with contiguous rows")
+    if t.dtype != dtype:
+        raise TypeError("all 16-bit tensors of a call must share one element type")
+    if any(want is not None and n != want for n, want in zip(t.shape, shape)):
+        raise ValueError(f"{name}: shape {tuple(t.shape)} where {tuple('any' if w is None else w for w in shape)} is needed")
+    return t.data_ptr()
+
+
+def _dev_array(t, name: str, shape, dtype):
+    """A contiguous device tensor of this shape and type -> its pointer; None -> NULL."""
+    if t is None:
+        return None
+    if not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name} must be a contiguous device tensor of {dtype} and shape {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _enqueue(call, tensors):
+    """call() with the tensors' device current; they have to be on one."""
+    import torch
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) != 1:
+        raise ValueError("all tensors of a call must be on one device")
+    index = devices.pop().index
+    if index == torch.cuda.current_device():
+        return call()
+    with torch.cuda.device(index):
+        return call()
+
+
+def _workspace(nbytes: int, given, like, stream):
+    """`given`, if it is large enough, or memory that torch's allocator ties to `stream`: (tensor to keep, pointer, bytes)."""
+    import torch
+    if given is not None:
+        if not given.is_cuda or not given.is_contiguous() or given.device != like.device:
+            raise ValueError("the workspace must be a contiguous tensor on the device of the others")
+        return given, given.data_ptr(), given.numel() * given.element_size()
+    if nbytes == 0:
+        return None, None, 0
+    handle = _stream_handle(stream) or 0
+    if handle == torch.cuda.current_stream(like.device).cuda_stream:
+        t = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    else:
+        own = torch.cuda.default_stream(like.device) if handle == 0 else torch.cuda.ExternalStream(handle, device=like.device)
+        with torch.cuda.stream(own):
+            t = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    return t, t.data_ptr(), nbytes
+
+
+def tree_mask(parents):
+    """The `tree` words of dep_tree_attn for drafted tokens with these parents: an integer tensor [T] or [B, T] in host memory, -1 (or any
+    negative value) for a root, every parent before its children.  Each token sees itself and its ancestors.  -> int64 [.., T, ceil(T / 64)]"""
+    import torch
+    p = torch.as_tensor(parents)
+    if p.is_cuda or p.dim() not in (1, 2) or p.shape[-1] < 1:
+        raise ValueError("parents must be a host tensor [tokens] or [batch, tokens]")
+    flat = p.reshape(-1, p.shape[-1]).tolist()
+    n = p.shape[-1]
+    rows = []
+    for seq in flat:
+        seen = []
+        for t, parent in enumerate(seq):
+            if parent >= t:
+                raise ValueError(f"token {t}: its parent {parent} must come before it")
+            seen.append((seen[parent] if parent >= 0 else 0) | 1 << t)
+        for bits in seen:
+            words = [bits >> 64 * w & (1 << 64) - 1 for w in range((n + 63) // 64)]
+            rows.append([w - (1 << 64) if w >> 63 else w for w in words])
+    return torch.tensor(rows, dtype=torch.int64).reshape(*p.shape, -1)
+
+
+def _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached) -> TreeAttnDesc:
+    import torch
+    if q.dim() != 4 or k_new.dim() != 4:
+        raise ValueError("q and k_new must be [batch, tokens, heads, head_dim]")
+    B, T, Hq, D = q.shape
+    Hk = k_new.shape[2]
+    d = TreeAttnDesc()
+    d.dtype = _dtype_code(q)
+    d.batch, d.tokens, d.heads, d.kv_heads, d.head_dim = B, T, Hq, Hk, D
+    d.q = _dev4(q, "q", q.shape, q.dtype)
+    d.q_batch, d.q_token, d.q_head = q.stride()[:3]
+    d.k_new, d.v_new = _dev4(k_new, "k_new", (B, T, Hk, D), q.dtype), _dev4(v_new, "v_new", (B, T, Hk, D), q.dtype)
+    if k_new.stride() != v_new.stride():
+        raise ValueError("k_new and v_new must have the same strides")
+    d.new_batch, d.new_token, d.new_head = k_new.stride()[:3]
+    if k_cache is not None:
+        if v_cache is None or cached is None:
+            raise ValueError("a cache is k_cache, v_cache and cached")
+        _cache_fields(d, k_cache, v_cache, B, Hk, D, q.dtype)
+        d.cached = _dev_array(cached, "cached", (B,), torch.int32)
+    d.max_cached = max_cached or 0
+    d.drafted = _dev_array(drafted, "drafted", (B,), torch.int32)
+    if tree is not None:
+        words = (T, (T + 63) // 64)
+        d.tree = _dev_array(tree, "tree", words if tree.dim() == 2 else (B, *words), torch.int64)
+        d.tree_batch = 0 if tree.dim() == 2 else words[0] * words[1]
+    d.scale = scale or 0.0
+    d.out = _dev4(out, "out", (B, T, Hq, D), q.dtype)
+    d.out_batch, d.out_token, d.out_head = out.stride()[:3]
+    d.lse = _dev_array(lse, "lse", (B, T, Hq), torch.float32)
+    return d
+
+
+def _cache_fields(d, k_cache, v_cache, B, Hk, D, dtype) -> None:
+    d.k_cache = _dev4(k_cache, "k_cache", (B, None, Hk, D), dtype)
+    d.capacity = k_cache.shape[1]
+    d.cache_batch, d.cache_token, d.cache_head = k_cache.stride()[:3]
+    if v_cache is not None:
+        d.v_cache = _dev4(v_cache, "v_cache", k_cache.shape, dtype)
+        if k_cache.stride() != v_cache.stride():
+            raise ValueError("k_cache and v_cache must have the same strides")
+
+
+def dep_tree_attn(q, k_new, v_new, k_cache, v_cache, cached, out, lse=None, tree=None, drafted=None, scale: Optional[float] = None,
+                  max_cached: Optional[int] = None, workspace=None, stream=None) -> None:
+    """Enqueue out = softmax(scale q k^T) v of drafted tokens over a cache and, as `tree` (see tree_mask) says, one another.
+
+    q, out [B, T, Hq, D]; k_new, v_new [B, T, Hk, D]; k_cache, v_cache [B, capacity, Hk, D] (None: no cache) of which sequence b has
+    cached[b] rows (int32).  drafted[b] (int32): the tokens that sequence b has; the others' rows of out and lse are left alone.
+    lse [B, T, Hq] (float32) receives the logarithm of each row's sum.  max_cached: the most rows that a sequence has, where the host knows."""
+    d = _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached)
+
+    def call():
+        need = ctypes.c_size_t(0)
+        _check(_lib().depsync_tree_attn_workspace(ctypes.byref(d), 0, ctypes.byref(need)), "dep_tree_attn")
+        keep, ptr, size = _workspace(need.value, workspace, q, stream)
+        _check(_lib().dep_tree_attn(ctypes.byref(d), ptr, size, _stream_handle(stream)), "dep_tree_attn")
+    _enqueue(call, (q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted))
+
+
+def tree_attn_workspace(q, k_new, v_new, k_cache, v_cache, cached, out, lse=None, tree=None, drafted=None, scale: Optional[float] = None,
+                        max_cached: Optional[int] = None, n_cu: int = 0) -> int:
+    """Bytes of workspace that dep_tree_attn with these arguments needs."""
+    d = _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached)
+    need = ctypes.c_size_t(0)
+    _check(_lib().depsync_tree_attn_workspace(ctypes.byref(d), n_cu, ctypes.byref(need)), "depsync_tree_attn_workspace")
+    return need.value
+
+
+def _accepted_fields(d, tokens, accepted, n_accepted) -> None:
+    import torch
+    if accepted is not None and accepted.dim() != 2:
+        raise ValueError("accepted must be [batch, n_max]")
+    d.n_max = tokens if accepted is None else accepted.shape[1]
+    d.accepted = _dev_array(accepted, "accepted", (d.batch, d.n_max), torch.int32)
+    d.n_accepted = _dev_array(n_accepted, "n_accepted", (d.batch,), torch.int32)
+
+
+def dep_cache_append(k_new, v_new, k_cache, v_cache, cached, cached_out, accepted=None, n_accepted=None, weights=None, pos=None, start=None,
+                     stream=None) -> None:
+    """Enqueue: the keys and values of drafted tokens accepted[b, :n_accepted[b]] (int32; None: the first ones) go to rows cached[b].. of the cache,
+    their weights [B, Hk, capacity] (float32) become 0, their positions (int32, same shape) start[b].., and cached_out = cached + n."""
+    import torch
+    if k_new.dim() != 4:
+        raise ValueError("k_new must be [batch, tokens, kv_heads, head_dim]")
+    d = CacheAppendDesc()
+    d.dtype = _dtype_code(k_new)
+    d.batch, d.tokens, d.kv_heads, d.head_dim = k_new.shape
+    d.k_new, d.v_new = _dev4(k_new, "k_new", k_new.shape, k_new.dtype), _dev4(v_new, "v_new", k_new.shape, k_new.dtype)
+    if k_new.stride() != v_new.stride():
+        raise ValueError("k_new and v_new must have the same strides")
+    d.new_batch, d.new_token, d.new_head = k_new.stride()[:3]
+    _cache_fields(d, k_cache, v_cache, d.batch, d.kv_heads, d.head_dim, k_new.dtype)
+    d.cached, d.cached_out = _dev_array(cached, "cached", (d.batch,), torch.int32), _dev_array(cached_out, "cached_out", (d.batch,), torch.int32)
+    _accepted_fields(d, d.tokens, accepted, n_accepted)
+    rows = (d.batch, d.kv_heads, d.capacity)
+    d.weights, d.pos = _dev_array(weights, "weights", rows, torch.float32), _dev_array(pos, "pos", rows, torch.int32)
+    d.start = _dev_array(start, "start", (d.batch,), torch.int32)
+    _enqueue(lambda: _check(_lib().dep_cache_append(ctypes.byref(d), _stream_handle(stream)), "dep_cache_append"),
+             (k_new, v_new, k_cache, v_cache, cached, cached_out, accepted, n_accepted, weights, pos, start))
+
+
+def dep_cache_weights(q, lse, k_cache, cached, weights, accepted=None, n_accepted=None, scale: Optional[float] = None,
+                      max_cached: Optional[int] = None, stream=None) -> None:
+    """Enqueue weights[b, h, k] += the attention weight that cached row k received from the accepted tokens, whose own rows are the last
+    of cached[b].  q [B, T, Hq, D] and lse [B, T, Hq] are dep_tree_attn's; weights is [B, Hk, capacity] (float32)."""
+    import torch
+    if q.dim() != 4 or k_cache.dim() != 4:
+        raise ValueError("q and k_cache must be [batch, tokens, heads, head_dim]")
+    d = CacheWeightsDesc()
+    d.dtype = _dtype_code(q)
+    d.batch, d.tokens, d.heads, d.head_dim = q.shape
+    d.kv_heads = k_cache.shape[2]
+    d.q = _dev4(q, "q", q.shape, q.dtype)
+    d.q_batch, d.q_token, d.q_head = q.stride()[:3]
+    d.lse = _dev_array(lse, "lse", q.shape[:3], torch.float32)
+    d.k_cache = _dev4(k_cache, "k_cache", (d.batch, None, d.kv_heads, d.head_dim), q.dtype)
+    d.capacity = k_cache.shape[1]
+    d.cache_batch, d.cache_token, d.cache_head = k_cache.stride()[:3]
+    d.cached = _dev_array(cached, "cached", (d.batch,), torch.int32)
+    _accepted_fields(d, d.tokens, accepted, n_accepted)
+    d.scale, d.max_cached = scale or 0.0, max_cached or 0
+    d.weights = _dev_array(weights, "weights", (d.batch, d.kv_heads, d.capacity), torch.float32)
+    _enqueue(lambda: _check(_lib().dep_cache_weights(ctypes.byref(d), _stream_handle(stream)), "dep_cache_weights"),
+             (q, lse, k_cache, cached, weights, accepted, n_accepted))
+
+
+def _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out) -> CacheEvictDesc:
+    import torch
+    if k_cache.dim() != 4:
+        raise ValueError("k_cache must be [batch, capacity, kv_heads, head_dim]")
+    d = CacheEvictDesc()
+    d.dtype = _dtype_code(k_cache)
+    d.batch, _, d.kv_heads, d.head_dim = k_cache.shape
+    _cache_fields(d, k_cache, v_cache, d.batch, d.kv_heads, d.head_dim, k_cache.dtype)
+    rows = (d.batch, d.kv_heads, d.capacity)
+    d.weights, d.pos = _dev_array(weights, "weights", rows, torch.float32), _dev_array(pos, "pos", rows, torch.int32)
+    d.cached, d.cached_out = _dev_array(cached, "cached", (d.batch,), torch.int32), _dev_array(cached_out, "cached_out", (d.batch,), torch.int32)
+    d.budget, d.recent, d.max_cached = budget, recent, max_cached or 0
+    if k_out is not None:
+        d.k_out = _dev4(k_out, "k_out", (d.batch, None, d.kv_heads, d.head_dim), k_cache.dtype)
+        d.v_out = None if v_out is None else _dev4(v_out, "v_out", k_out.shape, k_cache.dtype)
+        if v_out is not None and k_out.stride() != v_out.stride():
+            raise ValueError("k_out and v_out must have the same strides")
+        d.capacity_out = k_out.shape[1]
+        d.out_batch, d.out_token, d.out_head = k_out.stride()[:3]
+    elif v_out is not None:
+        raise ValueError("the other buffers are k_out, v_out, weights_out and pos_out together")
+    rows = (d.batch, d.kv_heads, d.capacity_out)
+    d.weights_out, d.pos_out = _dev_array(weights_out, "weights_out", rows, torch.float32), _dev_array(pos_out, "pos_out", rows, torch.int32)
+    return d
+
+
+def dep_cache_evict(k_cache, v_cache, weights, pos, cached, cached_out, budget: int, recent: int = 0, max_cached: Optional[int] = None,
+                    k_out=None, v_out=None, weights_out=None, pos_out=None, workspace=None, stream=None) -> None:
+    """Enqueue: every sequence and head keeps `budget` rows: the `recent` newest by position, then the heaviest, among equals the lowest row.
+    In place kept rows behind the budget fill the places of those that go; into k_out .. pos_out (all four) the kept rows go in their order.
+    cached_out = min(cached, budget)."""
+    d = _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out)
+
+    def call():
+        need = ctypes.c_size_t(0)
+        _check(_lib().depsync_cache_evict_workspace(ctypes.byref(d), ctypes.byref(need)), "dep_cache_evict")
+        keep, ptr, size = _workspace(need.value, workspace, k_cache, stream)
+        _check(_lib().dep_cache_evict(ctypes.byref(d), ptr, size, _stream_handle(stream)), "dep_cache_evict")
+    _enqueue(call, (k_cache, v_cache, weights, pos, cached, cached_out, k_out, v_out, weights_out, pos_out))
+
+
+def cache_evict_workspace(k_cache, v_cache, weights, pos, cached, cached_out, budget: int, recent: int = 0, max_cached: Optional[int] = None,
+                          k_out=None, v_out=None, weights_out=None, pos_out=None) -> int:
+    """Bytes of workspace that dep_cache_evict with these arguments needs."""
+    d = _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out)
+    need = ctypes.c_size_t(0)
+    _check(_lib().depsync_cache_evict_workspace(ctypes.byref(d), ctypes.byref(need)), "depsync_cache_evict_workspace")
+    return need.value
 
 
 # ---- host mirrors -------------------------------------------------------------------------

@@ -23,6 +23,10 @@ SOURCES = [
     "kern_f16_gen.hip",
     "kern_bf16_attn.hip",
     "kern_f16_attn.hip",
+    "cache_api.hip",
+    "kern_cache.hip",
+    "kern_bf16_tree.hip",
+    "kern_f16_tree.hip",
 ]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -21,8 +21,15 @@
 using namespace depsync;
 
 namespace {
-
 thread_local int g_last_hip_error = 0;
+}  // namespace
+
+int depsync::hip_fail(hipError_t e) {
+    g_last_hip_error = (int)e;
+    return DEPSYNC_EHIP;
+}
+
+namespace {
 
 // Workspace layout in 32-bit words.
 constexpr uint32_t WS_TICKET = 0;        // 4 stages x 8 dispatch counters, one per 128-byte line
@@ -61,10 +68,6 @@ constexpr size_t STATIC_PARTIAL_FLOATS = 32u << 20;
 static_assert(STATIC_LAYOUT.words % 64 == 0, "the partial tiles start on a 256-byte boundary");
 constexpr size_t STATIC_WORDS = (size_t)STATIC_LAYOUT.words + STATIC_PARTIAL_FLOATS;
 
-int hip_fail(hipError_t e) {
-    g_last_hip_error = (int)e;
-    return DEPSYNC_EHIP;
-}
 #define HIP_TRY(expr)                                  \
     do {                                               \
         hipError_t e__ = (expr);                       \

@@ -1,0 +1,208 @@
+// C-ABI layer of the cache operators (declarations in include/depsync.h): checks of arguments, division of the work.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/depsync.h"
+#include "cache_ops.h"
+#include "launch.h"
+
+using namespace depsync;
+
+namespace {
+
+constexpr int64_t MAX_TOKEN_STRIDE = 1 << 24;     // 64 rows of a cache, as far as a workgroup reaches from one base, stay below 2 GiB
+constexpr int64_t MAX_BLOCKS = 1 << 23;           // workgroups of a launch (HIP counts threads in 32 bits)
+
+bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+bool operand(const void* p) { return p && aligned(p, 16); }
+bool array(const void* p) { return p && aligned(p, 4); }
+bool optional(const void* p) { return aligned(p, 4); }
+int64_t cdiv64(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Strides of [batch][token][head][head_dim].  Those of dimensions of size one are not read: kernels get what a dense row has.
+// Where rows are written, or read by the bounds of a run of rows, they must not overlap.
+bool strides(Strides& s, int64_t batch, int64_t token, int64_t head, int64_t n_batch, int64_t n_token, int64_t n_head, int dim, bool written, bool run) {
+    s = {n_batch > 1 ? batch : dim, n_token > 1 ? token : dim, n_head > 1 ? head : dim};
+    for (int64_t x : {s.batch, s.token, s.head})
+        if (x < 0 || x % 8 != 0 || x > (int64_t)1 << 40 || (written && x < dim)) return false;
+    return !run || (s.token >= dim && s.token <= MAX_TOKEN_STRIDE);
+}
+
+// What the descriptors share.  head_dim and element types this build does not have: DEPSYNC_ENOTIMPL.
+int common(int batch, int tokens, int heads, int kv_heads, int head_dim, int dtype, int capacity) {
+    if (batch < 1 || batch > 1 << 20 || tokens < 1 || tokens > 65536 || kv_heads < 1 || heads < kv_heads || heads > 65536 || heads % kv_heads != 0 ||
+        capacity < 0 || capacity > 1 << 30 || head_dim < 1 || (dtype != DEPSYNC_BF16 && dtype != DEPSYNC_FP16))
+        return DEPSYNC_EINVAL;
+    return head_dim == 64 || head_dim == 128 ? DEPSYNC_OK : DEPSYNC_ENOTIMPL;
+}
+
+bool base2_scale(float given, int head_dim, float& out) {
+    if (!std::isfinite(given) || given < 0.0f) return false;
+    out = (given == 0.0f ? 1.0f / std::sqrt((float)head_dim) : given) * 1.4426950408889634f;
+    return true;
+}
+
+int rows_hint(int max_cached, int capacity) { return max_cached == 0 ? capacity : std::min(max_cached, capacity); }
+
+int tree_check(const depsync_tree_attn_desc* d) {
+    if (!d) return DEPSYNC_EINVAL;
+    if (int rc = common(d->batch, d->tokens, d->heads, d->kv_heads, d->head_dim, d->dtype, d->capacity); rc != DEPSYNC_OK) return rc;
+    return d->max_cached < 0 ? DEPSYNC_EINVAL : DEPSYNC_OK;
+}
+
+// How the key axis of dep_tree_attn is cut.  A workgroup's start, its rows' queries and its results cost about as much as reading
+// a block or two, so a part has two blocks at the least; beyond that, as many parts as give every CU four workgroups (two at a time).
+int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t& bytes) {
+    if (n_cu <= 0) {
+        int dev = 0;
+        if (hipError_t e = hipGetDevice(&dev); e != hipSuccess) return hip_fail(e);
+        if (hipError_t e = hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, dev); e != hipSuccess) return hip_fail(e);
+    }
+    a.batch = d->batch; a.tokens = d->tokens; a.heads = d->heads; a.kv_heads = d->kv_heads; a.capacity = d->capacity;
+    a.group = d->heads / d->kv_heads;
+    const int64_t rows = (int64_t)d->tokens * a.group;
+    if (rows > 1 << 24) return DEPSYNC_ENOTIMPL;
+    a.rows = (uint32_t)rows;
+    const int64_t keys = tree_block_keys(a.rows), row_blocks = a.rows <= TREE_FEW_ROWS ? 1 : cdiv64(rows, TREE_ROW_BLOCK);
+    const int64_t pairs = (int64_t)d->batch * d->kv_heads, base = pairs * row_blocks;
+    const int64_t blocks = cdiv64(rows_hint(d->max_cached, d->capacity), keys) + cdiv64(d->tokens, keys);
+    const int64_t part = std::min(blocks, std::max<int64_t>(2, cdiv64(blocks * base, 4 * (int64_t)n_cu)));
+    a.part_blocks = (uint32_t)part;
+    a.n_parts = (uint32_t)cdiv64(blocks, part);
+    if (cdiv64(pairs * a.n_parts, 8) * 8 * row_blocks > MAX_BLOCKS || cdiv64(pairs * rows, 4) > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;
+    bytes = a.n_parts > 1 ? (size_t)pairs * a.n_parts * rows * (d->head_dim + 2) * sizeof(float) : 0;
+    return DEPSYNC_OK;
+}
+
+int64_t evict_moves(const depsync_cache_evict_desc* d) {
+    return d->k_out ? d->budget : std::max(0, std::min(d->budget, d->capacity - d->budget));
+}
+
+int evict_check(const depsync_cache_evict_desc* d) {
+    if (!d) return DEPSYNC_EINVAL;
+    if (int rc = common(d->batch, 1, d->kv_heads, d->kv_heads, d->head_dim, d->dtype, d->capacity); rc != DEPSYNC_OK) return rc;
+    if (d->capacity < 1 || d->max_cached < 0 || d->budget < 1 || d->recent < 0 || d->recent > d->budget) return DEPSYNC_EINVAL;
+    return (int64_t)d->batch * d->kv_heads > MAX_BLOCKS / 512 ? DEPSYNC_ENOTIMPL : DEPSYNC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int depsync_tree_attn_workspace(const depsync_tree_attn_desc* d, int n_cu, size_t* bytes) {
+    if (!bytes) return DEPSYNC_EINVAL;
+    if (int rc = tree_check(d); rc != DEPSYNC_OK) return rc;
+    TreeAttnArgs a = {};
+    return tree_plan(d, n_cu, a, *bytes);
+}
+
+int dep_tree_attn(const depsync_tree_attn_desc* d, void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = tree_check(d); rc != DEPSYNC_OK) return rc;
+    TreeAttnArgs a = {};
+    size_t need = 0;
+    const int D = d->head_dim;
+    if (!operand(d->q) || !operand(d->k_new) || !operand(d->v_new) || !operand(d->out) || !optional(d->drafted) || !optional(d->lse) ||
+        (d->capacity > 0 && (!operand(d->k_cache) || !operand(d->v_cache) || !array(d->cached))) || !aligned(d->tree, 8))
+        return DEPSYNC_EINVAL;
+    if (!strides(a.q_s, d->q_batch, d->q_token, d->q_head, d->batch, d->tokens, d->heads, D, false, false) ||
+        !strides(a.new_s, d->new_batch, d->new_token, d->new_head, d->batch, d->tokens, d->kv_heads, D, false, true) ||
+        !strides(a.out_s, d->out_batch, d->out_token, d->out_head, d->batch, d->tokens, d->heads, D, true, false))
+        return DEPSYNC_EINVAL;
+    if (d->capacity > 0 && !strides(a.cache_s, d->cache_batch, d->cache_token, d->cache_head, d->batch, d->capacity, d->kv_heads, D, false, true))
+        return DEPSYNC_EINVAL;
+    if (d->tree && d->tree_batch != 0 && d->tree_batch < (int64_t)d->tokens * cdiv64(d->tokens, 64)) return DEPSYNC_EINVAL;
+    if (!base2_scale(d->scale, D, a.scale)) return DEPSYNC_EINVAL;
+    if (int rc = tree_plan(d, 0, a, need); rc != DEPSYNC_OK) return rc;
+    if (need > 0 && (!operand(workspace) || workspace_bytes < need)) return DEPSYNC_EINVAL;
+    a.q = d->q; a.k_new = d->k_new; a.v_new = d->v_new; a.k_cache = d->k_cache; a.v_cache = d->v_cache;
+    a.cached = d->cached; a.drafted = d->drafted; a.tree = d->tree; a.tree_batch = d->tree_batch;
+    a.out = d->out; a.lse = d->lse; a.parts = static_cast<float*>(workspace);
+    const hipError_t e = launch_tree_attn(a, d->dtype, D, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);
+}
+
+int dep_cache_append(const depsync_cache_append_desc* d, void* stream) {
+    if (!d) return DEPSYNC_EINVAL;
+    if (int rc = common(d->batch, d->tokens, d->kv_heads, d->kv_heads, d->head_dim, d->dtype, d->capacity); rc != DEPSYNC_OK) return rc;
+    CacheAppendArgs a = {};
+    const int D = d->head_dim;
+    if (d->capacity < 1 || d->n_max < 1 || d->n_max > 65536 || (!d->accepted && d->n_max > d->tokens)) return DEPSYNC_EINVAL;
+    if (!operand(d->k_new) || !operand(d->v_new) || !operand(d->k_cache) || !operand(d->v_cache) || !array(d->cached) || !array(d->cached_out) ||
+        d->cached == d->cached_out || !optional(d->accepted) || !optional(d->n_accepted) || !optional(d->weights) || !optional(d->pos) ||
+        (d->pos && !array(d->start)))
+        return DEPSYNC_EINVAL;
+    if (!strides(a.new_s, d->new_batch, d->new_token, d->new_head, d->batch, d->tokens, d->kv_heads, D, false, false) ||
+        !strides(a.cache_s, d->cache_batch, d->cache_token, d->cache_head, d->batch, d->capacity, d->kv_heads, D, true, true))
+        return DEPSYNC_EINVAL;
+    const int64_t rows = 256 / (D / 8);
+    if (d->batch * cdiv64((int64_t)d->n_max * d->kv_heads, rows) > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;
+    a.k_new = d->k_new; a.v_new = d->v_new; a.k_cache = d->k_cache; a.v_cache = d->v_cache;
+    a.cached = d->cached; a.cached_out = d->cached_out; a.accepted = d->accepted; a.n_accepted = d->n_accepted;
+    a.weights = d->weights; a.pos = d->pos; a.start = d->start;
+    a.batch = d->batch; a.tokens = d->tokens; a.kv_heads = d->kv_heads; a.capacity = d->capacity; a.n_max = d->n_max;
+    const hipError_t e = launch_cache_append(a, D, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);
+}
+
+int dep_cache_weights(const depsync_cache_weights_desc* d, void* stream) {
+    if (!d) return DEPSYNC_EINVAL;
+    if (int rc = common(d->batch, d->tokens, d->heads, d->kv_heads, d->head_dim, d->dtype, d->capacity); rc != DEPSYNC_OK) return rc;
+    CacheWeightsArgs a = {};
+    const int D = d->head_dim;
+    if (d->capacity < 1 || d->max_cached < 0 || d->n_max < 1 || d->n_max > 65536 || (!d->accepted && d->n_max > d->tokens)) return DEPSYNC_EINVAL;
+    if (!operand(d->q) || !array(d->lse) || !operand(d->k_cache) || !array(d->cached) || !optional(d->accepted) || !optional(d->n_accepted) || !array(d->weights))
+        return DEPSYNC_EINVAL;
+    if (!strides(a.q_s, d->q_batch, d->q_token, d->q_head, d->batch, d->tokens, d->heads, D, false, false) ||
+        !strides(a.cache_s, d->cache_batch, d->cache_token, d->cache_head, d->batch, d->capacity, d->kv_heads, D, false, true))
+        return DEPSYNC_EINVAL;
+    if (!base2_scale(d->scale, D, a.scale)) return DEPSYNC_EINVAL;
+    a.q = d->q; a.lse = d->lse; a.k_cache = d->k_cache; a.cached = d->cached; a.accepted = d->accepted; a.n_accepted = d->n_accepted; a.weights = d->weights;
+    a.batch = d->batch; a.tokens = d->tokens; a.heads = d->heads; a.kv_heads = d->kv_heads; a.group = d->heads / d->kv_heads; a.capacity = d->capacity; a.n_max = d->n_max;
+    a.max_cached = rows_hint(d->max_cached, d->capacity);
+    if ((int64_t)d->n_max * a.group > 1 << 24 || (int64_t)d->batch * d->kv_heads * cdiv64(a.max_cached, 64) > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;
+    const hipError_t e = launch_cache_weights(a, d->dtype, D, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);
+}
+
+int depsync_cache_evict_workspace(const depsync_cache_evict_desc* d, size_t* bytes) {
+    if (!bytes) return DEPSYNC_EINVAL;
+    if (int rc = evict_check(d); rc != DEPSYNC_OK) return rc;
+    *bytes = (size_t)d->batch * d->kv_heads * (1 + 2 * (size_t)evict_moves(d)) * sizeof(uint32_t);
+    return DEPSYNC_OK;
+}
+
+int dep_cache_evict(const depsync_cache_evict_desc* d, void* workspace, size_t workspace_bytes, void* stream) {
+    size_t need = 0;
+    if (int rc = depsync_cache_evict_workspace(d, &need); rc != DEPSYNC_OK) return rc;
+    CacheEvictArgs a = {};
+    const int D = d->head_dim;
+    const bool other = d->k_out != nullptr;
+    if (!operand(d->k_cache) || !operand(d->v_cache) || !array(d->weights) || !array(d->pos) || !array(d->cached) || !array(d->cached_out) ||
+        d->cached == d->cached_out || !operand(workspace) || workspace_bytes < need)
+        return DEPSYNC_EINVAL;
+    if ((d->v_out != nullptr) != other || (d->weights_out != nullptr) != other || (d->pos_out != nullptr) != other) return DEPSYNC_EINVAL;
+    if (!strides(a.cache_s, d->cache_batch, d->cache_token, d->cache_head, d->batch, d->capacity, d->kv_heads, D, !other, true)) return DEPSYNC_EINVAL;
+    if (other) {
+        if (!operand(d->k_out) || !operand(d->v_out) || !array(d->weights_out) || !array(d->pos_out) || d->capacity_out < d->budget || d->capacity_out > 1 << 30 ||
+            d->k_out == d->k_cache || d->v_out == d->v_cache || d->weights_out == d->weights || d->pos_out == d->pos ||
+            !strides(a.out_s, d->out_batch, d->out_token, d->out_head, d->batch, d->capacity_out, d->kv_heads, D, true, true))
+            return DEPSYNC_EINVAL;
+    } else {
+        a.out_s = a.cache_s;
+    }
+    a.k_cache = d->k_cache; a.v_cache = d->v_cache; a.weights = d->weights; a.pos = d->pos;
+    a.k_out = other ? d->k_out : d->k_cache; a.v_out = other ? d->v_out : d->v_cache;
+    a.weights_out = other ? d->weights_out : d->weights; a.pos_out = other ? d->pos_out : d->pos;
+    a.cached = d->cached; a.cached_out = d->cached_out; a.moves = static_cast<uint32_t*>(workspace);
+    a.batch = d->batch; a.kv_heads = d->kv_heads; a.capacity = d->capacity; a.capacity_out = other ? d->capacity_out : d->capacity;
+    a.budget = d->budget; a.recent = d->recent; a.max_cached = rows_hint(d->max_cached, d->capacity);
+    a.max_moves = (uint32_t)evict_moves(d);
+    a.in_place = other ? 0 : 1;
+    const hipError_t e = launch_cache_evict(a, D, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);
+}
+
+}  // extern "C"

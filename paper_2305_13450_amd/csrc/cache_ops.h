@@ -1,0 +1,81 @@
+// Kernel arguments and launchers of the cache operators (attention of drafted tokens, append, weights, eviction).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace depsync {
+
+// Elements from one sequence, token and head to the next.
+struct Strides { int64_t batch, token, head; };
+
+struct TreeAttnArgs {
+    const void *q, *k_new, *v_new, *k_cache, *v_cache;
+    const int32_t *cached, *drafted;      // drafted may be null
+    const uint64_t* tree;                 // may be null: token t sees 0..t
+    void* out;
+    float* lse;                           // may be null
+    float* parts;                         // n_parts > 1: partial results (see tree_attn.hpp)
+    Strides q_s, new_s, cache_s, out_s;
+    int64_t tree_batch;
+    uint32_t batch, tokens, heads, kv_heads, group, capacity;
+    uint32_t rows;                        // tokens * group: query rows of one key and value head
+    uint32_t n_parts, part_blocks;        // parts of the key axis, blocks of keys in each (the last part takes what is left)
+    float scale;                          // scores to base-2 exponents
+};
+
+struct CacheAppendArgs {
+    const void *k_new, *v_new;
+    void *k_cache, *v_cache;
+    const int32_t* cached;
+    int32_t* cached_out;
+    const int32_t *accepted, *n_accepted, *start;
+    float* weights;
+    int32_t* pos;
+    Strides new_s, cache_s;
+    uint32_t batch, tokens, kv_heads, capacity, n_max;
+};
+
+struct CacheWeightsArgs {
+    const void *q, *k_cache;
+    const float* lse;
+    const int32_t *cached, *accepted, *n_accepted;
+    float* weights;
+    Strides q_s, cache_s;
+    uint32_t batch, tokens, heads, kv_heads, group, capacity, n_max;
+    uint32_t max_cached;
+    float scale;                          // scores to base-2 exponents
+};
+
+struct CacheEvictArgs {
+    void *k_cache, *v_cache, *k_out, *v_out;       // (k_out = k_cache where the rows move in place)
+    float *weights, *weights_out;
+    int32_t *pos, *pos_out;
+    const int32_t* cached;
+    int32_t* cached_out;
+    uint32_t* moves;                      // workspace: per sequence and head the number of moves, then their rows
+    Strides cache_s, out_s;
+    uint32_t batch, kv_heads, capacity, capacity_out, budget, recent, max_cached;
+    uint32_t max_moves;
+    uint32_t in_place;
+};
+
+// Keys of one block of the attention kernel: 128 where at most 64 query rows share a head's keys, else 64.
+constexpr uint32_t TREE_FEW_ROWS = 64;
+inline __host__ __device__ uint32_t tree_block_keys(uint32_t rows) { return rows <= TREE_FEW_ROWS ? 128u : 64u; }
+constexpr uint32_t TREE_ROW_BLOCK = 128;  // query rows of a workgroup beyond TREE_FEW_ROWS
+
+hipError_t launch_tree_attn(const TreeAttnArgs& a, int dtype, int head_dim, hipStream_t stream);
+hipError_t launch_tree_attn_bf16(const TreeAttnArgs& a, int head_dim, hipStream_t stream);
+hipError_t launch_tree_attn_f16(const TreeAttnArgs& a, int head_dim, hipStream_t stream);
+hipError_t launch_cache_append(const CacheAppendArgs& a, int head_dim, hipStream_t stream);
+hipError_t launch_cache_weights(const CacheWeightsArgs& a, int dtype, int head_dim, hipStream_t stream);
+hipError_t launch_cache_evict(const CacheEvictArgs& a, int head_dim, hipStream_t stream);
+
+template <class F, class A>
+inline hipError_t launch_one(F* kernel, uint32_t n_blocks, uint32_t threads, hipStream_t stream, const A& a) {
+    void* args[] = {const_cast<A*>(&a)};
+    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(n_blocks), dim3(threads), args, 0, stream);
+}
+
+}  // namespace depsync

@@ -37,6 +37,9 @@ hipError_t launch_wait_draws(const ChainArgs& a, uint32_t stage, uint32_t want, 
 // per wave; src holds 1 MiB of operand bits, out n_blocks * 256 floats (practically never written).
 hipError_t launch_mfma_calibration(const void* src, float* out, int n_blocks, int iters, hipStream_t stream);
 
+// Remembers a failed HIP call's error for depsync_last_hip_error; DEPSYNC_EHIP.
+int hip_fail(hipError_t e);
+
 // One family per translation unit (kern_*.hip).
 hipError_t launch_bf16_gemm(int tile, bool sync, uint32_t n_blocks, hipStream_t stream, const ChainArgs& a);
 hipError_t launch_f16_gemm(int tile, bool sync, uint32_t n_blocks, hipStream_t stream, const ChainArgs& a);

@@ -1,0 +1,528 @@
+// Attention of drafted tokens over a cache: for every key and value head, rows = tokens x query heads that share it,
+//   o_r = sum_k p_rk v_k / sum_k p_rk,   p_rk = exp2(s_rk - m_r),   s_rk = scale log2(e) q_r . k_k
+// over the sequence's cached rows and those drafted tokens that the row's tree word names, in one pass over the keys with
+// a running maximum m, sum and un-normalised output per row.  All scores are computed transposed, as in attn_tile.hpp: a lane
+// owns one query row, S^T = K Q^T leaves 16 of 32 keys of it in its registers, and these are the B operand of O^T += V^T P^T as they stand.
+//
+// The key axis is the cached rows in blocks, then the drafted tokens in blocks; a block never mixes the two.  It is cut into
+// parts of `part_blocks` blocks, one workgroup each, as there are few (sequence, head) pairs on 256 CUs.  Parts leave their
+// maxima, sums and un-normalised outputs in the workspace and a second kernel joins them in order, so results do not depend on timing.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "attn_tile.hpp"
+#include "cache_ops.h"
+#include "gemm_tile.hpp"
+
+namespace depsync {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// The largest weight is 2^OFF: sums and outputs carry the factor alike and it cancels.  fp16 holds weights below 2^-14 with
+// fewer bits, and the weights of a long cache are mostly far below the largest: 2^14 leaves 28 binades above that.  bf16 has them anyway.
+template <typename T> constexpr float WEIGHT_OFF = 0.0f;
+template <> inline constexpr float WEIGHT_OFF<_Float16> = 14.0f;
+
+template <typename T> __device__ __forceinline__ bool any_not_finite(u32x4 v) {
+    constexpr uint32_t E = sizeof(T) == 2 && __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bad |= (v[i] & E) == E || (v[i] >> 16 & E) == E;
+    return bad;
+}
+
+__device__ __forceinline__ uint32_t clamp_count(int32_t v, uint32_t most) { return v < 0 ? 0u : min((uint32_t)v, most); }
+
+// What one 32-key tile of K and of V looks like in LDS, and a lane's offsets into it.
+template <typename T, int D> struct KeyTile {
+    static constexpr uint32_t PITCH = D * 2, CHUNKS = D / 8, BYTES = 32 * PITCH;
+    static constexpr uint32_t RPI = 1024 / PITCH, NI = 32 / RPI;       // rows and number of a wave's 1 KB copies
+    // Position of a row's 16-byte chunk: K fragments are a chunk of 32 rows, V fragments (transposing reads) 64 bytes of 4
+    // consecutive rows; either way the lanes that read together find different banks.
+    static __device__ __forceinline__ uint32_t kswz(uint32_t row) { return D == 128 ? row & 15u : swz(row); }
+    static __device__ __forceinline__ uint32_t vswz(uint32_t row) { return D == 128 ? att_vswz(row) : ((row & 2u) << 1) | ((row >> 2) & 3u); }
+    static __device__ __forceinline__ uint32_t koff(uint32_t lane) { return (lane & 31u) * PITCH + (((lane >> 5) ^ kswz(lane & 31u)) << 4); }
+    static __device__ __forceinline__ uint32_t voff(uint32_t lane) {
+        const uint32_t key = 4u * (lane >> 5) + ((lane & 15u) >> 2);
+        return key * PITCH + (((((lane >> 4) & 1u) * 2u + ((lane & 3u) >> 1)) ^ vswz(key)) << 4) + (lane & 1u) * 8u;
+    }
+};
+
+// A lane's query row: running maximum and sum, un-normalised output (O^T: D / 32 blocks of 32 d, 16 of them per lane).
+template <typename T, int D> struct RowState {
+    using V8 = typename Mma<T>::V8;
+    V8 q[D / 16];
+    f32x16 o[D / 32];
+    float m, l;
+};
+
+// One step: KT tiles of 32 keys in LDS against MR groups of 32 rows.  vis: the tile's keys that a lane's row sees, one bit each.
+// `odd`: a value of the tiles is not finite, and 0 x inf would reach rows that do not see its key: those steps multiply V in plain
+// arithmetic, key by key, and skip unseen keys (scratch: 2 KB of LDS of the wave's own).
+template <typename T, int D, int KT, int MR>
+__device__ __forceinline__ void tree_step(RowState<T, D> (&row)[MR], const char* ldsK, const char* ldsV, uint32_t lane, float sc,
+                                          const uint32_t (&vis)[MR][KT], bool masked, bool odd, T* scratch) {
+    using Tile = KeyTile<T, D>;
+    using M = Mma<T>;
+    using V8 = typename M::V8;
+    const uint32_t h2 = lane >> 5;
+    const uint32_t koff = Tile::koff(lane), voff = Tile::voff(lane);
+    f32x16 st[MR][KT];
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+#pragma unroll
+        for (int r = 0; r < MR; ++r)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) st[r][t][v] = 0.0f;
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+            const V8 kf = *(const V8*)(ldsK + (koff ^ (kk * 32u)) + t * Tile::BYTES);
+#pragma unroll
+            for (int r = 0; r < MR; ++r) st[r][t] = M::mma(kf, row[r].q[kk], st[r][t]);
+        }
+    }
+    V8 pf[MR][2 * KT];
+#pragma unroll
+    for (int r = 0; r < MR; ++r) {
+        if (masked) {
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (!(vis[r][t] >> (8 * (v / 4) + 4 * h2 + v % 4) & 1u)) st[r][t][v] = -INFINITY;
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) mx = fmaxf(mx, st[r][t][v]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32)) * sc;
+        const float m_new = fmaxf(row[r].m, mx);
+        const float m_use = m_new == -INFINITY ? 0.0f : m_new;       // no key seen yet: keep the exponents finite
+        const float alpha = __builtin_amdgcn_exp2f(row[r].m - m_use);
+        const float ref = m_use - WEIGHT_OFF<T>;
+        row[r].m = m_new;
+        float sum = 0.0f;
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[r][t][v], sc, -ref));
+                sum += p;                                            // summed in 32 bits, rounded to 16 for the product with V only
+                pf[r][2 * t + (v >> 3)][v & 7] = (T)p;
+            }
+        sum += __shfl_xor(sum, 32);
+        row[r].l = row[r].l * alpha + sum;
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) row[r].o[b][v] *= alpha;
+    }
+    if (__builtin_expect(odd, 0)) {
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < MR; ++r) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) scratch[(8 * (v / 4) + 4 * h2 + v % 4) * 32 + (lane & 31u)] = pf[r][2 * t + (v >> 3)][v & 7];
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+                for (uint32_t key = 0; key < 32; ++key) {
+                    const float p = (float)scratch[key * 32 + (lane & 31u)];
+                    if (!(vis[r][t] >> key & 1u) || p == 0.0f) continue;
+#pragma unroll
+                    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            typedef T T4 __attribute__((ext_vector_type(4)));
+                            const uint32_t d = 32 * b + 8 * g + 4 * h2;
+                            const T4 x = *(const T4*)(ldsV + t * Tile::BYTES + key * Tile::PITCH + (((d >> 3) ^ Tile::vswz(key)) << 4) + (d & 4u) * 2u);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) row[r].o[b][4 * g + e] = __builtin_fmaf(p, (float)x[e], row[r].o[b][4 * g + e]);
+                        }
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_wave_barrier();
+            }
+        return;
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2 * KT; ++ks)
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b) {
+            const auto lo = TrRead<T>::read(ldsV + (voff ^ (b * 64u)) + ks * 16 * Tile::PITCH);
+            const auto hi = TrRead<T>::read(ldsV + (voff ^ (b * 64u + 32u)) + (ks * 16 + 8) * Tile::PITCH);
+            const V8 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+            for (int r = 0; r < MR; ++r) row[r].o[b] = M::mma(vf, pf[r][ks], row[r].o[b]);
+        }
+}
+
+// What a workgroup works on, the same in every lane.
+struct TreeJob {
+    uint32_t b, h, part;                 // sequence, key and value head, part of the keys
+    uint32_t cached, drafted;            // of the sequence
+    uint32_t cache_blocks, begin, end;   // blocks of cached rows, this part's blocks
+};
+__device__ __forceinline__ TreeJob tree_job(const TreeAttnArgs& a, uint32_t unit, uint32_t block_keys) {
+    TreeJob j;
+    j.h = unit % a.kv_heads;
+    const uint32_t rest = unit / a.kv_heads;
+    j.part = rest % a.n_parts;
+    j.b = rest / a.n_parts;
+    j.cached = uni(a.capacity ? clamp_count(a.cached[j.b], a.capacity) : 0u);
+    j.drafted = uni(a.drafted ? clamp_count(a.drafted[j.b], a.tokens) : a.tokens);
+    j.cache_blocks = (j.cached + block_keys - 1) / block_keys;
+    const uint32_t blocks = j.cache_blocks + (j.drafted + block_keys - 1) / block_keys;
+    j.begin = min(blocks, j.part * a.part_blocks);
+    j.end = j.part + 1 == a.n_parts ? blocks : min(blocks, j.begin + a.part_blocks);
+    return j;
+}
+// Parts of a sequence that have blocks: the ones that leave results.
+__device__ __forceinline__ uint32_t tree_live_parts(const TreeAttnArgs& a, uint32_t cached, uint32_t drafted, uint32_t block_keys) {
+    const uint32_t blocks = (cached + block_keys - 1) / block_keys + (drafted + block_keys - 1) / block_keys;
+    return min(a.n_parts, (blocks + a.part_blocks - 1) / a.part_blocks);
+}
+
+// Workspace: outputs [pair][part][row][D], then maxima and sums [pair][part][row][2], pair = sequence x head.
+__device__ __forceinline__ size_t tree_part_row(const TreeAttnArgs& a, uint32_t pair, uint32_t part, uint32_t row) {
+    return ((size_t)pair * a.n_parts + part) * a.rows + row;
+}
+
+// A run of keys as a workgroup or wave copies it to LDS: where it lies, and how many of its 32 (or 64) rows are there.
+struct KeyRun {
+    const char *k, *v;
+    uint32_t pitch;      // bytes
+    uint32_t first, n;   // position among the cached rows or the drafted tokens, rows that are there
+    bool drafted;
+};
+template <int D>
+__device__ __forceinline__ KeyRun key_run(const TreeAttnArgs& a, const TreeJob& j, uint32_t block, uint32_t block_keys, uint32_t off, uint32_t keys) {
+    KeyRun x;
+    x.drafted = block >= j.cache_blocks;
+    x.first = (block - (x.drafted ? j.cache_blocks : 0u)) * block_keys + off;
+    const uint32_t have = x.drafted ? j.drafted : j.cached;
+    x.n = x.first < have ? min(keys, have - x.first) : 0u;
+    const Strides& s = x.drafted ? a.new_s : a.cache_s;
+    const int64_t at = ((int64_t)j.b * s.batch + (int64_t)x.first * s.token + (int64_t)j.h * s.head) * 2;
+    x.k = (const char*)(x.drafted ? a.k_new : a.k_cache) + at;
+    x.v = (const char*)(x.drafted ? a.v_new : a.v_cache) + at;
+    x.pitch = (uint32_t)s.token * 2u;
+    return x;
+}
+template <int D> __device__ __forceinline__ uint32_t run_bytes(const KeyRun& x) { return x.n ? (x.n - 1) * x.pitch + D * 2u : 0u; }
+
+// The keys of a drafted run of 32 that row `t` sees.
+__device__ __forceinline__ uint32_t tree_bits(const TreeAttnArgs& a, uint32_t b, uint32_t t, uint32_t first, uint32_t n) {
+    if (n == 0) return 0u;
+    const uint32_t there = n >= 32 ? ~0u : (1u << n) - 1u;
+    if (!a.tree) return t < first ? 0u : t - first >= 31 ? there : there & ((2u << (t - first)) - 1u);
+    const uint32_t words = (a.tokens + 63) / 64;
+    const uint32_t* w = (const uint32_t*)(a.tree + (int64_t)b * a.tree_batch + (int64_t)t * words);
+    return there & w[first >> 5];
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void load_row(RowState<T, D>& x, const TreeAttnArgs& a, const TreeJob& j, uint32_t r, uint32_t h2) {
+    using V8 = typename Mma<T>::V8;
+    const bool live = r < a.rows;
+    const uint32_t t = live ? r / a.group : 0u, g = live ? r - t * a.group : 0u;
+    const T* p = (const T*)a.q + (int64_t)j.b * a.q_s.batch + (int64_t)t * a.q_s.token + (int64_t)(j.h * a.group + g) * a.q_s.head + h2 * 8;
+    const V8 zero = {};
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) x.q[kk] = live ? *(const V8*)(p + kk * 16) : zero;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) x.o[b][v] = 0.0f;
+    x.m = -INFINITY;
+    x.l = 0.0f;
+}
+
+// Four output values of row r, d.. : rounded and stored, or left for the second kernel.
+template <typename T, int D>
+__device__ __forceinline__ void store_row4(const TreeAttnArgs& a, const TreeJob& j, uint32_t r, uint32_t d, f32x4 o, float m, float l) {
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    if (r >= a.rows) return;
+    const uint32_t t = r / a.group, g = r - t * a.group;
+    if (t >= j.drafted) return;
+    const uint32_t hq = j.h * a.group + g;
+    if (a.n_parts > 1) {
+        const size_t at = tree_part_row(a, j.b * a.kv_heads + j.h, j.part, r);
+        *(f32x4*)(a.parts + at * D + d) = o;
+        if (d == 0) {
+            float* ml = a.parts + (size_t)a.batch * a.kv_heads * a.n_parts * a.rows * D + at * 2;
+            ml[0] = m; ml[1] = l;
+        }
+        return;
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;                    // (no key seen: zeros)
+    T4 x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = (T)(o[e] * inv);
+    *(T4*)((T*)a.out + (int64_t)j.b * a.out_s.batch + (int64_t)t * a.out_s.token + (int64_t)hq * a.out_s.head + d) = x;
+    if (d == 0 && a.lse) a.lse[((size_t)j.b * a.tokens + t) * a.heads + hq] = (m + __builtin_amdgcn_logf(l) - WEIGHT_OFF<T>) * 0.69314718055994531f;
+}
+
+// ---- few rows ------------------------------------------------------------------------------------------------------------
+// At most 32 MR rows share a head's keys: the time is that of reading the keys and values once.  Each of the four waves walks 32
+// of a block's 128 keys by itself, with the next step's 16 KB on its way into registers while it works from its own 16 KB of LDS; no wave
+// waits for another until the end, when their results are joined through LDS.
+template <typename T, int D> constexpr uint32_t tree_wave_bytes() {
+    constexpr uint32_t stage = 2 * KeyTile<T, D>::BYTES, join = 32 * (D + 4) * 4;
+    return stage > join ? stage : join;
+}
+template <typename T, int D, int MR>
+__global__ __launch_bounds__(256, MR == 1 ? 2 : 1) void tree_attn_few(const TreeAttnArgs a) {
+    using Tile = KeyTile<T, D>;
+    constexpr uint32_t WAVE = tree_wave_bytes<T, D>();
+    __shared__ __align__(16) char lds[4 * WAVE];
+    __shared__ float ml[4][32][2];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6);
+    const TreeJob j = tree_job(a, blockIdx.x, 128);
+    if (j.begin >= j.end) return;
+    RowState<T, D> row[MR];
+    uint32_t token[MR];
+#pragma unroll
+    for (int r = 0; r < MR; ++r) {
+        const uint32_t at = r * 32 + (lane & 31u);
+        load_row(row[r], a, j, at, lane >> 5);
+        token[r] = min(at, a.rows - 1) / a.group;
+    }
+    char* const ldsK = lds + wave * WAVE;
+    char* const ldsV = ldsK + Tile::BYTES;
+    const uint32_t lrow = lane / Tile::CHUNKS, chunk = lane % Tile::CHUNKS;
+    u32x4 kreg[Tile::NI], vreg[Tile::NI];
+    auto fetch = [&](const KeyRun& x) __attribute__((always_inline)) {
+        const uint32_t bytes = uni(run_bytes<D>(x));
+        const OperandBuf K(uni_ptr(x.k), bytes), V(uni_ptr(x.v), bytes);   // rows that are not there: zeros
+#pragma unroll
+        for (uint32_t i = 0; i < Tile::NI; ++i) kreg[i] = K.load16((i * Tile::RPI + lrow) * x.pitch + chunk * 16, 0);
+#pragma unroll
+        for (uint32_t i = 0; i < Tile::NI; ++i) vreg[i] = V.load16((i * Tile::RPI + lrow) * x.pitch + chunk * 16, 0);
+    };
+    KeyRun x = key_run<D>(a, j, j.begin, 128, wave * 32, 32);
+    fetch(x);
+    for (uint32_t blk = j.begin; blk < j.end; ++blk) {
+        bool odd = false;
+        if (x.drafted) {
+            bool bad = false;
+#pragma unroll
+            for (uint32_t i = 0; i < Tile::NI; ++i) bad |= any_not_finite<T>(vreg[i]);
+            odd = __ballot(bad) != 0;
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < Tile::NI; ++i) {
+            const uint32_t rr = i * Tile::RPI + lrow;
+            *(u32x4*)(ldsK + rr * Tile::PITCH + ((chunk ^ Tile::kswz(rr)) << 4)) = kreg[i];
+            *(u32x4*)(ldsV + rr * Tile::PITCH + ((chunk ^ Tile::vswz(rr)) << 4)) = vreg[i];
+        }
+        const KeyRun now = x;
+        if (blk + 1 < j.end) {
+            x = key_run<D>(a, j, blk + 1, 128, wave * 32, 32);
+            fetch(x);
+        }
+        asm volatile("" ::: "memory");                                 // (a wave's LDS accesses keep their order)
+        __builtin_amdgcn_wave_barrier();
+        if (now.n) {
+            uint32_t vis[MR][1];
+#pragma unroll
+            for (int r = 0; r < MR; ++r) vis[r][0] = now.drafted ? tree_bits(a, j.b, token[r], now.first, now.n) : now.n >= 32 ? ~0u : (1u << now.n) - 1u;
+            tree_step<T, D, 1, MR>(row, ldsK, ldsV, lane, a.scale, vis, now.drafted || now.n < 32, odd, (T*)ldsK);
+        }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+    }
+    // ---- the four waves joined ----
+#pragma unroll
+    for (int r = 0; r < MR; ++r) {
+        __syncthreads();
+        if (lane < 32) { ml[wave][lane][0] = row[r].m; ml[wave][lane][1] = row[r].l; }
+        float* const mine = (float*)(lds + wave * WAVE);
+        __syncthreads();
+        float M = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) M = fmaxf(M, ml[w][lane & 31u][0]);
+        const float f = row[r].m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(row[r].m - M);
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                f32x4 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = row[r].m == -INFINITY && row[r].l == 0.0f ? 0.0f : row[r].o[b][4 * g + e] * f;
+                *(f32x4*)(mine + (lane & 31u) * (D + 4) + 32 * b + 8 * g + 4 * (lane >> 5)) = o;
+            }
+        __syncthreads();
+        const uint32_t rr = tid >> 3;
+        float mm = -INFINITY, L = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) mm = fmaxf(mm, ml[w][rr][0]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float mw = ml[w][rr][0], lw = ml[w][rr][1];
+            L += mw == -INFINITY ? lw : lw * __builtin_amdgcn_exp2f(mw - mm);     // (a sum without a maximum is 0, or NaN)
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < D / 32; ++i) {
+            const uint32_t d = (tid & 7u) * 4 + 32 * i;
+            f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) o += *(const f32x4*)((const float*)(lds + w * WAVE) + rr * (D + 4) + d);
+            store_row4<T, D>(a, j, r * 32 + rr, d, o, mm, L);
+        }
+    }
+}
+
+// ---- many rows -----------------------------------------------------------------------------------------------------------
+// 128 rows to a workgroup, 32 to a wave; all waves work on the same 64 keys, which the workgroup copies to LDS together, the
+// next block on its way through registers meanwhile.  Two workgroups share a CU and cover each other's waits.  A pair's row
+// blocks run on one XCD (every eighth workgroup does), so its keys come from HBM once.
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
+    using Tile = KeyTile<T, D>;
+    constexpr uint32_t BLK = 2 * Tile::BYTES;                          // 64 rows of K (or of V)
+    __shared__ __align__(16) char lds[2][2 * BLK];
+    __shared__ T scratch[4][32 * 32];
+    __shared__ uint32_t odd_flag[2];                                   // the buffer holds drafted values that are not finite
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6);
+    const uint32_t row_blocks = (a.rows + TREE_ROW_BLOCK - 1) / TREE_ROW_BLOCK;
+    const uint32_t slot = blockIdx.x >> 3;
+    const uint32_t unit = (slot / row_blocks) * 8 + (blockIdx.x & 7u), rb = slot % row_blocks;
+    if (unit >= a.batch * a.n_parts * a.kv_heads) return;
+    const TreeJob j = tree_job(a, unit, 64);
+    const uint32_t r0 = rb * TREE_ROW_BLOCK, t_last = (min(r0 + TREE_ROW_BLOCK, a.rows) - 1) / a.group;
+    if (j.begin >= j.end || r0 / a.group >= j.drafted) return;
+    RowState<T, D> row[1];
+    const uint32_t at = r0 + wave * 32 + (lane & 31u);
+    load_row(row[0], a, j, at, lane >> 5);
+    const uint32_t token = min(at, a.rows - 1) / a.group;
+    // without a tree nothing behind the block's last token is seen
+    const uint32_t end = a.tree ? j.end : min(j.end, max(j.begin, j.cache_blocks + t_last / 64 + 1));
+    constexpr uint32_t NI = Tile::NI / 2;                              // 1 KB copies of a wave: 64 rows over four waves
+    const uint32_t lrow = wave * (Tile::RPI * NI) + lane / Tile::CHUNKS, chunk = lane % Tile::CHUNKS;
+    u32x4 kreg[NI], vreg[NI];
+    auto fetch = [&](const KeyRun& x) __attribute__((always_inline)) {
+        const uint32_t bytes = uni(run_bytes<D>(x));
+        const OperandBuf K(uni_ptr(x.k), bytes), V(uni_ptr(x.v), bytes);
+#pragma unroll
+        for (uint32_t i = 0; i < NI; ++i) {
+            kreg[i] = K.load16((i * Tile::RPI + lrow) * x.pitch + chunk * 16, 0);
+            vreg[i] = V.load16((i * Tile::RPI + lrow) * x.pitch + chunk * 16, 0);
+        }
+    };
+    auto put = [&](uint32_t buf, bool drafted) __attribute__((always_inline)) {
+        bool bad = false;
+#pragma unroll
+        for (uint32_t i = 0; i < NI; ++i) {
+            const uint32_t rr = i * Tile::RPI + lrow;
+            *(u32x4*)(lds[buf] + rr * Tile::PITCH + ((chunk ^ Tile::kswz(rr)) << 4)) = kreg[i];
+            *(u32x4*)(lds[buf] + BLK + rr * Tile::PITCH + ((chunk ^ Tile::vswz(rr)) << 4)) = vreg[i];
+            if (drafted) bad |= any_not_finite<T>(vreg[i]);
+        }
+        if (drafted && __ballot(bad) && lane == 0) odd_flag[buf] = 1;
+    };
+    if (tid < 2) odd_flag[tid] = 0;
+    __syncthreads();
+    KeyRun x = key_run<D>(a, j, j.begin, 64, 0, 64), next = x;
+    if (j.begin < end) {
+        fetch(x);
+        put(0, x.drafted);
+        if (j.begin + 1 < end) { next = key_run<D>(a, j, j.begin + 1, 64, 0, 64); fetch(next); }
+    }
+    __syncthreads();
+    for (uint32_t blk = j.begin; blk < end; ++blk) {
+        const uint32_t buf = (blk - j.begin) & 1u;
+        const bool odd = odd_flag[buf] != 0;
+        uint32_t vis[1][2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const uint32_t n = x.n > 32u * t ? min(32u, x.n - 32u * t) : 0u;
+            vis[0][t] = x.drafted ? tree_bits(a, j.b, token, x.first + 32 * t, n) : n >= 32 ? ~0u : (1u << n) - 1u;
+        }
+        tree_step<T, D, 2, 1>(row, lds[buf], lds[buf] + BLK, lane, a.scale, vis, x.drafted || x.n < 64, x.drafted && odd, scratch[wave]);
+        if (blk + 1 < end) {
+            put(buf ^ 1u, next.drafted);
+            x = next;
+            if (blk + 2 < end) { next = key_run<D>(a, j, blk + 2, 64, 0, 64); fetch(next); }
+        }
+        __syncthreads();
+    }
+    const uint32_t h2 = lane >> 5;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            f32x4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = row[0].o[b][4 * g + e];
+            store_row4<T, D>(a, j, at, 32 * b + 8 * g + 4 * h2, o, row[0].m, row[0].l);
+        }
+}
+
+// ---- parts joined --------------------------------------------------------------------------------------------------------
+// One wave per query row: D / 4 lanes hold four output values each, and as many such groups as there are walk the parts.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void tree_attn_join(const TreeAttnArgs a) {
+    constexpr uint32_t VEC = D / 4, GROUPS = 64 / VEC;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    const uint32_t lane = threadIdx.x & 63u;
+    const uint64_t item = (uint64_t)blockIdx.x * 4 + uni(threadIdx.x >> 6);
+    const uint32_t pair = (uint32_t)(item / a.rows), r = (uint32_t)(item % a.rows);
+    if (pair >= a.batch * a.kv_heads) return;
+    const uint32_t b = pair / a.kv_heads, h = pair % a.kv_heads;
+    const uint32_t t = r / a.group, hq = h * a.group + r % a.group;
+    const uint32_t cached = a.capacity ? clamp_count(a.cached[b], a.capacity) : 0u;
+    const uint32_t drafted = a.drafted ? clamp_count(a.drafted[b], a.tokens) : a.tokens;
+    if (t >= drafted) return;
+    const uint32_t n = tree_live_parts(a, cached, drafted, tree_block_keys(a.rows));
+    const float* const ml = a.parts + (size_t)a.batch * a.kv_heads * a.n_parts * a.rows * D;
+    float M = -INFINITY;
+    for (uint32_t z = lane; z < n; z += 64) M = fmaxf(M, ml[tree_part_row(a, pair, z, r) * 2]);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) M = fmaxf(M, __shfl_xor(M, d));
+    float L = 0.0f;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t grp = lane / VEC, d = (lane % VEC) * 4;
+#pragma unroll 4
+    for (uint32_t z = grp; z < n; z += GROUPS) {
+        const size_t at = tree_part_row(a, pair, z, r);
+        const float mz = ml[at * 2], lz = ml[at * 2 + 1];
+        const f32x4 v = *(const f32x4*)(a.parts + at * D + d);
+        const float f = mz == -INFINITY ? (lz == 0.0f ? 0.0f : lz) : __builtin_amdgcn_exp2f(mz - M);   // (a sum without a maximum is 0, or NaN)
+        L += lz * f;
+        o += v * f;
+    }
+#pragma unroll
+    for (uint32_t x = VEC; x < 64; x <<= 1) {
+        L += __shfl_xor(L, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], x);
+    }
+    if (grp) return;
+    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    T4 x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = (T)(o[e] * inv);
+    *(T4*)((T*)a.out + (int64_t)b * a.out_s.batch + (int64_t)t * a.out_s.token + (int64_t)hq * a.out_s.head + d) = x;
+    if (d == 0 && a.lse) a.lse[((size_t)b * a.tokens + t) * a.heads + hq] = (M + __builtin_amdgcn_logf(L) - WEIGHT_OFF<T>) * 0.69314718055994531f;
+}
+
+template <typename T, int D>
+hipError_t launch_tree_attn_of(const TreeAttnArgs& a, hipStream_t stream) {
+    const uint32_t units = a.batch * a.kv_heads * a.n_parts;
+    hipError_t e;
+    if (a.rows <= 32) e = launch_one(tree_attn_few<T, D, 1>, units, 256, stream, a);
+    else if (a.rows <= TREE_FEW_ROWS) e = launch_one(tree_attn_few<T, D, 2>, units, 256, stream, a);
+    else e = launch_one(tree_attn_many<T, D>, (units + 7) / 8 * 8 * ((a.rows + TREE_ROW_BLOCK - 1) / TREE_ROW_BLOCK), 256, stream, a);
+    if (e != hipSuccess || a.n_parts == 1) return e;
+    return launch_one(tree_attn_join<T, D>, (uint32_t)(((uint64_t)a.batch * a.kv_heads * a.rows + 3) / 4), 256, stream, a);
+}
+
+template <typename T>
+hipError_t launch_tree_attn_type(const TreeAttnArgs& a, int head_dim, hipStream_t stream) {
+    return head_dim == 128 ? launch_tree_attn_of<T, 128>(a, stream) : launch_tree_attn_of<T, 64>(a, stream);
+}
+
+}  // namespace depsync
