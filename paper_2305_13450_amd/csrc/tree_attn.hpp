@@ -23,11 +23,16 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 template <typename T> constexpr float WEIGHT_OFF = 0.0f;
 template <> inline constexpr float WEIGHT_OFF<_Float16> = 14.0f;
 
-template <typename T> __device__ __forceinline__ bool any_not_finite(u32x4 v) {
-    constexpr uint32_t E = sizeof(T) == 2 && __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
+// Zeros in the place of infinities and NaN; whether there were any.
+template <typename T> __device__ __forceinline__ bool without_not_finite(u32x4& v) {
+    constexpr uint32_t E = __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
     bool bad = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) bad |= (v[i] & E) == E || (v[i] >> 16 & E) == E;
+    for (int i = 0; i < 4; ++i) {
+        const bool lo = (v[i] & E) == E, hi = (v[i] >> 16 & E) == E;
+        bad |= lo || hi;
+        v[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+    }
     return bad;
 }
 
@@ -48,38 +53,57 @@ template <typename T, int D> struct KeyTile {
     }
 };
 
-// A lane's query row: running maximum and sum, un-normalised output (O^T: D / 32 blocks of 32 d, 16 of them per lane).
-template <typename T, int D> struct RowState {
-    using V8 = typename Mma<T>::V8;
-    V8 q[D / 16];
+// A lane's query row: running maximum, un-normalised output (O^T: D / 32 blocks of 32 d, 16 of them per lane), and the sum of the
+// weights of this lane's keys (its half of every 32; the halves are added at the end).
+template <int D> struct RowState {
     f32x16 o[D / 32];
     float m, l;
 };
 
+// A value the compiler computes anew from: offsets derived from it are not kept in registers across a loop's steps.
+__device__ __forceinline__ uint32_t opaque(uint32_t x) { asm volatile("" : "+v"(x)); return x; }
+
+// The larger of a value and that of the lane 32 further on.  (The results by name: a bit cast of an element where it stands reads the first.)
+__device__ __forceinline__ float max_halves(float x) {
+    const auto y = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    const uint32_t lower = y[0], upper = y[1];
+    return fmaxf(__builtin_bit_cast(float, lower), __builtin_bit_cast(float, upper));
+}
+
 // One step: KT tiles of 32 keys in LDS against MR groups of 32 rows.  vis: the tile's keys that a lane's row sees, one bit each.
-// `odd`: a value of the tiles is not finite, and 0 x inf would reach rows that do not see its key: those steps multiply V in plain
-// arithmetic, key by key, and skip unseen keys (scratch: 2 KB of LDS of the wave's own).
-template <typename T, int D, int KT, int MR>
-__device__ __forceinline__ void tree_step(RowState<T, D> (&row)[MR], const char* ldsK, const char* ldsV, uint32_t lane, float sc,
-                                          const uint32_t (&vis)[MR][KT], bool masked, bool odd, T* scratch) {
+// Fragments are read two slices ahead of the MFMAs and the order is pinned: left alone the compiler reads them all at once, and spills, or each right
+// before the wait for it.  query(r, kk): the fragment of slice kk of row group r.
+template <typename T, int D, int KT, int MR, class Q>
+__device__ __forceinline__ void tree_step(RowState<D> (&row)[MR], Q query, const char* ldsK, const char* ldsV, uint32_t lane, float sc,
+                                          const uint32_t (&vis)[MR][KT], bool masked) {
     using Tile = KeyTile<T, D>;
     using M = Mma<T>;
     using V8 = typename M::V8;
+    constexpr int KF = D / 16;
     const uint32_t h2 = lane >> 5;
-    const uint32_t koff = Tile::koff(lane), voff = Tile::voff(lane);
+    const uint32_t koff = opaque(Tile::koff(lane)), voff = opaque(Tile::voff(lane));
     f32x16 st[MR][KT];
+    {
+        V8 kf[3], qf[3][MR];
+        auto rd = [&](int i) __attribute__((always_inline)) {
+            kf[i % 3] = *(const V8*)(ldsK + (koff ^ ((i % KF) * 32u)) + (i / KF) * Tile::BYTES);
 #pragma unroll
-    for (int t = 0; t < KT; ++t) {
+            for (int r = 0; r < MR; ++r) qf[i % 3][r] = query(r, i % KF);
+        };
+        rd(0); rd(1);
 #pragma unroll
-        for (int r = 0; r < MR; ++r)
+        for (int i = 0; i < KT * KF; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (i + 2 < KT * KF) rd(i + 2);
+            if (i % KF == 0)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) st[r][t][v] = 0.0f;
+                for (int r = 0; r < MR; ++r)
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-            const V8 kf = *(const V8*)(ldsK + (koff ^ (kk * 32u)) + t * Tile::BYTES);
+                    for (int v = 0; v < 16; ++v) st[r][i / KF][v] = 0.0f;
 #pragma unroll
-            for (int r = 0; r < MR; ++r) st[r][t] = M::mma(kf, row[r].q[kk], st[r][t]);
+            for (int r = 0; r < MR; ++r) st[r][i / KF] = M::mma(kf[i % 3], qf[i % 3][r], st[r][i / KF]);
         }
+        __builtin_amdgcn_sched_barrier(0);
     }
     V8 pf[MR][2 * KT];
 #pragma unroll
@@ -95,68 +119,47 @@ __device__ __forceinline__ void tree_step(RowState<T, D> (&row)[MR], const char*
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) mx = fmaxf(mx, st[r][t][v]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32)) * sc;
-        const float m_new = fmaxf(row[r].m, mx);
-        const float m_use = m_new == -INFINITY ? 0.0f : m_new;       // no key seen yet: keep the exponents finite
-        const float alpha = __builtin_amdgcn_exp2f(row[r].m - m_use);
-        const float ref = m_use - WEIGHT_OFF<T>;
-        row[r].m = m_new;
-        float sum = 0.0f;
+            for (int v = 0; v < 16; v += 2) mx = fmaxf(fmaxf(mx, st[r][t][v]), st[r][t][v + 1]);
+        mx = max_halves(mx) * sc;
+        if (__ballot(mx > row[r].m)) {                               // (rarely, after the first steps)
+            const float m_new = fmaxf(row[r].m, mx);
+            const float alpha = row[r].m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(row[r].m - m_new);
+            row[r].m = m_new;
+            row[r].l *= alpha;
+#pragma unroll
+            for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) row[r].o[b][v] *= alpha;
+        }
+        const float ref = (row[r].m == -INFINITY ? 0.0f : row[r].m) - WEIGHT_OFF<T>;   // no key seen yet: keep the exponents finite
+        float sum[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[r][t][v], sc, -ref));
-                sum += p;                                            // summed in 32 bits, rounded to 16 for the product with V only
+                sum[v & 1] += p;                                     // summed in 32 bits, rounded to 16 for the product with V only
                 pf[r][2 * t + (v >> 3)][v & 7] = (T)p;
             }
-        sum += __shfl_xor(sum, 32);
-        row[r].l = row[r].l * alpha + sum;
-#pragma unroll
-        for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) row[r].o[b][v] *= alpha;
+        row[r].l += sum[0] + sum[1];
     }
-    if (__builtin_expect(odd, 0)) {
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    T4 vf[3][2];
+    constexpr int NB = D / 32, NV = 2 * KT * NB;
+    auto rdv = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-        for (int t = 0; t < KT; ++t)
+        for (int c = 0; c < 2; ++c) vf[i % 3][c] = TrRead<T>::read(ldsV + (voff ^ ((i % NB) * 64u + c * 32u)) + ((i / NB) * 16 + c * 8) * Tile::PITCH);
+    };
+    rdv(0); rdv(1);
 #pragma unroll
-            for (int r = 0; r < MR; ++r) {
+    for (int i = 0; i < NV; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (i + 2 < NV) rdv(i + 2);
+        const V8 x = __builtin_shufflevector(vf[i % 3][0], vf[i % 3][1], 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-                for (int v = 0; v < 16; ++v) scratch[(8 * (v / 4) + 4 * h2 + v % 4) * 32 + (lane & 31u)] = pf[r][2 * t + (v >> 3)][v & 7];
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-                for (uint32_t key = 0; key < 32; ++key) {
-                    const float p = (float)scratch[key * 32 + (lane & 31u)];
-                    if (!(vis[r][t] >> key & 1u) || p == 0.0f) continue;
-#pragma unroll
-                    for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            typedef T T4 __attribute__((ext_vector_type(4)));
-                            const uint32_t d = 32 * b + 8 * g + 4 * h2;
-                            const T4 x = *(const T4*)(ldsV + t * Tile::BYTES + key * Tile::PITCH + (((d >> 3) ^ Tile::vswz(key)) << 4) + (d & 4u) * 2u);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) row[r].o[b][4 * g + e] = __builtin_fmaf(p, (float)x[e], row[r].o[b][4 * g + e]);
-                        }
-                }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                __builtin_amdgcn_wave_barrier();
-            }
-        return;
+        for (int r = 0; r < MR; ++r) row[r].o[i % NB] = M::mma(x, pf[r][i / NB], row[r].o[i % NB]);
     }
-#pragma unroll
-    for (int ks = 0; ks < 2 * KT; ++ks)
-#pragma unroll
-        for (int b = 0; b < D / 32; ++b) {
-            const auto lo = TrRead<T>::read(ldsV + (voff ^ (b * 64u)) + ks * 16 * Tile::PITCH);
-            const auto hi = TrRead<T>::read(ldsV + (voff ^ (b * 64u + 32u)) + (ks * 16 + 8) * Tile::PITCH);
-            const V8 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-            for (int r = 0; r < MR; ++r) row[r].o[b] = M::mma(vf, pf[r][ks], row[r].o[b]);
-        }
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 // What a workgroup works on, the same in every lane.
@@ -223,15 +226,14 @@ __device__ __forceinline__ uint32_t tree_bits(const TreeAttnArgs& a, uint32_t b,
     return there & w[first >> 5];
 }
 
-template <typename T, int D>
-__device__ __forceinline__ void load_row(RowState<T, D>& x, const TreeAttnArgs& a, const TreeJob& j, uint32_t r, uint32_t h2) {
-    using V8 = typename Mma<T>::V8;
-    const bool live = r < a.rows;
-    const uint32_t t = live ? r / a.group : 0u, g = live ? r - t * a.group : 0u;
-    const T* p = (const T*)a.q + (int64_t)j.b * a.q_s.batch + (int64_t)t * a.q_s.token + (int64_t)(j.h * a.group + g) * a.q_s.head + h2 * 8;
-    const V8 zero = {};
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) x.q[kk] = live ? *(const V8*)(p + kk * 16) : zero;
+// Where row r's query lies; rows that there are not get null.
+template <typename T>
+__device__ __forceinline__ const T* query_row(const TreeAttnArgs& a, const TreeJob& j, uint32_t r) {
+    if (r >= a.rows) return nullptr;
+    const uint32_t t = r / a.group, g = r - t * a.group;
+    return (const T*)a.q + (int64_t)j.b * a.q_s.batch + (int64_t)t * a.q_s.token + (int64_t)(j.h * a.group + g) * a.q_s.head;
+}
+template <int D> __device__ __forceinline__ void clear_row(RowState<D>& x) {
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
 #pragma unroll
@@ -240,14 +242,35 @@ __device__ __forceinline__ void load_row(RowState<T, D>& x, const TreeAttnArgs& 
     x.l = 0.0f;
 }
 
+// Values of drafted tokens that are not finite were multiplied as zeros, as 0 x inf would reach rows that do not see their key.  What rows
+// that do see it miss is added to their sums at the end (the weight is positive: an infinity stays what it is).
+template <typename T>
+__device__ __forceinline__ f32x4 add_not_finite(const TreeAttnArgs& a, const TreeJob& j, uint32_t block_keys, uint32_t t, uint32_t d, f32x4 o) {
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    if (j.end <= j.cache_blocks) return o;
+    const uint32_t first = (max(j.begin, j.cache_blocks) - j.cache_blocks) * block_keys, last = min(j.drafted, (j.end - j.cache_blocks) * block_keys);
+    for (uint32_t k0 = first; k0 < last; k0 += 32)
+        for (uint32_t bits = tree_bits(a, j.b, t, k0, min(32u, last - k0)); bits; bits &= bits - 1) {
+            const uint32_t k = k0 + (uint32_t)__builtin_ctz(bits);
+            const T4 x = *(const T4*)((const T*)a.v_new + (int64_t)j.b * a.new_s.batch + (int64_t)k * a.new_s.token + (int64_t)j.h * a.new_s.head + d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float v = (float)x[e];
+                if (!(fabsf(v) < INFINITY)) o[e] += v;
+            }
+        }
+    return o;
+}
+
 // Four output values of row r, d.. : rounded and stored, or left for the second kernel.
 template <typename T, int D>
-__device__ __forceinline__ void store_row4(const TreeAttnArgs& a, const TreeJob& j, uint32_t r, uint32_t d, f32x4 o, float m, float l) {
+__device__ __forceinline__ void store_row4(const TreeAttnArgs& a, const TreeJob& j, uint32_t r, uint32_t d, f32x4 o, float m, float l, bool odd, uint32_t block_keys) {
     typedef T T4 __attribute__((ext_vector_type(4)));
     if (r >= a.rows) return;
     const uint32_t t = r / a.group, g = r - t * a.group;
     if (t >= j.drafted) return;
     const uint32_t hq = j.h * a.group + g;
+    if (__builtin_expect(odd, 0)) o = add_not_finite<T>(a, j, block_keys, t, d, o);
     if (a.n_parts > 1) {
         const size_t at = tree_part_row(a, j.b * a.kv_heads + j.h, j.part, r);
         *(f32x4*)(a.parts + at * D + d) = o;
@@ -276,48 +299,57 @@ template <typename T, int D> constexpr uint32_t tree_wave_bytes() {
 template <typename T, int D, int MR>
 __global__ __launch_bounds__(256, MR == 1 ? 2 : 1) void tree_attn_few(const TreeAttnArgs a) {
     using Tile = KeyTile<T, D>;
+    using V8 = typename Mma<T>::V8;
     constexpr uint32_t WAVE = tree_wave_bytes<T, D>();
     __shared__ __align__(16) char lds[4 * WAVE];
+    __shared__ __align__(16) char ldsQ[MR * Tile::BYTES];              // the queries, laid out like keys
     __shared__ float ml[4][32][2];
+    __shared__ uint32_t odd;                                           // a drafted value is not finite
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6);
     const TreeJob j = tree_job(a, blockIdx.x, 128);
     if (j.begin >= j.end) return;
-    RowState<T, D> row[MR];
-    uint32_t token[MR];
-#pragma unroll
-    for (int r = 0; r < MR; ++r) {
-        const uint32_t at = r * 32 + (lane & 31u);
-        load_row(row[r], a, j, at, lane >> 5);
-        token[r] = min(at, a.rows - 1) / a.group;
-    }
+    if (tid == 0) odd = 0;
     char* const ldsK = lds + wave * WAVE;
     char* const ldsV = ldsK + Tile::BYTES;
     const uint32_t lrow = lane / Tile::CHUNKS, chunk = lane % Tile::CHUNKS;
     u32x4 kreg[Tile::NI], vreg[Tile::NI];
     auto fetch = [&](const KeyRun& x) __attribute__((always_inline)) {
-        const uint32_t bytes = uni(run_bytes<D>(x));
+        const uint32_t bytes = uni(run_bytes<D>(x)), first = lrow * x.pitch + chunk * 16;
         const OperandBuf K(uni_ptr(x.k), bytes), V(uni_ptr(x.v), bytes);   // rows that are not there: zeros
 #pragma unroll
-        for (uint32_t i = 0; i < Tile::NI; ++i) kreg[i] = K.load16((i * Tile::RPI + lrow) * x.pitch + chunk * 16, 0);
+        for (uint32_t i = 0; i < Tile::NI; ++i) kreg[i] = K.load16(first, i * Tile::RPI * x.pitch);
 #pragma unroll
-        for (uint32_t i = 0; i < Tile::NI; ++i) vreg[i] = V.load16((i * Tile::RPI + lrow) * x.pitch + chunk * 16, 0);
+        for (uint32_t i = 0; i < Tile::NI; ++i) vreg[i] = V.load16(first, i * Tile::RPI * x.pitch);
     };
     KeyRun x = key_run<D>(a, j, j.begin, 128, wave * 32, 32);
     fetch(x);
+    RowState<D> row[MR];
+    uint32_t token[MR];
+#pragma unroll
+    for (int r = 0; r < MR; ++r) {
+        clear_row(row[r]);
+        token[r] = min(r * 32 + (lane & 31u), a.rows - 1) / a.group;
+        for (uint32_t i = tid; i < 32 * Tile::CHUNKS; i += 256) {
+            const uint32_t rr = i / Tile::CHUNKS, c = i % Tile::CHUNKS;
+            const T* q = query_row<T>(a, j, r * 32 + rr);
+            *(u32x4*)(ldsQ + r * Tile::BYTES + rr * Tile::PITCH + ((c ^ Tile::kswz(rr)) << 4)) = q ? ((const u32x4*)q)[c] : u32x4{0, 0, 0, 0};
+        }
+    }
+    __syncthreads();
+    // a lane's first row of a tile; the swizzles are exclusive-ors that repeat every 16 rows
+    const uint32_t kput = lrow * Tile::PITCH + ((chunk ^ Tile::kswz(lrow)) << 4), vput = lrow * Tile::PITCH + ((chunk ^ Tile::vswz(lrow)) << 4);
     for (uint32_t blk = j.begin; blk < j.end; ++blk) {
-        bool odd = false;
         if (x.drafted) {
             bool bad = false;
 #pragma unroll
-            for (uint32_t i = 0; i < Tile::NI; ++i) bad |= any_not_finite<T>(vreg[i]);
-            odd = __ballot(bad) != 0;
+            for (uint32_t i = 0; i < Tile::NI; ++i) bad |= without_not_finite<T>(vreg[i]);
+            if (bad) odd = 1;
         }
+        const uint32_t kp = opaque(kput), vp = opaque(vput);
 #pragma unroll
-        for (uint32_t i = 0; i < Tile::NI; ++i) {
-            const uint32_t rr = i * Tile::RPI + lrow;
-            *(u32x4*)(ldsK + rr * Tile::PITCH + ((chunk ^ Tile::kswz(rr)) << 4)) = kreg[i];
-            *(u32x4*)(ldsV + rr * Tile::PITCH + ((chunk ^ Tile::vswz(rr)) << 4)) = vreg[i];
-        }
+        for (uint32_t i = 0; i < Tile::NI; ++i) *(u32x4*)(ldsK + (kp ^ ((Tile::kswz(i * Tile::RPI)) << 4)) + i * Tile::RPI * Tile::PITCH) = kreg[i];
+#pragma unroll
+        for (uint32_t i = 0; i < Tile::NI; ++i) *(u32x4*)(ldsV + (vp ^ ((Tile::vswz(i * Tile::RPI)) << 4)) + i * Tile::RPI * Tile::PITCH) = vreg[i];
         const KeyRun now = x;
         if (blk + 1 < j.end) {
             x = key_run<D>(a, j, blk + 1, 128, wave * 32, 32);
@@ -329,11 +361,15 @@ __global__ __launch_bounds__(256, MR == 1 ? 2 : 1) void tree_attn_few(const Tree
             uint32_t vis[MR][1];
 #pragma unroll
             for (int r = 0; r < MR; ++r) vis[r][0] = now.drafted ? tree_bits(a, j.b, token[r], now.first, now.n) : now.n >= 32 ? ~0u : (1u << now.n) - 1u;
-            tree_step<T, D, 1, MR>(row, ldsK, ldsV, lane, a.scale, vis, now.drafted || now.n < 32, odd, (T*)ldsK);
+            const uint32_t qoff = opaque(Tile::koff(lane));
+            tree_step<T, D, 1, MR>(row, [&](int r, int kk) __attribute__((always_inline)) { return *(const V8*)(ldsQ + (qoff ^ (kk * 32u)) + r * Tile::BYTES); },
+                                   ldsK, ldsV, lane, a.scale, vis, now.drafted || now.n < 32);
         }
         asm volatile("" ::: "memory");
         __builtin_amdgcn_wave_barrier();
     }
+#pragma unroll
+    for (int r = 0; r < MR; ++r) row[r].l += __shfl_xor(row[r].l, 32);
     // ---- the four waves joined ----
 #pragma unroll
     for (int r = 0; r < MR; ++r) {
@@ -370,7 +406,7 @@ __global__ __launch_bounds__(256, MR == 1 ? 2 : 1) void tree_attn_few(const Tree
             f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int w = 0; w < 4; ++w) o += *(const f32x4*)((const float*)(lds + w * WAVE) + rr * (D + 4) + d);
-            store_row4<T, D>(a, j, r * 32 + rr, d, o, mm, L);
+            store_row4<T, D>(a, j, r * 32 + rr, d, o, mm, L, odd != 0, 128);
         }
     }
 }
@@ -382,10 +418,10 @@ __global__ __launch_bounds__(256, MR == 1 ? 2 : 1) void tree_attn_few(const Tree
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
     using Tile = KeyTile<T, D>;
+    using V8 = typename Mma<T>::V8;
     constexpr uint32_t BLK = 2 * Tile::BYTES;                          // 64 rows of K (or of V)
     __shared__ __align__(16) char lds[2][2 * BLK];
-    __shared__ T scratch[4][32 * 32];
-    __shared__ uint32_t odd_flag[2];                                   // the buffer holds drafted values that are not finite
+    __shared__ uint32_t odd;                                           // a drafted value is not finite
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6);
     const uint32_t row_blocks = (a.rows + TREE_ROW_BLOCK - 1) / TREE_ROW_BLOCK;
     const uint32_t slot = blockIdx.x >> 3;
@@ -394,9 +430,16 @@ __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
     const TreeJob j = tree_job(a, unit, 64);
     const uint32_t r0 = rb * TREE_ROW_BLOCK, t_last = (min(r0 + TREE_ROW_BLOCK, a.rows) - 1) / a.group;
     if (j.begin >= j.end || r0 / a.group >= j.drafted) return;
-    RowState<T, D> row[1];
+    RowState<D> row[1];
+    clear_row(row[0]);
     const uint32_t at = r0 + wave * 32 + (lane & 31u);
-    load_row(row[0], a, j, at, lane >> 5);
+    V8 qf[D / 16];
+    {
+        const T* const q = query_row<T>(a, j, at);
+        const V8 zero = {};
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) qf[kk] = q ? *(const V8*)(q + kk * 16 + (lane >> 5) * 8) : zero;
+    }
     const uint32_t token = min(at, a.rows - 1) / a.group;
     // without a tree nothing behind the block's last token is seen
     const uint32_t end = a.tree ? j.end : min(j.end, max(j.begin, j.cache_blocks + t_last / 64 + 1));
@@ -404,26 +447,29 @@ __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
     const uint32_t lrow = wave * (Tile::RPI * NI) + lane / Tile::CHUNKS, chunk = lane % Tile::CHUNKS;
     u32x4 kreg[NI], vreg[NI];
     auto fetch = [&](const KeyRun& x) __attribute__((always_inline)) {
-        const uint32_t bytes = uni(run_bytes<D>(x));
+        const uint32_t bytes = uni(run_bytes<D>(x)), first = lrow * x.pitch + chunk * 16;
         const OperandBuf K(uni_ptr(x.k), bytes), V(uni_ptr(x.v), bytes);
 #pragma unroll
-        for (uint32_t i = 0; i < NI; ++i) {
-            kreg[i] = K.load16((i * Tile::RPI + lrow) * x.pitch + chunk * 16, 0);
-            vreg[i] = V.load16((i * Tile::RPI + lrow) * x.pitch + chunk * 16, 0);
-        }
-    };
-    auto put = [&](uint32_t buf, bool drafted) __attribute__((always_inline)) {
-        bool bad = false;
+        for (uint32_t i = 0; i < NI; ++i) kreg[i] = K.load16(first, i * Tile::RPI * x.pitch);
 #pragma unroll
-        for (uint32_t i = 0; i < NI; ++i) {
-            const uint32_t rr = i * Tile::RPI + lrow;
-            *(u32x4*)(lds[buf] + rr * Tile::PITCH + ((chunk ^ Tile::kswz(rr)) << 4)) = kreg[i];
-            *(u32x4*)(lds[buf] + BLK + rr * Tile::PITCH + ((chunk ^ Tile::vswz(rr)) << 4)) = vreg[i];
-            if (drafted) bad |= any_not_finite<T>(vreg[i]);
-        }
-        if (drafted && __ballot(bad) && lane == 0) odd_flag[buf] = 1;
+        for (uint32_t i = 0; i < NI; ++i) vreg[i] = V.load16(first, i * Tile::RPI * x.pitch);
     };
-    if (tid < 2) odd_flag[tid] = 0;
+    // (lrow is wave * 16 and a lane's row, so the swizzles of later rows differ by exclusive-ors alone)
+    const uint32_t kput = lrow * Tile::PITCH + ((chunk ^ Tile::kswz(lrow)) << 4), vput = lrow * Tile::PITCH + ((chunk ^ Tile::vswz(lrow)) << 4);
+    auto put = [&](uint32_t buf, bool drafted) __attribute__((always_inline)) {
+        const uint32_t kp = opaque(kput), vp = opaque(vput);
+        if (drafted) {
+            bool bad = false;
+#pragma unroll
+            for (uint32_t i = 0; i < NI; ++i) bad |= without_not_finite<T>(vreg[i]);
+            if (bad) odd = 1;
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < NI; ++i) *(u32x4*)(lds[buf] + (kp ^ ((Tile::kswz(i * Tile::RPI)) << 4)) + i * Tile::RPI * Tile::PITCH) = kreg[i];
+#pragma unroll
+        for (uint32_t i = 0; i < NI; ++i) *(u32x4*)(lds[buf] + BLK + (vp ^ ((Tile::vswz(i * Tile::RPI)) << 4)) + i * Tile::RPI * Tile::PITCH) = vreg[i];
+    };
+    if (tid == 0) odd = 0;
     __syncthreads();
     KeyRun x = key_run<D>(a, j, j.begin, 64, 0, 64), next = x;
     if (j.begin < end) {
@@ -434,14 +480,13 @@ __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
     __syncthreads();
     for (uint32_t blk = j.begin; blk < end; ++blk) {
         const uint32_t buf = (blk - j.begin) & 1u;
-        const bool odd = odd_flag[buf] != 0;
         uint32_t vis[1][2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const uint32_t n = x.n > 32u * t ? min(32u, x.n - 32u * t) : 0u;
             vis[0][t] = x.drafted ? tree_bits(a, j.b, token, x.first + 32 * t, n) : n >= 32 ? ~0u : (1u << n) - 1u;
         }
-        tree_step<T, D, 2, 1>(row, lds[buf], lds[buf] + BLK, lane, a.scale, vis, x.drafted || x.n < 64, x.drafted && odd, scratch[wave]);
+        tree_step<T, D, 2, 1>(row, [&](int, int kk) __attribute__((always_inline)) { return qf[kk]; }, lds[buf], lds[buf] + BLK, lane, a.scale, vis, x.drafted || x.n < 64);
         if (blk + 1 < end) {
             put(buf ^ 1u, next.drafted);
             x = next;
@@ -450,6 +495,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
         __syncthreads();
     }
     const uint32_t h2 = lane >> 5;
+    row[0].l += __shfl_xor(row[0].l, 32);
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
 #pragma unroll
@@ -457,7 +503,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
             f32x4 o;
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = row[0].o[b][4 * g + e];
-            store_row4<T, D>(a, j, at, 32 * b + 8 * g + 4 * h2, o, row[0].m, row[0].l);
+            store_row4<T, D>(a, j, at, 32 * b + 8 * g + 4 * h2, o, row[0].m, row[0].l, odd != 0, 64);
         }
 }
 
