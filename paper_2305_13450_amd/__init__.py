@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -201,12 +202,13 @@ def _lib() -> ctypes.CDLL:
         L.depsync_conv_chain_n_policy.argtypes = [ctypes.POINTER(ConvChainNDesc), vp, ctypes.POINTER(i32)]
         L.dep_gemm_chain_static.argtypes = [ctypes.POINTER(GemmChainDesc), i32, ctypes.POINTER(PolicyParams), vp]
         szp = ctypes.POINTER(ctypes.c_size_t)
-        L.dep_tree_attn.argtypes = [ctypes.POINTER(TreeAttnDesc), vp, ctypes.c_size_t, vp]
-        L.depsync_tree_attn_workspace.argtypes = [ctypes.POINTER(TreeAttnDesc), i32, szp]
-        L.dep_cache_append.argtypes = [ctypes.POINTER(CacheAppendDesc), vp]
-        L.dep_cache_weights.argtypes = [ctypes.POINTER(CacheWeightsDesc), vp]
-        L.dep_cache_evict.argtypes = [ctypes.POINTER(CacheEvictDesc), vp, ctypes.c_size_t, vp]
-        L.depsync_cache_evict_workspace.argtypes = [ctypes.POINTER(CacheEvictDesc), szp]
+        # (descriptors come by reference or packed into bytes)
+        L.dep_tree_attn.argtypes = [vp, vp, ctypes.c_size_t, vp]
+        L.depsync_tree_attn_workspace.argtypes = [vp, i32, szp]
+        L.dep_cache_append.argtypes = [vp, vp]
+        L.dep_cache_weights.argtypes = [vp, vp]
+        L.dep_cache_evict.argtypes = [vp, vp, ctypes.c_size_t, vp]
+        L.depsync_cache_evict_workspace.argtypes = [vp, szp]
         L.depsync_row_major.argtypes = [i32] * 4
         L.depsync_policy_sem.argtypes = [i32] * 6
         L.depsync_policy_value.argtypes = [i32] * 4
@@ -613,55 +615,70 @@ def conv_chain_n_check_waits(desc: ConvChainNDesc, kind: int, n_cu: int = 0, **p
 
 # ---- the cache of token generation ----------------------------------------------------------
 
-def _dev4(t, name: str, shape, dtype):
-    """A [batch, token, head, head_dim] device tensor of this shape (None: any size) with contiguous rows -> its pointer."""
-    if not t.is_cuda or t.dim() != 4 or t.stride(3) != 1:
-        raise ValueError(f"{name} must be a 4-D device tensor with contiguous rows")
-    if t.dtype != dtype:
+# These calls are short, so their descriptors are packed in one go (in the header's order, as the classes above have it) and each tensor is
+# asked once for what is needed: 35 fields set one by one and the former checks took 23 us a call, three times the two launches.
+
+_P_TREE = struct.Struct("8i P3q 2P3q 2P3q 3Pq f4x P3q P")
+_P_APPEND = struct.Struct("7i4x 2P3q 2P3q 7P")
+_P_WEIGHTS = struct.Struct("9i4x P3q P P3q 3P f4x P")
+_P_EVICT = struct.Struct("8i 2P3q 4P i4x 2P3q 2P")
+
+
+def _t4(t, name: str, dtype, device: int, shape=None):
+    """Pointer and the first three strides of a [batch, token, head, head_dim] tensor on this device with contiguous rows."""
+    s = t.stride()
+    if t.get_device() != device or device < 0 or len(s) != 4 or s[3] != 1:
+        raise ValueError(f"{name} must be a 4-D tensor with contiguous rows on the device of the others")
+    if t.dtype is not dtype:
         raise TypeError("all 16-bit tensors of a call must share one element type")
-    if any(want is not None and n != want for n, want in zip(t.shape, shape)):
-        raise ValueError(f"{name}: shape {tuple(t.shape)} where {tuple('any' if w is None else w for w in shape)} is needed")
-    return t.data_ptr()
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)} where {tuple(shape)} is needed")
+    return t.data_ptr(), s[0], s[1], s[2]
 
 
-def _dev_array(t, name: str, shape, dtype):
-    """A contiguous device tensor of this shape and type -> its pointer; None -> NULL."""
+def _pair(a, b, name: str, dtype, device: int, shape):
+    """The pointers of two tensors alike (keys and values), and their strides."""
+    pa, s0, s1, s2 = _t4(a, "k_" + name, dtype, device, shape)
+    pb, *sb = _t4(b, "v_" + name, dtype, device, shape)
+    if sb != [s0, s1, s2]:
+        raise ValueError(f"k_{name} and v_{name} must have the same strides")
+    return pa, pb, s0, s1, s2
+
+
+def _arr(t, name: str, dtype, device: int, shape) -> int:
+    """Pointer of a contiguous tensor of this shape and type on this device; None -> 0."""
     if t is None:
-        return None
-    if not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != tuple(shape) or t.dtype != dtype:
-        raise ValueError(f"{name} must be a contiguous device tensor of {dtype} and shape {tuple(shape)}")
+        return 0
+    if t.get_device() != device or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor of {dtype} and shape {tuple(shape)} on the device of the others")
     return t.data_ptr()
 
 
-def _enqueue(call, tensors):
-    """call() with the tensors' device current; they have to be on one."""
+def _on_device(index: int, call):
+    """call() with this device current."""
     import torch
-    devices = {t.device for t in tensors if t is not None}
-    if len(devices) != 1:
-        raise ValueError("all tensors of a call must be on one device")
-    index = devices.pop().index
     if index == torch.cuda.current_device():
         return call()
     with torch.cuda.device(index):
         return call()
 
 
-def _workspace(nbytes: int, given, like, stream):
-    """`given`, if it is large enough, or memory that torch's allocator ties to `stream`: (tensor to keep, pointer, bytes)."""
+def _workspace(nbytes: int, given, device: int, stream):
+    """`given`, or memory that torch's allocator ties to `stream`: (tensor to keep, pointer, bytes)."""
     import torch
     if given is not None:
-        if not given.is_cuda or not given.is_contiguous() or given.device != like.device:
+        if given.get_device() != device or not given.is_contiguous():
             raise ValueError("the workspace must be a contiguous tensor on the device of the others")
         return given, given.data_ptr(), given.numel() * given.element_size()
     if nbytes == 0:
         return None, None, 0
     handle = _stream_handle(stream) or 0
-    if handle == torch.cuda.current_stream(like.device).cuda_stream:
-        t = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    if handle == torch.cuda.current_stream(device).cuda_stream:
+        t = torch.empty(nbytes, dtype=torch.uint8, device=device)
     else:
-        own = torch.cuda.default_stream(like.device) if handle == 0 else torch.cuda.ExternalStream(handle, device=like.device)
+        own = torch.cuda.default_stream(device) if handle == 0 else torch.cuda.ExternalStream(handle, device=device)
         with torch.cuda.stream(own):
-            t = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+            t = torch.empty(nbytes, dtype=torch.uint8, device=device)
     return t, t.data_ptr(), nbytes
 
 
@@ -687,47 +704,39 @@ def tree_mask(parents):
     return torch.tensor(rows, dtype=torch.int64).reshape(*p.shape, -1)
 
 
-def _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached) -> TreeAttnDesc:
+def _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached):
+    """(descriptor, device) of a call."""
     import torch
+    device, dtype = q.get_device(), q.dtype
+    code = _dtype_code(q)
     if q.dim() != 4 or k_new.dim() != 4:
         raise ValueError("q and k_new must be [batch, tokens, heads, head_dim]")
     B, T, Hq, D = q.shape
     Hk = k_new.shape[2]
-    d = TreeAttnDesc()
-    d.dtype = _dtype_code(q)
-    d.batch, d.tokens, d.heads, d.kv_heads, d.head_dim = B, T, Hq, Hk, D
-    d.q = _dev4(q, "q", q.shape, q.dtype)
-    d.q_batch, d.q_token, d.q_head = q.stride()[:3]
-    d.k_new, d.v_new = _dev4(k_new, "k_new", (B, T, Hk, D), q.dtype), _dev4(v_new, "v_new", (B, T, Hk, D), q.dtype)
-    if k_new.stride() != v_new.stride():
-        raise ValueError("k_new and v_new must have the same strides")
-    d.new_batch, d.new_token, d.new_head = k_new.stride()[:3]
+    new = _pair(k_new, v_new, "new", dtype, device, (B, T, Hk, D))
+    cap, cache, lengths = 0, (0, 0, 0, 0, 0), 0
     if k_cache is not None:
-        if v_cache is None or cached is None:
-            raise ValueError("a cache is k_cache, v_cache and cached")
-        _cache_fields(d, k_cache, v_cache, B, Hk, D, q.dtype)
-        d.cached = _dev_array(cached, "cached", (B,), torch.int32)
-    d.max_cached = max_cached or 0
-    d.drafted = _dev_array(drafted, "drafted", (B,), torch.int32)
+        if v_cache is None or cached is None or k_cache.dim() != 4:
+            raise ValueError("a cache is k_cache and v_cache [batch, capacity, kv_heads, head_dim], and cached")
+        cap = k_cache.shape[1]
+        cache = _pair(k_cache, v_cache, "cache", dtype, device, (B, cap, Hk, D))
+        lengths = _arr(cached, "cached", torch.int32, device, (B,))
+    tree_ptr, tree_batch = 0, 0
     if tree is not None:
         words = (T, (T + 63) // 64)
-        d.tree = _dev_array(tree, "tree", words if tree.dim() == 2 else (B, *words), torch.int64)
-        d.tree_batch = 0 if tree.dim() == 2 else words[0] * words[1]
-    d.scale = scale or 0.0
-    d.out = _dev4(out, "out", (B, T, Hq, D), q.dtype)
-    d.out_batch, d.out_token, d.out_head = out.stride()[:3]
-    d.lse = _dev_array(lse, "lse", (B, T, Hq), torch.float32)
-    return d
+        if tree.dim() == 2:
+            tree_ptr = _arr(tree, "tree", torch.int64, device, words)
+        else:
+            tree_ptr, tree_batch = _arr(tree, "tree", torch.int64, device, (B, *words)), words[0] * words[1]
+    return _P_TREE.pack(B, T, Hq, Hk, D, code, cap, max_cached or 0, *_t4(q, "q", dtype, device), *new, *cache, lengths,
+                        _arr(drafted, "drafted", torch.int32, device, (B,)), tree_ptr, tree_batch, scale or 0.0,
+                        *_t4(out, "out", dtype, device, (B, T, Hq, D)), _arr(lse, "lse", torch.float32, device, (B, T, Hq))), device
 
 
-def _cache_fields(d, k_cache, v_cache, B, Hk, D, dtype) -> None:
-    d.k_cache = _dev4(k_cache, "k_cache", (B, None, Hk, D), dtype)
-    d.capacity = k_cache.shape[1]
-    d.cache_batch, d.cache_token, d.cache_head = k_cache.stride()[:3]
-    if v_cache is not None:
-        d.v_cache = _dev4(v_cache, "v_cache", k_cache.shape, dtype)
-        if k_cache.stride() != v_cache.stride():
-            raise ValueError("k_cache and v_cache must have the same strides")
+def _tree_attn_bytes(d, n_cu: int) -> int:
+    need = ctypes.c_size_t(0)
+    _check(_lib().depsync_tree_attn_workspace(d, n_cu, ctypes.byref(need)), "depsync_tree_attn_workspace")
+    return need.value
 
 
 def dep_tree_attn(q, k_new, v_new, k_cache, v_cache, cached, out, lse=None, tree=None, drafted=None, scale: Optional[float] = None,
@@ -737,32 +746,27 @@ def dep_tree_attn(q, k_new, v_new, k_cache, v_cache, cached, out, lse=None, tree
     q, out [B, T, Hq, D]; k_new, v_new [B, T, Hk, D]; k_cache, v_cache [B, capacity, Hk, D] (None: no cache) of which sequence b has
     cached[b] rows (int32).  drafted[b] (int32): the tokens that sequence b has; the others' rows of out and lse are left alone.
     lse [B, T, Hq] (float32) receives the logarithm of each row's sum.  max_cached: the most rows that a sequence has, where the host knows."""
-    d = _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached)
+    d, device = _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached)
 
     def call():
-        need = ctypes.c_size_t(0)
-        _check(_lib().depsync_tree_attn_workspace(ctypes.byref(d), 0, ctypes.byref(need)), "dep_tree_attn")
-        keep, ptr, size = _workspace(need.value, workspace, q, stream)
-        _check(_lib().dep_tree_attn(ctypes.byref(d), ptr, size, _stream_handle(stream)), "dep_tree_attn")
-    _enqueue(call, (q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted))
+        keep, ptr, size = _workspace(0 if workspace is not None else _tree_attn_bytes(d, 0), workspace, device, stream)
+        _check(_lib().dep_tree_attn(d, ptr, size, _stream_handle(stream)), "dep_tree_attn")
+    _on_device(device, call)
 
 
 def tree_attn_workspace(q, k_new, v_new, k_cache, v_cache, cached, out, lse=None, tree=None, drafted=None, scale: Optional[float] = None,
                         max_cached: Optional[int] = None, n_cu: int = 0) -> int:
     """Bytes of workspace that dep_tree_attn with these arguments needs."""
-    d = _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached)
-    need = ctypes.c_size_t(0)
-    _check(_lib().depsync_tree_attn_workspace(ctypes.byref(d), n_cu, ctypes.byref(need)), "depsync_tree_attn_workspace")
-    return need.value
+    d, device = _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached)
+    return _on_device(device, lambda: _tree_attn_bytes(d, n_cu))
 
 
-def _accepted_fields(d, tokens, accepted, n_accepted) -> None:
+def _accepted(B: int, tokens: int, accepted, n_accepted, device: int):
     import torch
     if accepted is not None and accepted.dim() != 2:
         raise ValueError("accepted must be [batch, n_max]")
-    d.n_max = tokens if accepted is None else accepted.shape[1]
-    d.accepted = _dev_array(accepted, "accepted", (d.batch, d.n_max), torch.int32)
-    d.n_accepted = _dev_array(n_accepted, "n_accepted", (d.batch,), torch.int32)
+    n_max = tokens if accepted is None else accepted.shape[1]
+    return n_max, _arr(accepted, "accepted", torch.int32, device, (B, n_max)), _arr(n_accepted, "n_accepted", torch.int32, device, (B,))
 
 
 def dep_cache_append(k_new, v_new, k_cache, v_cache, cached, cached_out, accepted=None, n_accepted=None, weights=None, pos=None, start=None,
@@ -770,23 +774,19 @@ def dep_cache_append(k_new, v_new, k_cache, v_cache, cached, cached_out, accepte
     """Enqueue: the keys and values of drafted tokens accepted[b, :n_accepted[b]] (int32; None: the first ones) go to rows cached[b].. of the cache,
     their weights [B, Hk, capacity] (float32) become 0, their positions (int32, same shape) start[b].., and cached_out = cached + n."""
     import torch
-    if k_new.dim() != 4:
-        raise ValueError("k_new must be [batch, tokens, kv_heads, head_dim]")
-    d = CacheAppendDesc()
-    d.dtype = _dtype_code(k_new)
-    d.batch, d.tokens, d.kv_heads, d.head_dim = k_new.shape
-    d.k_new, d.v_new = _dev4(k_new, "k_new", k_new.shape, k_new.dtype), _dev4(v_new, "v_new", k_new.shape, k_new.dtype)
-    if k_new.stride() != v_new.stride():
-        raise ValueError("k_new and v_new must have the same strides")
-    d.new_batch, d.new_token, d.new_head = k_new.stride()[:3]
-    _cache_fields(d, k_cache, v_cache, d.batch, d.kv_heads, d.head_dim, k_new.dtype)
-    d.cached, d.cached_out = _dev_array(cached, "cached", (d.batch,), torch.int32), _dev_array(cached_out, "cached_out", (d.batch,), torch.int32)
-    _accepted_fields(d, d.tokens, accepted, n_accepted)
-    rows = (d.batch, d.kv_heads, d.capacity)
-    d.weights, d.pos = _dev_array(weights, "weights", rows, torch.float32), _dev_array(pos, "pos", rows, torch.int32)
-    d.start = _dev_array(start, "start", (d.batch,), torch.int32)
-    _enqueue(lambda: _check(_lib().dep_cache_append(ctypes.byref(d), _stream_handle(stream)), "dep_cache_append"),
-             (k_new, v_new, k_cache, v_cache, cached, cached_out, accepted, n_accepted, weights, pos, start))
+    device, dtype = k_new.get_device(), k_new.dtype
+    code = _dtype_code(k_new)
+    if k_new.dim() != 4 or k_cache.dim() != 4:
+        raise ValueError("k_new and k_cache must be [batch, tokens or capacity, kv_heads, head_dim]")
+    B, T, Hk, D = k_new.shape
+    cap = k_cache.shape[1]
+    i32 = torch.int32
+    n_max, acc, n_acc = _accepted(B, T, accepted, n_accepted, device)
+    d = _P_APPEND.pack(B, T, Hk, D, code, cap, n_max, *_pair(k_new, v_new, "new", dtype, device, (B, T, Hk, D)),
+                       *_pair(k_cache, v_cache, "cache", dtype, device, (B, cap, Hk, D)), _arr(cached, "cached", i32, device, (B,)),
+                       _arr(cached_out, "cached_out", i32, device, (B,)), acc, n_acc, _arr(weights, "weights", torch.float32, device, (B, Hk, cap)),
+                       _arr(pos, "pos", i32, device, (B, Hk, cap)), _arr(start, "start", i32, device, (B,)))
+    _on_device(device, lambda: _check(_lib().dep_cache_append(d, _stream_handle(stream)), "dep_cache_append"))
 
 
 def dep_cache_weights(q, lse, k_cache, cached, weights, accepted=None, n_accepted=None, scale: Optional[float] = None,
@@ -794,50 +794,47 @@ def dep_cache_weights(q, lse, k_cache, cached, weights, accepted=None, n_accepte
     """Enqueue weights[b, h, k] += the attention weight that cached row k received from the accepted tokens, whose own rows are the last
     of cached[b].  q [B, T, Hq, D] and lse [B, T, Hq] are dep_tree_attn's; weights is [B, Hk, capacity] (float32)."""
     import torch
+    device, dtype = q.get_device(), q.dtype
+    code = _dtype_code(q)
     if q.dim() != 4 or k_cache.dim() != 4:
-        raise ValueError("q and k_cache must be [batch, tokens, heads, head_dim]")
-    d = CacheWeightsDesc()
-    d.dtype = _dtype_code(q)
-    d.batch, d.tokens, d.heads, d.head_dim = q.shape
-    d.kv_heads = k_cache.shape[2]
-    d.q = _dev4(q, "q", q.shape, q.dtype)
-    d.q_batch, d.q_token, d.q_head = q.stride()[:3]
-    d.lse = _dev_array(lse, "lse", q.shape[:3], torch.float32)
-    d.k_cache = _dev4(k_cache, "k_cache", (d.batch, None, d.kv_heads, d.head_dim), q.dtype)
-    d.capacity = k_cache.shape[1]
-    d.cache_batch, d.cache_token, d.cache_head = k_cache.stride()[:3]
-    d.cached = _dev_array(cached, "cached", (d.batch,), torch.int32)
-    _accepted_fields(d, d.tokens, accepted, n_accepted)
-    d.scale, d.max_cached = scale or 0.0, max_cached or 0
-    d.weights = _dev_array(weights, "weights", (d.batch, d.kv_heads, d.capacity), torch.float32)
-    _enqueue(lambda: _check(_lib().dep_cache_weights(ctypes.byref(d), _stream_handle(stream)), "dep_cache_weights"),
-             (q, lse, k_cache, cached, weights, accepted, n_accepted))
+        raise ValueError("q and k_cache must be [batch, tokens or capacity, heads, head_dim]")
+    B, T, Hq, D = q.shape
+    cap, Hk = k_cache.shape[1:3]
+    n_max, acc, n_acc = _accepted(B, T, accepted, n_accepted, device)
+    d = _P_WEIGHTS.pack(B, T, Hq, Hk, D, code, cap, max_cached or 0, n_max, *_t4(q, "q", dtype, device), _arr(lse, "lse", torch.float32, device, (B, T, Hq)),
+                        *_t4(k_cache, "k_cache", dtype, device, (B, cap, Hk, D)), _arr(cached, "cached", torch.int32, device, (B,)), acc, n_acc,
+                        scale or 0.0, _arr(weights, "weights", torch.float32, device, (B, Hk, cap)))
+    _on_device(device, lambda: _check(_lib().dep_cache_weights(d, _stream_handle(stream)), "dep_cache_weights"))
 
 
-def _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out) -> CacheEvictDesc:
+def _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out):
+    """(descriptor, device) of a call."""
     import torch
+    device, dtype = k_cache.get_device(), k_cache.dtype
+    code = _dtype_code(k_cache)
     if k_cache.dim() != 4:
         raise ValueError("k_cache must be [batch, capacity, kv_heads, head_dim]")
-    d = CacheEvictDesc()
-    d.dtype = _dtype_code(k_cache)
-    d.batch, _, d.kv_heads, d.head_dim = k_cache.shape
-    _cache_fields(d, k_cache, v_cache, d.batch, d.kv_heads, d.head_dim, k_cache.dtype)
-    rows = (d.batch, d.kv_heads, d.capacity)
-    d.weights, d.pos = _dev_array(weights, "weights", rows, torch.float32), _dev_array(pos, "pos", rows, torch.int32)
-    d.cached, d.cached_out = _dev_array(cached, "cached", (d.batch,), torch.int32), _dev_array(cached_out, "cached_out", (d.batch,), torch.int32)
-    d.budget, d.recent, d.max_cached = budget, recent, max_cached or 0
+    B, cap, Hk, D = k_cache.shape
+    f32, i32 = torch.float32, torch.int32
+    given = [x is not None for x in (k_out, v_out, weights_out, pos_out)]
+    if any(given) != all(given):
+        raise DepsyncError(EINVAL, "dep_cache_evict: k_out, v_out, weights_out and pos_out go together")
+    cap_out, outs, rows_out = 0, (0, 0, 0, 0, 0), (0, 0)
     if k_out is not None:
-        d.k_out = _dev4(k_out, "k_out", (d.batch, None, d.kv_heads, d.head_dim), k_cache.dtype)
-        d.v_out = None if v_out is None else _dev4(v_out, "v_out", k_out.shape, k_cache.dtype)
-        if v_out is not None and k_out.stride() != v_out.stride():
-            raise ValueError("k_out and v_out must have the same strides")
-        d.capacity_out = k_out.shape[1]
-        d.out_batch, d.out_token, d.out_head = k_out.stride()[:3]
-    elif v_out is not None:
-        raise ValueError("the other buffers are k_out, v_out, weights_out and pos_out together")
-    rows = (d.batch, d.kv_heads, d.capacity_out)
-    d.weights_out, d.pos_out = _dev_array(weights_out, "weights_out", rows, torch.float32), _dev_array(pos_out, "pos_out", rows, torch.int32)
-    return d
+        if k_out.dim() != 4:
+            raise ValueError("k_out must be [batch, capacity, kv_heads, head_dim]")
+        cap_out = k_out.shape[1]
+        outs = _pair(k_out, v_out, "out", dtype, device, (B, cap_out, Hk, D))
+        rows_out = _arr(weights_out, "weights_out", f32, device, (B, Hk, cap_out)), _arr(pos_out, "pos_out", i32, device, (B, Hk, cap_out))
+    return _P_EVICT.pack(B, Hk, D, code, cap, max_cached or 0, budget, recent, *_pair(k_cache, v_cache, "cache", dtype, device, (B, cap, Hk, D)),
+                         _arr(weights, "weights", f32, device, (B, Hk, cap)), _arr(pos, "pos", i32, device, (B, Hk, cap)),
+                         _arr(cached, "cached", i32, device, (B,)), _arr(cached_out, "cached_out", i32, device, (B,)), cap_out, *outs, *rows_out), device
+
+
+def _cache_evict_bytes(d) -> int:
+    need = ctypes.c_size_t(0)
+    _check(_lib().depsync_cache_evict_workspace(d, ctypes.byref(need)), "depsync_cache_evict_workspace")
+    return need.value
 
 
 def dep_cache_evict(k_cache, v_cache, weights, pos, cached, cached_out, budget: int, recent: int = 0, max_cached: Optional[int] = None,
@@ -845,23 +842,19 @@ def dep_cache_evict(k_cache, v_cache, weights, pos, cached, cached_out, budget: 
     """Enqueue: every sequence and head keeps `budget` rows: the `recent` newest by position, then the heaviest, among equals the lowest row.
     In place kept rows behind the budget fill the places of those that go; into k_out .. pos_out (all four) the kept rows go in their order.
     cached_out = min(cached, budget)."""
-    d = _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out)
+    d, device = _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out)
 
     def call():
-        need = ctypes.c_size_t(0)
-        _check(_lib().depsync_cache_evict_workspace(ctypes.byref(d), ctypes.byref(need)), "dep_cache_evict")
-        keep, ptr, size = _workspace(need.value, workspace, k_cache, stream)
-        _check(_lib().dep_cache_evict(ctypes.byref(d), ptr, size, _stream_handle(stream)), "dep_cache_evict")
-    _enqueue(call, (k_cache, v_cache, weights, pos, cached, cached_out, k_out, v_out, weights_out, pos_out))
+        keep, ptr, size = _workspace(0 if workspace is not None else _cache_evict_bytes(d), workspace, device, stream)
+        _check(_lib().dep_cache_evict(d, ptr, size, _stream_handle(stream)), "dep_cache_evict")
+    _on_device(device, call)
 
 
 def cache_evict_workspace(k_cache, v_cache, weights, pos, cached, cached_out, budget: int, recent: int = 0, max_cached: Optional[int] = None,
                           k_out=None, v_out=None, weights_out=None, pos_out=None) -> int:
     """Bytes of workspace that dep_cache_evict with these arguments needs."""
-    d = _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out)
-    need = ctypes.c_size_t(0)
-    _check(_lib().depsync_cache_evict_workspace(ctypes.byref(d), ctypes.byref(need)), "depsync_cache_evict_workspace")
-    return need.value
+    d, _ = _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out)
+    return _cache_evict_bytes(d)
 
 
 # ---- host mirrors -------------------------------------------------------------------------

@@ -53,8 +53,20 @@ int tree_check(const depsync_tree_attn_desc* d) {
     return d->max_cached < 0 ? DEPSYNC_EINVAL : DEPSYNC_OK;
 }
 
-// How the key axis of dep_tree_attn is cut.  A workgroup's start, its rows' queries and its results cost about as much as reading
-// a block or two, so a part has two blocks at the least; beyond that, as many parts as give every CU four workgroups (two at a time).
+// How the key axis of dep_tree_attn is cut: few (sequence, head) pairs and row blocks leave CUs idle unless it is, but parts leave results of
+// 4 (head_dim + 2) bytes a row in memory, which a second kernel reads.  The model, in microseconds, fitted to times of 28 shapes under
+// up to 29 cuts each (1 to 2048 rows, caches of 0 to 120000; its choice is within 10 % of the best cut in all but three, 17 % in those):
+// a workgroup's start, a block of keys where its workgroup is alone on the CU and where two share it, the keys' way from HBM, the
+// second kernel and the results' way there and back.
+double tree_cost(int64_t base, int64_t part, int64_t blocks, int64_t pairs, int64_t rows, int64_t row_blocks, int head_dim, int n_cu, bool few) {
+    const int64_t parts = cdiv64(blocks, part), groups = base * parts, slots = 2 * (int64_t)n_cu;
+    const double at_once = (double)std::min(groups, slots), wide = head_dim / 128.0;
+    const double step = few ? 0.13 + 1.32 * wide : (at_once > n_cu ? 2.05 : 1.6) * (0.3 + 0.7 * wide);
+    const double hbm = at_once / row_blocks * (few ? TREE_FEW_KEYS : TREE_MANY_KEYS) * 4.0 * head_dim / 5.2e6;
+    const double join = parts > 1 ? 2.8 + (double)parts * pairs * rows * (head_dim + 2) * 8.0 / 4e6 : 0.0;
+    return (double)cdiv64(groups, slots) * (3.0 + part * std::cbrt(step * step * step + hbm * hbm * hbm)) + join;   // (between the larger and the sum)
+}
+
 int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t& bytes) {
     if (n_cu <= 0) {
         int dev = 0;
@@ -66,10 +78,24 @@ int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t
     const int64_t rows = (int64_t)d->tokens * a.group;
     if (rows > 1 << 24) return DEPSYNC_ENOTIMPL;
     a.rows = (uint32_t)rows;
-    const int64_t keys = tree_block_keys(a.rows), row_blocks = a.rows <= TREE_FEW_ROWS ? 1 : cdiv64(rows, TREE_ROW_BLOCK);
+    // Two workgroups of 32 rows, whose second finds the keys in L2, are ahead of one of 128 up to 64 rows (16 x 40 rows over 1000 keys 22 and
+    // 25 us, 52 over 120000 with heads of 64 49 and 53; 80 rows over 4000 17 and 18; 100 over 2000 33 and 31; 252 over 4096 66 and 48)
+    a.few = rows <= 64;
+    const int64_t keys = a.few ? TREE_FEW_KEYS : TREE_MANY_KEYS, row_blocks = cdiv64(rows, a.few ? TREE_FEW_ROWS : TREE_MANY_ROWS);
     const int64_t pairs = (int64_t)d->batch * d->kv_heads, base = pairs * row_blocks;
     const int64_t blocks = cdiv64(rows_hint(d->max_cached, d->capacity), keys) + cdiv64(d->tokens, keys);
-    const int64_t part = std::min(blocks, std::max<int64_t>(2, cdiv64(blocks * base, 4 * (int64_t)n_cu)));
+    int64_t part = blocks;
+    double best = tree_cost(base, part, blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few);
+    for (int64_t rounds = 1; rounds <= 4; ++rounds) {             // parts that fill the chip a whole number of times
+        const int64_t parts = std::min(blocks, std::max<int64_t>(1, rounds * 2 * n_cu / base)), p = cdiv64(blocks, parts);
+        const double t = tree_cost(base, p, blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few);
+        if (t < best) { best = t; part = p; }
+        if (p + 1 > blocks) continue;
+        for (int64_t q : {2 * p, 4 * p}) {                         // or fewer, where their results cost more
+            const double u = tree_cost(base, std::min(q, blocks), blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few);
+            if (u < best) { best = u; part = std::min(q, blocks); }
+        }
+    }
     a.part_blocks = (uint32_t)part;
     a.n_parts = (uint32_t)cdiv64(blocks, part);
     if (cdiv64(pairs * a.n_parts, 8) * 8 * row_blocks > MAX_BLOCKS || cdiv64(pairs * rows, 4) > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;

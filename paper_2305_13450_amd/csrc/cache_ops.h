@@ -20,6 +20,7 @@ struct TreeAttnArgs {
     int64_t tree_batch;
     uint32_t batch, tokens, heads, kv_heads, group, capacity;
     uint32_t rows;                        // tokens * group: query rows of one key and value head
+    uint32_t few;                         // 1: the form for few rows
     uint32_t n_parts, part_blocks;        // parts of the key axis, blocks of keys in each (the last part takes what is left)
     float scale;                          // scores to base-2 exponents
 };
@@ -60,10 +61,8 @@ struct CacheEvictArgs {
     uint32_t in_place;
 };
 
-// Keys of one block of the attention kernel: 128 where at most 64 query rows share a head's keys, else 64.
-constexpr uint32_t TREE_FEW_ROWS = 64;
-inline __host__ __device__ uint32_t tree_block_keys(uint32_t rows) { return rows <= TREE_FEW_ROWS ? 128u : 64u; }
-constexpr uint32_t TREE_ROW_BLOCK = 128;  // query rows of a workgroup beyond TREE_FEW_ROWS
+// The attention kernel's two forms: query rows of a workgroup and keys of a block.
+constexpr uint32_t TREE_FEW_ROWS = 32, TREE_FEW_KEYS = 128, TREE_MANY_ROWS = 128, TREE_MANY_KEYS = 64;
 
 hipError_t launch_tree_attn(const TreeAttnArgs& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t launch_tree_attn_bf16(const TreeAttnArgs& a, int head_dim, hipStream_t stream);

@@ -70,25 +70,24 @@ __device__ __forceinline__ float max_halves(float x) {
     return fmaxf(__builtin_bit_cast(float, lower), __builtin_bit_cast(float, upper));
 }
 
-// One step: KT tiles of 32 keys in LDS against MR groups of 32 rows.  vis: the tile's keys that a lane's row sees, one bit each.
+// One step: KT tiles of 32 keys in LDS against 32 rows.  vis: the tile's keys that a lane's row sees, one bit each.
 // Fragments are read two slices ahead of the MFMAs and the order is pinned: left alone the compiler reads them all at once, and spills, or each right
-// before the wait for it.  query(r, kk): the fragment of slice kk of row group r.
-template <typename T, int D, int KT, int MR, class Q>
-__device__ __forceinline__ void tree_step(RowState<D> (&row)[MR], Q query, const char* ldsK, const char* ldsV, uint32_t lane, float sc,
-                                          const uint32_t (&vis)[MR][KT], bool masked) {
+// before the wait for it.  query(kk): the rows' fragment of slice kk.
+template <typename T, int D, int KT, class Q>
+__device__ __forceinline__ void tree_step(RowState<D>& row, Q query, const char* ldsK, const char* ldsV, uint32_t lane, float sc,
+                                          const uint32_t (&vis)[KT], bool masked) {
     using Tile = KeyTile<T, D>;
     using M = Mma<T>;
     using V8 = typename M::V8;
     constexpr int KF = D / 16;
     const uint32_t h2 = lane >> 5;
     const uint32_t koff = opaque(Tile::koff(lane)), voff = opaque(Tile::voff(lane));
-    f32x16 st[MR][KT];
+    f32x16 st[KT];
     {
-        V8 kf[3], qf[3][MR];
+        V8 kf[3], qf[3];
         auto rd = [&](int i) __attribute__((always_inline)) {
             kf[i % 3] = *(const V8*)(ldsK + (koff ^ ((i % KF) * 32u)) + (i / KF) * Tile::BYTES);
-#pragma unroll
-            for (int r = 0; r < MR; ++r) qf[i % 3][r] = query(r, i % KF);
+            qf[i % 3] = query(i % KF);
         };
         rd(0); rd(1);
 #pragma unroll
@@ -97,52 +96,46 @@ __device__ __forceinline__ void tree_step(RowState<D> (&row)[MR], Q query, const
             if (i + 2 < KT * KF) rd(i + 2);
             if (i % KF == 0)
 #pragma unroll
-                for (int r = 0; r < MR; ++r)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) st[r][i / KF][v] = 0.0f;
-#pragma unroll
-            for (int r = 0; r < MR; ++r) st[r][i / KF] = M::mma(kf[i % 3], qf[i % 3][r], st[r][i / KF]);
+                for (int v = 0; v < 16; ++v) st[i / KF][v] = 0.0f;
+            st[i / KF] = M::mma(kf[i % 3], qf[i % 3], st[i / KF]);
         }
         __builtin_amdgcn_sched_barrier(0);
     }
-    V8 pf[MR][2 * KT];
-#pragma unroll
-    for (int r = 0; r < MR; ++r) {
-        if (masked) {
-#pragma unroll
-            for (int t = 0; t < KT; ++t)
-#pragma unroll
-                for (int v = 0; v < 16; ++v)
-                    if (!(vis[r][t] >> (8 * (v / 4) + 4 * h2 + v % 4) & 1u)) st[r][t][v] = -INFINITY;
-        }
-        float mx = -INFINITY;
+    if (masked) {
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
-            for (int v = 0; v < 16; v += 2) mx = fmaxf(fmaxf(mx, st[r][t][v]), st[r][t][v + 1]);
-        mx = max_halves(mx) * sc;
-        if (__ballot(mx > row[r].m)) {                               // (rarely, after the first steps)
-            const float m_new = fmaxf(row[r].m, mx);
-            const float alpha = row[r].m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(row[r].m - m_new);
-            row[r].m = m_new;
-            row[r].l *= alpha;
-#pragma unroll
-            for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) row[r].o[b][v] *= alpha;
-        }
-        const float ref = (row[r].m == -INFINITY ? 0.0f : row[r].m) - WEIGHT_OFF<T>;   // no key seen yet: keep the exponents finite
-        float sum[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int t = 0; t < KT; ++t)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[r][t][v], sc, -ref));
-                sum[v & 1] += p;                                     // summed in 32 bits, rounded to 16 for the product with V only
-                pf[r][2 * t + (v >> 3)][v & 7] = (T)p;
-            }
-        row[r].l += sum[0] + sum[1];
+            for (int v = 0; v < 16; ++v)
+                if (!(vis[t] >> (8 * (v / 4) + 4 * h2 + v % 4) & 1u)) st[t][v] = -INFINITY;
     }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int v = 0; v < 16; v += 2) mx = fmaxf(fmaxf(mx, st[t][v]), st[t][v + 1]);
+    mx = max_halves(mx) * sc;
+    if (__ballot(mx > row.m)) {                                      // (rarely, after the first steps)
+        const float m_new = fmaxf(row.m, mx);
+        const float alpha = row.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(row.m - m_new);
+        row.m = m_new;
+        row.l *= alpha;
+#pragma unroll
+        for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) row.o[b][v] *= alpha;
+    }
+    const float ref = (row.m == -INFINITY ? 0.0f : row.m) - WEIGHT_OFF<T>;   // no key seen yet: keep the exponents finite
+    V8 pf[2 * KT];
+    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[t][v], sc, -ref));
+            sum[v & 1] += p;                                         // summed in 32 bits, rounded to 16 for the product with V only
+            pf[2 * t + (v >> 3)][v & 7] = (T)p;
+        }
+    row.l += sum[0] + sum[1];
     typedef T T4 __attribute__((ext_vector_type(4)));
     T4 vf[3][2];
     constexpr int NB = D / 32, NV = 2 * KT * NB;
@@ -156,8 +149,7 @@ __device__ __forceinline__ void tree_step(RowState<D> (&row)[MR], Q query, const
         __builtin_amdgcn_sched_barrier(0);
         if (i + 2 < NV) rdv(i + 2);
         const V8 x = __builtin_shufflevector(vf[i % 3][0], vf[i % 3][1], 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-        for (int r = 0; r < MR; ++r) row[r].o[i % NB] = M::mma(x, pf[r][i / NB], row[r].o[i % NB]);
+        row.o[i % NB] = M::mma(x, pf[i / NB], row.o[i % NB]);
     }
     __builtin_amdgcn_sched_barrier(0);
 }
@@ -181,6 +173,12 @@ __device__ __forceinline__ TreeJob tree_job(const TreeAttnArgs& a, uint32_t unit
     j.begin = min(blocks, j.part * a.part_blocks);
     j.end = j.part + 1 == a.n_parts ? blocks : min(blocks, j.begin + a.part_blocks);
     return j;
+}
+// A pair's row blocks run on one XCD (every eighth workgroup does), one after the other, so that its keys come from HBM once.
+struct TreeUnit { uint32_t unit, row_block; };
+__device__ __forceinline__ TreeUnit tree_unit(uint32_t row_blocks) {
+    const uint32_t slot = blockIdx.x >> 3;
+    return {(slot / row_blocks) * 8 + (blockIdx.x & 7u), slot % row_blocks};
 }
 // Parts of a sequence that have blocks: the ones that leave results.
 __device__ __forceinline__ uint32_t tree_live_parts(const TreeAttnArgs& a, uint32_t cached, uint32_t drafted, uint32_t block_keys) {
@@ -289,25 +287,28 @@ __device__ __forceinline__ void store_row4(const TreeAttnArgs& a, const TreeJob&
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------------------------
-// At most 32 MR rows share a head's keys: the time is that of reading the keys and values once.  Each of the four waves walks 32
-// of a block's 128 keys by itself, with the next step's 16 KB on its way into registers while it works from its own 16 KB of LDS; no wave
+// 32 rows to a workgroup.  Where no more share a head's keys, the time is that of reading the keys and values once.  Each of the four waves walks
+// 32 of a block's 128 keys by itself, with the next step's 16 KB on its way into registers while it works from its own 16 KB of LDS; no wave
 // waits for another until the end, when their results are joined through LDS.
 template <typename T, int D> constexpr uint32_t tree_wave_bytes() {
     constexpr uint32_t stage = 2 * KeyTile<T, D>::BYTES, join = 32 * (D + 4) * 4;
     return stage > join ? stage : join;
 }
-template <typename T, int D, int MR>
-__global__ __launch_bounds__(256, MR == 1 ? 2 : 1) void tree_attn_few(const TreeAttnArgs a) {
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void tree_attn_few(const TreeAttnArgs a) {
     using Tile = KeyTile<T, D>;
     using V8 = typename Mma<T>::V8;
     constexpr uint32_t WAVE = tree_wave_bytes<T, D>();
     __shared__ __align__(16) char lds[4 * WAVE];
-    __shared__ __align__(16) char ldsQ[MR * Tile::BYTES];              // the queries, laid out like keys
+    __shared__ __align__(16) char ldsQ[Tile::BYTES];                  // the queries, laid out like keys
     __shared__ float ml[4][32][2];
     __shared__ uint32_t odd;                                           // a drafted value is not finite
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6);
-    const TreeJob j = tree_job(a, blockIdx.x, 128);
-    if (j.begin >= j.end) return;
+    const TreeUnit u = tree_unit((a.rows + TREE_FEW_ROWS - 1) / TREE_FEW_ROWS);
+    if (u.unit >= a.batch * a.n_parts * a.kv_heads) return;
+    const TreeJob j = tree_job(a, u.unit, TREE_FEW_KEYS);
+    const uint32_t r0 = u.row_block * TREE_FEW_ROWS;
+    if (j.begin >= j.end || r0 / a.group >= j.drafted) return;
     if (tid == 0) odd = 0;
     char* const ldsK = lds + wave * WAVE;
     char* const ldsV = ldsK + Tile::BYTES;
@@ -321,19 +322,15 @@ __global__ __launch_bounds__(256, MR == 1 ? 2 : 1) void tree_attn_few(const Tree
 #pragma unroll
         for (uint32_t i = 0; i < Tile::NI; ++i) vreg[i] = V.load16(first, i * Tile::RPI * x.pitch);
     };
-    KeyRun x = key_run<D>(a, j, j.begin, 128, wave * 32, 32);
+    KeyRun x = key_run<D>(a, j, j.begin, TREE_FEW_KEYS, wave * 32, 32);
     fetch(x);
-    RowState<D> row[MR];
-    uint32_t token[MR];
-#pragma unroll
-    for (int r = 0; r < MR; ++r) {
-        clear_row(row[r]);
-        token[r] = min(r * 32 + (lane & 31u), a.rows - 1) / a.group;
-        for (uint32_t i = tid; i < 32 * Tile::CHUNKS; i += 256) {
-            const uint32_t rr = i / Tile::CHUNKS, c = i % Tile::CHUNKS;
-            const T* q = query_row<T>(a, j, r * 32 + rr);
-            *(u32x4*)(ldsQ + r * Tile::BYTES + rr * Tile::PITCH + ((c ^ Tile::kswz(rr)) << 4)) = q ? ((const u32x4*)q)[c] : u32x4{0, 0, 0, 0};
-        }
+    RowState<D> row;
+    clear_row(row);
+    const uint32_t token = min(r0 + (lane & 31u), a.rows - 1) / a.group;
+    for (uint32_t i = tid; i < 32 * Tile::CHUNKS; i += 256) {
+        const uint32_t rr = i / Tile::CHUNKS, c = i % Tile::CHUNKS;
+        const T* q = query_row<T>(a, j, r0 + rr);
+        *(u32x4*)(ldsQ + rr * Tile::PITCH + ((c ^ Tile::kswz(rr)) << 4)) = q ? ((const u32x4*)q)[c] : u32x4{0, 0, 0, 0};
     }
     __syncthreads();
     // a lane's first row of a tile; the swizzles are exclusive-ors that repeat every 16 rows
@@ -352,69 +349,61 @@ __global__ __launch_bounds__(256, MR == 1 ? 2 : 1) void tree_attn_few(const Tree
         for (uint32_t i = 0; i < Tile::NI; ++i) *(u32x4*)(ldsV + (vp ^ ((Tile::vswz(i * Tile::RPI)) << 4)) + i * Tile::RPI * Tile::PITCH) = vreg[i];
         const KeyRun now = x;
         if (blk + 1 < j.end) {
-            x = key_run<D>(a, j, blk + 1, 128, wave * 32, 32);
+            x = key_run<D>(a, j, blk + 1, TREE_FEW_KEYS, wave * 32, 32);
             fetch(x);
         }
         asm volatile("" ::: "memory");                                 // (a wave's LDS accesses keep their order)
         __builtin_amdgcn_wave_barrier();
         if (now.n) {
-            uint32_t vis[MR][1];
-#pragma unroll
-            for (int r = 0; r < MR; ++r) vis[r][0] = now.drafted ? tree_bits(a, j.b, token[r], now.first, now.n) : now.n >= 32 ? ~0u : (1u << now.n) - 1u;
+            const uint32_t vis[1] = {now.drafted ? tree_bits(a, j.b, token, now.first, now.n) : now.n >= 32 ? ~0u : (1u << now.n) - 1u};
             const uint32_t qoff = opaque(Tile::koff(lane));
-            tree_step<T, D, 1, MR>(row, [&](int r, int kk) __attribute__((always_inline)) { return *(const V8*)(ldsQ + (qoff ^ (kk * 32u)) + r * Tile::BYTES); },
-                                   ldsK, ldsV, lane, a.scale, vis, now.drafted || now.n < 32);
+            tree_step<T, D, 1>(row, [&](int kk) __attribute__((always_inline)) { return *(const V8*)(ldsQ + (qoff ^ (kk * 32u))); },
+                               ldsK, ldsV, lane, a.scale, vis, now.drafted || now.n < 32);
         }
         asm volatile("" ::: "memory");
         __builtin_amdgcn_wave_barrier();
     }
-#pragma unroll
-    for (int r = 0; r < MR; ++r) row[r].l += __shfl_xor(row[r].l, 32);
     // ---- the four waves joined ----
+    row.l += __shfl_xor(row.l, 32);
+    if (lane < 32) { ml[wave][lane][0] = row.m; ml[wave][lane][1] = row.l; }
+    __syncthreads();
+    float M = -INFINITY;
 #pragma unroll
-    for (int r = 0; r < MR; ++r) {
-        __syncthreads();
-        if (lane < 32) { ml[wave][lane][0] = row[r].m; ml[wave][lane][1] = row[r].l; }
-        float* const mine = (float*)(lds + wave * WAVE);
-        __syncthreads();
-        float M = -INFINITY;
+    for (int w = 0; w < 4; ++w) M = fmaxf(M, ml[w][lane & 31u][0]);
+    const float f = row.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(row.m - M);
+    float* const mine = (float*)(lds + wave * WAVE);                   // (this wave is done with its keys)
 #pragma unroll
-        for (int w = 0; w < 4; ++w) M = fmaxf(M, ml[w][lane & 31u][0]);
-        const float f = row[r].m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(row[r].m - M);
+    for (int b = 0; b < D / 32; ++b)
 #pragma unroll
-        for (int b = 0; b < D / 32; ++b)
+        for (int g = 0; g < 4; ++g) {
+            f32x4 o;
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                f32x4 o;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = row[r].m == -INFINITY && row[r].l == 0.0f ? 0.0f : row[r].o[b][4 * g + e] * f;
-                *(f32x4*)(mine + (lane & 31u) * (D + 4) + 32 * b + 8 * g + 4 * (lane >> 5)) = o;
-            }
-        __syncthreads();
-        const uint32_t rr = tid >> 3;
-        float mm = -INFINITY, L = 0.0f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) mm = fmaxf(mm, ml[w][rr][0]);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float mw = ml[w][rr][0], lw = ml[w][rr][1];
-            L += mw == -INFINITY ? lw : lw * __builtin_amdgcn_exp2f(mw - mm);     // (a sum without a maximum is 0, or NaN)
+            for (int e = 0; e < 4; ++e) o[e] = row.m == -INFINITY && row.l == 0.0f ? 0.0f : row.o[b][4 * g + e] * f;
+            *(f32x4*)(mine + (lane & 31u) * (D + 4) + 32 * b + 8 * g + 4 * (lane >> 5)) = o;
         }
+    __syncthreads();
+    const uint32_t rr = tid >> 3;
+    float mm = -INFINITY, L = 0.0f;
 #pragma unroll
-        for (uint32_t i = 0; i < D / 32; ++i) {
-            const uint32_t d = (tid & 7u) * 4 + 32 * i;
-            f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, ml[w][rr][0]);
 #pragma unroll
-            for (int w = 0; w < 4; ++w) o += *(const f32x4*)((const float*)(lds + w * WAVE) + rr * (D + 4) + d);
-            store_row4<T, D>(a, j, r * 32 + rr, d, o, mm, L, odd != 0, 128);
-        }
+    for (int w = 0; w < 4; ++w) {
+        const float mw = ml[w][rr][0], lw = ml[w][rr][1];
+        L += mw == -INFINITY ? lw : lw * __builtin_amdgcn_exp2f(mw - mm);         // (a sum without a maximum is 0, or NaN)
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < D / 32; ++i) {
+        const uint32_t d = (tid & 7u) * 4 + 32 * i;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) o += *(const f32x4*)((const float*)(lds + w * WAVE) + rr * (D + 4) + d);
+        store_row4<T, D>(a, j, r0 + rr, d, o, mm, L, odd != 0, TREE_FEW_KEYS);
     }
 }
 
 // ---- many rows -----------------------------------------------------------------------------------------------------------
 // 128 rows to a workgroup, 32 to a wave; all waves work on the same 64 keys, which the workgroup copies to LDS together, the
-// next block on its way through registers meanwhile.  Two workgroups share a CU and cover each other's waits.  A pair's row
-// blocks run on one XCD (every eighth workgroup does), so its keys come from HBM once.
+// next block on its way through registers meanwhile.  Two workgroups share a CU and cover each other's waits.
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
     using Tile = KeyTile<T, D>;
@@ -423,15 +412,13 @@ __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
     __shared__ __align__(16) char lds[2][2 * BLK];
     __shared__ uint32_t odd;                                           // a drafted value is not finite
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6);
-    const uint32_t row_blocks = (a.rows + TREE_ROW_BLOCK - 1) / TREE_ROW_BLOCK;
-    const uint32_t slot = blockIdx.x >> 3;
-    const uint32_t unit = (slot / row_blocks) * 8 + (blockIdx.x & 7u), rb = slot % row_blocks;
-    if (unit >= a.batch * a.n_parts * a.kv_heads) return;
-    const TreeJob j = tree_job(a, unit, 64);
-    const uint32_t r0 = rb * TREE_ROW_BLOCK, t_last = (min(r0 + TREE_ROW_BLOCK, a.rows) - 1) / a.group;
+    const TreeUnit u = tree_unit((a.rows + TREE_MANY_ROWS - 1) / TREE_MANY_ROWS);
+    if (u.unit >= a.batch * a.n_parts * a.kv_heads) return;
+    const TreeJob j = tree_job(a, u.unit, TREE_MANY_KEYS);
+    const uint32_t r0 = u.row_block * TREE_MANY_ROWS, t_last = (min(r0 + TREE_MANY_ROWS, a.rows) - 1) / a.group;
     if (j.begin >= j.end || r0 / a.group >= j.drafted) return;
-    RowState<D> row[1];
-    clear_row(row[0]);
+    RowState<D> row;
+    clear_row(row);
     const uint32_t at = r0 + wave * 32 + (lane & 31u);
     V8 qf[D / 16];
     {
@@ -471,39 +458,39 @@ __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
     };
     if (tid == 0) odd = 0;
     __syncthreads();
-    KeyRun x = key_run<D>(a, j, j.begin, 64, 0, 64), next = x;
+    KeyRun x = key_run<D>(a, j, j.begin, TREE_MANY_KEYS, 0, TREE_MANY_KEYS), next = x;
     if (j.begin < end) {
         fetch(x);
         put(0, x.drafted);
-        if (j.begin + 1 < end) { next = key_run<D>(a, j, j.begin + 1, 64, 0, 64); fetch(next); }
+        if (j.begin + 1 < end) { next = key_run<D>(a, j, j.begin + 1, TREE_MANY_KEYS, 0, TREE_MANY_KEYS); fetch(next); }
     }
     __syncthreads();
     for (uint32_t blk = j.begin; blk < end; ++blk) {
         const uint32_t buf = (blk - j.begin) & 1u;
-        uint32_t vis[1][2];
+        uint32_t vis[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const uint32_t n = x.n > 32u * t ? min(32u, x.n - 32u * t) : 0u;
-            vis[0][t] = x.drafted ? tree_bits(a, j.b, token, x.first + 32 * t, n) : n >= 32 ? ~0u : (1u << n) - 1u;
+            vis[t] = x.drafted ? tree_bits(a, j.b, token, x.first + 32 * t, n) : n >= 32 ? ~0u : (1u << n) - 1u;
         }
-        tree_step<T, D, 2, 1>(row, [&](int, int kk) __attribute__((always_inline)) { return qf[kk]; }, lds[buf], lds[buf] + BLK, lane, a.scale, vis, x.drafted || x.n < 64);
+        tree_step<T, D, 2>(row, [&](int kk) __attribute__((always_inline)) { return qf[kk]; }, lds[buf], lds[buf] + BLK, lane, a.scale, vis, x.drafted || x.n < 64);
         if (blk + 1 < end) {
             put(buf ^ 1u, next.drafted);
             x = next;
-            if (blk + 2 < end) { next = key_run<D>(a, j, blk + 2, 64, 0, 64); fetch(next); }
+            if (blk + 2 < end) { next = key_run<D>(a, j, blk + 2, TREE_MANY_KEYS, 0, TREE_MANY_KEYS); fetch(next); }
         }
         __syncthreads();
     }
     const uint32_t h2 = lane >> 5;
-    row[0].l += __shfl_xor(row[0].l, 32);
+    row.l += __shfl_xor(row.l, 32);
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             f32x4 o;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = row[0].o[b][4 * g + e];
-            store_row4<T, D>(a, j, at, 32 * b + 8 * g + 4 * h2, o, row[0].m, row[0].l, odd != 0, 64);
+            for (int e = 0; e < 4; ++e) o[e] = row.o[b][4 * g + e];
+            store_row4<T, D>(a, j, at, 32 * b + 8 * g + 4 * h2, o, row.m, row.l, odd != 0, TREE_MANY_KEYS);
         }
 }
 
@@ -522,7 +509,7 @@ __global__ __launch_bounds__(256) void tree_attn_join(const TreeAttnArgs a) {
     const uint32_t cached = a.capacity ? clamp_count(a.cached[b], a.capacity) : 0u;
     const uint32_t drafted = a.drafted ? clamp_count(a.drafted[b], a.tokens) : a.tokens;
     if (t >= drafted) return;
-    const uint32_t n = tree_live_parts(a, cached, drafted, tree_block_keys(a.rows));
+    const uint32_t n = tree_live_parts(a, cached, drafted, a.few ? TREE_FEW_KEYS : TREE_MANY_KEYS);
     const float* const ml = a.parts + (size_t)a.batch * a.kv_heads * a.n_parts * a.rows * D;
     float M = -INFINITY;
     for (uint32_t z = lane; z < n; z += 64) M = fmaxf(M, ml[tree_part_row(a, pair, z, r) * 2]);
@@ -557,11 +544,10 @@ __global__ __launch_bounds__(256) void tree_attn_join(const TreeAttnArgs a) {
 
 template <typename T, int D>
 hipError_t launch_tree_attn_of(const TreeAttnArgs& a, hipStream_t stream) {
-    const uint32_t units = a.batch * a.kv_heads * a.n_parts;
+    const uint32_t units = (a.batch * a.kv_heads * a.n_parts + 7) / 8 * 8;
     hipError_t e;
-    if (a.rows <= 32) e = launch_one(tree_attn_few<T, D, 1>, units, 256, stream, a);
-    else if (a.rows <= TREE_FEW_ROWS) e = launch_one(tree_attn_few<T, D, 2>, units, 256, stream, a);
-    else e = launch_one(tree_attn_many<T, D>, (units + 7) / 8 * 8 * ((a.rows + TREE_ROW_BLOCK - 1) / TREE_ROW_BLOCK), 256, stream, a);
+    if (a.few) e = launch_one(tree_attn_few<T, D>, units * ((a.rows + TREE_FEW_ROWS - 1) / TREE_FEW_ROWS), 256, stream, a);
+    else e = launch_one(tree_attn_many<T, D>, units * ((a.rows + TREE_MANY_ROWS - 1) / TREE_MANY_ROWS), 256, stream, a);
     if (e != hipSuccess || a.n_parts == 1) return e;
     return launch_one(tree_attn_join<T, D>, (uint32_t)(((uint64_t)a.batch * a.kv_heads * a.rows + 3) / 4), 256, stream, a);
 }
