@@ -548,7 +548,7 @@ int dep_cache_append(const depsync_cache_append_desc* d, void* stream);
  * dep_tree_attn's.  The sum is taken in 32 bits in an order that depends on sizes alone.                                            */
 typedef struct {
     int32_t batch, tokens, heads, kv_heads, head_dim, dtype, capacity;
-    int32_t max_cached;                                 /* 0 = capacity.  Rows behind it get no weight                              */
+    int32_t max_cached;                                 /* as for dep_tree_attn                                                    */
     int32_t n_max;                                      /* as for dep_cache_append                                                 */
     const void* q;     int64_t q_batch, q_token, q_head;
     const float* lse;                                   /* [batch][tokens][heads]                                                  */

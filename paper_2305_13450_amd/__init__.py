@@ -654,17 +654,20 @@ def _arr(t, name: str, dtype, device: int, shape) -> int:
     return t.data_ptr()
 
 
-def _on_device(index: int, call):
-    """call() with this device current."""
+def _call(device: int, what: str, f, *args) -> None:
+    """f(*args) with this device current, and its status checked."""
     import torch
-    if index == torch.cuda.current_device():
-        return call()
-    with torch.cuda.device(index):
-        return call()
+    if device == torch.cuda.current_device():
+        rc = f(*args)
+    else:
+        with torch.cuda.device(device):
+            rc = f(*args)
+    if rc != OK:
+        raise DepsyncError(rc, what)
 
 
 def _workspace(nbytes: int, given, device: int, stream):
-    """`given`, or memory that torch's allocator ties to `stream`: (tensor to keep, pointer, bytes)."""
+    """`given`, or memory that torch's allocator ties to `stream` (a hipStream_t): (tensor to keep, pointer, bytes)."""
     import torch
     if given is not None:
         if given.get_device() != device or not given.is_contiguous():
@@ -672,11 +675,10 @@ def _workspace(nbytes: int, given, device: int, stream):
         return given, given.data_ptr(), given.numel() * given.element_size()
     if nbytes == 0:
         return None, None, 0
-    handle = _stream_handle(stream) or 0
-    if handle == torch.cuda.current_stream(device).cuda_stream:
+    if (stream or 0) == torch.cuda.current_stream(device).cuda_stream:
         t = torch.empty(nbytes, dtype=torch.uint8, device=device)
     else:
-        own = torch.cuda.default_stream(device) if handle == 0 else torch.cuda.ExternalStream(handle, device=device)
+        own = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
         with torch.cuda.stream(own):
             t = torch.empty(nbytes, dtype=torch.uint8, device=device)
     return t, t.data_ptr(), nbytes
@@ -733,9 +735,10 @@ def _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, d
                         *_t4(out, "out", dtype, device, (B, T, Hq, D)), _arr(lse, "lse", torch.float32, device, (B, T, Hq))), device
 
 
-def _tree_attn_bytes(d, n_cu: int) -> int:
+def _bytes(what: str, device: int, f, *args) -> int:
+    """What a workspace query says."""
     need = ctypes.c_size_t(0)
-    _check(_lib().depsync_tree_attn_workspace(d, n_cu, ctypes.byref(need)), "depsync_tree_attn_workspace")
+    _call(device, what, f, *args, ctypes.byref(need))
     return need.value
 
 
@@ -747,18 +750,17 @@ def dep_tree_attn(q, k_new, v_new, k_cache, v_cache, cached, out, lse=None, tree
     cached[b] rows (int32).  drafted[b] (int32): the tokens that sequence b has; the others' rows of out and lse are left alone.
     lse [B, T, Hq] (float32) receives the logarithm of each row's sum.  max_cached: the most rows that a sequence has, where the host knows."""
     d, device = _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached)
-
-    def call():
-        keep, ptr, size = _workspace(0 if workspace is not None else _tree_attn_bytes(d, 0), workspace, device, stream)
-        _check(_lib().dep_tree_attn(d, ptr, size, _stream_handle(stream)), "dep_tree_attn")
-    _on_device(device, call)
+    stream = _stream_handle(stream)
+    need = 0 if workspace is not None else _bytes("dep_tree_attn", device, _lib().depsync_tree_attn_workspace, d, 0)
+    keep, ptr, size = _workspace(need, workspace, device, stream)
+    _call(device, "dep_tree_attn", _lib().dep_tree_attn, d, ptr, size, stream)
 
 
 def tree_attn_workspace(q, k_new, v_new, k_cache, v_cache, cached, out, lse=None, tree=None, drafted=None, scale: Optional[float] = None,
                         max_cached: Optional[int] = None, n_cu: int = 0) -> int:
     """Bytes of workspace that dep_tree_attn with these arguments needs."""
     d, device = _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached)
-    return _on_device(device, lambda: _tree_attn_bytes(d, n_cu))
+    return _bytes("depsync_tree_attn_workspace", device, _lib().depsync_tree_attn_workspace, d, n_cu)
 
 
 def _accepted(B: int, tokens: int, accepted, n_accepted, device: int):
@@ -786,7 +788,7 @@ def dep_cache_append(k_new, v_new, k_cache, v_cache, cached, cached_out, accepte
                        *_pair(k_cache, v_cache, "cache", dtype, device, (B, cap, Hk, D)), _arr(cached, "cached", i32, device, (B,)),
                        _arr(cached_out, "cached_out", i32, device, (B,)), acc, n_acc, _arr(weights, "weights", torch.float32, device, (B, Hk, cap)),
                        _arr(pos, "pos", i32, device, (B, Hk, cap)), _arr(start, "start", i32, device, (B,)))
-    _on_device(device, lambda: _check(_lib().dep_cache_append(d, _stream_handle(stream)), "dep_cache_append"))
+    _call(device, "dep_cache_append", _lib().dep_cache_append, d, _stream_handle(stream))
 
 
 def dep_cache_weights(q, lse, k_cache, cached, weights, accepted=None, n_accepted=None, scale: Optional[float] = None,
@@ -804,7 +806,7 @@ def dep_cache_weights(q, lse, k_cache, cached, weights, accepted=None, n_accepte
     d = _P_WEIGHTS.pack(B, T, Hq, Hk, D, code, cap, max_cached or 0, n_max, *_t4(q, "q", dtype, device), _arr(lse, "lse", torch.float32, device, (B, T, Hq)),
                         *_t4(k_cache, "k_cache", dtype, device, (B, cap, Hk, D)), _arr(cached, "cached", torch.int32, device, (B,)), acc, n_acc,
                         scale or 0.0, _arr(weights, "weights", torch.float32, device, (B, Hk, cap)))
-    _on_device(device, lambda: _check(_lib().dep_cache_weights(d, _stream_handle(stream)), "dep_cache_weights"))
+    _call(device, "dep_cache_weights", _lib().dep_cache_weights, d, _stream_handle(stream))
 
 
 def _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out):
@@ -831,30 +833,23 @@ def _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget
                          _arr(cached, "cached", i32, device, (B,)), _arr(cached_out, "cached_out", i32, device, (B,)), cap_out, *outs, *rows_out), device
 
 
-def _cache_evict_bytes(d) -> int:
-    need = ctypes.c_size_t(0)
-    _check(_lib().depsync_cache_evict_workspace(d, ctypes.byref(need)), "depsync_cache_evict_workspace")
-    return need.value
-
-
 def dep_cache_evict(k_cache, v_cache, weights, pos, cached, cached_out, budget: int, recent: int = 0, max_cached: Optional[int] = None,
                     k_out=None, v_out=None, weights_out=None, pos_out=None, workspace=None, stream=None) -> None:
     """Enqueue: every sequence and head keeps `budget` rows: the `recent` newest by position, then the heaviest, among equals the lowest row.
     In place kept rows behind the budget fill the places of those that go; into k_out .. pos_out (all four) the kept rows go in their order.
     cached_out = min(cached, budget)."""
     d, device = _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out)
-
-    def call():
-        keep, ptr, size = _workspace(0 if workspace is not None else _cache_evict_bytes(d), workspace, device, stream)
-        _check(_lib().dep_cache_evict(d, ptr, size, _stream_handle(stream)), "dep_cache_evict")
-    _on_device(device, call)
+    stream = _stream_handle(stream)
+    need = 0 if workspace is not None else _bytes("dep_cache_evict", device, _lib().depsync_cache_evict_workspace, d)
+    keep, ptr, size = _workspace(need, workspace, device, stream)
+    _call(device, "dep_cache_evict", _lib().dep_cache_evict, d, ptr, size, stream)
 
 
 def cache_evict_workspace(k_cache, v_cache, weights, pos, cached, cached_out, budget: int, recent: int = 0, max_cached: Optional[int] = None,
                           k_out=None, v_out=None, weights_out=None, pos_out=None) -> int:
     """Bytes of workspace that dep_cache_evict with these arguments needs."""
-    d, _ = _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out)
-    return _cache_evict_bytes(d)
+    d, device = _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out)
+    return _bytes("depsync_cache_evict_workspace", device, _lib().depsync_cache_evict_workspace, d)
 
 
 # ---- host mirrors -------------------------------------------------------------------------

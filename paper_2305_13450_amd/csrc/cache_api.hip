@@ -47,6 +47,13 @@ bool base2_scale(float given, int head_dim, float& out) {
 
 int rows_hint(int max_cached, int capacity) { return max_cached == 0 ? capacity : std::min(max_cached, capacity); }
 
+int cu_count(int& n_cu) {
+    int dev = 0;
+    if (hipError_t e = hipGetDevice(&dev); e != hipSuccess) return hip_fail(e);
+    const hipError_t e = hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, dev);
+    return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);
+}
+
 int tree_check(const depsync_tree_attn_desc* d) {
     if (!d) return DEPSYNC_EINVAL;
     if (int rc = common(d->batch, d->tokens, d->heads, d->kv_heads, d->head_dim, d->dtype, d->capacity); rc != DEPSYNC_OK) return rc;
@@ -68,11 +75,8 @@ double tree_cost(int64_t base, int64_t part, int64_t blocks, int64_t pairs, int6
 }
 
 int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t& bytes) {
-    if (n_cu <= 0) {
-        int dev = 0;
-        if (hipError_t e = hipGetDevice(&dev); e != hipSuccess) return hip_fail(e);
-        if (hipError_t e = hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, dev); e != hipSuccess) return hip_fail(e);
-    }
+    if (n_cu <= 0)
+        if (int rc = cu_count(n_cu); rc != DEPSYNC_OK) return rc;
     a.batch = d->batch; a.tokens = d->tokens; a.heads = d->heads; a.kv_heads = d->kv_heads; a.capacity = d->capacity;
     a.group = d->heads / d->kv_heads;
     const int64_t rows = (int64_t)d->tokens * a.group;
@@ -187,8 +191,17 @@ int dep_cache_weights(const depsync_cache_weights_desc* d, void* stream) {
     if (!base2_scale(d->scale, D, a.scale)) return DEPSYNC_EINVAL;
     a.q = d->q; a.lse = d->lse; a.k_cache = d->k_cache; a.cached = d->cached; a.accepted = d->accepted; a.n_accepted = d->n_accepted; a.weights = d->weights;
     a.batch = d->batch; a.tokens = d->tokens; a.heads = d->heads; a.kv_heads = d->kv_heads; a.group = d->heads / d->kv_heads; a.capacity = d->capacity; a.n_max = d->n_max;
-    a.max_cached = rows_hint(d->max_cached, d->capacity);
-    if ((int64_t)d->n_max * a.group > 1 << 24 || (int64_t)d->batch * d->kv_heads * cdiv64(a.max_cached, 64) > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;
+    const int64_t keys = rows_hint(d->max_cached, d->capacity), pairs = (int64_t)d->batch * d->kv_heads;
+    if ((int64_t)d->n_max * a.group > 1 << 24 || pairs * cdiv64(keys, 64) > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;
+    a.few = (int64_t)d->n_max * a.group <= 64;
+    if (a.few) {
+        int n_cu = 0;
+        if (int rc = cu_count(n_cu); rc != DEPSYNC_OK) return rc;
+        a.part_blocks = (uint32_t)std::max<int64_t>(1, cdiv64(cdiv64(keys, 128) * pairs, 3 * (int64_t)n_cu));   // three workgroups share a CU
+        a.n_parts = (uint32_t)cdiv64(cdiv64(keys, 128), a.part_blocks);
+    } else {
+        a.n_parts = (uint32_t)cdiv64(keys, 64);
+    }
     const hipError_t e = launch_cache_weights(a, d->dtype, D, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);
 }

@@ -44,7 +44,8 @@ struct CacheWeightsArgs {
     float* weights;
     Strides q_s, cache_s;
     uint32_t batch, tokens, heads, kv_heads, group, capacity, n_max;
-    uint32_t max_cached;
+    uint32_t few;                         // 1: the form for few rows
+    uint32_t n_parts, part_blocks;        // workgroups along the keys, and (few rows) blocks of 128 keys in each
     float scale;                          // scores to base-2 exponents
 };
 
@@ -59,6 +60,7 @@ struct CacheEvictArgs {
     uint32_t batch, kv_heads, capacity, capacity_out, budget, recent, max_cached;
     uint32_t max_moves;
     uint32_t in_place;
+    uint32_t fused, lanes;                // the rows move in the same launch; threads to a row
 };
 
 // The attention kernel's two forms: query rows of a workgroup and keys of a block.

@@ -38,159 +38,221 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const CacheAppendArgs
 
 // ---- weights ---------------------------------------------------------------------------------------------------------------
 // W_k += sum_r exp2(s_rk - lse_r): no running maximum is needed, as the sums are known, so every key is one workgroup's own and the
-// sum over rows needs no atomics.  S = Q K^T this time: a lane owns one key, and its 16 accumulators are 16 of 32 rows.  A wave
-// keeps its 32 keys' fragments in registers and walks the rows, which the workgroup copies to LDS 64 at a time, two stages in turn.
-// Few rows (an accepted path): the time is that of reading K once.  Many (a prompt): the matrix cores' and the exponentials'.
-// KW waves lie along the keys and 4 / KW along the rows.
-template <typename T, int D, int KW>
-__global__ __launch_bounds__(256) void cache_weights_kernel(const CacheWeightsArgs a) {
+// sum over rows needs no atomics.  S = Q K^T this time: a lane owns one key, and its 16 accumulators are 16 of 32 rows.
+
+// The accepted token i of a sequence.
+__device__ __forceinline__ uint32_t accepted_token(const CacheWeightsArgs& a, uint32_t b, uint32_t i) {
+    return a.accepted ? clamp_count(a.accepted[(size_t)b * a.n_max + i], a.tokens - 1) : i;
+}
+// Its row's sum, base 2 (a row that saw nothing gives no weight).
+__device__ __forceinline__ float row_sum(const CacheWeightsArgs& a, uint32_t b, uint32_t token, uint32_t hq) {
+    const float x = a.lse[((size_t)b * a.tokens + token) * a.heads + hq];
+    return x == -INFINITY ? INFINITY : x * 1.4426950408889634f;
+}
+// Sum over 16 rows of a lane's weights for its key: scores st, sums in LDS.  LAST(row) is the last key that a row sees, asked where `cut`.
+template <class L>
+__device__ __forceinline__ float rows_weight(const f32x16& st, const float* lse, uint32_t h2, float sc, bool cut, int32_t key, L last) {
+    float part[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const f32x4 l4 = *(const f32x4*)(lse + 8 * g + 4 * h2);
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[4 * g + e], sc, -l4[e]));
+        if (cut) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (key > last(8 * g + 4 * h2 + e)) p[e] = 0.0f;
+        }
+        part[g] = (p[0] + p[1]) + (p[2] + p[3]);
+    }
+    return (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+// At most 64 rows, those of an accepted path: the time is that of reading K once.  The rows stay in LDS; each wave walks 32 of a block's
+// 128 keys, the next ones on their way into registers meanwhile, and no wave waits for another.
+template <typename T, int D>
+__global__ __launch_bounds__(256, 3) void cache_weights_few_kernel(const CacheWeightsArgs a) {
     using Tile = KeyTile<T, D>;
     using M = Mma<T>;
     using V8 = typename M::V8;
-    constexpr uint32_t KEYS = 32 * KW, STAGE = 2 * Tile::BYTES;
-    __shared__ __align__(16) char lds[2 * STAGE];                  // first the keys, then two stages of 64 query rows
-    __shared__ __align__(16) float lse[2][64];                     // base 2
-    __shared__ __align__(16) int32_t last[2][64];                  // the last key that the row sees
-    __shared__ float joined[2][64];
+    __shared__ __align__(16) char ldsQ[2 * Tile::BYTES];
+    __shared__ __align__(16) char ldsK[4][Tile::BYTES];
+    __shared__ __align__(16) float lse[64];
+    __shared__ __align__(16) int32_t last[64];                     // the last key that the row sees
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6), h2 = lane >> 5;
-    const uint32_t blocks = (a.max_cached + KEYS - 1) / KEYS;
-    const uint32_t pair = blockIdx.x / blocks, b = pair / a.kv_heads, h = pair % a.kv_heads;
+    const uint32_t h = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, part = rest % a.n_parts, b = rest / a.n_parts;
     const uint32_t cached = uni(clamp_count(a.cached[b], a.capacity));
     const uint32_t n = uni(a.n_accepted ? clamp_count(a.n_accepted[b], a.n_max) : a.n_max);
-    if (n == 0) return;
-    for (uint32_t k0 = (blockIdx.x % blocks) * KEYS; k0 < cached; k0 += blocks * KEYS) {   // (once, unless max_cached is less than a sequence has)
+    const uint32_t blocks = (cached + 127) / 128, begin = part * a.part_blocks;
+    const uint32_t end = part + 1 == a.n_parts ? blocks : min(blocks, begin + a.part_blocks);
+    if (begin >= end || n == 0) return;
+    const uint32_t pitch = (uint32_t)a.cache_s.token * 2u, lrow = lane / Tile::CHUNKS, chunk = lane % Tile::CHUNKS;
+    const char* const keys = (const char*)a.k_cache + ((int64_t)b * a.cache_s.batch + (int64_t)h * a.cache_s.head) * 2;
+    float* const weights = a.weights + ((size_t)b * a.kv_heads + h) * a.capacity;
+    u32x4 kreg[Tile::NI];
+    float old = 0.0f;
+    auto fetch = [&](uint32_t blk) __attribute__((always_inline)) {
+        const uint32_t first = blk * 128 + wave * 32, have = first < cached ? min(32u, cached - first) : 0u;
+        const OperandBuf K(uni_ptr(keys + (int64_t)first * pitch), uni(have ? (have - 1) * pitch + D * 2u : 0u));   // (rows that are not there: zeros)
+        const uint32_t off = lrow * pitch + chunk * 16;
+#pragma unroll
+        for (uint32_t i = 0; i < Tile::NI; ++i) kreg[i] = K.load16(off, i * Tile::RPI * pitch);
+        if (lane < have) old = weights[first + lane];
+    };
+    fetch(begin);
     const int32_t base = (int32_t)cached - (int32_t)n;             // row i sees keys 0..base + i
-    const uint32_t i_first = (int32_t)k0 > base ? (uint32_t)((int32_t)k0 - base) : 0u;   // the first row that sees one of these keys
-    const uint32_t rows = n * a.group, r_first = i_first * a.group / 64 * 64;
-    const uint32_t lrow = lane / Tile::CHUNKS, chunk = lane % Tile::CHUNKS;
-    V8 kf[D / 16];
-    const uint32_t kw = wave % KW, rw = wave / KW;
-    {
-        const uint32_t first = k0 + kw * 32, have = first < cached ? min(32u, cached - first) : 0u;
-        const uint32_t pitch = (uint32_t)a.cache_s.token * 2u;
-        const char* p = (const char*)a.k_cache + ((int64_t)b * a.cache_s.batch + (int64_t)first * a.cache_s.token + (int64_t)h * a.cache_s.head) * 2;
-        const OperandBuf K(uni_ptr(p), uni(have ? (have - 1) * pitch + D * 2u : 0u));
-        char* const mine = lds + wave * Tile::BYTES;
-        u32x4 reg[Tile::NI];
+    const uint32_t rows = n * a.group;
+    for (uint32_t x = tid; x < 64 * Tile::CHUNKS; x += 256) {
+        const uint32_t r = x / Tile::CHUNKS, c = x % Tile::CHUNKS, i = r / a.group, g = r - i * a.group;
+        u32x4 q = {0, 0, 0, 0};
+        if (r < rows) q = ((const u32x4*)((const T*)a.q + (int64_t)b * a.q_s.batch + (int64_t)accepted_token(a, b, i) * a.q_s.token + (int64_t)(h * a.group + g) * a.q_s.head))[c];
+        *(u32x4*)(ldsQ + r * Tile::PITCH + ((c ^ Tile::kswz(r)) << 4)) = q;
+    }
+    if (tid < 64) {
+        const uint32_t i = tid / a.group, g = tid - i * a.group;
+        lse[tid] = tid < rows ? row_sum(a, b, accepted_token(a, b, i), h * a.group + g) : INFINITY;   // (no such row: no weight)
+        last[tid] = base + (int32_t)i;
+    }
+    __syncthreads();
+    char* const mine = ldsK[wave];
+    const uint32_t koff = Tile::koff(lane), kput = lrow * Tile::PITCH + ((chunk ^ Tile::kswz(lrow)) << 4);
+    for (uint32_t blk = begin; blk < end; ++blk) {
+        const uint32_t kp = opaque(kput);
 #pragma unroll
-        for (uint32_t i = 0; i < Tile::NI; ++i) reg[i] = K.load16((i * Tile::RPI + lrow) * pitch + chunk * 16, 0);
-#pragma unroll
-        for (uint32_t i = 0; i < Tile::NI; ++i) {
-            const uint32_t rr = i * Tile::RPI + lrow;
-            *(u32x4*)(mine + rr * Tile::PITCH + ((chunk ^ Tile::kswz(rr)) << 4)) = reg[i];
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        for (uint32_t i = 0; i < Tile::NI; ++i) *(u32x4*)(mine + (kp ^ ((Tile::kswz(i * Tile::RPI)) << 4)) + i * Tile::RPI * Tile::PITCH) = kreg[i];
+        const float before = old;
+        if (blk + 1 < end) fetch(blk + 1);
+        asm volatile("" ::: "memory");                             // (a wave's LDS accesses keep their order)
         __builtin_amdgcn_wave_barrier();
-        const uint32_t koff = Tile::koff(lane);
+        V8 kf[D / 16];
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) kf[kk] = *(const V8*)(mine + (koff ^ (kk * 32u)));
-    }
-    // 64 rows of Q: each thread copies 16 bytes of every fourth 1 KB, and one of 64 rows' sum
-    constexpr uint32_t NI = Tile::NI / 2;
-    const uint32_t qrow = wave * (Tile::RPI * NI) + lrow;
-    u32x4 qreg[NI];
-    float lse_reg = INFINITY;
-    int32_t last_reg = -1;
-    auto token = [&](uint32_t i) __attribute__((always_inline)) {
-        return a.accepted ? clamp_count(a.accepted[(size_t)b * a.n_max + i], a.tokens - 1) : i;
-    };
-    auto fetch = [&](uint32_t r0) __attribute__((always_inline)) {
-#pragma unroll
-        for (uint32_t i = 0; i < NI; ++i) {
-            const uint32_t r = r0 + i * Tile::RPI + qrow;
-            qreg[i] = u32x4{0, 0, 0, 0};
-            if (r < rows) {
-                const uint32_t at = r / a.group, g = r - at * a.group;
-                const T* p = (const T*)a.q + (int64_t)b * a.q_s.batch + (int64_t)token(at) * a.q_s.token + (int64_t)(h * a.group + g) * a.q_s.head;
-                qreg[i] = ((const u32x4*)p)[chunk];
-            }
-        }
-        if (tid < 64) {
-            const uint32_t r = r0 + tid;
-            lse_reg = INFINITY; last_reg = -1;                     // no such row: no weight
-            if (r < rows) {
-                const uint32_t at = r / a.group, g = r - at * a.group;
-                const float x = a.lse[((size_t)b * a.tokens + token(at)) * a.heads + h * a.group + g];
-                lse_reg = x == -INFINITY ? INFINITY : x * 1.4426950408889634f;   // (a row that saw nothing gives none)
-                last_reg = base + (int32_t)at;
-            }
-        }
-    };
-    auto put = [&](uint32_t s) __attribute__((always_inline)) {
-#pragma unroll
-        for (uint32_t i = 0; i < NI; ++i) {
-            const uint32_t rr = i * Tile::RPI + qrow;
-            *(u32x4*)(lds + s * STAGE + rr * Tile::PITCH + ((chunk ^ Tile::kswz(rr)) << 4)) = qreg[i];
-        }
-        if (tid < 64) { lse[s][tid] = lse_reg; last[s][tid] = last_reg; }
-    };
-    float w = 0.0f;
-    const int32_t key = (int32_t)(k0 + kw * 32 + (lane & 31u));
-    const uint32_t koff = Tile::koff(lane);
-    fetch(r_first);
-    __syncthreads();                                               // every wave has its keys: the stages may be written
-    put(0);
-    if (r_first + 64 < rows) fetch(r_first + 64);
-    __syncthreads();
-    for (uint32_t r0 = r_first, s = 0; r0 < rows; r0 += 64, s ^= 1u) {
-#pragma unroll
-        for (uint32_t u = 0; u < 2; ++u) {
-            if (KW < 4 && u != rw) continue;
+        const int32_t first = (int32_t)(blk * 128 + wave * 32), key = first + (int32_t)(lane & 31u);
+        float w = 0.0f;
+        for (uint32_t u = 0; u * 32 < rows; ++u) {
             f32x16 st;
 #pragma unroll
             for (int v = 0; v < 16; ++v) st[v] = 0.0f;
 #pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) st = M::mma(*(const V8*)(ldsQ + u * Tile::BYTES + (koff ^ (kk * 32u))), kf[kk], st);
+            w += rows_weight(st, lse + 32 * u, h2, a.scale, first + 31 > base, key, [&](uint32_t r) __attribute__((always_inline)) { return last[32 * u + r]; });
+        }
+        w += __shfl_xor(w, 32);
+        if (lane < 32 && key < (int32_t)cached) weights[key] = before + w;
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// More rows, those of a prompt: the time is that of the matrix cores and the exponentials.  A workgroup keeps 64 keys' fragments in
+// registers, in every wave, and its four waves walk the rows, 32 tokens of one query head at a time each, the next ones on their way into
+// registers meanwhile.  (Rows by head and not by token: their addresses are a line then, and the last key they see as well.)
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void cache_weights_many_kernel(const CacheWeightsArgs a) {
+    using Tile = KeyTile<T, D>;
+    using M = Mma<T>;
+    using V8 = typename M::V8;
+    __shared__ __align__(16) char lds[4][Tile::BYTES];             // the keys, then each wave's rows
+    __shared__ __align__(16) float lse[4][32];
+    __shared__ float joined[4][64];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6), h2 = lane >> 5;
+    const uint32_t h = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, part = rest % a.n_parts, b = rest / a.n_parts;
+    const uint32_t cached = uni(clamp_count(a.cached[b], a.capacity));
+    const uint32_t n = uni(a.n_accepted ? clamp_count(a.n_accepted[b], a.n_max) : a.n_max);
+    if (n == 0) return;
+    const uint32_t lrow = lane / Tile::CHUNKS, chunk = lane % Tile::CHUNKS;
+    const uint32_t koff = Tile::koff(lane), put = lrow * Tile::PITCH + ((chunk ^ Tile::kswz(lrow)) << 4);
+    char* const mine = lds[wave];
+    const int32_t base = (int32_t)cached - (int32_t)n;             // row i sees keys 0..base + i
+    for (uint32_t k0 = part * 64; k0 < cached; k0 += a.n_parts * 64) {   // (once, unless max_cached is less than a sequence has)
+        V8 kf[2][D / 16];
+        {
+            const uint32_t pitch = (uint32_t)a.cache_s.token * 2u;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const uint32_t first = k0 + 32 * t, have = first < cached ? min(32u, cached - first) : 0u;
+                const char* p = (const char*)a.k_cache + ((int64_t)b * a.cache_s.batch + (int64_t)first * a.cache_s.token + (int64_t)h * a.cache_s.head) * 2;
+                const OperandBuf K(uni_ptr(p), uni(have ? (have - 1) * pitch + D * 2u : 0u));
+                __syncthreads();
+                for (uint32_t i = wave; i < Tile::NI; i += 4)
+                    *(u32x4*)(lds[t] + (put ^ ((Tile::kswz(i * Tile::RPI)) << 4)) + i * Tile::RPI * Tile::PITCH) = K.load16(lrow * pitch + chunk * 16, i * Tile::RPI * pitch);
+                __syncthreads();
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk) kf[t][kk] = *(const V8*)(lds[t] + (koff ^ (kk * 32u)));
+            }
+            __syncthreads();
+        }
+        const uint32_t i_first = (int32_t)k0 > base ? (uint32_t)((int32_t)k0 - base) & ~31u : 0u;   // rows before see none of these keys
+        const uint32_t steps_of_head = i_first < n ? (n - i_first + 31) / 32 : 0u, steps = steps_of_head * a.group;
+        u32x4 qreg[Tile::NI];
+        float sum = INFINITY;
+        auto fetch = [&](uint32_t s) __attribute__((always_inline)) {
+            const uint32_t g = s / steps_of_head, i0 = i_first + (s - g * steps_of_head) * 32, hq = h * a.group + g;
+            const T* const q = (const T*)a.q + (int64_t)b * a.q_s.batch + (int64_t)hq * a.q_s.head + chunk * 8;
+#pragma unroll
+            for (uint32_t i = 0; i < Tile::NI; ++i) {
+                const uint32_t at = i0 + i * Tile::RPI + lrow;
+                qreg[i] = at < n ? *(const u32x4*)(q + (int64_t)accepted_token(a, b, at) * a.q_s.token) : u32x4{0, 0, 0, 0};
+            }
+            const uint32_t at = i0 + (lane & 31u);
+            sum = at < n ? row_sum(a, b, accepted_token(a, b, at), hq) : INFINITY;   // (no such row: no weight)
+        };
+        float w[2] = {0.0f, 0.0f};
+        const int32_t key = (int32_t)(k0 + (lane & 31u));
+        if (wave < steps) fetch(wave);
+        for (uint32_t s = wave; s < steps; s += 4) {
+            const uint32_t p = opaque(put);
+#pragma unroll
+            for (uint32_t i = 0; i < Tile::NI; ++i) *(u32x4*)(mine + (p ^ ((Tile::kswz(i * Tile::RPI)) << 4)) + i * Tile::RPI * Tile::PITCH) = qreg[i];
+            if (lane < 32) lse[wave][lane] = sum;
+            const int32_t see = base + (int32_t)(i_first + s % steps_of_head * 32);   // the last key that the first of these rows sees
+            if (s + 4 < steps) fetch(s + 4);
+            asm volatile("" ::: "memory");                         // (a wave's LDS accesses keep their order)
+            __builtin_amdgcn_wave_barrier();
+            f32x16 st[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) st[t][v] = 0.0f;
+#pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
-                const V8 qf = *(const V8*)(lds + s * STAGE + u * Tile::BYTES + (koff ^ (kk * 32u)));
-                st = M::mma(qf, kf[kk], st);
+                const V8 q = *(const V8*)(mine + (koff ^ (kk * 32u)));
+#pragma unroll
+                for (int t = 0; t < 2; ++t) st[t] = M::mma(q, kf[t][kk], st[t]);
             }
-            const bool cut = base + (int32_t)((r0 + 32 * u) / a.group) < (int32_t)(k0 + KEYS - 1);
-            float part = 0.0f;
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const f32x4 l4 = *(const f32x4*)(&lse[s][32 * u + 8 * g + 4 * h2]);
-                float p[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[4 * g + e], a.scale, -l4[e]));
-                if (cut) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (key > last[s][32 * u + 8 * g + 4 * h2 + e]) p[e] = 0.0f;
-                }
-                part += (p[0] + p[1]) + (p[2] + p[3]);
-            }
-            w += part;
+            for (int t = 0; t < 2; ++t)
+                w[t] += rows_weight(st[t], lse[wave], h2, a.scale, (int32_t)k0 + 32 * t + 31 > see, key + 32 * t,
+                                    [&](uint32_t r) __attribute__((always_inline)) { return see + (int32_t)r; });
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_wave_barrier();
         }
-        if (r0 + 64 < rows) {
-            put(s ^ 1u);
-            if (r0 + 128 < rows) fetch(r0 + 128);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            w[t] += __shfl_xor(w[t], 32);
+            if (lane < 32) joined[wave][32 * t + lane] = w[t];
         }
         __syncthreads();
-    }
-    w += __shfl_xor(w, 32);
-    if constexpr (KW < 4) {
-        if (rw == 1 && lane < 32) joined[kw][lane] = w;
-        __syncthreads();
-        if (rw == 0 && lane < 32) w += joined[kw][lane];
-    }
-    if (rw == 0 && lane < 32 && key < (int32_t)cached) a.weights[((size_t)b * a.kv_heads + h) * a.capacity + key] += w;
-    __syncthreads();                                               // the stages are done with
+        if (tid < 64 && k0 + tid < cached)
+            a.weights[((size_t)b * a.kv_heads + h) * a.capacity + k0 + tid] += (joined[0][tid] + joined[1][tid]) + (joined[2][tid] + joined[3][tid]);
     }
 }
 
 // ---- evict -----------------------------------------------------------------------------------------------------------------
 // The rows that stay are those with the `budget` largest 32-bit keys (weight as an ordered integer; the newest above all), the
 // lowest rows among equal ones: four passes over 8 bits each find the smallest key that stays and how many of its equals do, a
-// walk in row order then lists the moves.  One workgroup per sequence and head; the keys stay in LDS where they fit.
-constexpr uint32_t EVICT_THREADS = 1024, EVICT_LDS_KEYS = 32768, EVICT_VPT = 4;
+// walk in row order then lists the moves.  One workgroup per sequence and head; the keys stay in LDS where they fit.  A few rows' worth of
+// arithmetic on 8 bytes a row: bound by the latencies of its steps (2053 rows of 256 heads 9 us, 16384 of 32 heads 24 us), so loads go out eight to
+// a thread at once, and a step that appended few rows moves them in the same launch.
+constexpr uint32_t EVICT_THREADS = 1024, EVICT_LDS_KEYS = 32768, EVICT_VPT = 4, EVICT_LOADS = 8, EVICT_FUSED = 256;
 
-__device__ __forceinline__ uint32_t evict_key(float w, int32_t pos, int32_t newest, int32_t recent) {
-    if ((int64_t)pos > (int64_t)newest - recent) return 0xffffffffu;
-    if (!(w == w)) return 0u;
+// Larger float, larger integer; NaN is the least.  Infinity is below 0xffffffff, the key of the newest rows.
+__device__ __forceinline__ uint32_t evict_key(float w) {
     const uint32_t x = __builtin_bit_cast(uint32_t, w + 0.0f);       // (-0 counts as 0)
-    const uint32_t k = x & 0x80000000u ? ~x : x | 0x80000000u;       // larger float, larger integer; infinity is below the newest
-    return k;
+    return w == w ? (x & 0x80000000u ? ~x : x | 0x80000000u) : 0u;
 }
+__device__ __forceinline__ bool evict_new(int32_t pos, int32_t newest, uint32_t recent) { return (int64_t)pos > (int64_t)newest - (int64_t)recent; }
 
 // Exclusive sum over the threads of the workgroup, and the total.
 __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* wave_sums, uint32_t& total) {
@@ -215,62 +277,108 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* wave_sums, 
     return before + x - v;
 }
 
+// Row src of the cache to row dst, 16 bytes to each of `lanes` threads.
+__device__ __forceinline__ void move_row(const CacheEvictArgs& a, uint32_t pair, uint32_t src, uint32_t dst, uint32_t unit) {
+    const uint32_t b = pair / a.kv_heads, h = pair % a.kv_heads;
+    const int64_t from = (int64_t)b * a.cache_s.batch + (int64_t)src * a.cache_s.token + (int64_t)h * a.cache_s.head;
+    const int64_t to = (int64_t)b * a.out_s.batch + (int64_t)dst * a.out_s.token + (int64_t)h * a.out_s.head;
+    const u32x4 k = ((const u32x4*)((const uint16_t*)a.k_cache + from))[unit];
+    const u32x4 v = ((const u32x4*)((const uint16_t*)a.v_cache + from))[unit];
+    ((u32x4*)((uint16_t*)a.k_out + to))[unit] = k;
+    ((u32x4*)((uint16_t*)a.v_out + to))[unit] = v;
+    if (unit == 0) {
+        const size_t f = (size_t)pair * a.capacity + src, t = (size_t)pair * a.capacity_out + dst;
+        a.weights_out[t] = a.weights[f];
+        a.pos_out[t] = a.pos[f];
+    }
+}
+
 __global__ __launch_bounds__(1024) void cache_evict_select_kernel(const CacheEvictArgs a) {
     __shared__ uint32_t keys[EVICT_LDS_KEYS];
-    __shared__ uint32_t hist[256], wave_sums[EVICT_THREADS / 64], found[2];
+    __shared__ uint32_t hist[2][256], wave_sums[EVICT_THREADS / 64], found[2];
     __shared__ int32_t newest_of[EVICT_THREADS / 64];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
     const uint32_t b = blockIdx.x / a.kv_heads, h = blockIdx.x % a.kv_heads;
     const uint32_t n = uni(clamp_count(a.cached[b], a.capacity));
     uint32_t* const list = a.moves + (size_t)blockIdx.x * (1 + 2 * (size_t)a.max_moves);
     if (h == 0 && tid == 0) a.cached_out[b] = (int32_t)min(n, a.budget);
+    const uint32_t unit = tid % a.lanes;
     if (n <= a.budget) {
         const uint32_t moves = a.in_place ? 0u : n;
         if (tid == 0) list[0] = moves;
-        for (uint32_t i = tid; i < moves; i += EVICT_THREADS) list[1 + i] = i;
+        if (a.fused)
+            for (uint32_t i = tid / a.lanes; i < moves; i += EVICT_THREADS / a.lanes) move_row(a, blockIdx.x, i, i, unit);
+        else
+            for (uint32_t i = tid; i < moves; i += EVICT_THREADS) list[1 + i] = i;
         return;
     }
     const float* const w = a.weights + (size_t)blockIdx.x * a.capacity;
     const int32_t* const pos = a.pos + (size_t)blockIdx.x * a.capacity;
+    const bool in_lds = n <= EVICT_LDS_KEYS;
+    if (tid < 256) hist[0][tid] = 0;
     int32_t newest = INT32_MIN;
-    for (uint32_t i = tid; i < n; i += EVICT_THREADS) newest = max(newest, pos[i]);
+    for (uint32_t i0 = 0; i0 < n; i0 += EVICT_THREADS * EVICT_LOADS) {
+        float x[EVICT_LOADS];
+        int32_t y[EVICT_LOADS];
+#pragma unroll
+        for (uint32_t e = 0; e < EVICT_LOADS; ++e) {
+            const uint32_t i = min(i0 + e * EVICT_THREADS + tid, n - 1);
+            x[e] = w[i]; y[e] = pos[i];
+        }
+#pragma unroll
+        for (uint32_t e = 0; e < EVICT_LOADS; ++e) {
+            const uint32_t i = min(i0 + e * EVICT_THREADS + tid, n - 1);   // (the last row again and again: the same key)
+            if (in_lds) keys[i] = evict_key(x[e]);
+            newest = max(newest, y[e]);
+        }
+    }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) newest = max(newest, __shfl_xor(newest, d));
     if (lane == 0) newest_of[wave] = newest;
     __syncthreads();
 #pragma unroll
     for (uint32_t i = 0; i < EVICT_THREADS / 64; ++i) newest = max(newest, newest_of[i]);
-    const bool in_lds = n <= EVICT_LDS_KEYS;
-    if (in_lds)
-        for (uint32_t i = tid; i < n; i += EVICT_THREADS) keys[i] = evict_key(w[i], pos[i], newest, (int32_t)a.recent);
-    auto key = [&](uint32_t i) __attribute__((always_inline)) { return in_lds ? keys[i] : evict_key(w[i], pos[i], newest, (int32_t)a.recent); };
+    if (in_lds && a.recent) {
+        for (uint32_t i0 = 0; i0 < n; i0 += EVICT_THREADS * EVICT_LOADS) {
+            int32_t y[EVICT_LOADS];
+#pragma unroll
+            for (uint32_t e = 0; e < EVICT_LOADS; ++e) y[e] = pos[min(i0 + e * EVICT_THREADS + tid, n - 1)];
+#pragma unroll
+            for (uint32_t e = 0; e < EVICT_LOADS; ++e)
+                if (evict_new(y[e], newest, a.recent)) keys[min(i0 + e * EVICT_THREADS + tid, n - 1)] = 0xffffffffu;
+        }
+        __syncthreads();
+    }
+    auto key = [&](uint32_t i) __attribute__((always_inline)) { return in_lds ? keys[i] : evict_new(pos[i], newest, a.recent) ? 0xffffffffu : evict_key(w[i]); };
     // the smallest key that stays, from its highest 8 bits down; `need` keys with these bits stay
     uint32_t prefix = 0, need = a.budget;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (uint32_t i = tid; i < 256; i += EVICT_THREADS) hist[i] = 0;
-        __syncthreads();
-        for (uint32_t i0 = 0; i0 < n; i0 += EVICT_THREADS) {
-            const uint32_t i = i0 + tid;
-            const uint32_t k = i < n ? key(i) : 0u;
-            bool todo = i < n && (shift == 24 || k >> (shift + 8) == prefix);
-            const uint32_t bin = (k >> shift) & 255u;
-            // many keys share a bin (weights of one magnitude, rows that nothing attended to): a wave adds its first two bins at once
+    for (int shift = 24, buf = 0; shift >= 0; shift -= 8, buf ^= 1) {
+        for (uint32_t i0 = 0; i0 < n; i0 += EVICT_THREADS * 4) {
+            uint32_t k[4];
 #pragma unroll
-            for (int peel = 0; peel < 2; ++peel) {
-                const uint64_t left = __ballot(todo);
-                if (!left) break;
-                const uint32_t lead = (uint32_t)__builtin_ctzll(left), bin0 = __shfl(bin, lead);
-                const uint64_t same = __ballot(todo && bin == bin0);
-                if (lane == lead) atomicAdd(&hist[bin0], (uint32_t)__popcll(same));
-                todo = todo && bin != bin0;
+            for (uint32_t e = 0; e < 4; ++e) k[e] = key(min(i0 + e * EVICT_THREADS + tid, n - 1));
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+                bool todo = i0 + e * EVICT_THREADS + tid < n && (shift == 24 || k[e] >> (shift + 8) == prefix);
+                const uint32_t bin = (k[e] >> shift) & 255u;
+                // many keys share a bin (weights of one magnitude, rows that nothing attended to): a wave adds its first two bins at once
+#pragma unroll
+                for (int peel = 0; peel < 2; ++peel) {
+                    const uint64_t left = __ballot(todo);
+                    if (!left) break;
+                    const uint32_t bin0 = (uint32_t)__builtin_amdgcn_readlane((int)bin, (int)__builtin_ctzll(left));
+                    const uint64_t same = __ballot(todo && bin == bin0);
+                    if (lane == 0) atomicAdd(&hist[buf][bin0], (uint32_t)__popcll(same));
+                    todo = todo && bin != bin0;
+                }
+                if (todo) atomicAdd(&hist[buf][bin], 1u);
             }
-            if (todo) atomicAdd(&hist[bin], 1u);
         }
         __syncthreads();
         if (wave == 0) {                                             // lane l: bins 255 - 4 l .. 252 - 4 l, from the top
             uint32_t c[4], sum = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { c[e] = hist[255 - 4 * lane - e]; sum += c[e]; }
+            for (int e = 0; e < 4; ++e) { c[e] = hist[buf][255 - 4 * lane - e]; sum += c[e]; }
             uint32_t x = sum;
 #pragma unroll
             for (int d = 1; d < 64; d <<= 1) {
@@ -283,6 +391,8 @@ __global__ __launch_bounds__(1024) void cache_evict_select_kernel(const CacheEvi
                 if (above < need && need <= above + c[e]) { found[0] = 255 - 4 * lane - e; found[1] = need - above; }
                 above += c[e];
             }
+        } else if (wave < 5) {
+            hist[buf ^ 1][tid - 64] = 0;
         }
         __syncthreads();
         prefix = prefix << 8 | found[0];
@@ -321,39 +431,27 @@ __global__ __launch_bounds__(1024) void cache_evict_select_kernel(const CacheEvi
         holes += all & 0xffffu;
         sources += all >> 16;
     }
-    if (tid == 0) list[0] = sources;
+    if (!a.fused) {
+        if (tid == 0) list[0] = sources;
+        return;
+    }
+    __syncthreads();
+    for (uint32_t m = tid / a.lanes; m < sources; m += EVICT_THREADS / a.lanes)
+        move_row(a, blockIdx.x, list[1 + m], a.in_place ? list[1 + a.max_moves + m] : m, unit);
 }
 
-// The listed rows moved, D / 8 lanes to a row.  In place sources lie behind the budget and their places before it, so no row is both.
-template <int D>
+// The listed rows moved.  In place sources lie behind the budget and their places before it, so no row is both.
 __global__ __launch_bounds__(256) void cache_evict_move_kernel(const CacheEvictArgs a, uint32_t blocks) {
-    constexpr uint32_t LANES = D / 8, ROWS = 256 / LANES;
-    const uint32_t pair = blockIdx.x / blocks, blk = blockIdx.x % blocks;
-    const uint32_t b = pair / a.kv_heads, h = pair % a.kv_heads, unit = threadIdx.x % LANES;
+    const uint32_t pair = blockIdx.x / blocks, blk = blockIdx.x % blocks, rows = 256 / a.lanes;
     const uint32_t* const list = a.moves + (size_t)pair * (1 + 2 * (size_t)a.max_moves);
     const uint32_t n = list[0];
-    for (uint32_t m = blk * ROWS + threadIdx.x / LANES; m < n; m += blocks * ROWS) {
-        const uint32_t src = list[1 + m], dst = a.in_place ? list[1 + a.max_moves + m] : m;
-        const int64_t from = (int64_t)b * a.cache_s.batch + (int64_t)src * a.cache_s.token + (int64_t)h * a.cache_s.head;
-        const int64_t to = (int64_t)b * a.out_s.batch + (int64_t)dst * a.out_s.token + (int64_t)h * a.out_s.head;
-        const u32x4 k = ((const u32x4*)((const uint16_t*)a.k_cache + from))[unit];
-        const u32x4 v = ((const u32x4*)((const uint16_t*)a.v_cache + from))[unit];
-        ((u32x4*)((uint16_t*)a.k_out + to))[unit] = k;
-        ((u32x4*)((uint16_t*)a.v_out + to))[unit] = v;
-        if (unit == 0) {
-            const size_t f = (size_t)pair * a.capacity + src, t = (size_t)pair * a.capacity_out + dst;
-            a.weights_out[t] = a.weights[f];
-            a.pos_out[t] = a.pos[f];
-        }
-    }
+    for (uint32_t m = blk * rows + threadIdx.x / a.lanes; m < n; m += blocks * rows)
+        move_row(a, pair, list[1 + m], a.in_place ? list[1 + a.max_moves + m] : m, threadIdx.x % a.lanes);
 }
 
 template <typename T, int D>
 hipError_t launch_weights_of(const CacheWeightsArgs& a, hipStream_t stream) {
-    const uint64_t pairs = (uint64_t)a.batch * a.kv_heads, wide = pairs * ((a.max_cached + 127) / 128);
-    // Few workgroups and many rows: half the keys to a workgroup, its waves two by two
-    if (wide < 512 && a.n_max * a.group > 64) return launch_one(cache_weights_kernel<T, D, 2>, (uint32_t)(pairs * ((a.max_cached + 63) / 64)), 256, stream, a);
-    return launch_one(cache_weights_kernel<T, D, 4>, (uint32_t)wide, 256, stream, a);
+    return launch_one(a.few ? cache_weights_few_kernel<T, D> : cache_weights_many_kernel<T, D>, a.batch * a.kv_heads * a.n_parts, 256, stream, a);
 }
 
 }  // namespace
@@ -369,18 +467,20 @@ hipError_t launch_cache_weights(const CacheWeightsArgs& a, int dtype, int head_d
     return head_dim == 128 ? launch_weights_of<_Float16, 128>(a, stream) : launch_weights_of<_Float16, 64>(a, stream);
 }
 
-hipError_t launch_cache_evict(const CacheEvictArgs& a, int head_dim, hipStream_t stream) {
-    const uint32_t pairs = a.batch * a.kv_heads, rows = 256 / (head_dim / 8);
+hipError_t launch_cache_evict(const CacheEvictArgs& given, int head_dim, hipStream_t stream) {
+    CacheEvictArgs a = given;
+    const uint32_t pairs = a.batch * a.kv_heads;
+    a.lanes = head_dim / 8;
+    // As many moves as a sequence of max_cached rows makes (the kernels walk any number).  A workgroup moves 64 or 128 rows at a time, so up to
+    // EVICT_FUSED they are not worth another launch.
+    const uint32_t most = a.in_place ? (a.max_cached > a.budget ? a.max_cached - a.budget : 0u) : a.budget;
+    a.fused = most <= EVICT_FUSED;
     hipError_t e = launch_one(cache_evict_select_kernel, pairs, EVICT_THREADS, stream, a);
-    if (e != hipSuccess) return e;
-    // as many moves as a sequence of max_cached rows makes; the kernel walks any number
-    const uint32_t most = a.in_place ? (a.max_cached > a.budget ? a.max_cached - a.budget : 1u) : a.budget;
-    uint32_t blocks = (most < a.max_moves ? most : a.max_moves) / rows + 1;
+    if (e != hipSuccess || a.fused) return e;
+    uint32_t blocks = (most < a.max_moves ? most : a.max_moves) / (256 / a.lanes) + 1;
     if (blocks > 256) blocks = 256;
-    CacheEvictArgs x = a;
-    void* args[] = {&x, &blocks};
-    const void* move = head_dim == 128 ? reinterpret_cast<const void*>(cache_evict_move_kernel<128>) : reinterpret_cast<const void*>(cache_evict_move_kernel<64>);
-    return hipLaunchKernel(move, dim3(pairs * blocks), dim3(256), args, 0, stream);
+    void* args[] = {&a, &blocks};
+    return hipLaunchKernel(reinterpret_cast<const void*>(cache_evict_move_kernel), dim3(pairs * blocks), dim3(256), args, 0, stream);
 }
 
 hipError_t launch_tree_attn(const TreeAttnArgs& a, int dtype, int head_dim, hipStream_t stream) {
