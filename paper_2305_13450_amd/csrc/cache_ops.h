@@ -64,7 +64,7 @@ struct CacheEvictArgs {
 };
 
 // The attention kernel's two forms: query rows of a workgroup and keys of a block.
-constexpr uint32_t TREE_FEW_ROWS = 32, TREE_FEW_KEYS = 128, TREE_MANY_ROWS = 128, TREE_MANY_KEYS = 64;
+constexpr uint32_t TREE_FEW_ROWS = 32, TREE_FEW_KEYS = 128, TREE_MANY_ROWS = 128, TREE_MANY_KEYS = 32;
 
 hipError_t launch_tree_attn(const TreeAttnArgs& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t launch_tree_attn_bf16(const TreeAttnArgs& a, int head_dim, hipStream_t stream);

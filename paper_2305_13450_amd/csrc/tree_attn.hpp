@@ -1,7 +1,7 @@
 // Attention of drafted tokens over a cache: for every key and value head, rows = tokens x query heads that share it,
 //   o_r = sum_k p_rk v_k / sum_k p_rk,   p_rk = exp2(s_rk - m_r),   s_rk = scale log2(e) q_r . k_k
 // over the sequence's cached rows and those drafted tokens that the row's tree word names, in one pass over the keys with
-// a running maximum m, sum and un-normalised output per row.  All scores are computed transposed, as in attn_tile.hpp: a lane
+// a reference value m (a maximum that may lag), sum and un-normalised output per row.  All scores are computed transposed, as in attn_tile.hpp: a lane
 // owns one query row, S^T = K Q^T leaves 16 of 32 keys of it in its registers, and these are the B operand of O^T += V^T P^T as they stand.
 //
 // The key axis is the cached rows in blocks, then the drafted tokens in blocks; a block never mixes the two.  It is cut into
@@ -18,10 +18,14 @@ namespace depsync {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// The largest weight is 2^OFF: sums and outputs carry the factor alike and it cancels.  fp16 holds weights below 2^-14 with
-// fewer bits, and the weights of a long cache are mostly far below the largest: 2^14 leaves 28 binades above that.  bf16 has them anyway.
+// The reference value that weights are relative to follows the running maximum only where that has grown by more than SLACK (base 2): with 32 rows
+// to a wave every third step of 500 would rescale the outputs for the sake of some row's new maximum, so hardly one in thirty does.
+// Weights are then at most 2^SLACK, which costs 16-bit weights nothing: their error is relative.  But fp16 has 2^-14 to 2^16 only, and the weights of a
+// long cache are mostly far below the largest, so there they carry a factor of 2^OFF, 2^15 at most: below the reference 23 binades keep all bits.
+// Sums and outputs carry the factor alike and it cancels.
+constexpr float WEIGHT_SLACK = 6.0f;
 template <typename T> constexpr float WEIGHT_OFF = 0.0f;
-template <> inline constexpr float WEIGHT_OFF<_Float16> = 14.0f;
+template <> inline constexpr float WEIGHT_OFF<_Float16> = 9.0f;
 
 // Zeros in the place of infinities and NaN; whether there were any.
 template <typename T> __device__ __forceinline__ bool without_not_finite(u32x4& v) {
@@ -73,7 +77,7 @@ __device__ __forceinline__ float max_halves(float x) {
 // One step: KT tiles of 32 keys in LDS against 32 rows.  vis: the tile's keys that a lane's row sees, one bit each.
 // Fragments are read two slices ahead of the MFMAs and the order is pinned: left alone the compiler reads them all at once, and spills, or each right
 // before the wait for it.  query(kk): the rows' fragment of slice kk.
-template <typename T, int D, int KT, class Q>
+template <typename T, int D, int KT, int AHEAD, class Q>
 __device__ __forceinline__ void tree_step(RowState<D>& row, Q query, const char* ldsK, const char* ldsV, uint32_t lane, float sc,
                                           const uint32_t (&vis)[KT], bool masked) {
     using Tile = KeyTile<T, D>;
@@ -84,20 +88,21 @@ __device__ __forceinline__ void tree_step(RowState<D>& row, Q query, const char*
     const uint32_t koff = opaque(Tile::koff(lane)), voff = opaque(Tile::voff(lane));
     f32x16 st[KT];
     {
-        V8 kf[3], qf[3];
+        V8 kf[AHEAD + 1], qf[AHEAD + 1];
         auto rd = [&](int i) __attribute__((always_inline)) {
-            kf[i % 3] = *(const V8*)(ldsK + (koff ^ ((i % KF) * 32u)) + (i / KF) * Tile::BYTES);
-            qf[i % 3] = query(i % KF);
+            kf[i % (AHEAD + 1)] = *(const V8*)(ldsK + (koff ^ ((i % KF) * 32u)) + (i / KF) * Tile::BYTES);
+            qf[i % (AHEAD + 1)] = query(i % KF);
         };
-        rd(0); rd(1);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) rd(i);
 #pragma unroll
         for (int i = 0; i < KT * KF; ++i) {
             __builtin_amdgcn_sched_barrier(0);
-            if (i + 2 < KT * KF) rd(i + 2);
+            if (i + AHEAD < KT * KF) rd(i + AHEAD);
             if (i % KF == 0)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) st[i / KF][v] = 0.0f;
-            st[i / KF] = M::mma(kf[i % 3], qf[i % 3], st[i / KF]);
+            st[i / KF] = M::mma(kf[i % (AHEAD + 1)], qf[i % (AHEAD + 1)], st[i / KF]);
         }
         __builtin_amdgcn_sched_barrier(0);
     }
@@ -114,7 +119,7 @@ __device__ __forceinline__ void tree_step(RowState<D>& row, Q query, const char*
 #pragma unroll
         for (int v = 0; v < 16; v += 2) mx = fmaxf(fmaxf(mx, st[t][v]), st[t][v + 1]);
     mx = max_halves(mx) * sc;
-    if (__ballot(mx > row.m)) {                                      // (rarely, after the first steps)
+    if (__ballot(mx > row.m + WEIGHT_SLACK)) {                       // (rarely, after the first steps)
         const float m_new = fmaxf(row.m, mx);
         const float alpha = row.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(row.m - m_new);
         row.m = m_new;
@@ -137,18 +142,20 @@ __device__ __forceinline__ void tree_step(RowState<D>& row, Q query, const char*
         }
     row.l += sum[0] + sum[1];
     typedef T T4 __attribute__((ext_vector_type(4)));
-    T4 vf[3][2];
+    T4 vf[AHEAD + 1][2];
     constexpr int NB = D / 32, NV = 2 * KT * NB;
     auto rdv = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-        for (int c = 0; c < 2; ++c) vf[i % 3][c] = TrRead<T>::read(ldsV + (voff ^ ((i % NB) * 64u + c * 32u)) + ((i / NB) * 16 + c * 8) * Tile::PITCH);
+        for (int c = 0; c < 2; ++c)
+            vf[i % (AHEAD + 1)][c] = TrRead<T>::read(ldsV + (voff ^ ((i % NB) * 64u + c * 32u)) + ((i / NB) * 16 + c * 8) * Tile::PITCH);
     };
-    rdv(0); rdv(1);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) rdv(i);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         __builtin_amdgcn_sched_barrier(0);
-        if (i + 2 < NV) rdv(i + 2);
-        const V8 x = __builtin_shufflevector(vf[i % 3][0], vf[i % 3][1], 0, 1, 2, 3, 4, 5, 6, 7);
+        if (i + AHEAD < NV) rdv(i + AHEAD);
+        const V8 x = __builtin_shufflevector(vf[i % (AHEAD + 1)][0], vf[i % (AHEAD + 1)][1], 0, 1, 2, 3, 4, 5, 6, 7);
         row.o[i % NB] = M::mma(x, pf[i / NB], row.o[i % NB]);
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -357,7 +364,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_few(const TreeAttnArgs a) {
         if (now.n) {
             const uint32_t vis[1] = {now.drafted ? tree_bits(a, j.b, token, now.first, now.n) : now.n >= 32 ? ~0u : (1u << now.n) - 1u};
             const uint32_t qoff = opaque(Tile::koff(lane));
-            tree_step<T, D, 1>(row, [&](int kk) __attribute__((always_inline)) { return *(const V8*)(ldsQ + (qoff ^ (kk * 32u))); },
+            tree_step<T, D, 1, 2>(row, [&](int kk) __attribute__((always_inline)) { return *(const V8*)(ldsQ + (qoff ^ (kk * 32u))); },
                                ldsK, ldsV, lane, a.scale, vis, now.drafted || now.n < 32);
         }
         asm volatile("" ::: "memory");
@@ -402,89 +409,225 @@ __global__ __launch_bounds__(256, 2) void tree_attn_few(const TreeAttnArgs a) {
 }
 
 // ---- many rows -----------------------------------------------------------------------------------------------------------
-// 128 rows to a workgroup, 32 to a wave; all waves work on the same 64 keys, which the workgroup copies to LDS together, the
-// next block on its way through registers meanwhile.  Two workgroups share a CU and cover each other's waits.
+// 128 rows to a workgroup of four waves, 32 to a wave, two workgroups to a CU.  Here the matrix cores and the exponentials are what bounds, so a wave
+// does both at once: beside the weights of tile s of 32 keys (16 scores a lane: about 100 VALU instructions, 600 clocks) run the MFMAs of the
+// scores of tile s + 1 and of the output of tile s - 1 (16 of 33 clocks at D = 128), in an order that is pinned.  All waves work on the same
+// tiles, which the workgroup copies to four LDS slots: K of s + 1 and V of s - 1 are being read, tile s + 2 goes into the slot that V of s - 2
+// has left, and s + 3 and s + 4 are on their way through registers.
+//
+// Rows lie in LDS at pitches that put what is read together into different banks (16 rows of K 16 bytes each, 4 rows of V 64 bytes each) and leave every
+// fragment at a constant distance from a lane's first: with exclusive-ors instead, as above, 24 address instructions a tile went beside the MFMAs.
+template <int D> struct PaddedTile {
+    static constexpr uint32_t K_PITCH = D * 2 + 16, V_PITCH = D * 2 + 64, K_BYTES = 32 * K_PITCH, BYTES = K_BYTES + 32 * V_PITCH;
+};
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
     using Tile = KeyTile<T, D>;
-    using V8 = typename Mma<T>::V8;
-    constexpr uint32_t BLK = 2 * Tile::BYTES;                          // 64 rows of K (or of V)
-    __shared__ __align__(16) char lds[2][2 * BLK];
+    using Mm = Mma<T>;
+    using V8 = typename Mm::V8;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    using Pad = PaddedTile<D>;
+    constexpr uint32_t SLOT = Pad::BYTES;                              // a tile of K and one of V
+    constexpr int KF = D / 16, NB = D / 32, NV = 2 * NB, AHEAD = 3;    // MFMAs of a tile's scores, of its output (as many), LDS reads ahead of them
+    __shared__ __align__(16) char lds[4 * SLOT];
     __shared__ uint32_t odd;                                           // a drafted value is not finite
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6);
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6), h2 = lane >> 5;
     const TreeUnit u = tree_unit((a.rows + TREE_MANY_ROWS - 1) / TREE_MANY_ROWS);
     if (u.unit >= a.batch * a.n_parts * a.kv_heads) return;
     const TreeJob j = tree_job(a, u.unit, TREE_MANY_KEYS);
     const uint32_t r0 = u.row_block * TREE_MANY_ROWS, t_last = (min(r0 + TREE_MANY_ROWS, a.rows) - 1) / a.group;
     if (j.begin >= j.end || r0 / a.group >= j.drafted) return;
+    // without a tree nothing behind the block's last token is seen
+    const uint32_t end = a.tree ? j.end : min(j.end, max(j.begin, j.cache_blocks + t_last / TREE_MANY_KEYS + 1));
+    constexpr uint32_t NI = Tile::NI / 4;                              // 1 KB copies of a wave: 32 rows over four waves
+    const uint32_t lrow = wave * (Tile::RPI * NI) + lane / Tile::CHUNKS, chunk = lane % Tile::CHUNKS;
+    struct Staged { u32x4 k[NI], v[NI]; bool drafted; } staged[2];
+    auto fetch = [&](Staged& f, uint32_t tile) __attribute__((always_inline)) {
+        KeyRun x = key_run<D>(a, j, tile, TREE_MANY_KEYS, 0, TREE_MANY_KEYS);
+        if (tile >= end) x.n = 0;                                      // (behind the last: zeros)
+        const uint32_t bytes = uni(run_bytes<D>(x)), first = lrow * x.pitch + chunk * 16;
+        const OperandBuf K(uni_ptr(x.k), bytes), V(uni_ptr(x.v), bytes);
+        f.drafted = x.drafted;
+#pragma unroll
+        for (uint32_t i = 0; i < NI; ++i) f.k[i] = K.load16(first, i * Tile::RPI * x.pitch);
+#pragma unroll
+        for (uint32_t i = 0; i < NI; ++i) f.v[i] = V.load16(first, i * Tile::RPI * x.pitch);
+    };
+    auto finite = [&](Staged& f) __attribute__((always_inline)) {
+        bool bad = false;
+#pragma unroll
+        for (uint32_t i = 0; i < NI; ++i) bad |= without_not_finite<T>(f.v[i]);
+        if (bad) odd = 1;
+    };
+    auto put = [&](Staged& f, uint32_t slot) __attribute__((always_inline)) {
+        char* const to = lds + (slot & 3u) * SLOT + chunk * 16;
+#pragma unroll
+        for (uint32_t i = 0; i < NI; ++i) {
+            *(u32x4*)(to + lrow * Pad::K_PITCH + i * Tile::RPI * Pad::K_PITCH) = f.k[i];
+            *(u32x4*)(to + lrow * Pad::V_PITCH + Pad::K_BYTES + i * Tile::RPI * Pad::V_PITCH) = f.v[i];
+        }
+    };
+    if (tid == 0) odd = 0;
+    // V of the tile before the first, whose weights are zeros: in slot 3
+    for (uint32_t i = tid; i < 32 * Pad::V_PITCH / 16; i += 256) *(u32x4*)(lds + 3 * SLOT + Pad::K_BYTES + i * 16) = u32x4{0, 0, 0, 0};
+    __syncthreads();
+    fetch(staged[0], j.begin);
+    fetch(staged[1], j.begin + 1);
+    if (staged[0].drafted) finite(staged[0]);
+    put(staged[0], 0);
+    fetch(staged[0], j.begin + 2);
+    if (staged[1].drafted) finite(staged[1]);
+    put(staged[1], 1);
+    fetch(staged[1], j.begin + 3);
     RowState<D> row;
     clear_row(row);
-    const uint32_t at = r0 + wave * 32 + (lane & 31u);
-    V8 qf[D / 16];
+    const uint32_t at = r0 + wave * 32 + (lane & 31u), token = min(at, a.rows - 1) / a.group;
+    V8 qf[KF];
     {
         const T* const q = query_row<T>(a, j, at);
         const V8 zero = {};
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) qf[kk] = q ? *(const V8*)(q + kk * 16 + (lane >> 5) * 8) : zero;
+        for (int kk = 0; kk < KF; ++kk) qf[kk] = q ? *(const V8*)(q + kk * 16 + h2 * 8) : zero;
     }
-    const uint32_t token = min(at, a.rows - 1) / a.group;
-    // without a tree nothing behind the block's last token is seen
-    const uint32_t end = a.tree ? j.end : min(j.end, max(j.begin, j.cache_blocks + t_last / 64 + 1));
-    constexpr uint32_t NI = Tile::NI / 2;                              // 1 KB copies of a wave: 64 rows over four waves
-    const uint32_t lrow = wave * (Tile::RPI * NI) + lane / Tile::CHUNKS, chunk = lane % Tile::CHUNKS;
-    u32x4 kreg[NI], vreg[NI];
-    auto fetch = [&](const KeyRun& x) __attribute__((always_inline)) {
-        const uint32_t bytes = uni(run_bytes<D>(x)), first = lrow * x.pitch + chunk * 16;
-        const OperandBuf K(uni_ptr(x.k), bytes), V(uni_ptr(x.v), bytes);
+    const uint32_t koff = (lane & 31u) * Pad::K_PITCH + h2 * 16;
+    const uint32_t voff = Pad::K_BYTES + (4 * h2 + ((lane & 15u) >> 2)) * Pad::V_PITCH + ((lane >> 4) & 1u) * 32 + (lane & 3u) * 8;
+    auto read_k = [&](const char* slot, int i) __attribute__((always_inline)) { return *(const V8*)(slot + koff + i * 32); };
+    auto read_v = [&](const char* slot, int i) __attribute__((always_inline)) {   // slice i / NB of 16 keys, block i % NB of 32 d
+        T4 x[2];
 #pragma unroll
-        for (uint32_t i = 0; i < NI; ++i) kreg[i] = K.load16(first, i * Tile::RPI * x.pitch);
-#pragma unroll
-        for (uint32_t i = 0; i < NI; ++i) vreg[i] = V.load16(first, i * Tile::RPI * x.pitch);
+        for (int c = 0; c < 2; ++c) x[c] = TrRead<T>::read(slot + voff + ((i / NB) * 16 + c * 8) * Pad::V_PITCH + (i % NB) * 64);
+        return __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    // (lrow is wave * 16 and a lane's row, so the swizzles of later rows differ by exclusive-ors alone)
-    const uint32_t kput = lrow * Tile::PITCH + ((chunk ^ Tile::kswz(lrow)) << 4), vput = lrow * Tile::PITCH + ((chunk ^ Tile::vswz(lrow)) << 4);
-    auto put = [&](uint32_t buf, bool drafted) __attribute__((always_inline)) {
-        const uint32_t kp = opaque(kput), vp = opaque(vput);
-        if (drafted) {
-            bool bad = false;
+    f32x16 st[2];
+    V8 pf[2][2] = {};
+    const float sc = a.scale;
+    __syncthreads();
 #pragma unroll
-            for (uint32_t i = 0; i < NI; ++i) bad |= without_not_finite<T>(vreg[i]);
-            if (bad) odd = 1;
-        }
+    for (int v = 0; v < 16; ++v) st[0][v] = 0.0f;                      // scores of the first tile
 #pragma unroll
-        for (uint32_t i = 0; i < NI; ++i) *(u32x4*)(lds[buf] + (kp ^ ((Tile::kswz(i * Tile::RPI)) << 4)) + i * Tile::RPI * Tile::PITCH) = kreg[i];
-#pragma unroll
-        for (uint32_t i = 0; i < NI; ++i) *(u32x4*)(lds[buf] + BLK + (vp ^ ((Tile::vswz(i * Tile::RPI)) << 4)) + i * Tile::RPI * Tile::PITCH) = vreg[i];
+    for (int i = 0; i < KF; ++i) st[0] = Mm::mma(read_k(lds, i), qf[i], st[0]);
+    auto largest = [&](const f32x16& x) __attribute__((always_inline)) {
+        float m0 = fmaxf(fmaxf(x[0], x[1]), x[2]), m1 = fmaxf(fmaxf(x[3], x[4]), x[5]);
+        m0 = fmaxf(fmaxf(m0, x[6]), x[7]); m1 = fmaxf(fmaxf(m1, x[8]), x[9]);
+        m0 = fmaxf(fmaxf(m0, x[10]), x[11]); m1 = fmaxf(fmaxf(m1, x[12]), x[13]);
+        return fmaxf(fmaxf(fmaxf(m0, x[14]), x[15]), m1);
     };
-    if (tid == 0) odd = 0;
-    __syncthreads();
-    KeyRun x = key_run<D>(a, j, j.begin, TREE_MANY_KEYS, 0, TREE_MANY_KEYS), next = x;
-    if (j.begin < end) {
-        fetch(x);
-        put(0, x.drafted);
-        if (j.begin + 1 < end) { next = key_run<D>(a, j, j.begin + 1, TREE_MANY_KEYS, 0, TREE_MANY_KEYS); fetch(next); }
-    }
-    __syncthreads();
-    for (uint32_t blk = j.begin; blk < end; ++blk) {
-        const uint32_t buf = (blk - j.begin) & 1u;
-        uint32_t vis[2];
+    float top = largest(st[0]);                                        // of this lane's scores of the tile to be weighed
+    // Weights of the tile whose scores are in `sx`, into `px`; scores of the next tile (in slot `next`) into `sy`, and their largest; output of the
+    // one before (in slot `before`) with `py`.
+    auto segment = [&](f32x16& sx, V8 (&px)[2], f32x16& sy, const V8 (&py)[2], const char* next, const char* before, bool masked, uint32_t vis)
+                       __attribute__((always_inline)) {
+        V8 fr[AHEAD + 1];                                              // fragments on their way
+        auto rd = [&](int i) __attribute__((always_inline)) { fr[i % (AHEAD + 1)] = i < KF ? read_k(next, i) : read_v(before, i - KF); };
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const uint32_t n = x.n > 32u * t ? min(32u, x.n - 32u * t) : 0u;
-            vis[t] = x.drafted ? tree_bits(a, j.b, token, x.first + 32 * t, n) : n >= 32 ? ~0u : (1u << n) - 1u;
+        for (int i = 0; i < AHEAD; ++i) rd(i);
+        if (masked) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                if (!(vis >> (8 * (v / 4) + 4 * h2 + v % 4) & 1u)) sx[v] = -INFINITY;
+            top = largest(sx);
         }
-        tree_step<T, D, 2>(row, [&](int kk) __attribute__((always_inline)) { return qf[kk]; }, lds[buf], lds[buf] + BLK, lane, a.scale, vis, x.drafted || x.n < 64);
-        if (blk + 1 < end) {
-            put(buf ^ 1u, next.drafted);
-            x = next;
-            if (blk + 2 < end) { next = key_run<D>(a, j, blk + 2, TREE_MANY_KEYS, 0, TREE_MANY_KEYS); fetch(next); }
+        const float mx = max_halves(top) * sc;
+        const bool grown = __ballot(mx > row.m + WEIGHT_SLACK) != 0;   // (rarely, after the first steps)
+        float alpha = 1.0f;
+        if (grown) {
+            const float m_new = fmaxf(row.m, mx);
+            alpha = row.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(row.m - m_new);
+            row.m = m_new;
+            row.l *= alpha;
         }
-        __syncthreads();
+        const float ref = (row.m == -INFINITY ? 0.0f : row.m) - WEIGHT_OFF<T>;   // no key seen yet: keep the exponents finite
+        float sum[2] = {0.0f, 0.0f}, x0 = 0.0f, x1 = 0.0f, m0 = -INFINITY, m1 = -INFINITY;
+        auto weigh = [&](int v, int half) __attribute__((always_inline)) {       // scores v and v + 1, in two halves
+            if (half == 0) {
+                x0 = __builtin_fmaf(sx[v], sc, -ref);
+                x1 = __builtin_fmaf(sx[v + 1], sc, -ref);
+                x0 = __builtin_amdgcn_exp2f(x0);
+            } else {
+                x1 = __builtin_amdgcn_exp2f(x1);
+                sum[0] += x0; sum[1] += x1;                            // summed in 32 bits, rounded to 16 for the product with V only
+                px[v >> 3][v & 7] = (T)x0; px[v >> 3][(v & 7) + 1] = (T)x1;
+            }
+        };
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sy[v] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < KF + NV; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (i + AHEAD < KF + NV) rd(i + AHEAD);
+            if (i < KF) sy = Mm::mma(fr[i % (AHEAD + 1)], qf[i], sy);
+            else row.o[(i - KF) % NB] = Mm::mma(fr[i % (AHEAD + 1)], py[(i - KF) / NB], row.o[(i - KF) % NB]);
+            if constexpr (KF == 8) weigh(i & ~1, i & 1);
+            else { weigh(2 * i, 0); weigh(2 * i, 1); }
+            constexpr int FIRST = KF + NV - 4;                         // the next scores are there by then: four of them to a slot
+            if (i >= FIRST) {
+                m0 = fmaxf(fmaxf(m0, sy[4 * (i - FIRST)]), sy[4 * (i - FIRST) + 1]);
+                m1 = fmaxf(fmaxf(m1, sy[4 * (i - FIRST) + 2]), sy[4 * (i - FIRST) + 3]);
+            }
+        }
+        asm volatile("" ::"v"(px[0]), "v"(px[1]), "v"(sum[0]), "v"(sum[1]), "v"(m0), "v"(m1));   // (computed here, and not where they are used)
+        __builtin_amdgcn_sched_barrier(0);
+        row.l += sum[0] + sum[1];
+        top = fmaxf(m0, m1);
+        if (grown) {                                                   // what was added so far went by the reference value before
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) row.o[b][v] *= alpha;
+        }
+    };
+    // One tile: what it copies goes out two tiles before it is put into LDS, and that is a tile before it is read.
+    auto step = [&](uint32_t tile, int odd_one) __attribute__((always_inline)) {
+        KeyRun x = key_run<D>(a, j, tile, TREE_MANY_KEYS, 0, TREE_MANY_KEYS);
+        if (tile >= end) x.n = 0;
+        const bool masked = x.drafted || x.n < 32;
+        uint32_t vis = ~0u;
+        if (masked) vis = x.drafted ? tree_bits(a, j.b, token, x.first, x.n) : (1u << x.n) - 1u;
+        const uint32_t slot = tile - j.begin;
+        // (behind the last tile the scores are of whatever the slot holds, and not used)
+        segment(st[odd_one], pf[odd_one], st[odd_one ^ 1], pf[odd_one ^ 1], lds + ((slot + 1) & 3u) * SLOT, lds + ((slot - 1) & 3u) * SLOT, masked, vis);
+        if (staged[odd_one].drafted) finite(staged[odd_one]);
+        put(staged[odd_one], slot + 2);
+        fetch(staged[odd_one], tile + 4);
+        __syncthreads();                                               // the tile put is in its slot, the one read is done with
+    };
+    uint32_t tile = j.begin;
+    // The bulk: whole tiles of cached rows up to the last one fetched, without the general step's 110 scalar instructions and branches a tile.
+    const uint32_t whole = min(end, j.cached / TREE_MANY_KEYS);
+    if (tile + 5 < whole) {
+        const KeyRun x = key_run<D>(a, j, tile + 4, TREE_MANY_KEYS, 0, TREE_MANY_KEYS);
+        const char *kp = uni_ptr(x.k), *vp = uni_ptr(x.v);
+        const uint32_t bytes = uni(run_bytes<D>(x)), pitch = uni(x.pitch), first = lrow * pitch + chunk * 16;
+        auto quick = [&](int odd_one, uint32_t slot) __attribute__((always_inline)) {
+            segment(st[odd_one], pf[odd_one], st[odd_one ^ 1], pf[odd_one ^ 1], lds + ((slot + 1) & 3u) * SLOT, lds + ((slot - 1) & 3u) * SLOT, false, ~0u);
+            put(staged[odd_one], slot + 2);
+            const OperandBuf K(kp, bytes), V(vp, bytes);
+#pragma unroll
+            for (uint32_t i = 0; i < NI; ++i) staged[odd_one].k[i] = K.load16(first, i * Tile::RPI * pitch);
+#pragma unroll
+            for (uint32_t i = 0; i < NI; ++i) staged[odd_one].v[i] = V.load16(first, i * Tile::RPI * pitch);
+            kp += TREE_MANY_KEYS * (uint64_t)pitch;
+            vp += TREE_MANY_KEYS * (uint64_t)pitch;
+            __syncthreads();
+        };
+        for (; tile + 5 < whole; tile += 2) {
+            quick(0, tile - j.begin);
+            quick(1, tile - j.begin + 1);
+        }
+        staged[0].drafted = staged[1].drafted = false;
     }
-    const uint32_t h2 = lane >> 5;
+    for (; tile < end; tile += 2) {                                    // (a last one without keys where their number is odd)
+        step(tile, 0);
+        step(tile + 1, 1);
+    }
+    if (j.begin < end) {                                               // the output of the last tile
+        const char* const last = lds + ((((end - j.begin) + 1) & ~1u) - 1 & 3u) * SLOT;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) row.o[i % NB] = Mm::mma(read_v(last, i), pf[1][i / NB], row.o[i % NB]);
+    }
     row.l += __shfl_xor(row.l, 32);
 #pragma unroll
-    for (int b = 0; b < D / 32; ++b)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             f32x4 o;
