@@ -8,6 +8,7 @@ an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import struct
 from typing import Optional
@@ -618,6 +619,18 @@ def conv_chain_n_check_waits(desc: ConvChainNDesc, kind: int, n_cu: int = 0, **p
 # These calls are short, so their descriptors are packed in one go (in the header's order, as the classes above have it) and each tensor is
 # asked once for what is needed: 35 fields set one by one and the former checks took 23 us a call, three times the two launches.
 
+_TORCH = None
+
+
+def _torch():
+    """torch, imported at the first call (nothing else of this module needs it)."""
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        _TORCH = torch
+    return _TORCH
+
+
 _P_TREE = struct.Struct("8i P3q 2P3q 2P3q 3Pq f4x P3q P")
 _P_APPEND = struct.Struct("7i4x 2P3q 2P3q 7P")
 _P_WEIGHTS = struct.Struct("9i4x P3q P P3q 3P f4x P")
@@ -656,7 +669,7 @@ def _arr(t, name: str, dtype, device: int, shape) -> int:
 
 def _call(device: int, what: str, f, *args) -> None:
     """f(*args) with this device current, and its status checked."""
-    import torch
+    torch = _torch()
     if device == torch.cuda.current_device():
         rc = f(*args)
     else:
@@ -668,14 +681,14 @@ def _call(device: int, what: str, f, *args) -> None:
 
 def _workspace(nbytes: int, given, device: int, stream):
     """`given`, or memory that torch's allocator ties to `stream` (a hipStream_t): (tensor to keep, pointer, bytes)."""
-    import torch
+    torch = _torch()
     if given is not None:
         if given.get_device() != device or not given.is_contiguous():
             raise ValueError("the workspace must be a contiguous tensor on the device of the others")
         return given, given.data_ptr(), given.numel() * given.element_size()
     if nbytes == 0:
         return None, None, 0
-    if (stream or 0) == torch.cuda.current_stream(device).cuda_stream:
+    if (stream or 0) == torch._C._cuda_getCurrentRawStream(device):
         t = torch.empty(nbytes, dtype=torch.uint8, device=device)
     else:
         own = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
@@ -687,7 +700,7 @@ def _workspace(nbytes: int, given, device: int, stream):
 def tree_mask(parents):
     """The `tree` words of dep_tree_attn for drafted tokens with these parents: an integer tensor [T] or [B, T] in host memory, -1 (or any
     negative value) for a root, every parent before its children.  Each token sees itself and its ancestors.  -> int64 [.., T, ceil(T / 64)]"""
-    import torch
+    torch = _torch()
     p = torch.as_tensor(parents)
     if p.is_cuda or p.dim() not in (1, 2) or p.shape[-1] < 1:
         raise ValueError("parents must be a host tensor [tokens] or [batch, tokens]")
@@ -708,7 +721,7 @@ def tree_mask(parents):
 
 def _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached):
     """(descriptor, device) of a call."""
-    import torch
+    torch = _torch()
     device, dtype = q.get_device(), q.dtype
     code = _dtype_code(q)
     if q.dim() != 4 or k_new.dim() != 4:
@@ -742,6 +755,12 @@ def _bytes(what: str, device: int, f, *args) -> int:
     return need.value
 
 
+@functools.lru_cache(maxsize=4096)
+def _tree_attn_bytes(device: int, sizes: bytes) -> int:
+    """The workspace of dep_tree_attn, by the descriptor's eight sizes: all that it depends on beside the device."""
+    return _bytes("dep_tree_attn", device, _lib().depsync_tree_attn_workspace, sizes + bytes(_P_TREE.size - len(sizes)), 0)
+
+
 def dep_tree_attn(q, k_new, v_new, k_cache, v_cache, cached, out, lse=None, tree=None, drafted=None, scale: Optional[float] = None,
                   max_cached: Optional[int] = None, workspace=None, stream=None) -> None:
     """Enqueue out = softmax(scale q k^T) v of drafted tokens over a cache and, as `tree` (see tree_mask) says, one another.
@@ -751,7 +770,7 @@ def dep_tree_attn(q, k_new, v_new, k_cache, v_cache, cached, out, lse=None, tree
     lse [B, T, Hq] (float32) receives the logarithm of each row's sum.  max_cached: the most rows that a sequence has, where the host knows."""
     d, device = _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached)
     stream = _stream_handle(stream)
-    need = 0 if workspace is not None else _bytes("dep_tree_attn", device, _lib().depsync_tree_attn_workspace, d, 0)
+    need = 0 if workspace is not None else _tree_attn_bytes(device, d[:32])
     keep, ptr, size = _workspace(need, workspace, device, stream)
     _call(device, "dep_tree_attn", _lib().dep_tree_attn, d, ptr, size, stream)
 
@@ -764,7 +783,7 @@ def tree_attn_workspace(q, k_new, v_new, k_cache, v_cache, cached, out, lse=None
 
 
 def _accepted(B: int, tokens: int, accepted, n_accepted, device: int):
-    import torch
+    torch = _torch()
     if accepted is not None and accepted.dim() != 2:
         raise ValueError("accepted must be [batch, n_max]")
     n_max = tokens if accepted is None else accepted.shape[1]
@@ -775,7 +794,7 @@ def dep_cache_append(k_new, v_new, k_cache, v_cache, cached, cached_out, accepte
                      stream=None) -> None:
     """Enqueue: the keys and values of drafted tokens accepted[b, :n_accepted[b]] (int32; None: the first ones) go to rows cached[b].. of the cache,
     their weights [B, Hk, capacity] (float32) become 0, their positions (int32, same shape) start[b].., and cached_out = cached + n."""
-    import torch
+    torch = _torch()
     device, dtype = k_new.get_device(), k_new.dtype
     code = _dtype_code(k_new)
     if k_new.dim() != 4 or k_cache.dim() != 4:
@@ -795,7 +814,7 @@ def dep_cache_weights(q, lse, k_cache, cached, weights, accepted=None, n_accepte
                       max_cached: Optional[int] = None, stream=None) -> None:
     """Enqueue weights[b, h, k] += the attention weight that cached row k received from the accepted tokens, whose own rows are the last
     of cached[b].  q [B, T, Hq, D] and lse [B, T, Hq] are dep_tree_attn's; weights is [B, Hk, capacity] (float32)."""
-    import torch
+    torch = _torch()
     device, dtype = q.get_device(), q.dtype
     code = _dtype_code(q)
     if q.dim() != 4 or k_cache.dim() != 4:
@@ -811,7 +830,7 @@ def dep_cache_weights(q, lse, k_cache, cached, weights, accepted=None, n_accepte
 
 def _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out):
     """(descriptor, device) of a call."""
-    import torch
+    torch = _torch()
     device, dtype = k_cache.get_device(), k_cache.dtype
     code = _dtype_code(k_cache)
     if k_cache.dim() != 4:

@@ -245,7 +245,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_many_kernel(const CacheW
 // walk in row order then lists the moves.  One workgroup per sequence and head; the keys stay in LDS where they fit.  A few rows' worth of
 // arithmetic on 8 bytes a row: bound by the latencies of its steps (2053 rows of 256 heads 9 us, 16384 of 32 heads 24 us), so loads go out eight to
 // a thread at once, and a step that appended few rows moves them in the same launch.
-constexpr uint32_t EVICT_THREADS = 1024, EVICT_LDS_KEYS = 32768, EVICT_VPT = 4, EVICT_LOADS = 8, EVICT_FUSED = 256;
+constexpr uint32_t EVICT_LDS_KEYS = 32768, EVICT_VPT = 4, EVICT_LOADS = 8, EVICT_FUSED = 256;
 
 // Larger float, larger integer; NaN is the least.  Infinity is below 0xffffffff, the key of the newest rows.
 __device__ __forceinline__ uint32_t evict_key(float w) {
@@ -255,6 +255,7 @@ __device__ __forceinline__ uint32_t evict_key(float w) {
 __device__ __forceinline__ bool evict_new(int32_t pos, int32_t newest, uint32_t recent) { return (int64_t)pos > (int64_t)newest - (int64_t)recent; }
 
 // Exclusive sum over the threads of the workgroup, and the total.
+template <uint32_t THREADS>
 __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* wave_sums, uint32_t& total) {
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     uint32_t x = v;
@@ -268,7 +269,7 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* wave_sums, 
     __syncthreads();
     uint32_t before = 0, all = 0;
 #pragma unroll
-    for (uint32_t i = 0; i < EVICT_THREADS / 64; ++i) {
+    for (uint32_t i = 0; i < THREADS / 64; ++i) {
         const uint32_t s = wave_sums[i];
         before += i < wave ? s : 0u;
         all += s;
@@ -293,10 +294,12 @@ __device__ __forceinline__ void move_row(const CacheEvictArgs& a, uint32_t pair,
     }
 }
 
-__global__ __launch_bounds__(1024) void cache_evict_select_kernel(const CacheEvictArgs a) {
-    __shared__ uint32_t keys[EVICT_LDS_KEYS];
-    __shared__ uint32_t hist[2][256], wave_sums[EVICT_THREADS / 64], found[2];
-    __shared__ int32_t newest_of[EVICT_THREADS / 64];
+template <uint32_t THREADS, uint32_t LDS_KEYS>
+__global__ __launch_bounds__(THREADS) void cache_evict_select_kernel(const CacheEvictArgs a) {
+    __shared__ uint32_t keys[LDS_KEYS];
+    __shared__ uint32_t hist[2][256], wave_sums[THREADS / 64], found[3];
+    __shared__ int32_t newest_of[THREADS / 64];
+    __shared__ uint32_t moved[2][EVICT_FUSED];                       // the first moves: where from, where to
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
     const uint32_t b = blockIdx.x / a.kv_heads, h = blockIdx.x % a.kv_heads;
     const uint32_t n = uni(clamp_count(a.cached[b], a.capacity));
@@ -307,28 +310,26 @@ __global__ __launch_bounds__(1024) void cache_evict_select_kernel(const CacheEvi
         const uint32_t moves = a.in_place ? 0u : n;
         if (tid == 0) list[0] = moves;
         if (a.fused)
-            for (uint32_t i = tid / a.lanes; i < moves; i += EVICT_THREADS / a.lanes) move_row(a, blockIdx.x, i, i, unit);
+            for (uint32_t i = tid / a.lanes; i < moves; i += THREADS / a.lanes) move_row(a, blockIdx.x, i, i, unit);
         else
-            for (uint32_t i = tid; i < moves; i += EVICT_THREADS) list[1 + i] = i;
+            for (uint32_t i = tid; i < moves; i += THREADS) list[1 + i] = i;
         return;
     }
     const float* const w = a.weights + (size_t)blockIdx.x * a.capacity;
     const int32_t* const pos = a.pos + (size_t)blockIdx.x * a.capacity;
-    const bool in_lds = n <= EVICT_LDS_KEYS;
+    const bool in_lds = n <= LDS_KEYS, at_once = n <= THREADS * EVICT_LOADS;
     if (tid < 256) hist[0][tid] = 0;
-    int32_t newest = INT32_MIN;
-    for (uint32_t i0 = 0; i0 < n; i0 += EVICT_THREADS * EVICT_LOADS) {
+    int32_t newest = INT32_MIN, y[EVICT_LOADS];
+    for (uint32_t i0 = 0; i0 < n; i0 += THREADS * EVICT_LOADS) {
         float x[EVICT_LOADS];
-        int32_t y[EVICT_LOADS];
 #pragma unroll
         for (uint32_t e = 0; e < EVICT_LOADS; ++e) {
-            const uint32_t i = min(i0 + e * EVICT_THREADS + tid, n - 1);
+            const uint32_t i = min(i0 + e * THREADS + tid, n - 1);    // (the last row again and again: the same key)
             x[e] = w[i]; y[e] = pos[i];
         }
 #pragma unroll
         for (uint32_t e = 0; e < EVICT_LOADS; ++e) {
-            const uint32_t i = min(i0 + e * EVICT_THREADS + tid, n - 1);   // (the last row again and again: the same key)
-            if (in_lds) keys[i] = evict_key(x[e]);
+            if (in_lds) keys[min(i0 + e * THREADS + tid, n - 1)] = evict_key(x[e]);
             newest = max(newest, y[e]);
         }
     }
@@ -337,35 +338,37 @@ __global__ __launch_bounds__(1024) void cache_evict_select_kernel(const CacheEvi
     if (lane == 0) newest_of[wave] = newest;
     __syncthreads();
 #pragma unroll
-    for (uint32_t i = 0; i < EVICT_THREADS / 64; ++i) newest = max(newest, newest_of[i]);
+    for (uint32_t i = 0; i < THREADS / 64; ++i) newest = max(newest, newest_of[i]);
     if (in_lds && a.recent) {
-        for (uint32_t i0 = 0; i0 < n; i0 += EVICT_THREADS * EVICT_LOADS) {
-            int32_t y[EVICT_LOADS];
+        for (uint32_t i0 = 0; i0 < n; i0 += THREADS * EVICT_LOADS) {
+            if (!at_once) {
 #pragma unroll
-            for (uint32_t e = 0; e < EVICT_LOADS; ++e) y[e] = pos[min(i0 + e * EVICT_THREADS + tid, n - 1)];
+                for (uint32_t e = 0; e < EVICT_LOADS; ++e) y[e] = pos[min(i0 + e * THREADS + tid, n - 1)];
+            }
 #pragma unroll
             for (uint32_t e = 0; e < EVICT_LOADS; ++e)
-                if (evict_new(y[e], newest, a.recent)) keys[min(i0 + e * EVICT_THREADS + tid, n - 1)] = 0xffffffffu;
+                if (evict_new(y[e], newest, a.recent)) keys[min(i0 + e * THREADS + tid, n - 1)] = 0xffffffffu;
         }
         __syncthreads();
     }
     auto key = [&](uint32_t i) __attribute__((always_inline)) { return in_lds ? keys[i] : evict_new(pos[i], newest, a.recent) ? 0xffffffffu : evict_key(w[i]); };
-    // the smallest key that stays, from its highest 8 bits down; `need` keys with these bits stay
+    // The smallest key that stays, from its highest 8 bits down; `need` keys with these bits stay.  Where all of them do, the rest is zeros.
     uint32_t prefix = 0, need = a.budget;
     for (int shift = 24, buf = 0; shift >= 0; shift -= 8, buf ^= 1) {
-        for (uint32_t i0 = 0; i0 < n; i0 += EVICT_THREADS * 4) {
+        for (uint32_t i0 = 0; i0 < n; i0 += THREADS * 4) {
             uint32_t k[4];
 #pragma unroll
-            for (uint32_t e = 0; e < 4; ++e) k[e] = key(min(i0 + e * EVICT_THREADS + tid, n - 1));
+            for (uint32_t e = 0; e < 4; ++e) k[e] = key(min(i0 + e * THREADS + tid, n - 1));
 #pragma unroll
             for (uint32_t e = 0; e < 4; ++e) {
-                bool todo = i0 + e * EVICT_THREADS + tid < n && (shift == 24 || k[e] >> (shift + 8) == prefix);
+                bool todo = i0 + e * THREADS + tid < n && (shift == 24 || k[e] >> (shift + 8) == prefix);
                 const uint32_t bin = (k[e] >> shift) & 255u;
-                // many keys share a bin (weights of one magnitude, rows that nothing attended to): a wave adds its first two bins at once
+                // Many keys share a bin (weights of one magnitude, rows that nothing attended to): a wave adds its first two bins at once where they
+                // are worth it.
 #pragma unroll
                 for (int peel = 0; peel < 2; ++peel) {
                     const uint64_t left = __ballot(todo);
-                    if (!left) break;
+                    if (__popcll(left) < 24) break;
                     const uint32_t bin0 = (uint32_t)__builtin_amdgcn_readlane((int)bin, (int)__builtin_ctzll(left));
                     const uint64_t same = __ballot(todo && bin == bin0);
                     if (lane == 0) atomicAdd(&hist[buf][bin0], (uint32_t)__popcll(same));
@@ -382,13 +385,13 @@ __global__ __launch_bounds__(1024) void cache_evict_select_kernel(const CacheEvi
             uint32_t x = sum;
 #pragma unroll
             for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t y = __shfl_up(x, d);
-                if (lane >= (uint32_t)d) x += y;
+                const uint32_t z = __shfl_up(x, d);
+                if (lane >= (uint32_t)d) x += z;
             }
             uint32_t above = x - sum;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (above < need && need <= above + c[e]) { found[0] = 255 - 4 * lane - e; found[1] = need - above; }
+                if (above < need && need <= above + c[e]) { found[0] = 255 - 4 * lane - e; found[1] = need - above; found[2] = need == above + c[e]; }
                 above += c[e];
             }
         } else if (wave < 5) {
@@ -397,10 +400,11 @@ __global__ __launch_bounds__(1024) void cache_evict_select_kernel(const CacheEvi
         __syncthreads();
         prefix = prefix << 8 | found[0];
         need = found[1];
+        if (found[2]) { prefix <<= shift; need = 0xffffffffu; break; }   // (uniform)
     }
     // in row order: of the rows with that key the first `need` stay
     uint32_t equal = 0, holes = 0, sources = 0;
-    for (uint32_t i0 = 0; i0 < n; i0 += EVICT_THREADS * EVICT_VPT) {
+    for (uint32_t i0 = 0; i0 < n; i0 += THREADS * EVICT_VPT) {
         const uint32_t first = i0 + tid * EVICT_VPT;
         uint32_t k[EVICT_VPT], eq = 0;
 #pragma unroll
@@ -408,8 +412,11 @@ __global__ __launch_bounds__(1024) void cache_evict_select_kernel(const CacheEvi
             k[e] = first + e < n ? key(first + e) : 0u;
             eq += first + e < n && k[e] == prefix;
         }
-        uint32_t all, rank = equal + block_scan(eq, wave_sums, all);
-        equal += all;
+        uint32_t all, rank = 0;
+        if (need != 0xffffffffu) {
+            rank = equal + block_scan<THREADS>(eq, wave_sums, all);
+            equal += all;
+        }
         bool hole[EVICT_VPT], source[EVICT_VPT];
         uint32_t both = 0;                                           // holes in the low half, sources in the high (at most 4096 of each)
 #pragma unroll
@@ -421,12 +428,20 @@ __global__ __launch_bounds__(1024) void cache_evict_select_kernel(const CacheEvi
             source[e] = stays && (!a.in_place || first + e >= a.budget);
             both += (hole[e] ? 1u : 0u) + (source[e] ? 0x10000u : 0u);
         }
-        const uint32_t at = block_scan(both, wave_sums, all);
+        const uint32_t at = block_scan<THREADS>(both, wave_sums, all);
         uint32_t hi = holes + (at & 0xffffu), si = sources + (at >> 16);
 #pragma unroll
         for (uint32_t e = 0; e < EVICT_VPT; ++e) {
-            if (source[e]) list[1 + si++] = first + e;
-            if (hole[e]) list[1 + a.max_moves + hi++] = first + e;
+            if (source[e]) {
+                list[1 + si] = first + e;
+                if (si < EVICT_FUSED) moved[0][si] = first + e;
+                ++si;
+            }
+            if (hole[e]) {
+                list[1 + a.max_moves + hi] = first + e;
+                if (hi < EVICT_FUSED) moved[1][hi] = first + e;
+                ++hi;
+            }
         }
         holes += all & 0xffffu;
         sources += all >> 16;
@@ -436,8 +451,11 @@ __global__ __launch_bounds__(1024) void cache_evict_select_kernel(const CacheEvi
         return;
     }
     __syncthreads();
-    for (uint32_t m = tid / a.lanes; m < sources; m += EVICT_THREADS / a.lanes)
-        move_row(a, blockIdx.x, list[1 + m], a.in_place ? list[1 + a.max_moves + m] : m, unit);
+    for (uint32_t m = tid / a.lanes; m < sources; m += THREADS / a.lanes) {
+        const uint32_t src = m < EVICT_FUSED ? moved[0][m] : list[1 + m];
+        const uint32_t dst = !a.in_place ? m : m < EVICT_FUSED ? moved[1][m] : list[1 + a.max_moves + m];
+        move_row(a, blockIdx.x, src, dst, unit);
+    }
 }
 
 // The listed rows moved.  In place sources lie behind the budget and their places before it, so no row is both.
@@ -475,7 +493,9 @@ hipError_t launch_cache_evict(const CacheEvictArgs& given, int head_dim, hipStre
     // EVICT_FUSED they are not worth another launch.
     const uint32_t most = a.in_place ? (a.max_cached > a.budget ? a.max_cached - a.budget : 0u) : a.budget;
     a.fused = most <= EVICT_FUSED;
-    hipError_t e = launch_one(cache_evict_select_kernel, pairs, EVICT_THREADS, stream, a);
+    // Half the waves have half the way to a barrier, and less LDS leaves room for other workgroups (2053 rows of 256 heads 14.1 and 10.6 us)
+    const hipError_t e = a.max_cached <= 512 * EVICT_LOADS ? launch_one(cache_evict_select_kernel<512, 8192>, pairs, 512, stream, a)
+                                                           : launch_one(cache_evict_select_kernel<1024, EVICT_LDS_KEYS>, pairs, 1024, stream, a);
     if (e != hipSuccess || a.fused) return e;
     uint32_t blocks = (most < a.max_moves ? most : a.max_moves) / (256 / a.lanes) + 1;
     if (blocks > 256) blocks = 256;
