@@ -245,7 +245,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_many_kernel(const CacheW
 // walk in row order then lists the moves.  One workgroup per sequence and head; the keys stay in LDS where they fit.  A few rows' worth of
 // arithmetic on 8 bytes a row: bound by the latencies of its steps (2053 rows of 256 heads 9 us, 16384 of 32 heads 24 us), so loads go out eight to
 // a thread at once, and a step that appended few rows moves them in the same launch.
-constexpr uint32_t EVICT_LDS_KEYS = 32768, EVICT_VPT = 4, EVICT_LOADS = 8, EVICT_FUSED = 256;
+constexpr uint32_t EVICT_LDS_KEYS = 32768, EVICT_LOADS = 8, EVICT_FUSED = 256, EVICT_FEW = 16;
 
 // Larger float, larger integer; NaN is the least.  Infinity is below 0xffffffff, the key of the newest rows.
 __device__ __forceinline__ uint32_t evict_key(float w) {
@@ -254,16 +254,24 @@ __device__ __forceinline__ uint32_t evict_key(float w) {
 }
 __device__ __forceinline__ bool evict_new(int32_t pos, int32_t newest, uint32_t recent) { return (int64_t)pos > (int64_t)newest - (int64_t)recent; }
 
+// A wave's prefix by DPP: rows of 16 lanes, then each row's last lane to the next row, and lane 31 to the upper half.  (Six steps through
+// ds_bpermute took 0.4 us.)
+template <class F>
+__device__ __forceinline__ uint32_t wave_prefix(uint32_t x, uint32_t none, F f) {
+#define DS_DPP(ctrl, rows) f(x, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)x, ctrl, rows, 0xf, false))
+    x = DS_DPP(0x111, 0xf); x = DS_DPP(0x112, 0xf); x = DS_DPP(0x114, 0xf); x = DS_DPP(0x118, 0xf);   // row_shr 1, 2, 4, 8
+    x = DS_DPP(0x142, 0xa); x = DS_DPP(0x143, 0xc);                                                  // row_bcast 15, 31
+#undef DS_DPP
+    return x;
+}
+__device__ __forceinline__ uint32_t wave_sums_to(uint32_t x) { return wave_prefix(x, 0u, [](uint32_t p, uint32_t q) { return p + q; }); }
+__device__ __forceinline__ uint32_t last_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); }
+
 // Exclusive sum over the threads of the workgroup, and the total.
 template <uint32_t THREADS>
 __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* wave_sums, uint32_t& total) {
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    uint32_t x = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t y = __shfl_up(x, d);
-        if (lane >= (uint32_t)d) x += y;
-    }
+    const uint32_t x = wave_sums_to(v);
     __syncthreads();                                                 // (the sums of the scan before are read)
     if (lane == 63) wave_sums[wave] = x;
     __syncthreads();
@@ -299,6 +307,8 @@ __global__ __launch_bounds__(THREADS) void cache_evict_select_kernel(const Cache
     __shared__ uint32_t keys[LDS_KEYS];
     __shared__ uint32_t hist[2][256], wave_sums[THREADS / 64], found[3];
     __shared__ int32_t newest_of[THREADS / 64];
+    __shared__ uint64_t least_of[2][THREADS / 64];
+    __shared__ uint32_t gone[EVICT_FEW];
     __shared__ uint32_t moved[2][EVICT_FUSED];                       // the first moves: where from, where to
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
     const uint32_t b = blockIdx.x / a.kv_heads, h = blockIdx.x % a.kv_heads;
@@ -333,8 +343,8 @@ __global__ __launch_bounds__(THREADS) void cache_evict_select_kernel(const Cache
             newest = max(newest, y[e]);
         }
     }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) newest = max(newest, __shfl_xor(newest, d));
+    // (positions as unsigned numbers in the same order)
+    newest = (int32_t)(last_lane(wave_prefix((uint32_t)newest ^ 0x80000000u, 0u, [](uint32_t p, uint32_t q) { return max(p, q); })) ^ 0x80000000u);
     if (lane == 0) newest_of[wave] = newest;
     __syncthreads();
 #pragma unroll
@@ -352,6 +362,47 @@ __global__ __launch_bounds__(THREADS) void cache_evict_select_kernel(const Cache
         __syncthreads();
     }
     auto key = [&](uint32_t i) __attribute__((always_inline)) { return in_lds ? keys[i] : evict_new(pos[i], newest, a.recent) ? 0xffffffffu : evict_key(w[i]); };
+    uint32_t sources = 0;
+    const uint32_t leaving = n - a.budget;
+    if (a.in_place && leaving <= EVICT_FEW) {
+        // A step's few: the least key (of equal ones the highest row) is looked for as often as rows have to go.
+        uint64_t least = 0;
+        for (uint32_t m = 0; m < leaving; ++m) {
+            uint64_t mine = ~0ull;
+            for (uint32_t i0 = 0; i0 < n; i0 += THREADS * 4) {
+                uint32_t k[4];
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) k[e] = key(min(i0 + e * THREADS + tid, n - 1));
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) {
+                    const uint64_t c = (uint64_t)k[e] << 32 | ~min(i0 + e * THREADS + tid, n - 1);
+                    if (c > least && c < mine) mine = c;
+                }
+            }
+            const uint32_t hi = last_lane(wave_prefix((uint32_t)(mine >> 32), ~0u, [](uint32_t p, uint32_t q) { return min(p, q); }));
+            const uint32_t lo = last_lane(wave_prefix((uint32_t)(mine >> 32) == hi ? (uint32_t)mine : ~0u, ~0u, [](uint32_t p, uint32_t q) { return min(p, q); }));
+            if (lane == 0) least_of[m & 1][wave] = (uint64_t)hi << 32 | lo;
+            __syncthreads();
+            least = ~0ull;
+#pragma unroll
+            for (uint32_t i = 0; i < THREADS / 64; ++i) least = min(least, least_of[m & 1][i]);
+            if (tid == 0) gone[m] = ~(uint32_t)least;
+        }
+        __syncthreads();
+        if (wave == 0) {                                             // lane l < leaving: the row gone[l], and row budget + l
+            const uint32_t g = lane < leaving ? gone[lane] : ~0u, r = a.budget + lane;
+            uint32_t at = 0;
+            bool stays = lane < leaving;
+            for (uint32_t m = 0; m < leaving; ++m) { at += gone[m] < g ? 1u : 0u; stays = stays && gone[m] != r; }
+            if (g < a.budget) { moved[1][at] = g; list[1 + a.max_moves + at] = g; }
+            const uint64_t all = __ballot(stays);
+            const uint32_t si = (uint32_t)__popcll(all & ((1ull << lane) - 1));
+            if (stays) { moved[0][si] = r; list[1 + si] = r; }
+            if (lane == 0) found[0] = (uint32_t)__popcll(all);
+        }
+        __syncthreads();
+        sources = found[0];
+    } else {
     // The smallest key that stays, from its highest 8 bits down; `need` keys with these bits stay.  Where all of them do, the rest is zeros.
     uint32_t prefix = 0, need = a.budget;
     for (int shift = 24, buf = 0; shift >= 0; shift -= 8, buf ^= 1) {
@@ -363,8 +414,8 @@ __global__ __launch_bounds__(THREADS) void cache_evict_select_kernel(const Cache
             for (uint32_t e = 0; e < 4; ++e) {
                 bool todo = i0 + e * THREADS + tid < n && (shift == 24 || k[e] >> (shift + 8) == prefix);
                 const uint32_t bin = (k[e] >> shift) & 255u;
-                // Many keys share a bin (weights of one magnitude, rows that nothing attended to): a wave adds its first two bins at once where they
-                // are worth it.
+                // Many keys share a bin (weights of one magnitude, rows that nothing attended to): a wave adds its first bins at once while that is
+                // worth it.
 #pragma unroll
                 for (int peel = 0; peel < 2; ++peel) {
                     const uint64_t left = __ballot(todo);
@@ -382,13 +433,7 @@ __global__ __launch_bounds__(THREADS) void cache_evict_select_kernel(const Cache
             uint32_t c[4], sum = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) { c[e] = hist[buf][255 - 4 * lane - e]; sum += c[e]; }
-            uint32_t x = sum;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t z = __shfl_up(x, d);
-                if (lane >= (uint32_t)d) x += z;
-            }
-            uint32_t above = x - sum;
+            uint32_t above = wave_sums_to(sum) - sum;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if (above < need && need <= above + c[e]) { found[0] = 255 - 4 * lane - e; found[1] = need - above; found[2] = need == above + c[e]; }
@@ -403,12 +448,12 @@ __global__ __launch_bounds__(THREADS) void cache_evict_select_kernel(const Cache
         if (found[2]) { prefix <<= shift; need = 0xffffffffu; break; }   // (uniform)
     }
     // in row order: of the rows with that key the first `need` stay
-    uint32_t equal = 0, holes = 0, sources = 0;
-    for (uint32_t i0 = 0; i0 < n; i0 += THREADS * EVICT_VPT) {
-        const uint32_t first = i0 + tid * EVICT_VPT;
-        uint32_t k[EVICT_VPT], eq = 0;
+    uint32_t equal = 0, holes = 0;
+    for (uint32_t i0 = 0; i0 < n; i0 += THREADS * EVICT_LOADS) {
+        const uint32_t first = i0 + tid * EVICT_LOADS;
+        uint32_t k[EVICT_LOADS], eq = 0;
 #pragma unroll
-        for (uint32_t e = 0; e < EVICT_VPT; ++e) {
+        for (uint32_t e = 0; e < EVICT_LOADS; ++e) {
             k[e] = first + e < n ? key(first + e) : 0u;
             eq += first + e < n && k[e] == prefix;
         }
@@ -417,27 +462,26 @@ __global__ __launch_bounds__(THREADS) void cache_evict_select_kernel(const Cache
             rank = equal + block_scan<THREADS>(eq, wave_sums, all);
             equal += all;
         }
-        bool hole[EVICT_VPT], source[EVICT_VPT];
-        uint32_t both = 0;                                           // holes in the low half, sources in the high (at most 4096 of each)
+        uint32_t hole = 0, source = 0;                               // one bit a row
 #pragma unroll
-        for (uint32_t e = 0; e < EVICT_VPT; ++e) {
+        for (uint32_t e = 0; e < EVICT_LOADS; ++e) {
             const bool there = first + e < n, is = there && k[e] == prefix;
             const bool stays = there && (k[e] > prefix || (is && rank < need));
             rank += is;
-            hole[e] = a.in_place && there && !stays && first + e < a.budget;
-            source[e] = stays && (!a.in_place || first + e >= a.budget);
-            both += (hole[e] ? 1u : 0u) + (source[e] ? 0x10000u : 0u);
+            hole |= (a.in_place && there && !stays && first + e < a.budget ? 1u : 0u) << e;
+            source |= (stays && (!a.in_place || first + e >= a.budget) ? 1u : 0u) << e;
         }
-        const uint32_t at = block_scan<THREADS>(both, wave_sums, all);
+        // holes in the low half, sources in the high (at most 8192 of each)
+        const uint32_t at = block_scan<THREADS>(__popc(hole) | __popc(source) << 16, wave_sums, all);
         uint32_t hi = holes + (at & 0xffffu), si = sources + (at >> 16);
 #pragma unroll
-        for (uint32_t e = 0; e < EVICT_VPT; ++e) {
-            if (source[e]) {
+        for (uint32_t e = 0; e < EVICT_LOADS; ++e) {
+            if (source >> e & 1u) {
                 list[1 + si] = first + e;
                 if (si < EVICT_FUSED) moved[0][si] = first + e;
                 ++si;
             }
-            if (hole[e]) {
+            if (hole >> e & 1u) {
                 list[1 + a.max_moves + hi] = first + e;
                 if (hi < EVICT_FUSED) moved[1][hi] = first + e;
                 ++hi;
@@ -445,6 +489,7 @@ __global__ __launch_bounds__(THREADS) void cache_evict_select_kernel(const Cache
         }
         holes += all & 0xffffu;
         sources += all >> 16;
+    }
     }
     if (!a.fused) {
         if (tid == 0) list[0] = sources;
