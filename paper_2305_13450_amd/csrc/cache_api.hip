@@ -185,22 +185,25 @@ int dep_cache_weights(const depsync_cache_weights_desc* d, void* stream) {
     if (d->capacity < 1 || d->max_cached < 0 || d->n_max < 1 || d->n_max > 65536 || (!d->accepted && d->n_max > d->tokens)) return DEPSYNC_EINVAL;
     if (!operand(d->q) || !array(d->lse) || !operand(d->k_cache) || !array(d->cached) || !optional(d->accepted) || !optional(d->n_accepted) || !array(d->weights))
         return DEPSYNC_EINVAL;
-    if (!strides(a.q_s, d->q_batch, d->q_token, d->q_head, d->batch, d->tokens, d->heads, D, false, false) ||
+    if (!strides(a.q_s, d->q_batch, d->q_token, d->q_head, d->batch, d->tokens, d->heads, D, false, true) ||
         !strides(a.cache_s, d->cache_batch, d->cache_token, d->cache_head, d->batch, d->capacity, d->kv_heads, D, false, true))
         return DEPSYNC_EINVAL;
     if (!base2_scale(d->scale, D, a.scale)) return DEPSYNC_EINVAL;
     a.q = d->q; a.lse = d->lse; a.k_cache = d->k_cache; a.cached = d->cached; a.accepted = d->accepted; a.n_accepted = d->n_accepted; a.weights = d->weights;
     a.batch = d->batch; a.tokens = d->tokens; a.heads = d->heads; a.kv_heads = d->kv_heads; a.group = d->heads / d->kv_heads; a.capacity = d->capacity; a.n_max = d->n_max;
     const int64_t keys = rows_hint(d->max_cached, d->capacity), pairs = (int64_t)d->batch * d->kv_heads;
-    if ((int64_t)d->n_max * a.group > 1 << 24 || pairs * cdiv64(keys, 64) > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;
+    if ((int64_t)d->n_max * a.group > 1 << 24 || pairs * cdiv64(keys, 32) > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;
     a.few = (int64_t)d->n_max * a.group <= 64;
+    int n_cu = 0;
+    if (int rc = cu_count(n_cu); rc != DEPSYNC_OK) return rc;
     if (a.few) {
-        int n_cu = 0;
-        if (int rc = cu_count(n_cu); rc != DEPSYNC_OK) return rc;
         a.part_blocks = (uint32_t)std::max<int64_t>(1, cdiv64(cdiv64(keys, 128) * pairs, 3 * (int64_t)n_cu));   // three workgroups share a CU
         a.n_parts = (uint32_t)cdiv64(cdiv64(keys, 128), a.part_blocks);
     } else {
-        a.n_parts = (uint32_t)cdiv64(keys, 64);
+        // 64 keys to a workgroup read the queries half as often as 32, but the first keys' have all rows to walk and the last ones' few: where they are
+        // not many, twice as many even that out
+        a.keys = pairs * cdiv64(keys, 64) < 4 * (int64_t)n_cu ? 32 : 64;
+        a.n_parts = (uint32_t)cdiv64(keys, a.keys);
     }
     const hipError_t e = launch_cache_weights(a, d->dtype, D, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);

@@ -145,17 +145,18 @@ __global__ __launch_bounds__(256, 3) void cache_weights_few_kernel(const CacheWe
     }
 }
 
-// More rows, those of a prompt: the time is that of the matrix cores and the exponentials.  A workgroup keeps 64 keys' fragments in
+// More rows, those of a prompt: the time is that of the matrix cores and the exponentials.  A workgroup keeps 32 KT keys' fragments in
 // registers, in every wave, and its four waves walk the rows, 32 tokens of one query head at a time each, the next ones on their way into
 // registers meanwhile.  (Rows by head and not by token: their addresses are a line then, and the last key they see as well.)
-template <typename T, int D>
+template <typename T, int D, int KT>
 __global__ __launch_bounds__(256, 2) void cache_weights_many_kernel(const CacheWeightsArgs a) {
     using Tile = KeyTile<T, D>;
     using M = Mma<T>;
     using V8 = typename M::V8;
+    constexpr uint32_t KEYS = 32 * KT, NK = Tile::NI * KT / 4;       // a wave's 1 KB copies of keys
     __shared__ __align__(16) char lds[4][Tile::BYTES];             // the keys, then each wave's rows
     __shared__ __align__(16) float lse[4][32];
-    __shared__ float joined[4][64];
+    __shared__ float joined[4][KEYS];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6), h2 = lane >> 5;
     const uint32_t h = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, part = rest % a.n_parts, b = rest / a.n_parts;
     const uint32_t cached = uni(clamp_count(a.cached[b], a.capacity));
@@ -164,77 +165,95 @@ __global__ __launch_bounds__(256, 2) void cache_weights_many_kernel(const CacheW
     const uint32_t lrow = lane / Tile::CHUNKS, chunk = lane % Tile::CHUNKS;
     const uint32_t koff = Tile::koff(lane), put = lrow * Tile::PITCH + ((chunk ^ Tile::kswz(lrow)) << 4);
     char* const mine = lds[wave];
+    const uint32_t q_pitch = (uint32_t)a.q_s.token * 2u;
     const int32_t base = (int32_t)cached - (int32_t)n;             // row i sees keys 0..base + i
-    for (uint32_t k0 = part * 64; k0 < cached; k0 += a.n_parts * 64) {   // (once, unless max_cached is less than a sequence has)
-        V8 kf[2][D / 16];
+    for (uint32_t k0 = part * KEYS; k0 < cached; k0 += a.n_parts * KEYS) {   // (once, unless max_cached is less than a sequence has)
+        V8 kf[KT][D / 16];
         {
-            const uint32_t pitch = (uint32_t)a.cache_s.token * 2u;
+            const uint32_t pitch = (uint32_t)a.cache_s.token * 2u, have = min(KEYS, cached - k0);
+            const char* p = (const char*)a.k_cache + ((int64_t)b * a.cache_s.batch + (int64_t)k0 * a.cache_s.token + (int64_t)h * a.cache_s.head) * 2;
+            const OperandBuf K(uni_ptr(p), uni((have - 1) * pitch + D * 2u));   // (rows that are not there: zeros)
+            u32x4 reg[NK];                                         // (tiles of 32 keys behind one another)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const uint32_t first = k0 + 32 * t, have = first < cached ? min(32u, cached - first) : 0u;
-                const char* p = (const char*)a.k_cache + ((int64_t)b * a.cache_s.batch + (int64_t)first * a.cache_s.token + (int64_t)h * a.cache_s.head) * 2;
-                const OperandBuf K(uni_ptr(p), uni(have ? (have - 1) * pitch + D * 2u : 0u));
-                __syncthreads();
-                for (uint32_t i = wave; i < Tile::NI; i += 4)
-                    *(u32x4*)(lds[t] + (put ^ ((Tile::kswz(i * Tile::RPI)) << 4)) + i * Tile::RPI * Tile::PITCH) = K.load16(lrow * pitch + chunk * 16, i * Tile::RPI * pitch);
-                __syncthreads();
+            for (uint32_t i = 0; i < NK; ++i) reg[i] = K.load16(lrow * pitch + chunk * 16, (wave * NK + i) * Tile::RPI * pitch);
+            __syncthreads();                                       // (the rows of the keys before are done with)
+#pragma unroll
+            for (uint32_t i = 0; i < NK; ++i) {
+                const uint32_t rr = (wave * NK + i) * Tile::RPI + lrow;
+                *(u32x4*)(lds[0] + rr * Tile::PITCH + ((chunk ^ Tile::kswz(rr & 31u)) << 4)) = reg[i];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) kf[t][kk] = *(const V8*)(lds[t] + (koff ^ (kk * 32u)));
-            }
             __syncthreads();
         }
         const uint32_t i_first = (int32_t)k0 > base ? (uint32_t)((int32_t)k0 - base) & ~31u : 0u;   // rows before see none of these keys
-        const uint32_t steps_of_head = i_first < n ? (n - i_first + 31) / 32 : 0u, steps = steps_of_head * a.group;
+        const uint32_t i_end = i_first < n ? i_first + ((n - i_first + 31) & ~31u) : i_first;
+        struct Place { uint32_t g, i; };                           // a step's query head and first token
+        auto onward = [&](Place& x) __attribute__((always_inline)) {   // the wave's next step: four on
+            x.i += 128;
+            while (x.i >= i_end && x.g < a.group) { x.i -= i_end - i_first; ++x.g; }
+        };
         u32x4 qreg[Tile::NI];
         float sum = INFINITY;
-        auto fetch = [&](uint32_t s) __attribute__((always_inline)) {
-            const uint32_t g = s / steps_of_head, i0 = i_first + (s - g * steps_of_head) * 32, hq = h * a.group + g;
-            const T* const q = (const T*)a.q + (int64_t)b * a.q_s.batch + (int64_t)hq * a.q_s.head + chunk * 8;
+        auto fetch = [&](const Place& at) __attribute__((always_inline)) {
+            const uint32_t hq = h * a.group + at.g, mine = at.i + (lane & 31u);
+            const T* const q = (const T*)a.q + (int64_t)b * a.q_s.batch + (int64_t)hq * a.q_s.head;
+            if (!a.accepted) {                                     // (rows that are not there: zeros)
+                const OperandBuf Q(uni_ptr(q + (int64_t)at.i * a.q_s.token), uni((min(32u, n - at.i) - 1) * q_pitch + D * 2u));
 #pragma unroll
-            for (uint32_t i = 0; i < Tile::NI; ++i) {
-                const uint32_t at = i0 + i * Tile::RPI + lrow;
-                qreg[i] = at < n ? *(const u32x4*)(q + (int64_t)accepted_token(a, b, at) * a.q_s.token) : u32x4{0, 0, 0, 0};
+                for (uint32_t i = 0; i < Tile::NI; ++i) qreg[i] = Q.load16(lrow * q_pitch + chunk * 16, i * Tile::RPI * q_pitch);
+            } else {                                               // (the last one)
+#pragma unroll
+                for (uint32_t i = 0; i < Tile::NI; ++i)
+                    qreg[i] = *(const u32x4*)(q + (int64_t)accepted_token(a, b, min(at.i + i * Tile::RPI + lrow, n - 1)) * a.q_s.token + chunk * 8);
             }
-            const uint32_t at = i0 + (lane & 31u);
-            sum = at < n ? row_sum(a, b, accepted_token(a, b, at), hq) : INFINITY;   // (no such row: no weight)
+            const float x = row_sum(a, b, accepted_token(a, b, min(mine, n - 1)), hq);
+            sum = mine < n ? x : INFINITY;                         // (no such row: no weight)
         };
-        float w[2] = {0.0f, 0.0f};
+        float w[KT] = {};
         const int32_t key = (int32_t)(k0 + (lane & 31u));
-        if (wave < steps) fetch(wave);
-        for (uint32_t s = wave; s < steps; s += 4) {
+        Place now = {0, i_first + wave * 32};
+        while (now.i >= i_end && now.g < a.group && i_end > i_first) { now.i -= i_end - i_first; ++now.g; }
+        if (i_end == i_first) now.g = a.group;                     // (no row sees these keys)
+        if (now.g < a.group) fetch(now);
+        while (now.g < a.group) {
             const uint32_t p = opaque(put);
 #pragma unroll
             for (uint32_t i = 0; i < Tile::NI; ++i) *(u32x4*)(mine + (p ^ ((Tile::kswz(i * Tile::RPI)) << 4)) + i * Tile::RPI * Tile::PITCH) = qreg[i];
             if (lane < 32) lse[wave][lane] = sum;
-            const int32_t see = base + (int32_t)(i_first + s % steps_of_head * 32);   // the last key that the first of these rows sees
-            if (s + 4 < steps) fetch(s + 4);
+            const int32_t see = base + (int32_t)now.i;             // the last key that the first of these rows sees
+            onward(now);
+            if (now.g < a.group) fetch(now);
             asm volatile("" ::: "memory");                         // (a wave's LDS accesses keep their order)
             __builtin_amdgcn_wave_barrier();
-            f32x16 st[2];
+            V8 q[D / 16];
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int kk = 0; kk < D / 16; ++kk) q[kk] = *(const V8*)(mine + (koff ^ (kk * 32u)));
+            f32x16 st[KT];
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {                         // (one tile's scores beside the other's exponentials)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) st[t][v] = 0.0f;
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                const V8 q = *(const V8*)(mine + (koff ^ (kk * 32u)));
-#pragma unroll
-                for (int t = 0; t < 2; ++t) st[t] = M::mma(q, kf[t][kk], st[t]);
+                for (int kk = 0; kk < D / 16; ++kk) st[t] = M::mma(q[kk], kf[t][kk], st[t]);
             }
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < KT; ++t)
                 w[t] += rows_weight(st[t], lse[wave], h2, a.scale, (int32_t)k0 + 32 * t + 31 > see, key + 32 * t,
                                     [&](uint32_t r) __attribute__((always_inline)) { return see + (int32_t)r; });
             asm volatile("" ::: "memory");
             __builtin_amdgcn_wave_barrier();
         }
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < KT; ++t) {
             w[t] += __shfl_xor(w[t], 32);
             if (lane < 32) joined[wave][32 * t + lane] = w[t];
         }
         __syncthreads();
-        if (tid < 64 && k0 + tid < cached)
+        if (tid < KEYS && k0 + tid < cached)
             a.weights[((size_t)b * a.kv_heads + h) * a.capacity + k0 + tid] += (joined[0][tid] + joined[1][tid]) + (joined[2][tid] + joined[3][tid]);
     }
 }
@@ -514,7 +533,9 @@ __global__ __launch_bounds__(256) void cache_evict_move_kernel(const CacheEvictA
 
 template <typename T, int D>
 hipError_t launch_weights_of(const CacheWeightsArgs& a, hipStream_t stream) {
-    return launch_one(a.few ? cache_weights_few_kernel<T, D> : cache_weights_many_kernel<T, D>, a.batch * a.kv_heads * a.n_parts, 256, stream, a);
+    const uint32_t blocks = a.batch * a.kv_heads * a.n_parts;
+    if (a.few) return launch_one(cache_weights_few_kernel<T, D>, blocks, 256, stream, a);
+    return a.keys == 32 ? launch_one(cache_weights_many_kernel<T, D, 1>, blocks, 256, stream, a) : launch_one(cache_weights_many_kernel<T, D, 2>, blocks, 256, stream, a);
 }
 
 }  // namespace
