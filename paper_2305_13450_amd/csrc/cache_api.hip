@@ -61,8 +61,8 @@ int tree_check(const depsync_tree_attn_desc* d) {
 }
 
 // How the key axis of dep_tree_attn is cut: few (sequence, head) pairs and row blocks leave CUs idle unless it is, but parts leave results of
-// 4 (head_dim + 2) bytes a row in memory, which a second kernel reads.  The model, in microseconds, fitted to times of 28 shapes under
-// up to 29 cuts each (1 to 2048 rows, caches of 0 to 120000; its choice is within 10 % of the best cut in all but three, 17 % in those):
+// 4 (head_dim + 2) bytes a row in memory, which a second kernel reads.  The model, in microseconds, fitted to times of 27 shapes under
+// up to 28 cuts each (1 to 2048 rows, caches of 0 to 120000; its choice is 4 % behind the best cut in the mean, in the worst case 21 %):
 // a workgroup's start, a block of keys where its workgroup is alone on the CU and where two share it, the keys' way from HBM, the
 // second kernel and the results' way there and back.
 double tree_cost(int64_t base, int64_t part, int64_t blocks, int64_t pairs, int64_t rows, int64_t row_blocks, int head_dim, int n_cu, bool few) {
@@ -82,9 +82,11 @@ int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t
     const int64_t rows = (int64_t)d->tokens * a.group;
     if (rows > 1 << 24) return DEPSYNC_ENOTIMPL;
     a.rows = (uint32_t)rows;
-    // Two workgroups of 32 rows, whose second finds the keys in L2, are ahead of one of 128 up to 64 rows (16 x 40 rows over 1000 keys 22 and
-    // 25 us, 52 over 120000 with heads of 64 49 and 53; 80 rows over 4000 17 and 18; 100 over 2000 33 and 31; 252 over 4096 66 and 48)
-    a.few = rows <= 64;
+    // From 33 to 64 rows two workgroups of 32 walk the same keys, the second from L2; that is ahead of one of 128 rows until the caches are larger than
+    // what L2 and the Infinity Cache keep between the two (16 x 40 rows over 1000 keys of 8 heads, 70 MB: 21 and 26 us; 4 x 52 rows over 8000, 131 MB: 39 and
+    // 35; 16 x 40 over 4000, 268 MB: 64 and 60; 64 x 64 over 1000, 215 MB: 64 and 54).
+    const int64_t cache_bytes = (int64_t)d->batch * d->kv_heads * rows_hint(d->max_cached, d->capacity) * d->head_dim * 4;
+    a.few = rows <= (cache_bytes < 100000000 ? 64 : 32);
     const int64_t keys = a.few ? TREE_FEW_KEYS : TREE_MANY_KEYS, row_blocks = cdiv64(rows, a.few ? TREE_FEW_ROWS : TREE_MANY_ROWS);
     const int64_t pairs = (int64_t)d->batch * d->kv_heads, base = pairs * row_blocks;
     const int64_t blocks = cdiv64(rows_hint(d->max_cached, d->capacity), keys) + cdiv64(d->tokens, keys);
@@ -115,7 +117,7 @@ int evict_check(const depsync_cache_evict_desc* d) {
     if (!d) return DEPSYNC_EINVAL;
     if (int rc = common(d->batch, 1, d->kv_heads, d->kv_heads, d->head_dim, d->dtype, d->capacity); rc != DEPSYNC_OK) return rc;
     if (d->capacity < 1 || d->max_cached < 0 || d->budget < 1 || d->recent < 0 || d->recent > d->budget) return DEPSYNC_EINVAL;
-    return (int64_t)d->batch * d->kv_heads > MAX_BLOCKS / 512 ? DEPSYNC_ENOTIMPL : DEPSYNC_OK;
+    return (int64_t)d->batch * d->kv_heads > MAX_BLOCKS / 4 ? DEPSYNC_ENOTIMPL : DEPSYNC_OK;   // (1024 threads each)
 }
 
 }  // namespace

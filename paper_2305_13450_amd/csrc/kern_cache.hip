@@ -564,7 +564,7 @@ hipError_t launch_cache_evict(const CacheEvictArgs& given, int head_dim, hipStre
                                                            : launch_one(cache_evict_select_kernel<1024, EVICT_LDS_KEYS>, pairs, 1024, stream, a);
     if (e != hipSuccess || a.fused) return e;
     uint32_t blocks = (most < a.max_moves ? most : a.max_moves) / (256 / a.lanes) + 1;
-    if (blocks > 256) blocks = 256;
+    blocks = min(blocks, max(1u, min(256u, (1u << 23) / pairs)));
     void* args[] = {&a, &blocks};
     return hipLaunchKernel(reinterpret_cast<const void*>(cache_evict_move_kernel), dim3(pairs * blocks), dim3(256), args, 0, stream);
 }

@@ -101,7 +101,7 @@ def test_refusals(name):
 def test_launches_too_large_are_refused():
     assert call("dep_cache_append", append(batch=1 << 20, n_max=8, tokens=8, kv_heads=64)) == ds.ENOTIMPL
     assert call("dep_cache_weights", weights(batch=1 << 20, capacity=1 << 20)) == ds.ENOTIMPL
-    assert call("dep_cache_evict", evict(batch=1 << 20)) == ds.ENOTIMPL
+    assert call("dep_cache_evict", evict(batch=1 << 20, kv_heads=64)) == ds.ENOTIMPL
     n = ctypes.c_size_t(0)
     assert ds._lib().depsync_tree_attn_workspace(ctypes.byref(tree(batch=1 << 20, capacity=1 << 20, heads=64, kv_heads=64)), 256, ctypes.byref(n)) == ds.ENOTIMPL
 

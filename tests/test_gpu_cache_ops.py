@@ -93,7 +93,8 @@ def near(w, want, tol):
 @pytest.mark.parametrize("B,T,A,Hq,Hk,D,lens,counts", [
     (1, 1, None, 1, 1, 128, [1], None), (3, 16, 5, 8, 2, 64, [31, 128, 200], [5, 1, 0]), (2, 8, 4, 16, 1, 128, [127, 129], [4, 3]),
     (4, 12, 3, 6, 6, 128, [0, 2, 700, 33], [1, 3, 2, 3]), (2, 70, None, 4, 2, 64, [70, 333], None), (1, 300, None, 3, 1, 128, [300], None),
-    (2, 65, None, 1, 1, 128, [300, 64], [65, 20]), (1, 700, None, 12, 12, 128, [1500], None)])
+    (2, 65, None, 1, 1, 128, [300, 64], [65, 20]), (1, 700, None, 12, 12, 128, [1500], None),
+    (2, 90, 60, 4, 2, 64, [500, 61], [60, 33]), (3, 50, 40, 8, 2, 128, [40, 900, 0], [40, 7, 40]), (40, 80, None, 2, 1, 128, [2100] * 40, None)])
 def test_weights(B, T, A, Hq, Hk, D, lens, counts, dtype):
     print("weights", B, T, A, Hq, Hk, D, lens, dtype, flush=True)
     g = gen(4)
@@ -175,6 +176,51 @@ def test_evict_with_equal_positions_and_strides():
     torch.cuda.synchronize()
     same((kc, vc, w, pos, out), want)
     assert torch.equal(kv[..., D:], edge)
+
+
+def test_offsets_past_32_bits():
+    # rows 4 MiB apart: the last ones lie behind 4 GiB
+    print("offsets past 32 bits", flush=True)
+    rows, pitch, Hk, D = 1200, 1 << 21, 2, 128
+    buf = torch.zeros(rows * pitch, dtype=BF, device="cuda")
+    kc, vc = (buf.as_strided((1, rows, Hk, D), (0, pitch, D, 1), at) for at in (0, 4096))
+    g = gen(30)
+    kc.copy_(normal(g, kc.shape, BF))
+    vc.copy_(normal(g, vc.shape, BF))
+    w, pos = torch.rand((1, Hk, rows), generator=g, device="cuda"), torch.arange(rows, device="cuda").int().expand(1, Hk, rows).contiguous()
+    kn, vn = normal(g, (1, 40, Hk, D), BF), normal(g, (1, 40, Hk, D), BF)
+    cached, mid, out = ints([rows - 40]), ints([0]), ints([0])
+    want = ref.append(kn, vn, kc, vc, cached, w, pos, cached)
+    ds.dep_cache_append(kn, vn, kc, vc, cached, mid, weights=w, pos=pos, start=cached)
+    torch.cuda.synchronize()
+    same((kc, vc, w, pos, mid), want)
+    for T in (3, 40):
+        q, lse = normal(g, (1, T, 4, D), BF, 2.0), torch.full((1, T, 4), 8.0, device="cuda")
+        want_w, tol = ref.add_weights(q, lse, kc, mid, w)
+        ds.dep_cache_weights(q, lse, kc, mid, w)
+        torch.cuda.synchronize()
+        near(w, want_w, tol)
+    for budget in (rows - 5, 600):                          # a few rows one by one, many through the list
+        want = ref.evict(kc, vc, w, pos, mid, budget, 50)
+        ds.dep_cache_evict(kc, vc, w, pos, mid, out, budget, 50)
+        torch.cuda.synchronize()
+        same((kc, vc, w, pos, out), want)
+
+
+def test_calls_at_once_on_two_streams():
+    print("two streams", flush=True)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    jobs = []
+    for k, (cap, lens, budget) in enumerate(((3000, [3000, 2500], 1000), (300, [300, 290], 297))):
+        t = cache(2, 4, 128, cap, BF, 40 + k)
+        cached = ints(lens)
+        jobs.append((t, cached, budget, ref.evict(*t, cached, budget, 20), ints([0, 0])))
+    torch.cuda.synchronize()
+    for (t, cached, budget, _, out), s in zip(jobs, streams):
+        ds.dep_cache_evict(*t, cached, out, budget, 20, stream=s)
+    torch.cuda.synchronize()
+    for t, _, _, want, out in jobs:
+        same((*t, out), want)
 
 
 # ---- the loop ----------------------------------------------------------------------------------------------------------------

@@ -79,7 +79,8 @@ SHAPES = [
     (1, 1, 1, 1, 128, [0]), (1, 1, 1, 1, 64, [1]), (3, 1, 12, 12, 128, [31, 32, 33]), (3, 1, 8, 1, 64, [127, 128, 129]),
     (2, 31, 2, 2, 128, [63, 64]), (2, 4, 16, 2, 128, [65, 500]), (2, 11, 6, 2, 64, [0, 300]), (2, 7, 18, 2, 128, [130, 1]),
     (2, 64, 2, 2, 64, [255, 257]), (1, 65, 1, 1, 128, [200]), (2, 13, 10, 2, 128, [95, 700]), (2, 16, 8, 1, 64, [640, 0]),
-    (1, 43, 3, 1, 128, [129]), (2, 130, 4, 2, 128, [70, 1000]), (1, 257, 2, 2, 64, [77]),
+    (1, 43, 3, 1, 128, [129]), (2, 130, 4, 2, 128, [70, 1000]), (1, 257, 2, 2, 64, [77]), (2, 40, 8, 2, 64, [1000, 203]),
+    (3, 33, 4, 1, 128, [223, 224, 1025]),
 ]
 
 
@@ -233,6 +234,23 @@ def test_side_streams_and_graphs():
         torch.cuda.synchronize()
         want = run(*t, cached, tree=tree)
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+def test_calls_at_once_on_two_streams():
+    print("two streams", flush=True)
+    t = [make(2, T, 8, 2, 128, 6000, BF, 20 + T) for T in (1, 40)]
+    tree, cached = [random_tree(T, 21, 2) for T in (1, 40)], ints([6000, 3333])
+    want = [run(*x, cached, tree=m) for x, m in zip(t, tree)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    outs = [[(torch.zeros_like(w[0]), torch.zeros_like(w[1])) for _ in range(10)] for w in want]
+    torch.cuda.synchronize()
+    for i in range(10):
+        for k in (0, 1):
+            ds.dep_tree_attn(*t[k], cached, outs[k][i][0], lse=outs[k][i][1], tree=tree[k], stream=streams[k])
+    torch.cuda.synchronize()
+    for k in (0, 1):
+        for o, l in outs[k]:
+            assert torch.equal(o, want[k][0]) and torch.equal(l, want[k][1])
 
 
 def test_refusals_of_the_binding():
