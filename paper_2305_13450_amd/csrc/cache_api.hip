@@ -102,10 +102,14 @@ int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t
             if (u < best) { best = u; part = std::min(q, blocks); }
         }
     }
+    // (the kernels add up all sequences' blocks in 32 bits)
+    const int64_t parts = d->batch * (cdiv64(d->capacity, keys) + cdiv64(d->tokens, keys)) < 1ll << 32 ? cdiv64(blocks, part) : 1;
+    if (cdiv64(pairs * parts, 8) * 8 * row_blocks > MAX_BLOCKS || cdiv64(pairs * rows, 4) > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;
+    a.slots = (uint32_t)(d->batch * parts);
+    a.part_slots = (uint32_t)parts;
     a.part_blocks = (uint32_t)part;
-    a.n_parts = (uint32_t)cdiv64(blocks, part);
-    if (cdiv64(pairs * a.n_parts, 8) * 8 * row_blocks > MAX_BLOCKS || cdiv64(pairs * rows, 4) > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;
-    bytes = a.n_parts > 1 ? (size_t)pairs * a.n_parts * rows * (d->head_dim + 2) * sizeof(float) : 0;
+    a.part_least = (uint32_t)std::min<int64_t>(part, a.few ? 1 : 4);
+    bytes = parts > 1 ? (size_t)pairs * parts * rows * (d->head_dim + 2) * sizeof(float) : 0;
     return DEPSYNC_OK;
 }
 

@@ -15,13 +15,15 @@ struct TreeAttnArgs {
     const uint64_t* tree;                 // may be null: token t sees 0..t
     void* out;
     float* lse;                           // may be null
-    float* parts;                         // n_parts > 1: partial results (see tree_attn.hpp)
+    float* parts;                         // slots > batch: partial results (see tree_attn.hpp)
     Strides q_s, new_s, cache_s, out_s;
     int64_t tree_batch;
     uint32_t batch, tokens, heads, kv_heads, group, capacity;
     uint32_t rows;                        // tokens * group: query rows of one key and value head
     uint32_t few;                         // 1: the form for few rows
-    uint32_t n_parts, part_blocks;        // parts of the key axis, blocks of keys in each (the last part takes what is left)
+    uint32_t slots;                       // the most parts that all sequences' key axes are cut into (batch: none is cut)
+    uint32_t part_slots, part_blocks;     // of a sequence where each has as many: its parts, blocks of keys in one
+    uint32_t part_least;                  // blocks of keys in a part at least, where all share the slots
     float scale;                          // scores to base-2 exponents
 };
 

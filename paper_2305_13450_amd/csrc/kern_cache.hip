@@ -273,19 +273,6 @@ __device__ __forceinline__ uint32_t evict_key(float w) {
 }
 __device__ __forceinline__ bool evict_new(int32_t pos, int32_t newest, uint32_t recent) { return (int64_t)pos > (int64_t)newest - (int64_t)recent; }
 
-// A wave's prefix by DPP: rows of 16 lanes, then each row's last lane to the next row, and lane 31 to the upper half.  (Six steps through
-// ds_bpermute took 0.4 us.)
-template <class F>
-__device__ __forceinline__ uint32_t wave_prefix(uint32_t x, uint32_t none, F f) {
-#define DS_DPP(ctrl, rows) f(x, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)x, ctrl, rows, 0xf, false))
-    x = DS_DPP(0x111, 0xf); x = DS_DPP(0x112, 0xf); x = DS_DPP(0x114, 0xf); x = DS_DPP(0x118, 0xf);   // row_shr 1, 2, 4, 8
-    x = DS_DPP(0x142, 0xa); x = DS_DPP(0x143, 0xc);                                                  // row_bcast 15, 31
-#undef DS_DPP
-    return x;
-}
-__device__ __forceinline__ uint32_t wave_sums_to(uint32_t x) { return wave_prefix(x, 0u, [](uint32_t p, uint32_t q) { return p + q; }); }
-__device__ __forceinline__ uint32_t last_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); }
-
 // Exclusive sum over the threads of the workgroup, and the total.
 template <uint32_t THREADS>
 __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* wave_sums, uint32_t& total) {

@@ -4,8 +4,8 @@
 // a reference value m (a maximum that may lag), sum and un-normalised output per row.  All scores are computed transposed, as in attn_tile.hpp: a lane
 // owns one query row, S^T = K Q^T leaves 16 of 32 keys of it in its registers, and these are the B operand of O^T += V^T P^T as they stand.
 //
-// The key axis is the cached rows in blocks, then the drafted tokens in blocks; a block never mixes the two.  It is cut into
-// parts of `part_blocks` blocks, one workgroup each, as there are few (sequence, head) pairs on 256 CUs.  Parts leave their
+// The key axis is the cached rows in blocks, then the drafted tokens in blocks; a block never mixes the two.  Where there are few (sequence,
+// head) pairs on 256 CUs it is cut into parts of equally many blocks, one workgroup each.  Parts leave their
 // maxima, sums and un-normalised outputs in the workspace and a second kernel joins them in order, so results do not depend on timing.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -27,17 +27,18 @@ constexpr float WEIGHT_SLACK = 6.0f;
 template <typename T> constexpr float WEIGHT_OFF = 0.0f;
 template <> inline constexpr float WEIGHT_OFF<_Float16> = 9.0f;
 
-// Zeros in the place of infinities and NaN; whether there were any.
+// Zeros in the place of infinities and NaN; whether there were any.  Two values at a time: what is added carries an exponent of all ones into the sign's
+// place, and that bit becomes 16 (comparisons kept 128 scalar registers of conditions).
 template <typename T> __device__ __forceinline__ bool without_not_finite(u32x4& v) {
-    constexpr uint32_t E = __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
-    bool bad = false;
+    constexpr uint32_t ONE = __is_same(T, __bf16) ? 0x00800080u : 0x04000400u;   // 1 in the exponents
+    uint32_t bad = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const bool lo = (v[i] & E) == E, hi = (v[i] >> 16 & E) == E;
-        bad |= lo || hi;
-        v[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+        const uint32_t m = ((v[i] & 0x7fff7fffu) + ONE) & 0x80008000u;
+        bad |= m;
+        v[i] &= ~((m << 1) - (m >> 15));
     }
-    return bad;
+    return bad != 0;
 }
 
 __device__ __forceinline__ uint32_t clamp_count(int32_t v, uint32_t most) { return v < 0 ? 0u : min((uint32_t)v, most); }
@@ -161,24 +162,100 @@ __device__ __forceinline__ void tree_step(RowState<D>& row, Q query, const char*
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// A wave's prefix by DPP: rows of 16 lanes, then each row's last lane to the next row, and lane 31 to the upper half.  (Six steps through
+// ds_bpermute took 0.4 us.)
+template <class F>
+__device__ __forceinline__ uint32_t wave_prefix(uint32_t x, uint32_t none, F f) {
+#define DS_DPP(ctrl, rows) f(x, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)x, ctrl, rows, 0xf, false))
+    x = DS_DPP(0x111, 0xf); x = DS_DPP(0x112, 0xf); x = DS_DPP(0x114, 0xf); x = DS_DPP(0x118, 0xf);   // row_shr 1, 2, 4, 8
+    x = DS_DPP(0x142, 0xa); x = DS_DPP(0x143, 0xc);                                                  // row_bcast 15, 31
+#undef DS_DPP
+    return x;
+}
+__device__ __forceinline__ uint32_t wave_sums_to(uint32_t x) { return wave_prefix(x, 0u, [](uint32_t p, uint32_t q) { return p + q; }); }
+__device__ __forceinline__ uint32_t last_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); }
+
+// How the key axes of all sequences are cut: the lengths are known here only, so every wave works it out for itself.  Up to 64 sequences, a lane
+// each: all parts have as many blocks as lets them fit `slots`, whichever sequence they belong to, and an uneven batch keeps the chip as busy as an even one
+// (8 x 63 tokens of 32 heads over 500 to 4096 rows: 39 us, and 47 with each sequence cut as the longest one is).  More sequences leave little to cut: there
+// each has as many slots.  All of it stands before the first keys are asked for, so it is kept short (divisions are products: compiled ones, and
+// a walk over any number of sequences, made a call of one token 1.1 us longer).
+struct TreeCut {
+    uint32_t b, cached, drafted;         // a sequence and its lengths
+    uint32_t first, n, size;             // its first slot, its parts, blocks in each (the last has what is left)
+};
+template <bool SLOT>                     // of the sequence that slot x belongs to (b = batch: to none), or of sequence x
+__device__ __forceinline__ TreeCut tree_cut(const TreeAttnArgs& a, uint32_t x, uint32_t keys) {
+    TreeCut c;
+    const bool wide = a.batch > 64;
+    const uint32_t b = !wide ? threadIdx.x & 63u : SLOT ? x / a.part_slots : x;
+    const uint32_t cached = b < a.batch && a.capacity ? clamp_count(a.cached[b], a.capacity) : 0u;
+    const uint32_t drafted = b >= a.batch ? 0u : a.drafted ? clamp_count(a.drafted[b], a.tokens) : a.tokens;
+    const uint32_t blocks = (cached + keys - 1) / keys + (drafted + keys - 1) / keys;
+    if (wide) return {b, cached, drafted, b * a.part_slots, min(a.part_slots, (blocks + a.part_blocks - 1) / a.part_blocks), a.part_blocks};
+    const uint32_t all = last_lane(wave_sums_to(blocks));
+    // A sequence's last part is half empty in the mean, and nearly so at worst: then parts that fit in any case (slots is at least twice batch).  q is the
+    // quotient or, by rounding, one less, so one block more makes up for it.
+    uint32_t n, to, by = a.slots - a.batch / 2;
+    for (uint32_t more = 0;; more = 1, by = a.slots - a.batch) {
+        const uint32_t q = (uint32_t)((float)all * (__builtin_amdgcn_rcpf((float)by) * (1.0f - 0x1p-20f)));
+        c.size = uni(max(a.part_least, q + (q * by < all ? 1u + more : 0u) + (q >> 18)));
+        // never more parts than there are blocks for: one too few, which a million blocks can come to, makes the last part longer
+        n = (uint32_t)((float)blocks * (__builtin_amdgcn_rcpf((float)c.size) * (1.0f - 0x1p-20f)));
+        n += n * c.size < blocks ? 1u : 0u;
+        to = wave_sums_to(n);
+        if (more || last_lane(to) <= a.slots) break;
+    }
+    const uint64_t hit = SLOT ? __ballot(to > x) : 1ull << x;
+    if (!hit) { c.b = a.batch; return c; }
+    c.b = (uint32_t)__builtin_ctzll(hit);
+    c.cached = (uint32_t)__builtin_amdgcn_readlane((int)cached, (int)c.b);
+    c.drafted = (uint32_t)__builtin_amdgcn_readlane((int)drafted, (int)c.b);
+    c.n = (uint32_t)__builtin_amdgcn_readlane((int)n, (int)c.b);
+    c.first = (uint32_t)__builtin_amdgcn_readlane((int)to, (int)c.b) - c.n;
+    return c;
+}
+
+// The kernel's arguments, read anew: held from the start on they, and what follows from them, go through more scalar registers than there are (128 of
+// them spilled, a third of the few rows' kernel was moves from and to lanes).
+__device__ __forceinline__ const TreeAttnArgs& tree_args() {
+    typedef const __attribute__((address_space(4))) TreeAttnArgs* Segment;
+    Segment p = (Segment)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const TreeAttnArgs*)p;
+}
+
 // What a workgroup works on, the same in every lane.
 struct TreeJob {
-    uint32_t b, h, part;                 // sequence, key and value head, part of the keys
+    uint32_t b, h;                       // sequence, key and value head
+    uint32_t slot, n_parts;              // of all parts, parts of this sequence (0: there is no work)
     uint32_t cached, drafted;            // of the sequence
     uint32_t cache_blocks, begin, end;   // blocks of cached rows, this part's blocks
 };
 __device__ __forceinline__ TreeJob tree_job(const TreeAttnArgs& a, uint32_t unit, uint32_t block_keys) {
     TreeJob j;
     j.h = unit % a.kv_heads;
-    const uint32_t rest = unit / a.kv_heads;
-    j.part = rest % a.n_parts;
-    j.b = rest / a.n_parts;
-    j.cached = uni(a.capacity ? clamp_count(a.cached[j.b], a.capacity) : 0u);
-    j.drafted = uni(a.drafted ? clamp_count(a.drafted[j.b], a.tokens) : a.tokens);
+    j.slot = unit / a.kv_heads;
+    uint32_t part = 0, size = ~0u;
+    j.n_parts = 1;
+    if (a.slots > a.batch) {
+        const TreeCut c = tree_cut<true>(a, j.slot, block_keys);
+        j.b = uni(c.b);
+        j.cached = uni(c.cached);
+        j.drafted = uni(c.drafted);
+        j.n_parts = uni(c.n);
+        part = uni(j.slot - c.first);
+        size = c.size;
+        if (j.b >= a.batch || part >= j.n_parts) { j.n_parts = 0; return j; }
+    } else {
+        j.b = j.slot;
+        j.cached = uni(a.capacity ? clamp_count(a.cached[j.b], a.capacity) : 0u);
+        j.drafted = uni(a.drafted ? clamp_count(a.drafted[j.b], a.tokens) : a.tokens);
+    }
     j.cache_blocks = (j.cached + block_keys - 1) / block_keys;
     const uint32_t blocks = j.cache_blocks + (j.drafted + block_keys - 1) / block_keys;
-    j.begin = min(blocks, j.part * a.part_blocks);
-    j.end = j.part + 1 == a.n_parts ? blocks : min(blocks, j.begin + a.part_blocks);
+    j.begin = uni(part * size);
+    j.end = part + 1 == j.n_parts ? blocks : j.begin + size;
     return j;
 }
 // A pair's row blocks run on one XCD (every eighth workgroup does), one after the other, so that its keys come from HBM once.
@@ -187,16 +264,11 @@ __device__ __forceinline__ TreeUnit tree_unit(uint32_t row_blocks) {
     const uint32_t slot = blockIdx.x >> 3;
     return {(slot / row_blocks) * 8 + (blockIdx.x & 7u), slot % row_blocks};
 }
-// Parts of a sequence that have blocks: the ones that leave results.
-__device__ __forceinline__ uint32_t tree_live_parts(const TreeAttnArgs& a, uint32_t cached, uint32_t drafted, uint32_t block_keys) {
-    const uint32_t blocks = (cached + block_keys - 1) / block_keys + (drafted + block_keys - 1) / block_keys;
-    return min(a.n_parts, (blocks + a.part_blocks - 1) / a.part_blocks);
+// Workspace: outputs [slot][head][row][D], then maxima and sums [slot][head][row][2].
+__device__ __forceinline__ size_t tree_part_row(const TreeAttnArgs& a, uint32_t slot, uint32_t h, uint32_t row) {
+    return ((size_t)slot * a.kv_heads + h) * a.rows + row;
 }
-
-// Workspace: outputs [pair][part][row][D], then maxima and sums [pair][part][row][2], pair = sequence x head.
-__device__ __forceinline__ size_t tree_part_row(const TreeAttnArgs& a, uint32_t pair, uint32_t part, uint32_t row) {
-    return ((size_t)pair * a.n_parts + part) * a.rows + row;
-}
+__device__ __forceinline__ float* tree_sums(const TreeAttnArgs& a, int dim) { return a.parts + (size_t)a.slots * a.kv_heads * a.rows * dim; }
 
 // A run of keys as a workgroup or wave copies it to LDS: where it lies, and how many of its 32 (or 64) rows are there.
 struct KeyRun {
@@ -276,11 +348,11 @@ __device__ __forceinline__ void store_row4(const TreeAttnArgs& a, const TreeJob&
     if (t >= j.drafted) return;
     const uint32_t hq = j.h * a.group + g;
     if (__builtin_expect(odd, 0)) o = add_not_finite<T>(a, j, block_keys, t, d, o);
-    if (a.n_parts > 1) {
-        const size_t at = tree_part_row(a, j.b * a.kv_heads + j.h, j.part, r);
+    if (j.n_parts > 1) {
+        const size_t at = tree_part_row(a, j.slot, j.h, r);
         *(f32x4*)(a.parts + at * D + d) = o;
         if (d == 0) {
-            float* ml = a.parts + (size_t)a.batch * a.kv_heads * a.n_parts * a.rows * D + at * 2;
+            float* const ml = tree_sums(a, D) + at * 2;
             ml[0] = m; ml[1] = l;
         }
         return;
@@ -312,10 +384,10 @@ __global__ __launch_bounds__(256, 2) void tree_attn_few(const TreeAttnArgs a) {
     __shared__ uint32_t odd;                                           // a drafted value is not finite
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6);
     const TreeUnit u = tree_unit((a.rows + TREE_FEW_ROWS - 1) / TREE_FEW_ROWS);
-    if (u.unit >= a.batch * a.n_parts * a.kv_heads) return;
+    if (u.unit >= a.slots * a.kv_heads) return;
     const TreeJob j = tree_job(a, u.unit, TREE_FEW_KEYS);
     const uint32_t r0 = u.row_block * TREE_FEW_ROWS;
-    if (j.begin >= j.end || r0 / a.group >= j.drafted) return;
+    if (j.n_parts == 0 || j.begin >= j.end || r0 / a.group >= j.drafted) return;
     if (tid == 0) odd = 0;
     char* const ldsK = lds + wave * WAVE;
     char* const ldsV = ldsK + Tile::BYTES;
@@ -334,6 +406,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_few(const TreeAttnArgs a) {
     RowState<D> row;
     clear_row(row);
     const uint32_t token = min(r0 + (lane & 31u), a.rows - 1) / a.group;
+    const float sc = a.scale;
     for (uint32_t i = tid; i < 32 * Tile::CHUNKS; i += 256) {
         const uint32_t rr = i / Tile::CHUNKS, c = i % Tile::CHUNKS;
         const T* q = query_row<T>(a, j, r0 + rr);
@@ -356,16 +429,24 @@ __global__ __launch_bounds__(256, 2) void tree_attn_few(const TreeAttnArgs a) {
         for (uint32_t i = 0; i < Tile::NI; ++i) *(u32x4*)(ldsV + (vp ^ ((Tile::vswz(i * Tile::RPI)) << 4)) + i * Tile::RPI * Tile::PITCH) = vreg[i];
         const KeyRun now = x;
         if (blk + 1 < j.end) {
-            x = key_run<D>(a, j, blk + 1, TREE_FEW_KEYS, wave * 32, 32);
+            if (blk + 1 == j.cache_blocks) {
+                x = key_run<D>(tree_args(), j, blk + 1, TREE_FEW_KEYS, wave * 32, 32);
+            } else {
+                const uint32_t have = x.drafted ? j.drafted : j.cached;
+                x.k += TREE_FEW_KEYS * (uint64_t)x.pitch;
+                x.v += TREE_FEW_KEYS * (uint64_t)x.pitch;
+                x.first += TREE_FEW_KEYS;
+                x.n = x.first < have ? min(32u, have - x.first) : 0u;
+            }
             fetch(x);
         }
         asm volatile("" ::: "memory");                                 // (a wave's LDS accesses keep their order)
         __builtin_amdgcn_wave_barrier();
         if (now.n) {
-            const uint32_t vis[1] = {now.drafted ? tree_bits(a, j.b, token, now.first, now.n) : now.n >= 32 ? ~0u : (1u << now.n) - 1u};
+            const uint32_t vis[1] = {now.drafted ? tree_bits(tree_args(), j.b, token, now.first, now.n) : now.n >= 32 ? ~0u : (1u << now.n) - 1u};
             const uint32_t qoff = opaque(Tile::koff(lane));
             tree_step<T, D, 1, 2>(row, [&](int kk) __attribute__((always_inline)) { return *(const V8*)(ldsQ + (qoff ^ (kk * 32u))); },
-                               ldsK, ldsV, lane, a.scale, vis, now.drafted || now.n < 32);
+                               ldsK, ldsV, lane, sc, vis, now.drafted || now.n < 32);
         }
         asm volatile("" ::: "memory");
         __builtin_amdgcn_wave_barrier();
@@ -389,6 +470,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_few(const TreeAttnArgs a) {
             *(f32x4*)(mine + (lane & 31u) * (D + 4) + 32 * b + 8 * g + 4 * (lane >> 5)) = o;
         }
     __syncthreads();
+    const TreeAttnArgs& late = tree_args();
     const uint32_t rr = tid >> 3;
     float mm = -INFINITY, L = 0.0f;
 #pragma unroll
@@ -404,7 +486,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_few(const TreeAttnArgs a) {
         f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int w = 0; w < 4; ++w) o += *(const f32x4*)((const float*)(lds + w * WAVE) + rr * (D + 4) + d);
-        store_row4<T, D>(a, j, r0 + rr, d, o, mm, L, odd != 0, TREE_FEW_KEYS);
+        store_row4<T, D>(late, j, r0 + rr, d, o, mm, L, odd != 0, TREE_FEW_KEYS);
     }
 }
 
@@ -433,17 +515,17 @@ __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
     __shared__ uint32_t odd;                                           // a drafted value is not finite
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6), h2 = lane >> 5;
     const TreeUnit u = tree_unit((a.rows + TREE_MANY_ROWS - 1) / TREE_MANY_ROWS);
-    if (u.unit >= a.batch * a.n_parts * a.kv_heads) return;
+    if (u.unit >= a.slots * a.kv_heads) return;
     const TreeJob j = tree_job(a, u.unit, TREE_MANY_KEYS);
     const uint32_t r0 = u.row_block * TREE_MANY_ROWS, t_last = (min(r0 + TREE_MANY_ROWS, a.rows) - 1) / a.group;
-    if (j.begin >= j.end || r0 / a.group >= j.drafted) return;
+    if (j.n_parts == 0 || j.begin >= j.end || r0 / a.group >= j.drafted) return;
     // without a tree nothing behind the block's last token is seen
     const uint32_t end = a.tree ? j.end : min(j.end, max(j.begin, j.cache_blocks + t_last / TREE_MANY_KEYS + 1));
     constexpr uint32_t NI = Tile::NI / 4;                              // 1 KB copies of a wave: 32 rows over four waves
     const uint32_t lrow = wave * (Tile::RPI * NI) + lane / Tile::CHUNKS, chunk = lane % Tile::CHUNKS;
     struct Staged { u32x4 k[NI], v[NI]; bool drafted; } staged[2];
-    auto fetch = [&](Staged& f, uint32_t tile) __attribute__((always_inline)) {
-        KeyRun x = key_run<D>(a, j, tile, TREE_MANY_KEYS, 0, TREE_MANY_KEYS);
+    auto fetch = [&](const TreeAttnArgs& args, Staged& f, uint32_t tile) __attribute__((always_inline)) {
+        KeyRun x = key_run<D>(args, j, tile, TREE_MANY_KEYS, 0, TREE_MANY_KEYS);
         if (tile >= end) x.n = 0;                                      // (behind the last: zeros)
         const uint32_t bytes = uni(run_bytes<D>(x)), first = lrow * x.pitch + chunk * 16;
         const OperandBuf K(uni_ptr(x.k), bytes), V(uni_ptr(x.v), bytes);
@@ -471,14 +553,14 @@ __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
     // V of the tile before the first, whose weights are zeros: in slot 3
     for (uint32_t i = tid; i < 32 * Pad::V_PITCH / 16; i += 256) *(u32x4*)(lds + 3 * SLOT + Pad::K_BYTES + i * 16) = u32x4{0, 0, 0, 0};
     __syncthreads();
-    fetch(staged[0], j.begin);
-    fetch(staged[1], j.begin + 1);
+    fetch(a, staged[0], j.begin);
+    fetch(a, staged[1], j.begin + 1);
     if (staged[0].drafted) finite(staged[0]);
     put(staged[0], 0);
-    fetch(staged[0], j.begin + 2);
+    fetch(a, staged[0], j.begin + 2);
     if (staged[1].drafted) finite(staged[1]);
     put(staged[1], 1);
-    fetch(staged[1], j.begin + 3);
+    fetch(a, staged[1], j.begin + 3);
     RowState<D> row;
     clear_row(row);
     const uint32_t at = r0 + wave * 32 + (lane & 31u), token = min(at, a.rows - 1) / a.group;
@@ -577,18 +659,18 @@ __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
         }
     };
     // One tile: what it copies goes out two tiles before it is put into LDS, and that is a tile before it is read.
-    auto step = [&](uint32_t tile, int odd_one) __attribute__((always_inline)) {
-        KeyRun x = key_run<D>(a, j, tile, TREE_MANY_KEYS, 0, TREE_MANY_KEYS);
+    auto step = [&](const TreeAttnArgs& args, uint32_t tile, int odd_one) __attribute__((always_inline)) {
+        KeyRun x = key_run<D>(args, j, tile, TREE_MANY_KEYS, 0, TREE_MANY_KEYS);
         if (tile >= end) x.n = 0;
         const bool masked = x.drafted || x.n < 32;
         uint32_t vis = ~0u;
-        if (masked) vis = x.drafted ? tree_bits(a, j.b, token, x.first, x.n) : (1u << x.n) - 1u;
+        if (masked) vis = x.drafted ? tree_bits(args, j.b, token, x.first, x.n) : (1u << x.n) - 1u;
         const uint32_t slot = tile - j.begin;
         // (behind the last tile the scores are of whatever the slot holds, and not used)
         segment(st[odd_one], pf[odd_one], st[odd_one ^ 1], pf[odd_one ^ 1], lds + ((slot + 1) & 3u) * SLOT, lds + ((slot - 1) & 3u) * SLOT, masked, vis);
         if (staged[odd_one].drafted) finite(staged[odd_one]);
         put(staged[odd_one], slot + 2);
-        fetch(staged[odd_one], tile + 4);
+        fetch(args, staged[odd_one], tile + 4);
         __syncthreads();                                               // the tile put is in its slot, the one read is done with
     };
     uint32_t tile = j.begin;
@@ -616,15 +698,17 @@ __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
         }
         staged[0].drafted = staged[1].drafted = false;
     }
+    const TreeAttnArgs& later = tree_args();
     for (; tile < end; tile += 2) {                                    // (a last one without keys where their number is odd)
-        step(tile, 0);
-        step(tile + 1, 1);
+        step(later, tile, 0);
+        step(later, tile + 1, 1);
     }
     if (j.begin < end) {                                               // the output of the last tile
         const char* const last = lds + ((((end - j.begin) + 1) & ~1u) - 1 & 3u) * SLOT;
 #pragma unroll
         for (int i = 0; i < NV; ++i) row.o[i % NB] = Mm::mma(read_v(last, i), pf[1][i / NB], row.o[i % NB]);
     }
+    const TreeAttnArgs& last_args = tree_args();
     row.l += __shfl_xor(row.l, 32);
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -633,7 +717,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
             f32x4 o;
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = row.o[b][4 * g + e];
-            store_row4<T, D>(a, j, at, 32 * b + 8 * g + 4 * h2, o, row.m, row.l, odd != 0, TREE_MANY_KEYS);
+            store_row4<T, D>(last_args, j, at, 32 * b + 8 * g + 4 * h2, o, row.m, row.l, odd != 0, TREE_MANY_KEYS);
         }
 }
 
@@ -649,13 +733,13 @@ __global__ __launch_bounds__(256) void tree_attn_join(const TreeAttnArgs a) {
     if (pair >= a.batch * a.kv_heads) return;
     const uint32_t b = pair / a.kv_heads, h = pair % a.kv_heads;
     const uint32_t t = r / a.group, hq = h * a.group + r % a.group;
-    const uint32_t cached = a.capacity ? clamp_count(a.cached[b], a.capacity) : 0u;
-    const uint32_t drafted = a.drafted ? clamp_count(a.drafted[b], a.tokens) : a.tokens;
-    if (t >= drafted) return;
-    const uint32_t n = tree_live_parts(a, cached, drafted, a.few ? TREE_FEW_KEYS : TREE_MANY_KEYS);
-    const float* const ml = a.parts + (size_t)a.batch * a.kv_heads * a.n_parts * a.rows * D;
+    if (t >= (a.drafted ? clamp_count(a.drafted[b], a.tokens) : a.tokens)) return;
+    const TreeCut c = tree_cut<false>(a, b, a.few ? TREE_FEW_KEYS : TREE_MANY_KEYS);
+    const uint32_t first = uni(c.first), n = uni(c.n);
+    if (n < 2) return;                                                // (the part was the whole, and its row is out)
+    const float* const ml = tree_sums(a, D);
     float M = -INFINITY;
-    for (uint32_t z = lane; z < n; z += 64) M = fmaxf(M, ml[tree_part_row(a, pair, z, r) * 2]);
+    for (uint32_t z = lane; z < n; z += 64) M = fmaxf(M, ml[tree_part_row(a, first + z, h, r) * 2]);
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) M = fmaxf(M, __shfl_xor(M, d));
     float L = 0.0f;
@@ -663,7 +747,7 @@ __global__ __launch_bounds__(256) void tree_attn_join(const TreeAttnArgs a) {
     const uint32_t grp = lane / VEC, d = (lane % VEC) * 4;
 #pragma unroll 4
     for (uint32_t z = grp; z < n; z += GROUPS) {
-        const size_t at = tree_part_row(a, pair, z, r);
+        const size_t at = tree_part_row(a, first + z, h, r);
         const float mz = ml[at * 2], lz = ml[at * 2 + 1];
         const f32x4 v = *(const f32x4*)(a.parts + at * D + d);
         const float f = mz == -INFINITY ? (lz == 0.0f ? 0.0f : lz) : __builtin_amdgcn_exp2f(mz - M);   // (a sum without a maximum is 0, or NaN)
@@ -687,11 +771,11 @@ __global__ __launch_bounds__(256) void tree_attn_join(const TreeAttnArgs a) {
 
 template <typename T, int D>
 hipError_t launch_tree_attn_of(const TreeAttnArgs& a, hipStream_t stream) {
-    const uint32_t units = (a.batch * a.kv_heads * a.n_parts + 7) / 8 * 8;
+    const uint32_t units = (a.slots * a.kv_heads + 7) / 8 * 8;
     hipError_t e;
     if (a.few) e = launch_one(tree_attn_few<T, D>, units * ((a.rows + TREE_FEW_ROWS - 1) / TREE_FEW_ROWS), 256, stream, a);
     else e = launch_one(tree_attn_many<T, D>, units * ((a.rows + TREE_MANY_ROWS - 1) / TREE_MANY_ROWS), 256, stream, a);
-    if (e != hipSuccess || a.n_parts == 1) return e;
+    if (e != hipSuccess || a.slots == a.batch) return e;
     return launch_one(tree_attn_join<T, D>, (uint32_t)(((uint64_t)a.batch * a.kv_heads * a.rows + 3) / 4), 256, stream, a);
 }
 
