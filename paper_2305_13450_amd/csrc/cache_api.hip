@@ -70,7 +70,7 @@ double tree_cost(int64_t base, int64_t part, int64_t blocks, int64_t pairs, int6
     const double at_once = (double)std::min(groups, slots), wide = head_dim / 128.0;
     const double step = few ? 0.13 + 1.32 * wide : (at_once > n_cu ? 1.0 : at_once > n_cu / 2 ? 0.8 : 0.55) * (0.3 + 0.7 * wide);
     const double hbm = at_once / row_blocks * (few ? TREE_FEW_KEYS : TREE_MANY_KEYS) * 4.0 * head_dim / 5.2e6;
-    const double join = parts > 1 ? 2.8 + (double)parts * pairs * rows * (head_dim + 2) * 8.0 / 4e6 : 0.0;
+    const double join = parts > 1 ? 5.9 + (double)parts * pairs * rows * (head_dim + 2) * 8.0 / 4e6 : 0.0;
     return (double)cdiv64(groups, slots) * (3.0 + part * std::cbrt(step * step * step + hbm * hbm * hbm)) + join;   // (between the larger and the sum)
 }
 
