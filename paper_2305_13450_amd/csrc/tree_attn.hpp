@@ -194,10 +194,11 @@ __device__ __forceinline__ TreeCut tree_cut(const TreeAttnArgs& a, uint32_t x, u
     const uint32_t blocks = (cached + keys - 1) / keys + (drafted + keys - 1) / keys;
     if (wide) return {b, cached, drafted, b * a.part_slots, min(a.part_slots, (blocks + a.part_blocks - 1) / a.part_blocks), a.part_blocks};
     const uint32_t all = last_lane(wave_sums_to(blocks));
-    // A sequence's last part is half empty in the mean, and nearly so at worst: then parts that fit in any case (slots is at least twice batch).  q is the
-    // quotient or, by rounding, one less, so one block more makes up for it.
-    uint32_t n, to, by = a.slots - a.batch / 2;
-    for (uint32_t more = 0;; more = 1, by = a.slots - a.batch) {
+    // Even sequences fill the slots; of uneven ones the last parts are partly empty, up to nearly one part each, and with so many slots less parts fit in
+    // any case (there are at least twice as many as sequences).  q is the quotient or, by rounding, one less, which one block more then makes up for.
+    uint32_t n, to;
+    for (uint32_t quarter = 0;; ++quarter) {
+        const uint32_t by = a.slots - (a.batch * quarter >> 2), more = quarter >> 2;
         const uint32_t q = (uint32_t)((float)all * (__builtin_amdgcn_rcpf((float)by) * (1.0f - 0x1p-20f)));
         c.size = uni(max(a.part_least, q + (q * by < all ? 1u + more : 0u) + (q >> 18)));
         // never more parts than there are blocks for: one too few, which a million blocks can come to, makes the last part longer

@@ -271,3 +271,20 @@ def test_refusals_of_the_binding():
         ds.dep_tree_attn(*(x[..., :32].contiguous() for x in (q, kn, vn, kc, vc)), cached, out[..., :32].contiguous())
     assert e.value.status == ds.ENOTIMPL
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("B,T,Hq,Hk,D,lens", [
+    (20, 1, 4, 2, 128, [15000] + [0] * 18 + [7]),                     # one long sequence among empty ones
+    (20, 40, 4, 1, 64, [300 * i for i in range(20)]),
+    (64, 3, 2, 1, 128, [0] * 63 + [9000]),
+    (70, 1, 2, 1, 128, [4000 - 57 * i for i in range(70)]),           # more sequences than lanes
+    (66, 33, 4, 1, 64, [0] * 65 + [3000]),
+])
+def test_uneven_batches(B, T, Hq, Hk, D, lens):
+    print("uneven", B, T, D, flush=True)
+    t = make(B, T, Hq, Hk, D, max(lens), BF, 21)
+    cached, drafted = ints(lens), ints([T - i % 2 * (T // 2) if i % 7 else 0 for i in range(B)])
+    assert ds.tree_attn_workspace(*t, cached, t[0]) > 0
+    out, lse = run(*t, cached, drafted=drafted)
+    want = ref.attn(*t, cached, None, drafted=drafted)
+    check(out, lse, want, drafted)
