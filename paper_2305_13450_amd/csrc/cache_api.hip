@@ -203,7 +203,10 @@ int dep_cache_weights(const depsync_cache_weights_desc* d, void* stream) {
     int n_cu = 0;
     if (int rc = cu_count(n_cu); rc != DEPSYNC_OK) return rc;
     if (a.few) {
-        a.part_blocks = (uint32_t)std::max<int64_t>(1, cdiv64(cdiv64(keys, 128) * pairs, 3 * (int64_t)n_cu));   // three workgroups share a CU
+        // Three workgroups share a CU.  Where each would have 8 blocks or more, twice as many even out sequences of different lengths (8 of 500 to
+        // 20000 rows: 36 and 29 us, 2 of 20000 and 39000: 35 and 33); with fewer they cost more than that (4 of 4000 to 8000, 3 blocks: 12.7 and 13.7).
+        const int64_t blocks = cdiv64(keys, 128) * pairs, share = cdiv64(blocks, 3 * (int64_t)n_cu);
+        a.part_blocks = (uint32_t)std::max<int64_t>(1, share < 8 ? share : cdiv64(blocks, 6 * (int64_t)n_cu));
         a.n_parts = (uint32_t)cdiv64(cdiv64(keys, 128), a.part_blocks);
     } else {
         // 64 keys to a workgroup read the queries half as often as 32, but the first keys' have all rows to walk and the last ones' few: where they are
