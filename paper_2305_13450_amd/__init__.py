@@ -852,6 +852,16 @@ def _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget
                          _arr(cached, "cached", i32, device, (B,)), _arr(cached_out, "cached_out", i32, device, (B,)), cap_out, *outs, *rows_out), device
 
 
+@functools.lru_cache(maxsize=4096)
+def _evict_bytes(sizes: bytes, other: bool) -> int:
+    """The workspace of dep_cache_evict, by the descriptor's eight sizes and whether other buffers are given: all that it depends on."""
+    d = CacheEvictDesc.from_buffer_copy(sizes + bytes(_P_EVICT.size - len(sizes)))
+    d.k_out = 16 if other else None
+    need = ctypes.c_size_t(0)
+    _check(_lib().depsync_cache_evict_workspace(ctypes.byref(d), ctypes.byref(need)), "dep_cache_evict")
+    return need.value
+
+
 def dep_cache_evict(k_cache, v_cache, weights, pos, cached, cached_out, budget: int, recent: int = 0, max_cached: Optional[int] = None,
                     k_out=None, v_out=None, weights_out=None, pos_out=None, workspace=None, stream=None) -> None:
     """Enqueue: every sequence and head keeps `budget` rows: the `recent` newest by position, then the heaviest, among equals the lowest row.
@@ -859,7 +869,7 @@ def dep_cache_evict(k_cache, v_cache, weights, pos, cached, cached_out, budget: 
     cached_out = min(cached, budget)."""
     d, device = _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out)
     stream = _stream_handle(stream)
-    need = 0 if workspace is not None else _bytes("dep_cache_evict", device, _lib().depsync_cache_evict_workspace, d)
+    need = 0 if workspace is not None else _evict_bytes(d[:32], k_out is not None)
     keep, ptr, size = _workspace(need, workspace, device, stream)
     _call(device, "dep_cache_evict", _lib().dep_cache_evict, d, ptr, size, stream)
 
