@@ -492,7 +492,8 @@ int depsync_copy_chain_plan(const depsync_copy_chain_desc* d, const sync_policy_
  * These are plain launches on one stream, in order; they use no policy object.  Conventions beside those at the top:
  *  - head_dim 64 or 128 (other values: DEPSYNC_ENOTIMPL).  Tensors are [batch][token][head][head_dim] with a stride in
  *    elements for each of the first three (multiples of 8, not negative; strides of dimensions of size 1 are not read); the innermost is contiguous,
- *    bases are 16-byte aligned.  Query head h reads key and value head h / (heads / kv_heads).  A cache's token stride is at most 2^24.
+ *    bases are 16-byte aligned.  Query head h reads key and value head h / (heads / kv_heads).  The token strides of caches, of
+ *    dep_tree_attn's k_new and v_new and of dep_cache_weights' q lie between head_dim and 2^24.
  *  - `cached` holds the valid rows of each sequence, in device memory; values outside 0..capacity are taken as the nearer end.
  *    Rows at and behind it are never read.  Rows that a call does not name are left as they were.
  *  - All memory is the current device's.  A workspace belongs to one call at a time: calls that may run at once, graphs that may be
@@ -503,13 +504,15 @@ int depsync_copy_chain_plan(const depsync_copy_chain_desc* d, const sync_policy_
 
 /* out = softmax(scale q k^T) v over, for drafted token t of a sequence, all cached rows and those drafted tokens j whose bit is set
  * in row t of `tree`: bit j % 64 of word j / 64.  Masked keys count for nothing, whatever bits (infinities, NaN) they and their values
- * hold.  A token that sees no key gets out = 0 and lse = -infinity.                                                                */
+ * hold.  A token that sees no key gets out = 0 and lse = -infinity.  The same call gives the same bits; how sums are divided depends on
+ * the lengths of all sequences of a call, so those of one differ in their rounding with its neighbours'.                          */
 typedef struct {
     int32_t batch, tokens, heads, kv_heads, head_dim;   /* tokens: drafted ones per sequence, at least 1, at most 65536           */
     int32_t dtype;                                      /* depsync_dtype                                                          */
     int32_t capacity;                                   /* rows of each sequence's cache; 0: no cache (its pointers are not read)  */
-    int32_t max_cached;                                 /* what the work is divided by: the most rows that a sequence has now,
-                                                           as far as the host knows; 0 = capacity.  A wrong value costs time only  */
+    int32_t max_cached;                                 /* what the workspace and the number of workgroups go by: the most rows that a
+                                                           sequence has now, as far as the host knows; 0 = capacity.  A wrong value
+                                                           costs time only                                                        */
     const void* q;     int64_t q_batch, q_token, q_head;
     const void* k_new; const void* v_new; int64_t new_batch, new_token, new_head;     /* both alike                                */
     const void* k_cache; const void* v_cache; int64_t cache_batch, cache_token, cache_head;

@@ -64,7 +64,9 @@ int tree_check(const depsync_tree_attn_desc* d) {
 // 4 (head_dim + 2) bytes a row in memory, which a second kernel reads.  The model, in microseconds, fitted to times of 27 shapes under
 // up to 28 cuts each (1 to 2048 rows, caches of 0 to 120000; its choice is 4 % behind the best cut in the mean, in the worst case 21 %):
 // a workgroup's start, a block of keys where its workgroup is alone on the CU and where two share it, the keys' way from HBM, the
-// second kernel and the results' way there and back.
+// second kernel and the results' way there and back.  5.9 is what a second launch costs a program that waits for the host (one token of 12 heads over 500
+// rows 11.5 us in one launch, 15.1 in two); captured into a graph it is about 4 (11.7 and 11.5).  The lengths are the longest sequence's; the
+// kernels then share out the parts by the real ones.
 double tree_cost(int64_t base, int64_t part, int64_t blocks, int64_t pairs, int64_t rows, int64_t row_blocks, int head_dim, int n_cu, bool few) {
     const int64_t parts = cdiv64(blocks, part), groups = base * parts, slots = 2 * (int64_t)n_cu;
     const double at_once = (double)std::min(groups, slots), wide = head_dim / 128.0;
@@ -199,7 +201,7 @@ int dep_cache_weights(const depsync_cache_weights_desc* d, void* stream) {
     a.batch = d->batch; a.tokens = d->tokens; a.heads = d->heads; a.kv_heads = d->kv_heads; a.group = d->heads / d->kv_heads; a.capacity = d->capacity; a.n_max = d->n_max;
     const int64_t keys = rows_hint(d->max_cached, d->capacity), pairs = (int64_t)d->batch * d->kv_heads;
     if ((int64_t)d->n_max * a.group > 1 << 24 || pairs * cdiv64(keys, 32) > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;
-    a.few = (int64_t)d->n_max * a.group <= 64;
+    a.few = (int64_t)d->n_max * a.group <= 64;       // (what LDS keeps beside the keys on their way)
     int n_cu = 0;
     if (int rc = cu_count(n_cu); rc != DEPSYNC_OK) return rc;
     if (a.few) {
@@ -210,7 +212,7 @@ int dep_cache_weights(const depsync_cache_weights_desc* d, void* stream) {
         a.n_parts = (uint32_t)cdiv64(cdiv64(keys, 128), a.part_blocks);
     } else {
         // 64 keys to a workgroup read the queries half as often as 32, but the first keys' have all rows to walk and the last ones' few: where they are
-        // not many, twice as many even that out
+        // not many, twice as many even that out (2048 tokens of 12 heads: 29 us with 64 and 21 with 32)
         a.keys = pairs * cdiv64(keys, 64) < 4 * (int64_t)n_cu ? 32 : 64;
         a.n_parts = (uint32_t)cdiv64(keys, a.keys);
     }

