@@ -134,3 +134,8 @@ def test_tree_words():
             ds.tree_mask(bad)
     with pytest.raises(ValueError):
         ds.tree_mask(torch.zeros((0,), dtype=torch.int64))
+
+
+def test_token_strides_of_the_queries_of_weights():
+    for kw in (dict(q_token=64), dict(q_token=0), dict(q_token=(1 << 24) + 8)):
+        assert call("dep_cache_weights", weights(**kw)) == ds.EINVAL, kw

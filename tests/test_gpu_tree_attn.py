@@ -288,3 +288,25 @@ def test_uneven_batches(B, T, Hq, Hk, D, lens):
     out, lse = run(*t, cached, drafted=drafted)
     want = ref.attn(*t, cached, None, drafted=drafted)
     check(out, lse, want, drafted)
+
+
+def test_lengths_that_change_between_replays():
+    print("replays of other lengths", flush=True)
+    B, T = 5, 20
+    t = make(B, T, 8, 2, 128, 6000, BF, 22)
+    cached, out, lse = ints([100] * B), torch.empty_like(t[0]), torch.empty(t[0].shape[:3], device="cuda")
+    s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s):
+        ds.dep_tree_attn(*t, cached, out, lse=lse, stream=s)
+        s.synchronize()
+        with torch.cuda.graph(g, stream=s):
+            ds.dep_tree_attn(*t, cached, out, lse=lse, stream=s)
+    for lens in ([6000, 0, 0, 31, 5], [0] * 5, [1200, 2400, 3600, 4800, 6000], [6000] * 5, [100] * 5):
+        cached.copy_(ints(lens))
+        out.zero_(), lse.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        eager = run(*t, cached)
+        assert torch.equal(out, eager[0]) and torch.equal(lse, eager[1])
+        check(out, lse, ref.attn(*t, cached))
