@@ -215,6 +215,7 @@ int dep_cache_weights(const depsync_cache_weights_desc* d, void* stream) {
         // not many, twice as many even that out (2048 tokens of 12 heads: 29 us with 64 and 21 with 32)
         a.keys = pairs * cdiv64(keys, 64) < 4 * (int64_t)n_cu ? 32 : 64;
         a.n_parts = (uint32_t)cdiv64(keys, a.keys);
+        a.waves = a.keys == 32 && (pairs * a.n_parts <= 4 * (int64_t)n_cu || cdiv64(d->n_max, 32) * a.group >= 32) ? 8 : 4;
     }
     const hipError_t e = launch_cache_weights(a, d->dtype, D, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);

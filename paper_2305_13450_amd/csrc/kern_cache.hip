@@ -150,15 +150,15 @@ __global__ __launch_bounds__(256, 3) void cache_weights_few_kernel(const CacheWe
 // exponentials in 20 us; the first keys' workgroups walk 2048 rows, and every walk ends in a sum over four waves).  A workgroup keeps 32 KT keys' fragments in
 // registers, in every wave, and its four waves walk the rows, 32 tokens of one query head at a time each, the next ones on their way into
 // registers meanwhile.  (Rows by head and not by token: their addresses are a line then, and the last key they see as well.)
-template <typename T, int D, int KT>
-__global__ __launch_bounds__(256, 2) void cache_weights_many_kernel(const CacheWeightsArgs a) {
+template <typename T, int D, int KT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, WAVES / 2) void cache_weights_many_kernel(const CacheWeightsArgs a) {
     using Tile = KeyTile<T, D>;
     using M = Mma<T>;
     using V8 = typename M::V8;
-    constexpr uint32_t KEYS = 32 * KT, NK = Tile::NI * KT / 4;       // a wave's 1 KB copies of keys
-    __shared__ __align__(16) char lds[4][Tile::BYTES];             // the keys, then each wave's rows
-    __shared__ __align__(16) float lse[4][32];
-    __shared__ float joined[4][KEYS];
+    constexpr uint32_t KEYS = 32 * KT, COPIES = Tile::NI * KT, NK = (COPIES + WAVES - 1) / WAVES;   // 1 KB copies of keys, a wave's
+    __shared__ __align__(16) char lds[WAVES][Tile::BYTES];         // the keys, then each wave's rows
+    __shared__ __align__(16) float lse[WAVES][32];
+    __shared__ float joined[WAVES][KEYS];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6), h2 = lane >> 5;
     const uint32_t h = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, part = rest % a.n_parts, b = rest / a.n_parts;
     const uint32_t cached = uni(clamp_count(a.cached[b], a.capacity));
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_many_kernel(const CacheW
 #pragma unroll
             for (uint32_t i = 0; i < NK; ++i) {
                 const uint32_t rr = (wave * NK + i) * Tile::RPI + lrow;
-                *(u32x4*)(lds[0] + rr * Tile::PITCH + ((chunk ^ Tile::kswz(rr & 31u)) << 4)) = reg[i];
+                if (COPIES % WAVES == 0 || wave * NK + i < COPIES) *(u32x4*)(lds[0] + rr * Tile::PITCH + ((chunk ^ Tile::kswz(rr & 31u)) << 4)) = reg[i];
             }
             __syncthreads();
 #pragma unroll
@@ -194,8 +194,8 @@ __global__ __launch_bounds__(256, 2) void cache_weights_many_kernel(const CacheW
         const uint32_t i_first = (int32_t)k0 > base ? (uint32_t)((int32_t)k0 - base) & ~31u : 0u;   // rows before see none of these keys
         const uint32_t i_end = i_first < n ? i_first + ((n - i_first + 31) & ~31u) : i_first;
         struct Place { uint32_t g, i; };                           // a step's query head and first token
-        auto onward = [&](Place& x) __attribute__((always_inline)) {   // the wave's next step: four on
-            x.i += 128;
+        auto onward = [&](Place& x) __attribute__((always_inline)) {   // the wave's next step
+            x.i += 32 * WAVES;
             while (x.i >= i_end && x.g < a.group) { x.i -= i_end - i_first; ++x.g; }
         };
         u32x4 qreg[Tile::NI];
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_many_kernel(const CacheW
             if (lane < 32) lse[wave][lane] = sum;
             const int32_t see = base + (int32_t)now.i;             // the last key that the first of these rows sees
             onward(now);
-            if (now.g < a.group) fetch(now);
+            if (WAVES == 4 && now.g < a.group) fetch(now);
             asm volatile("" ::: "memory");                         // (a wave's LDS accesses keep their order)
             __builtin_amdgcn_wave_barrier();
             V8 q[D / 16];
@@ -241,6 +241,10 @@ __global__ __launch_bounds__(256, 2) void cache_weights_many_kernel(const CacheW
                 for (int v = 0; v < 16; ++v) st[t][v] = 0.0f;
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk) st[t] = M::mma(q[kk], kf[t][kk], st[t]);
+            }
+            if (WAVES == 8) {                                      // (into the registers that the fragments have left: 128 are there)
+                __builtin_amdgcn_sched_barrier(0);
+                if (now.g < a.group) fetch(now);
             }
 #pragma unroll
             for (int t = 0; t < KT; ++t)
@@ -255,8 +259,11 @@ __global__ __launch_bounds__(256, 2) void cache_weights_many_kernel(const CacheW
             if (lane < 32) joined[wave][32 * t + lane] = w[t];
         }
         __syncthreads();
-        if (tid < KEYS && k0 + tid < cached)
-            a.weights[((size_t)b * a.kv_heads + h) * a.capacity + k0 + tid] += (joined[0][tid] + joined[1][tid]) + (joined[2][tid] + joined[3][tid]);
+        if (tid < KEYS && k0 + tid < cached) {
+            float x = (joined[0][tid] + joined[1][tid]) + (joined[2][tid] + joined[3][tid]);
+            if (WAVES == 8) x += (joined[4][tid] + joined[5][tid]) + (joined[6][tid] + joined[7][tid]);
+            a.weights[((size_t)b * a.kv_heads + h) * a.capacity + k0 + tid] += x;
+        }
     }
 }
 
@@ -525,7 +532,8 @@ template <typename T, int D>
 hipError_t launch_weights_of(const CacheWeightsArgs& a, hipStream_t stream) {
     const uint32_t blocks = a.batch * a.kv_heads * a.n_parts;
     if (a.few) return launch_one(cache_weights_few_kernel<T, D>, blocks, 256, stream, a);
-    return a.keys == 32 ? launch_one(cache_weights_many_kernel<T, D, 1>, blocks, 256, stream, a) : launch_one(cache_weights_many_kernel<T, D, 2>, blocks, 256, stream, a);
+    if (a.keys == 64) return launch_one(cache_weights_many_kernel<T, D, 2, 4>, blocks, 256, stream, a);
+    return a.waves == 8 ? launch_one(cache_weights_many_kernel<T, D, 1, 8>, blocks, 512, stream, a) : launch_one(cache_weights_many_kernel<T, D, 1, 4>, blocks, 256, stream, a);
 }
 
 }  // namespace
