@@ -211,11 +211,11 @@ int dep_cache_weights(const depsync_cache_weights_desc* d, void* stream) {
         a.part_blocks = (uint32_t)std::max<int64_t>(1, share < 8 ? share : cdiv64(blocks, 6 * (int64_t)n_cu));
         a.n_parts = (uint32_t)cdiv64(cdiv64(keys, 128), a.part_blocks);
     } else {
-        // 64 keys to a workgroup read the queries half as often as 32, but the first keys' have all rows to walk and the last ones' few: where they are
-        // not many, twice as many even that out (2048 tokens of 12 heads: 29 us with 64 and 21 with 32)
-        a.keys = pairs * cdiv64(keys, 64) < 4 * (int64_t)n_cu ? 32 : 64;
+        // 64 keys to a workgroup read the queries half as often as 32 (4 x 1500 tokens of 32 heads: 71 us, 92 with 32), but the first keys' have all rows to
+        // walk and the last ones' few: where workgroups are not many, twice as many of twice the waves even that out (2048 tokens of 12 heads: 29 us with 64
+        // and 21 with 32; of 32 heads on 4: 77 with 32, 112 with as many waves as for 64).  3 x 1500 tokens of 12 heads, 864 workgroups of 64: 20 us, 24 with 32.
+        a.keys = pairs * cdiv64(keys, 64) < 2 * (int64_t)n_cu ? 32 : 64;
         a.n_parts = (uint32_t)cdiv64(keys, a.keys);
-        a.waves = a.keys == 32 && (pairs * a.n_parts <= 4 * (int64_t)n_cu || cdiv64(d->n_max, 32) * a.group >= 32) ? 8 : 4;
     }
     const hipError_t e = launch_cache_weights(a, d->dtype, D, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);

@@ -48,7 +48,7 @@ struct CacheWeightsArgs {
     uint32_t batch, tokens, heads, kv_heads, group, capacity, n_max;
     uint32_t few;                         // 1: the form for few rows
     uint32_t n_parts, part_blocks;        // workgroups along the keys, and (few rows) blocks of 128 keys in each
-    uint32_t keys, waves;                 // (many rows) keys of a workgroup: 32 or 64; its waves: 4 or, with 32 keys, 8
+    uint32_t keys;                        // (many rows) keys of a workgroup: 32, in eight waves, or 64, in four
     float scale;                          // scores to base-2 exponents
 };
 

@@ -147,8 +147,8 @@ __global__ __launch_bounds__(256, 3) void cache_weights_few_kernel(const CacheWe
 }
 
 // More rows, those of a prompt: the time is that of the matrix cores and the exponentials (2048 tokens of 12 heads: 6.4 GFLOP and 25 million
-// exponentials in 20 us; the first keys' workgroups walk 2048 rows, and every walk ends in a sum over four waves).  A workgroup keeps 32 KT keys' fragments in
-// registers, in every wave, and its four waves walk the rows, 32 tokens of one query head at a time each, the next ones on their way into
+// exponentials in 20 us; the first keys' workgroups walk 2048 rows, and every walk ends in a sum over eight waves).  A workgroup keeps 32 KT keys' fragments in
+// registers, in every wave, and its waves walk the rows, 32 tokens of one query head at a time each, the next ones on their way into
 // registers meanwhile.  (Rows by head and not by token: their addresses are a line then, and the last key they see as well.)
 template <typename T, int D, int KT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, WAVES / 2) void cache_weights_many_kernel(const CacheWeightsArgs a) {
@@ -533,7 +533,7 @@ hipError_t launch_weights_of(const CacheWeightsArgs& a, hipStream_t stream) {
     const uint32_t blocks = a.batch * a.kv_heads * a.n_parts;
     if (a.few) return launch_one(cache_weights_few_kernel<T, D>, blocks, 256, stream, a);
     if (a.keys == 64) return launch_one(cache_weights_many_kernel<T, D, 2, 4>, blocks, 256, stream, a);
-    return a.waves == 8 ? launch_one(cache_weights_many_kernel<T, D, 1, 8>, blocks, 512, stream, a) : launch_one(cache_weights_many_kernel<T, D, 1, 4>, blocks, 256, stream, a);
+    return launch_one(cache_weights_many_kernel<T, D, 1, 8>, blocks, 512, stream, a);
 }
 
 }  // namespace

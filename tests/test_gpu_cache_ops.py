@@ -319,3 +319,22 @@ def test_refusals_of_the_binding():
         with pytest.raises((ValueError, TypeError)):
             f(*a)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_weights_of_many_sequences(D):
+    print("weights of many sequences", D, flush=True)
+    B, T, A, Hq, Hk = 33, 80, 70, 16, 8
+    lens, counts = [(37 * i) % 141 for i in range(B)], [A - i % 3 * 30 for i in range(B)]
+    g = gen(31)
+    kc, _, w, _ = cache(B, Hk, D, 145, BF, 32)
+    kc[:, max(lens):] = float("nan")
+    q, lse = normal(g, (B, T, Hq, D), BF, 2.0), 4.0 + torch.rand((B, T, Hq), generator=g, device="cuda")
+    accepted, cached, n = torch.randint(0, T, (B, A), generator=g, device="cuda").int(), ints(lens), ints(counts)
+    want, tol = ref.add_weights(q, lse, kc, cached, w, accepted, n)
+    w0 = w.clone()
+    ds.dep_cache_weights(q, lse, kc, cached, w, accepted=accepted, n_accepted=n)
+    torch.cuda.synchronize()
+    near(w, want, tol)
+    for b in range(B):
+        assert torch.equal(w[b, :, lens[b]:], w0[b, :, lens[b]:])
