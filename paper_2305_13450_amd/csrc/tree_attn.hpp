@@ -20,7 +20,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // The reference value that weights are relative to follows the running maximum only where that has grown by more than SLACK (base 2): with 32 rows
 // to a wave every third step of 500 would rescale the outputs for the sake of some row's new maximum, so hardly one in thirty does.
-// Weights are then at most 2^SLACK, which costs 16-bit weights nothing: their error is relative.  But fp16 has 2^-14 to 2^16 only, and the weights of a
+// Weights are then at most 2^SLACK, at which 16-bit ones are no coarser: their error is relative.  But fp16 has 2^-14 to 2^16 only, and the weights of a
 // long cache are mostly far below the largest, so there they carry a factor of 2^OFF, 2^15 at most: below the reference 23 binades keep all bits.
 // Sums and outputs carry the factor alike and it cancels.
 constexpr float WEIGHT_SLACK = 6.0f;
@@ -75,9 +75,38 @@ __device__ __forceinline__ float max_halves(float x) {
     return fmaxf(__builtin_bit_cast(float, lower), __builtin_bit_cast(float, upper));
 }
 
+// Two weights for products with 16-bit operands, each as a sum of two numbers of T: the weight cut off, and what that took away, rounded.  Together they are
+// off by 2 u^2 of the weight, u being T's half step (fp16: and 2^-24, of weights that carry a factor of 2^9), where one rounded number is off by u.
+// Neither is negative, and what was taken away counts for at least 2^-16 of the weight (bf16) or the smallest number (fp16): a zero there would make
+// NaN of an infinite value that its row does see.
+template <typename T> struct WeightPair {
+    typedef T T2 __attribute__((ext_vector_type(2)));
+    typedef uint16_t Bits __attribute__((ext_vector_type(2)));
+    T2 high, rest;
+    __device__ __forceinline__ WeightPair(float a, float b) {
+        Bits least;
+        if constexpr (__is_same(T, __bf16)) {
+            const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
+            high = __builtin_bit_cast(T2, __builtin_amdgcn_perm(y, x, 0x07060302u));
+            rest[0] = (T)(a - __builtin_bit_cast(float, x & 0xffff0000u));
+            rest[1] = (T)(b - __builtin_bit_cast(float, y & 0xffff0000u));
+            least = __builtin_elementwise_sub_sat(__builtin_bit_cast(Bits, high), Bits{16 << 7, 16 << 7});
+        } else {
+            high = __builtin_bit_cast(T2, __builtin_amdgcn_cvt_pkrtz(a, b));
+            rest[0] = (T)(a - (float)high[0]);
+            rest[1] = (T)(b - (float)high[1]);
+            least = __builtin_elementwise_min(__builtin_bit_cast(Bits, high), Bits{1, 1});
+        }
+        rest = __builtin_bit_cast(T2, __builtin_elementwise_max(__builtin_bit_cast(Bits, rest), least));
+    }
+};
+
 // One step: KT tiles of 32 keys in LDS against 32 rows.  vis: the tile's keys that a lane's row sees, one bit each.
 // Fragments are read two slices ahead of the MFMAs and the order is pinned: left alone the compiler reads them all at once, and spills, or each right
 // before the wait for it.  query(kk): the rows' fragment of slice kk.
+// Weights go into the product with V as two numbers each: the time here is that of the keys' way, so keeping their bits costs little (one token over 500 rows
+// 11.8 -> 12.8 us, 4 x 2048 rows 13.4 -> 14.4, 32 sequences of up to 8192 139 -> 142), and outputs are as near to 64 bits as with 32-bit weights (bf16: 1.62e-3 of
+// their norm, 2.07e-3 with rounded weights; nearly all of the former is the output's own rounding).
 template <typename T, int D, int KT, int AHEAD, class Q>
 __device__ __forceinline__ void tree_step(RowState<D>& row, Q query, const char* ldsK, const char* ldsV, uint32_t lane, float sc,
                                           const uint32_t (&vis)[KT], bool masked) {
@@ -131,15 +160,21 @@ __device__ __forceinline__ void tree_step(RowState<D>& row, Q query, const char*
             for (int v = 0; v < 16; ++v) row.o[b][v] *= alpha;
     }
     const float ref = (row.m == -INFINITY ? 0.0f : row.m) - WEIGHT_OFF<T>;   // no key seen yet: keep the exponents finite
-    V8 pf[2 * KT];
+    V8 pf[2 * KT], rest[2 * KT];
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[t][v], sc, -ref));
-            sum[v & 1] += p;                                         // summed in 32 bits, rounded to 16 for the product with V only
-            pf[2 * t + (v >> 3)][v & 7] = (T)p;
+        for (int v = 0; v < 16; v += 2) {
+            float p[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[t][v + e], sc, -ref));
+                sum[e] += p[e];
+            }
+            const WeightPair<T> w(p[0], p[1]);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) { pf[2 * t + (v >> 3)][(v & 7) + e] = w.high[e]; rest[2 * t + (v >> 3)][(v & 7) + e] = w.rest[e]; }
         }
     row.l += sum[0] + sum[1];
     typedef T T4 __attribute__((ext_vector_type(4)));
@@ -158,6 +193,7 @@ __device__ __forceinline__ void tree_step(RowState<D>& row, Q query, const char*
         if (i + AHEAD < NV) rdv(i + AHEAD);
         const V8 x = __builtin_shufflevector(vf[i % (AHEAD + 1)][0], vf[i % (AHEAD + 1)][1], 0, 1, 2, 3, 4, 5, 6, 7);
         row.o[i % NB] = M::mma(x, pf[i / NB], row.o[i % NB]);
+        row.o[i % NB] = M::mma(x, rest[i / NB], row.o[i % NB]);
     }
     __builtin_amdgcn_sched_barrier(0);
 }
@@ -499,6 +535,11 @@ __global__ __launch_bounds__(256, 2) void tree_attn_few(const TreeAttnArgs a) {
 // tiles, which the workgroup copies to four LDS slots: K of s + 1 and V of s - 1 are being read, tile s + 2 goes into the slot that V of s - 2
 // has left, and s + 3 and s + 4 are on their way through registers.
 //
+// Here weights are rounded to 16 bits for the product with V (sums keep 32).  Their errors, half a step each and independent, come to about as much as the
+// output's own rounding: 2.21e-3 of the outputs' norm in bf16 and 2.59e-4 in fp16, where 32-bit weights leave 1.66e-3 and 2.05e-4.  The form
+// for few rows keeps the rest of each weight; here, where MFMAs and conversions are the time, that took 464 -> 618 us (4 x 256 tokens) and 53 -> 79
+// (13 tokens of 32 heads of 64 over 120000 rows), too much for a quarter of an error that is within two roundings of T either way.
+//
 // Rows lie in LDS at pitches that put what is read together into different banks (16 rows of K 16 bytes each, 4 rows of V 64 bytes each) and leave every
 // fragment at a constant distance from a lane's first: with exclusive-ors instead, as above, 24 address instructions a tile went beside the MFMAs.
 template <int D> struct PaddedTile {
@@ -629,7 +670,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
                 x0 = __builtin_amdgcn_exp2f(x0);
             } else {
                 x1 = __builtin_amdgcn_exp2f(x1);
-                sum[0] += x0; sum[1] += x1;                            // summed in 32 bits, rounded to 16 for the product with V only
+                sum[0] += x0; sum[1] += x1;                            // summed in 32 bits, rounded to 16 for the product with V alone (above)
                 px[v >> 3][v & 7] = (T)x0; px[v >> 3][(v & 7) + 1] = (T)x1;
             }
         };

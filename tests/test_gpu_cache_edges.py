@@ -1,0 +1,87 @@
+"""GPU tests of the cache operators where values, lengths, strides or streams are unusual, against the 64-bit forms of tests/cache_ref.py."""
+import math
+
+import pytest
+import torch
+
+import cache_ref as ref
+import paper_2305_13450_amd as ds
+
+pytestmark = pytest.mark.gpu
+BF, FP = torch.bfloat16, torch.float16
+INF = float("inf")
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def normal(g, shape, dtype, std=1.0):
+    return (torch.randn(shape, generator=g, device="cuda") * std).to(dtype)
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def attn(q, kn, vn, kc, vc, cached, **kw):
+    out, lse = torch.full(q.shape, 5.0, dtype=q.dtype, device="cuda"), torch.full(q.shape[:3], 5.0, device="cuda")
+    ds.dep_tree_attn(q, kn, vn, kc, vc, cached, out, lse=lse, **kw)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+# ---- the form for few rows keeps the weights' bits ------------------------------------------------------------------------------
+
+def halves(g, shape, dtype):
+    """-1, -1/2 .. 1: sums of their products are exact in 32 bits."""
+    return (torch.randint(-2, 3, shape, generator=g, device="cuda") / 2).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("B,T,Hq,Hk,D,lens", [(3, 1, 12, 12, 128, [500, 33, 7]), (2, 4, 16, 2, 64, [300, 40]), (2, 13, 12, 4, 128, [64, 400]), (2, 1, 8, 2, 128, [9000, 4000])])
+def test_weights_of_few_rows_keep_their_bits(B, T, Hq, Hk, D, lens, dtype):
+    # Scores x are exact up to the factor to base 2 (four roundings), the exponent's argument rounds once more, 9 being what fp16 weights carry:
+    # a weight is off by e = U32 (8 max |x| + 8) + 2^-21, in the numerator and in the sum.  As two numbers it is off by 2 u^2 of itself (less than 2 u cut off, and
+    # that rounded by half a step u), and fp16 by one of its smallest numbers, 2^-24 of weights 2^9 times as large, a key.
+    print("few rows", B, T, Hq, Hk, D, lens, dtype, flush=True)
+    g = gen(1)
+    q, kn, kc = halves(g, (B, T, Hq, D), dtype), halves(g, (B, T, Hk, D), dtype), halves(g, (B, max(lens), Hk, D), dtype)
+    vn, vc = normal(g, (B, T, Hk, D), dtype), normal(g, (B, max(lens), Hk, D), dtype)
+    out, lse = attn(q, kn, vn, kc, vc, ints(lens))
+    q, kn, vn, kc, vc = (t.cpu().double() for t in (q, kn, vn, kc, vc))
+    u = ref.half_step(dtype)
+    worst = 0.0
+    for b, n in enumerate(lens):
+        for h in range(Hq):
+            k, v = (torch.cat([c[b, :n, h // (Hq // Hk)], new[b, :, h // (Hq // Hk)]]) for c, new in ((kc, kn), (vc, vn)))
+            x = q[b, :, h] @ k.T / math.sqrt(D)
+            seen = torch.cat([torch.ones((T, n)), torch.ones((T, T)).tril()], 1) > 0
+            e = ref.U32 * (8 * float(x.abs().max()) + 8) + 2.0 ** -21
+            p = torch.softmax(x.masked_fill(~seen, -INF), 1)
+            o, A = p @ v, p @ v.abs()
+            tol = 1.01 * (u * o.abs() + A * (2 * u * u + 2 * e + (n + T + 64) * ref.U32)) + (n + T) * 2.0 ** -33 * float(v.abs().max())
+            worst = max(worst, float(((out[b, :, h].cpu().double() - o).abs() / tol).max()))
+    assert worst <= 1.0, f"{worst:.3f} of the tolerance"
+
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("T,Hq,Hk,D,cap", [(1, 4, 2, 128, 200), (3, 8, 1, 64, 77), (20, 4, 1, 128, 300), (1, 2, 2, 64, 1)])
+def test_an_infinite_cached_value_stays_one(T, Hq, Hk, D, cap, dtype):
+    # weights of one, of numbers that T holds exactly and of numbers far below the largest are all positive
+    print("infinite cached value", T, Hq, Hk, D, cap, dtype, flush=True)
+    g = gen(2)
+    q, kn, vn = halves(g, (1, T, Hq, D), dtype), halves(g, (1, T, Hk, D), dtype), normal(g, (1, T, Hk, D), dtype)
+    kc, vc = halves(g, (1, cap, Hk, D), dtype), normal(g, (1, cap, Hk, D), dtype)
+    if cap > 5:
+        q[..., 0] = 4.0
+        kc[:, 4, :, 0] = 20.0                                # the score that outweighs the others, by 2^7 to 2^13
+    at = sorted({0, cap // 2, cap - 1})
+    for i, r in enumerate(at):
+        vc[:, r, :, i] = INF if i % 2 else -INF
+    out, _ = attn(q, kn, vn, kc, vc, ints([cap]))
+    for i in range(len(at)):
+        assert bool((out[..., i] == (INF if i % 2 else -INF)).all())
+    assert bool(out[..., len(at):].isfinite().all())
