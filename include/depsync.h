@@ -548,7 +548,8 @@ int dep_cache_append(const depsync_cache_append_desc* d, void* stream);
 
 /* weights[b][h][k] += sum of exp(scale q.k - lse) over the query heads of head h and the accepted tokens i < n that see row k.  `cached`
  * counts the accepted tokens' own rows, the last n: token i sees rows 0..cached - n + i (its path and all before).  q and lse are
- * dep_tree_attn's.  The sum is taken in 32 bits in an order that depends on sizes alone.                                            */
+ * dep_tree_attn's; where lse is -infinity the token saw nothing, and adds nothing.  A row's weight is touched by the tokens that see it alone, whatever
+ * bits (infinities, NaN) its key holds.  The sum is taken in 32 bits in an order that depends on sizes alone.                                            */
 typedef struct {
     int32_t batch, tokens, heads, kv_heads, head_dim, dtype, capacity;
     int32_t max_cached;                                 /* as for dep_tree_attn                                                    */

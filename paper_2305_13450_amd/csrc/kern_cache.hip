@@ -44,28 +44,36 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const CacheAppendArgs
 __device__ __forceinline__ uint32_t accepted_token(const CacheWeightsArgs& a, uint32_t b, uint32_t i) {
     return a.accepted ? clamp_count(a.accepted[(size_t)b * a.n_max + i], a.tokens - 1) : i;
 }
-// Its row's sum, base 2 (a row that saw nothing gives no weight).
+// In the place of its sum a row that is not there, and one that saw nothing, has this.  It makes the weights of finite scores 0; those of a key that is
+// not finite are NaN (a row that is not there is zeros, and 0 x inf no number) and have to be set to 0.
+constexpr float NO_ROW = 0x1.fffffep127f;
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+// A row's sum, base 2.
 __device__ __forceinline__ float row_sum(const CacheWeightsArgs& a, uint32_t b, uint32_t token, uint32_t hq) {
     const float x = a.lse[((size_t)b * a.tokens + token) * a.heads + hq];
-    return x == -INFINITY ? INFINITY : x * 1.4426950408889634f;
+    return x == -INFINITY ? NO_ROW : x * 1.4426950408889634f;
 }
-// Sum over 16 rows of a lane's weights for its key: scores st, sums in LDS.  LAST(row) is the last key that a row sees, asked where `cut`.
-template <class L>
-__device__ __forceinline__ float rows_weight(const f32x16& st, const float* lse, uint32_t h2, float sc, bool cut, int32_t key, L last) {
-    float part[4];
+// Sum over 16 rows of a lane's weights for its key: scores st, sums in LDS, and the last key that each row sees (-1 where its sum is NO_ROW), which
+// is asked for where `masked`: where a row does not see all keys.
+__device__ __forceinline__ float rows_weight(const f32x16& st, const float* lse, const int32_t* last, uint32_t h2, float sc, bool masked, int32_t key) {
+    float p[16], part[4];
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
         const f32x4 l4 = *(const f32x4*)(lse + 8 * g + 4 * h2);
-        float p[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[4 * g + e], sc, -l4[e]));
-        if (cut) {
+        for (int e = 0; e < 4; ++e) p[4 * g + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[4 * g + e], sc, -l4[e]));
+    }
+    if (masked) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const i32x4 last4 = *(const i32x4*)(last + 8 * g + 4 * h2);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (key > last(8 * g + 4 * h2 + e)) p[e] = 0.0f;
+                if (key > last4[e]) p[4 * g + e] = 0.0f;
         }
-        part[g] = (p[0] + p[1]) + (p[2] + p[3]);
     }
+#pragma unroll
+    for (int g = 0; g < 4; ++g) part[g] = (p[4 * g] + p[4 * g + 1]) + (p[4 * g + 2] + p[4 * g + 3]);
     return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
@@ -112,10 +120,12 @@ __global__ __launch_bounds__(256, 3) void cache_weights_few_kernel(const CacheWe
     }
     if (tid < 64) {
         const uint32_t i = tid / a.group, g = tid - i * a.group;
-        lse[tid] = tid < rows ? row_sum(a, b, accepted_token(a, b, i), h * a.group + g) : INFINITY;   // (no such row: no weight)
-        last[tid] = base + (int32_t)i;
+        const float sum = tid < rows ? row_sum(a, b, accepted_token(a, b, i), h * a.group + g) : NO_ROW;
+        lse[tid] = sum;
+        last[tid] = sum == NO_ROW ? -1 : base + (int32_t)i;
     }
     __syncthreads();
+    const uint64_t none = __ballot(lse[lane] == NO_ROW);
     char* const mine = ldsK[wave];
     const uint32_t koff = Tile::koff(lane), kput = lrow * Tile::PITCH + ((chunk ^ Tile::kswz(lrow)) << 4);
     for (uint32_t blk = begin; blk < end; ++blk) {
@@ -137,7 +147,7 @@ __global__ __launch_bounds__(256, 3) void cache_weights_few_kernel(const CacheWe
             for (int v = 0; v < 16; ++v) st[v] = 0.0f;
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) st = M::mma(*(const V8*)(ldsQ + u * Tile::BYTES + (koff ^ (kk * 32u))), kf[kk], st);
-            w += rows_weight(st, lse + 32 * u, h2, a.scale, first + 31 > base, key, [&](uint32_t r) __attribute__((always_inline)) { return last[32 * u + r]; });
+            w += rows_weight(st, lse + 32 * u, last + 32 * u, h2, a.scale, (uint32_t)(none >> (32 * u)) != 0 || first + 31 > base, key);
         }
         w += __shfl_xor(w, 32);
         if (lane < 32 && key < (int32_t)cached) weights[key] = before + w;
@@ -147,7 +157,7 @@ __global__ __launch_bounds__(256, 3) void cache_weights_few_kernel(const CacheWe
 }
 
 // More rows, those of a prompt: the time is that of the matrix cores and the exponentials (2048 tokens of 12 heads: 6.4 GFLOP and 25 million
-// exponentials in 20 us; the first keys' workgroups walk 2048 rows, and every walk ends in a sum over eight waves).  A workgroup keeps 32 KT keys' fragments in
+// exponentials in 18.6 us; the first keys' workgroups walk 2048 rows, and every walk ends in a sum over eight waves).  A workgroup keeps 32 KT keys' fragments in
 // registers, in every wave, and its waves walk the rows, 32 tokens of one query head at a time each, the next ones on their way into
 // registers meanwhile.  (Rows by head and not by token: their addresses are a line then, and the last key they see as well.)
 template <typename T, int D, int KT, int WAVES>
@@ -158,6 +168,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 2) void cache_weights_many_kern
     constexpr uint32_t KEYS = 32 * KT, COPIES = Tile::NI * KT, NK = (COPIES + WAVES - 1) / WAVES;   // 1 KB copies of keys, a wave's
     __shared__ __align__(16) char lds[WAVES][Tile::BYTES];         // the keys, then each wave's rows
     __shared__ __align__(16) float lse[WAVES][32];
+    __shared__ __align__(16) int32_t last[WAVES][32];              // the last key that the row sees
     __shared__ float joined[WAVES][KEYS];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6), h2 = lane >> 5;
     const uint32_t h = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads, part = rest % a.n_parts, b = rest / a.n_parts;
@@ -199,7 +210,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 2) void cache_weights_many_kern
             while (x.i >= i_end && x.g < a.group) { x.i -= i_end - i_first; ++x.g; }
         };
         u32x4 qreg[Tile::NI];
-        float sum = INFINITY;
+        float sum = NO_ROW;
         auto fetch = [&](const Place& at) __attribute__((always_inline)) {
             const uint32_t hq = h * a.group + at.g, mine = at.i + (lane & 31u);
             const T* const q = (const T*)a.q + (int64_t)b * a.q_s.batch + (int64_t)hq * a.q_s.head;
@@ -213,7 +224,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 2) void cache_weights_many_kern
                     qreg[i] = *(const u32x4*)(q + (int64_t)accepted_token(a, b, min(at.i + i * Tile::RPI + lrow, n - 1)) * a.q_s.token + chunk * 8);
             }
             const float x = row_sum(a, b, accepted_token(a, b, min(mine, n - 1)), hq);
-            sum = mine < n ? x : INFINITY;                         // (no such row: no weight)
+            sum = mine < n ? x : NO_ROW;
         };
         float w[KT] = {};
         const int32_t key = (int32_t)(k0 + (lane & 31u));
@@ -225,8 +236,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 2) void cache_weights_many_kern
             const uint32_t p = opaque(put);
 #pragma unroll
             for (uint32_t i = 0; i < Tile::NI; ++i) *(u32x4*)(mine + (p ^ ((Tile::kswz(i * Tile::RPI)) << 4)) + i * Tile::RPI * Tile::PITCH) = qreg[i];
-            if (lane < 32) lse[wave][lane] = sum;
             const int32_t see = base + (int32_t)now.i;             // the last key that the first of these rows sees
+            const bool none = __ballot(sum == NO_ROW) != 0;
+            if (lane < 32) { lse[wave][lane] = sum; last[wave][lane] = sum == NO_ROW ? -1 : see + (int32_t)lane; }
             onward(now);
             if (WAVES == 4 && now.g < a.group) fetch(now);
             asm volatile("" ::: "memory");                         // (a wave's LDS accesses keep their order)
@@ -248,8 +260,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 2) void cache_weights_many_kern
             }
 #pragma unroll
             for (int t = 0; t < KT; ++t)
-                w[t] += rows_weight(st[t], lse[wave], h2, a.scale, (int32_t)k0 + 32 * t + 31 > see, key + 32 * t,
-                                    [&](uint32_t r) __attribute__((always_inline)) { return see + (int32_t)r; });
+                w[t] += rows_weight(st[t], lse[wave], last[wave], h2, a.scale, none || (int32_t)k0 + 32 * t + 31 > see, key + 32 * t);
             asm volatile("" ::: "memory");
             __builtin_amdgcn_wave_barrier();
         }

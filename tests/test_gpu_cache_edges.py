@@ -85,3 +85,45 @@ def test_an_infinite_cached_value_stays_one(T, Hq, Hk, D, cap, dtype):
     for i in range(len(at)):
         assert bool((out[..., i] == (INF if i % 2 else -INF)).all())
     assert bool(out[..., len(at):].isfinite().all())
+
+
+# ---- weights of keys that are not finite ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("B,T,A,Hq,Hk,D,lens,counts", [
+    (2, 1, None, 1, 1, 128, [9, 130], None), (2, 16, 5, 8, 2, 64, [31, 200], [5, 1]), (1, 33, None, 1, 1, 128, [140], None), (2, 12, 3, 16, 2, 128, [64, 300], [2, 3]),
+    (1, 70, None, 4, 2, 64, [333], None), (2, 300, None, 3, 1, 128, [300, 500], [300, 33]), (2, 90, 60, 4, 2, 128, [500, 61], [60, 33]), (40, 80, None, 2, 1, 128, [2100] * 40, [65] * 40)])
+def test_weights_of_keys_that_are_not_finite(B, T, A, Hq, Hk, D, lens, counts, dtype):
+    print("weights, not finite", B, T, A, Hq, Hk, D, lens, dtype, flush=True)
+    g = gen(3)
+    cap = max(lens) + 2
+    kc, w = normal(g, (B, cap, Hk, D), dtype), torch.rand((B, Hk, cap), generator=g, device="cuda")
+    q, lse = normal(g, (B, T, Hq, D), dtype, 2.0), 4.0 + torch.rand((B, T, Hq), generator=g, device="cuda")
+    q[..., 5] = q[..., 5].abs() + 0.25
+    if T > 1:
+        lse[:, 1] = -INF                                    # a row that saw nothing gives no weight, whatever the key
+    accepted = None if A is None else torch.rand((B, T), generator=g, device="cuda").argsort(1)[:, :A].int().contiguous()
+    cached, n = ints(lens), None if counts is None else ints(counts)
+    want, tol = ref.add_weights(q, lse, kc, cached, w, accepted, n)
+    odd = [2, max(0, min(lens) - 70), min(lens) // 2]       # (every row sees these, or in part)
+    kc[:, odd, :, 5] = -INF                                 # scores of -infinity: the weight is what it was
+    before, got = w.clone(), w.clone()
+    ds.dep_cache_weights(q, lse, kc, cached, got, accepted=accepted, n_accepted=n)
+    torch.cuda.synchronize()
+    assert torch.equal(got[..., odd], before[..., odd])
+    fine = torch.ones(cap, dtype=torch.bool)
+    fine[odd] = False
+    over = (got.cpu().double() - want).abs()[..., fine] / tol[..., fine]
+    assert float(over.max()) <= 1.0
+    kc[:, odd, :, 5] = INF                                  # and of +infinity: an infinite weight where an accepted row that saw something sees the key
+    got = w.clone()
+    ds.dep_cache_weights(q, lse, kc, cached, got, accepted=accepted, n_accepted=n)
+    torch.cuda.synchronize()
+    for b in range(B):
+        rows = ref.accepted_of(accepted, n, b, T, T if A is None else A)
+        base = lens[b] - len(rows)
+        for r in odd:
+            seen = any(r <= base + i and not (T > 1 and t == 1) for i, t in enumerate(rows))
+            assert bool((got[b, :, r] == (INF if seen else before[b, :, r])).all())
+    over = (got.cpu().double() - want).abs()[..., fine] / tol[..., fine]
+    assert float(over.max()) <= 1.0
