@@ -796,7 +796,10 @@ __global__ __launch_bounds__(256) void tree_attn_join(const TreeAttnArgs a) {
         const f32x4 v = *(const f32x4*)(a.parts + at * D + d);
         const float f = mz == -INFINITY ? (lz == 0.0f ? 0.0f : lz) : __builtin_amdgcn_exp2f(mz - M);   // (a sum without a maximum is 0, or NaN)
         L += lz * f;
-        o += v * f;
+        // Where the factor is 0 a part is too far below the others to count, but its weights are positive: what is not finite in it stays what it is.
+        const bool below = f == 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += (below && fabsf(v[e]) < INFINITY ? 0.0f : v[e]) * (below ? 1.0f : f);
     }
 #pragma unroll
     for (uint32_t x = VEC; x < 64; x <<= 1) {

@@ -127,3 +127,27 @@ def test_weights_of_keys_that_are_not_finite(B, T, A, Hq, Hk, D, lens, counts, d
             assert bool((got[b, :, r] == (INF if seen else before[b, :, r])).all())
     over = (got.cpu().double() - want).abs()[..., fine] / tol[..., fine]
     assert float(over.max()) <= 1.0
+
+
+# ---- drafted values that are not finite, where the key axis is cut ----------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("T,Hq,Hk", [(2, 4, 2), (40, 4, 2)])
+def test_infinite_drafted_values_far_below_the_cached_scores(T, Hq, Hk, dtype):
+    # one cached key of the first part outweighs everything in the last by e^181, more than 32 bits hold
+    print("not finite, cut", T, Hq, Hk, dtype, flush=True)
+    B, D, cap = 2, 128, 9000
+    g = gen(4)
+    q, kn, vn = torch.full((B, T, Hq, D), 8.0, dtype=dtype, device="cuda"), torch.full((B, T, Hk, D), -1.0, dtype=dtype, device="cuda"), normal(g, (B, T, Hk, D), dtype)
+    kc, vc = torch.full((B, cap, Hk, D), -1.0, dtype=dtype, device="cuda"), normal(g, (B, cap, Hk, D), dtype)
+    kc[:, 5] = 1.0
+    cached = ints([9000, 8000])
+    assert ds.tree_attn_workspace(q, kn, vn, kc, vc, cached, q) > 0
+    plain, plain_lse = attn(q, kn, vn, kc, vc, cached)
+    vn[:, 1, :, 3], vn[0, 0, 0, 9], vn[1, 0, :, 40] = INF, float("nan"), -INF
+    want, _, tol, _ = ref.attn(q, kn, vn, kc, vc, cached)
+    out, lse = attn(q, kn, vn, kc, vc, cached)
+    got, odd = out.cpu().double(), ~want.isfinite()
+    assert bool(odd.any()) and torch.equal(got[odd].isnan(), want[odd].isnan()) and torch.equal(got[odd].nan_to_num(7), want[odd].nan_to_num(7))
+    assert bool(((got - want).abs() <= tol)[~odd].all())
+    assert torch.equal(out.cpu()[~odd], plain.cpu()[~odd]) and torch.equal(lse, plain_lse)
