@@ -618,6 +618,7 @@ def conv_chain_n_check_waits(desc: ConvChainNDesc, kind: int, n_cu: int = 0, **p
 
 # These calls are short, so their descriptors are packed in one go (in the header's order, as the classes above have it) and each tensor is
 # asked once for what is needed: 35 fields set one by one and the former checks took 23 us a call, three times the two launches.
+# They take part in a torch program's order: without a stream they run on torch's current one on the tensors' device (the chains above: on the default stream).
 
 _TORCH = None
 
@@ -665,6 +666,11 @@ def _arr(t, name: str, dtype, device: int, shape) -> int:
     if t.get_device() != device or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous tensor of {dtype} and shape {tuple(shape)} on the device of the others")
     return t.data_ptr()
+
+
+def _current_or(stream, device: int):
+    """The handle of `stream`, or of torch's current stream on this device where it is None: what made the tensors was enqueued there."""
+    return _torch()._C._cuda_getCurrentRawStream(device) or None if stream is None else _stream_handle(stream)
 
 
 def _call(device: int, what: str, f, *args) -> None:
@@ -767,9 +773,10 @@ def dep_tree_attn(q, k_new, v_new, k_cache, v_cache, cached, out, lse=None, tree
 
     q, out [B, T, Hq, D]; k_new, v_new [B, T, Hk, D]; k_cache, v_cache [B, capacity, Hk, D] (None: no cache) of which sequence b has
     cached[b] rows (int32).  drafted[b] (int32): the tokens that sequence b has; the others' rows of out and lse are left alone.
-    lse [B, T, Hq] (float32) receives the logarithm of each row's sum.  max_cached: the most rows that a sequence has, where the host knows."""
+    lse [B, T, Hq] (float32) receives the logarithm of each row's sum.  max_cached: the most rows that a sequence has, where the host knows.
+    stream: a torch stream or handle (0: the default stream); None: torch's current stream on the tensors' device."""
     d, device = _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached)
-    stream = _stream_handle(stream)
+    stream = _current_or(stream, device)
     need = 0 if workspace is not None else _tree_attn_bytes(device, d[:32])
     keep, ptr, size = _workspace(need, workspace, device, stream)
     _call(device, "dep_tree_attn", _lib().dep_tree_attn, d, ptr, size, stream)
@@ -793,7 +800,7 @@ def _accepted(B: int, tokens: int, accepted, n_accepted, device: int):
 def dep_cache_append(k_new, v_new, k_cache, v_cache, cached, cached_out, accepted=None, n_accepted=None, weights=None, pos=None, start=None,
                      stream=None) -> None:
     """Enqueue: the keys and values of drafted tokens accepted[b, :n_accepted[b]] (int32; None: the first ones) go to rows cached[b].. of the cache,
-    their weights [B, Hk, capacity] (float32) become 0, their positions (int32, same shape) start[b].., and cached_out = cached + n."""
+    their weights [B, Hk, capacity] (float32) become 0, their positions (int32, same shape) start[b].., and cached_out = cached + n.  stream: as for dep_tree_attn."""
     torch = _torch()
     device, dtype = k_new.get_device(), k_new.dtype
     code = _dtype_code(k_new)
@@ -807,13 +814,13 @@ def dep_cache_append(k_new, v_new, k_cache, v_cache, cached, cached_out, accepte
                        *_pair(k_cache, v_cache, "cache", dtype, device, (B, cap, Hk, D)), _arr(cached, "cached", i32, device, (B,)),
                        _arr(cached_out, "cached_out", i32, device, (B,)), acc, n_acc, _arr(weights, "weights", torch.float32, device, (B, Hk, cap)),
                        _arr(pos, "pos", i32, device, (B, Hk, cap)), _arr(start, "start", i32, device, (B,)))
-    _call(device, "dep_cache_append", _lib().dep_cache_append, d, _stream_handle(stream))
+    _call(device, "dep_cache_append", _lib().dep_cache_append, d, _current_or(stream, device))
 
 
 def dep_cache_weights(q, lse, k_cache, cached, weights, accepted=None, n_accepted=None, scale: Optional[float] = None,
                       max_cached: Optional[int] = None, stream=None) -> None:
     """Enqueue weights[b, h, k] += the attention weight that cached row k received from the accepted tokens, whose own rows are the last
-    of cached[b].  q [B, T, Hq, D] and lse [B, T, Hq] are dep_tree_attn's; weights is [B, Hk, capacity] (float32)."""
+    of cached[b].  q [B, T, Hq, D] and lse [B, T, Hq] are dep_tree_attn's; weights is [B, Hk, capacity] (float32).  stream: as there."""
     torch = _torch()
     device, dtype = q.get_device(), q.dtype
     code = _dtype_code(q)
@@ -825,7 +832,7 @@ def dep_cache_weights(q, lse, k_cache, cached, weights, accepted=None, n_accepte
     d = _P_WEIGHTS.pack(B, T, Hq, Hk, D, code, cap, max_cached or 0, n_max, *_t4(q, "q", dtype, device), _arr(lse, "lse", torch.float32, device, (B, T, Hq)),
                         *_t4(k_cache, "k_cache", dtype, device, (B, cap, Hk, D)), _arr(cached, "cached", torch.int32, device, (B,)), acc, n_acc,
                         scale or 0.0, _arr(weights, "weights", torch.float32, device, (B, Hk, cap)))
-    _call(device, "dep_cache_weights", _lib().dep_cache_weights, d, _stream_handle(stream))
+    _call(device, "dep_cache_weights", _lib().dep_cache_weights, d, _current_or(stream, device))
 
 
 def _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out):
@@ -866,9 +873,9 @@ def dep_cache_evict(k_cache, v_cache, weights, pos, cached, cached_out, budget: 
                     k_out=None, v_out=None, weights_out=None, pos_out=None, workspace=None, stream=None) -> None:
     """Enqueue: every sequence and head keeps `budget` rows: the `recent` newest by position, then the heaviest, among equals the lowest row.
     In place kept rows behind the budget fill the places of those that go; into k_out .. pos_out (all four) the kept rows go in their order.
-    cached_out = min(cached, budget)."""
+    cached_out = min(cached, budget).  stream: as for dep_tree_attn."""
     d, device = _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out)
-    stream = _stream_handle(stream)
+    stream = _current_or(stream, device)
     need = 0 if workspace is not None else _evict_bytes(d[:32], k_out is not None)
     keep, ptr, size = _workspace(need, workspace, device, stream)
     _call(device, "dep_cache_evict", _lib().dep_cache_evict, d, ptr, size, stream)

@@ -151,3 +151,93 @@ def test_infinite_drafted_values_far_below_the_cached_scores(T, Hq, Hk, dtype):
     assert bool(odd.any()) and torch.equal(got[odd].isnan(), want[odd].isnan()) and torch.equal(got[odd].nan_to_num(7), want[odd].nan_to_num(7))
     assert bool(((got - want).abs() <= tol)[~odd].all())
     assert torch.equal(out.cpu()[~odd], plain.cpu()[~odd]) and torch.equal(lse, plain_lse)
+
+
+# ---- calls without a stream run on torch's current one ----------------------------------------------------------------------------
+
+def loop_state(B, T, Hq, Hk, D, cap, seed):
+    g = gen(seed)
+    s = {"q": normal(g, (B, T, Hq, D), BF, 2.0), "kn": normal(g, (B, T, Hk, D), BF), "vn": normal(g, (B, T, Hk, D), BF),
+         "kc": normal(g, (B, cap, Hk, D), BF), "vc": normal(g, (B, cap, Hk, D), BF), "w": torch.rand((B, Hk, cap), generator=g, device="cuda"),
+         "pos": torch.arange(cap, device="cuda").int().expand(B, Hk, cap).contiguous(), "cached": ints([cap - T - 3 * b for b in range(B)]),
+         "start": ints([cap] * B), "mid": ints([0] * B), "end": ints([0] * B), "out": torch.zeros((B, T, Hq, D), dtype=BF, device="cuda"),
+         "lse": torch.zeros((B, T, Hq), device="cuda")}
+    torch.cuda.synchronize()
+    return s
+
+
+def loop_round(s, budget, **kw):
+    ds.dep_tree_attn(s["q"], s["kn"], s["vn"], s["kc"], s["vc"], s["cached"], s["out"], lse=s["lse"], **kw)
+    ds.dep_cache_append(s["kn"], s["vn"], s["kc"], s["vc"], s["cached"], s["mid"], weights=s["w"], pos=s["pos"], start=s["start"], **kw)
+    ds.dep_cache_weights(s["q"], s["lse"], s["kc"], s["mid"], s["w"], **kw)
+    ds.dep_cache_evict(s["kc"], s["vc"], s["w"], s["pos"], s["mid"], s["end"], budget, 9, **kw)
+
+
+SHAPE, BUDGET = (2, 5, 8, 2, 128, 3000), 2500
+
+
+@pytest.mark.parametrize("which", ["attn", "append", "weights", "evict"])
+def test_calls_without_a_stream_follow_the_current_one(which):
+    # what the call reads is written on a side stream behind some ten milliseconds of other work: a call that ran elsewhere would find what stood there
+    print("current stream", which, flush=True)
+    want, s = loop_state(*SHAPE, 5), loop_state(*SHAPE, 6)
+    calls = {
+        "attn": lambda x: ds.dep_tree_attn(x["q"], x["kn"], x["vn"], x["kc"], x["vc"], x["cached"], x["out"], lse=x["lse"]),
+        "append": lambda x: ds.dep_cache_append(x["kn"], x["vn"], x["kc"], x["vc"], x["cached"], x["mid"], weights=x["w"], pos=x["pos"], start=x["start"]),
+        "weights": lambda x: ds.dep_cache_weights(x["q"], x["lse"], x["kc"], x["cached"], x["w"]),
+        "evict": lambda x: ds.dep_cache_evict(x["kc"], x["vc"], x["w"], x["pos"], x["cached"], x["end"], BUDGET, 9),
+    }
+    source = {k: v.clone() for k, v in want.items()}
+    calls[which](want)
+    calls[which](loop_state(*SHAPE, 7))                     # (the sizes' workspace has been asked for)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        torch.cuda._sleep(20_000_000)
+        for k, v in source.items():
+            s[k].copy_(v)
+        calls[which](s)
+    torch.cuda.synchronize()
+    for k in s:
+        assert torch.equal(s[k], want[k]), k
+
+
+def test_calls_without_a_stream_are_captured():
+    print("capture without a stream", flush=True)
+    s, eager = loop_state(*SHAPE, 8), loop_state(*SHAPE, 8)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loop_round(s, BUDGET)
+    for it in range(4):
+        g = gen(9 + it)
+        for x in (s, eager):
+            g.manual_seed(9 + it)
+            x["q"].copy_(normal(g, x["q"].shape, BF, 2.0))
+            x["kn"].copy_(normal(g, x["kn"].shape, BF))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        loop_round(eager, BUDGET)
+        torch.cuda.synchronize()
+        for k in s:
+            assert torch.equal(s[k], eager[k]), (it, k)
+        for x in (s, eager):
+            x["cached"].copy_(x["end"])
+            x["start"] += 5
+
+
+def test_a_stream_that_is_given_goes_before_the_current_one():
+    print("given stream", flush=True)
+    s, want = loop_state(*SHAPE, 10), loop_state(*SHAPE, 10)
+    loop_round(want, BUDGET)
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        torch.cuda._sleep(60_000_000)
+        busy = torch.cuda.Event()
+        busy.record()
+        loop_round(s, BUDGET, stream=other)
+        other.synchronize()
+        assert not busy.query()                             # (it did not wait for the current stream's work)
+    torch.cuda.synchronize()
+    for k in s:
+        assert torch.equal(s[k], want[k]), k
