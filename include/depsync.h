@@ -532,7 +532,7 @@ int depsync_tree_attn_workspace(const depsync_tree_attn_desc* d, int n_cu, size_
 
 /* Cache row cached[b] + i of sequence b becomes the key and value of its drafted token accepted[b][i], for i < n_accepted[b]; the row's
  * weight becomes 0 and its position start[b] + i, in every head, and cached_out[b] = cached[b] + n.  Rows that would lie behind the
- * capacity are dropped, and do not count.                                                                                         */
+ * capacity are dropped, and do not count: n_out[b] is the n that is left, which dep_cache_weights then takes for its n_accepted.    */
 typedef struct {
     int32_t batch, tokens, kv_heads, head_dim, dtype, capacity;
     int32_t n_max;                                      /* entries of `accepted` per sequence (without it: 0..tokens, the first n are taken) */
@@ -543,11 +543,14 @@ typedef struct {
     const int32_t* n_accepted;                          /* [batch], clamped to 0..n_max; NULL: n_max                                */
     float* weights; int32_t* pos;                       /* [batch][kv_heads][capacity]; either may be NULL                          */
     const int32_t* start;                               /* [batch]; with pos only                                                   */
+    int32_t* n_out;                                     /* [batch], the rows appended; may be NULL.  Not the array of cached, cached_out or
+                                                           n_accepted                                                              */
 } depsync_cache_append_desc;
 int dep_cache_append(const depsync_cache_append_desc* d, void* stream);
 
 /* weights[b][h][k] += sum of exp(scale q.k - lse) over the query heads of head h and the accepted tokens i < n that see row k.  `cached`
- * counts the accepted tokens' own rows, the last n: token i sees rows 0..cached - n + i (its path and all before).  q and lse are
+ * counts the accepted tokens' own rows, the last n: token i sees rows 0..cached - n + i (its path and all before).  All n have to have a row: where
+ * an append may have dropped some at the capacity, n_accepted is its n_out (with the former n every row of the others would shift).  q and lse are
  * dep_tree_attn's; where lse is -infinity the token saw nothing, and adds nothing.  A row's weight is touched by the tokens that see it alone, whatever
  * bits (infinities, NaN) its key holds.  The sum is taken in 32 bits in an order that depends on sizes alone.                                            */
 typedef struct {

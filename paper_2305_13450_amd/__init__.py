@@ -140,7 +140,7 @@ class CacheAppendDesc(ctypes.Structure):
     _fields_ = _fields(batch="i", tokens="i", kv_heads="i", head_dim="i", dtype="i", capacity="i", n_max="i",
                        k_new="p", v_new="p", new_batch="l", new_token="l", new_head="l",
                        k_cache="p", v_cache="p", cache_batch="l", cache_token="l", cache_head="l",
-                       cached="p", cached_out="p", accepted="p", n_accepted="p", weights="p", pos="p", start="p")
+                       cached="p", cached_out="p", accepted="p", n_accepted="p", weights="p", pos="p", start="p", n_out="p")
 
 
 class CacheWeightsDesc(ctypes.Structure):
@@ -633,7 +633,7 @@ def _torch():
 
 
 _P_TREE = struct.Struct("8i P3q 2P3q 2P3q 3Pq f4x P3q P")
-_P_APPEND = struct.Struct("7i4x 2P3q 2P3q 7P")
+_P_APPEND = struct.Struct("7i4x 2P3q 2P3q 8P")
 _P_WEIGHTS = struct.Struct("9i4x P3q P P3q 3P f4x P")
 _P_EVICT = struct.Struct("8i 2P3q 4P i4x 2P3q 2P")
 
@@ -798,9 +798,10 @@ def _accepted(B: int, tokens: int, accepted, n_accepted, device: int):
 
 
 def dep_cache_append(k_new, v_new, k_cache, v_cache, cached, cached_out, accepted=None, n_accepted=None, weights=None, pos=None, start=None,
-                     stream=None) -> None:
+                     stream=None, n_out=None) -> None:
     """Enqueue: the keys and values of drafted tokens accepted[b, :n_accepted[b]] (int32; None: the first ones) go to rows cached[b].. of the cache,
-    their weights [B, Hk, capacity] (float32) become 0, their positions (int32, same shape) start[b].., and cached_out = cached + n.  stream: as for dep_tree_attn."""
+    their weights [B, Hk, capacity] (float32) become 0, their positions (int32, same shape) start[b].., and cached_out = cached + n.  n_out[b] (int32) receives n, which is
+    less than n_accepted[b] where the capacity was reached: what dep_cache_weights then takes for n_accepted.  stream: as for dep_tree_attn."""
     torch = _torch()
     device, dtype = k_new.get_device(), k_new.dtype
     code = _dtype_code(k_new)
@@ -813,14 +814,14 @@ def dep_cache_append(k_new, v_new, k_cache, v_cache, cached, cached_out, accepte
     d = _P_APPEND.pack(B, T, Hk, D, code, cap, n_max, *_pair(k_new, v_new, "new", dtype, device, (B, T, Hk, D)),
                        *_pair(k_cache, v_cache, "cache", dtype, device, (B, cap, Hk, D)), _arr(cached, "cached", i32, device, (B,)),
                        _arr(cached_out, "cached_out", i32, device, (B,)), acc, n_acc, _arr(weights, "weights", torch.float32, device, (B, Hk, cap)),
-                       _arr(pos, "pos", i32, device, (B, Hk, cap)), _arr(start, "start", i32, device, (B,)))
+                       _arr(pos, "pos", i32, device, (B, Hk, cap)), _arr(start, "start", i32, device, (B,)), _arr(n_out, "n_out", i32, device, (B,)))
     _call(device, "dep_cache_append", _lib().dep_cache_append, d, _current_or(stream, device))
 
 
 def dep_cache_weights(q, lse, k_cache, cached, weights, accepted=None, n_accepted=None, scale: Optional[float] = None,
                       max_cached: Optional[int] = None, stream=None) -> None:
     """Enqueue weights[b, h, k] += the attention weight that cached row k received from the accepted tokens, whose own rows are the last
-    of cached[b].  q [B, T, Hq, D] and lse [B, T, Hq] are dep_tree_attn's; weights is [B, Hk, capacity] (float32).  stream: as there."""
+    of cached[b] (n_accepted: the append's n_out, where that may have dropped tokens at the capacity).  q [B, T, Hq, D] and lse [B, T, Hq] are dep_tree_attn's; weights is [B, Hk, capacity] (float32).  stream: as there."""
     torch = _torch()
     device, dtype = q.get_device(), q.dtype
     code = _dtype_code(q)

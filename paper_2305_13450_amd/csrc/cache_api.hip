@@ -170,8 +170,9 @@ int dep_cache_append(const depsync_cache_append_desc* d, void* stream) {
     if (d->capacity < 1 || d->n_max < 1 || d->n_max > 65536 || (!d->accepted && d->n_max > d->tokens)) return DEPSYNC_EINVAL;
     if (!operand(d->k_new) || !operand(d->v_new) || !operand(d->k_cache) || !operand(d->v_cache) || !array(d->cached) || !array(d->cached_out) ||
         d->cached == d->cached_out || !optional(d->accepted) || !optional(d->n_accepted) || !optional(d->weights) || !optional(d->pos) ||
-        (d->pos && !array(d->start)))
+        (d->pos && !array(d->start)) || !optional(d->n_out))
         return DEPSYNC_EINVAL;
+    if (d->n_out && (d->n_out == d->cached || d->n_out == d->cached_out || d->n_out == d->n_accepted)) return DEPSYNC_EINVAL;
     if (!strides(a.new_s, d->new_batch, d->new_token, d->new_head, d->batch, d->tokens, d->kv_heads, D, false, false) ||
         !strides(a.cache_s, d->cache_batch, d->cache_token, d->cache_head, d->batch, d->capacity, d->kv_heads, D, true, true))
         return DEPSYNC_EINVAL;
@@ -179,7 +180,7 @@ int dep_cache_append(const depsync_cache_append_desc* d, void* stream) {
     if (d->batch * cdiv64((int64_t)d->n_max * d->kv_heads, rows) > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;
     a.k_new = d->k_new; a.v_new = d->v_new; a.k_cache = d->k_cache; a.v_cache = d->v_cache;
     a.cached = d->cached; a.cached_out = d->cached_out; a.accepted = d->accepted; a.n_accepted = d->n_accepted;
-    a.weights = d->weights; a.pos = d->pos; a.start = d->start;
+    a.weights = d->weights; a.pos = d->pos; a.start = d->start; a.n_out = d->n_out;
     a.batch = d->batch; a.tokens = d->tokens; a.kv_heads = d->kv_heads; a.capacity = d->capacity; a.n_max = d->n_max;
     const hipError_t e = launch_cache_append(a, D, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);

@@ -35,6 +35,7 @@ struct CacheAppendArgs {
     const int32_t *accepted, *n_accepted, *start;
     float* weights;
     int32_t* pos;
+    int32_t* n_out;                       // may be null
     Strides new_s, cache_s;
     uint32_t batch, tokens, kv_heads, capacity, n_max;
 };

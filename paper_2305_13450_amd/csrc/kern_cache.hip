@@ -18,7 +18,10 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const CacheAppendArgs
     const uint32_t b = blockIdx.x / blocks, blk = blockIdx.x % blocks;
     const uint32_t cached = clamp_count(a.cached[b], a.capacity);
     const uint32_t n = min(a.n_accepted ? clamp_count(a.n_accepted[b], a.n_max) : a.n_max, a.capacity - cached);
-    if (blk == 0 && threadIdx.x == 0) a.cached_out[b] = (int32_t)(cached + n);
+    if (blk == 0 && threadIdx.x == 0) {
+        a.cached_out[b] = (int32_t)(cached + n);
+        if (a.n_out) a.n_out[b] = (int32_t)n;
+    }
     const uint32_t item = blk * ROWS + threadIdx.x / LANES, unit = threadIdx.x % LANES;
     const uint32_t i = item / a.kv_heads, h = item % a.kv_heads;
     if (i >= n) return;

@@ -241,3 +241,45 @@ def test_a_stream_that_is_given_goes_before_the_current_one():
     torch.cuda.synchronize()
     for k in s:
         assert torch.equal(s[k], want[k]), k
+
+
+# ---- an append that reaches the capacity, and the weights behind it ---------------------------------------------------------------
+
+@pytest.mark.parametrize("T,A,Hq,Hk,cap,lens,counts", [
+    (3, None, 2, 1, 10, [9], None), (6, 4, 4, 2, 40, [38, 40, 10, 37], [4, 3, 2, 3]), (80, None, 2, 2, 100, [60, 100, 0, 20], [80, 70, 75, -2])])
+def test_weights_behind_an_append_that_reaches_the_capacity(T, A, Hq, Hk, cap, lens, counts):
+    # a token that was kept sees all rows up to its own; one that was dropped adds nothing
+    print("capacity", T, A, cap, lens, counts, flush=True)
+    B, D = len(lens), 128
+    g = gen(20)
+    q, kn, vn = normal(g, (B, T, Hq, D), BF, 2.0), normal(g, (B, T, Hk, D), BF), normal(g, (B, T, Hk, D), BF)
+    kc, vc, w = normal(g, (B, cap, Hk, D), BF), normal(g, (B, cap, Hk, D), BF), torch.rand((B, Hk, cap), generator=g, device="cuda")
+    pos, lse = torch.zeros((B, Hk, cap), dtype=torch.int32, device="cuda"), 4.0 + torch.rand((B, T, Hq), generator=g, device="cuda")
+    accepted = None if A is None else torch.rand((B, T), generator=g, device="cuda").argsort(1)[:, :A].int().contiguous()
+    cached, n = ints(lens), None if counts is None else ints(counts)
+    mid, kept = ints([-1] * B), ints([-1] * B)
+    k1, v1, w1, pos1, mid1 = ref.append(kn, vn, kc, vc, cached, w, pos, cached, accepted, n)
+    ds.dep_cache_append(kn, vn, kc, vc, cached, mid, accepted=accepted, n_accepted=n, weights=w, pos=pos, start=cached, n_out=kept)
+    ds.dep_cache_weights(q, lse, kc, mid, w, accepted=accepted, n_accepted=kept)
+    torch.cuda.synchronize()
+    for b in range(B):
+        want = max(0, min(cap - lens[b], len(ref.accepted_of(accepted, n, b, T, T if A is None else A))))
+        assert int(kept[b]) == want and int(mid[b]) == lens[b] + want == int(mid1[b])
+    assert torch.equal(kc.cpu(), k1) and torch.equal(vc.cpu(), v1) and torch.equal(pos.cpu(), pos1)
+    want, tol = ref.add_weights(q, lse, k1, mid1, w1, accepted, kept)
+    assert float(((w.cpu().double() - want).abs() / tol).max()) <= 1.0
+    for b in range(B):                                      # (the oracle: the last row that was appended was seen by its own token)
+        if int(kept[b]):
+            assert bool((want[b, :, int(mid[b]) - 1] > 0).all())
+
+
+def test_refusals_of_the_count_of_appended_rows():
+    g = gen(21)
+    kn, kc, cached, out, n = normal(g, (2, 3, 1, 64), BF), normal(g, (2, 9, 1, 64), BF), ints([1, 2]), ints([0, 0]), ints([1, 1])
+    for bad in (cached, out, n):
+        with pytest.raises(ds.DepsyncError) as e:
+            ds.dep_cache_append(kn, kn, kc, kc.clone(), cached, out, n_accepted=n, n_out=bad)
+        assert e.value.status == ds.EINVAL
+    for bad in (ints([0]), torch.zeros(2, device="cuda"), torch.zeros(2, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            ds.dep_cache_append(kn, kn, kc, kc.clone(), cached, out, n_accepted=n, n_out=bad)
