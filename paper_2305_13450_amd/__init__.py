@@ -654,7 +654,7 @@ def _pair(a, b, name: str, dtype, device: int, shape):
     """The pointers of two tensors alike (keys and values), and their strides."""
     pa, s0, s1, s2 = _t4(a, "k_" + name, dtype, device, shape)
     pb, *sb = _t4(b, "v_" + name, dtype, device, shape)
-    if sb != [s0, s1, s2]:
+    if sb != [s0, s1, s2] and any(x != y and n > 1 for x, y, n in zip(sb, (s0, s1, s2), shape)):   # (those of dimensions of size 1 are not read)
         raise ValueError(f"k_{name} and v_{name} must have the same strides")
     return pa, pb, s0, s1, s2
 

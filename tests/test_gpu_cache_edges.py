@@ -283,3 +283,32 @@ def test_refusals_of_the_count_of_appended_rows():
     for bad in (ints([0]), torch.zeros(2, device="cuda"), torch.zeros(2, dtype=torch.int32)):
         with pytest.raises(ValueError):
             ds.dep_cache_append(kn, kn, kc, kc.clone(), cached, out, n_accepted=n, n_out=bad)
+
+
+# ---- strides of dimensions of size 1 ----------------------------------------------------------------------------------------------
+
+def test_keys_and_values_that_differ_in_strides_nothing_reads():
+    print("strides of size 1", flush=True)
+    g = gen(30)
+    q, wide = normal(g, (1, 1, 4, 128), BF, 2.0), normal(g, (3, 5, 1, 640), BF)
+    kn, vn = wide[1:2, 3:4, :, 128:256], normal(g, (1, 1, 1, 128), BF)
+    rows, kc = normal(g, (2, 40, 2, 128), BF), normal(g, (1, 40, 1, 256), BF)[..., :128]
+    vc = rows[1:, :, 1:]                                    # rows 256 apart like the keys', sequences and heads not
+    assert kn.stride() != vn.stride() and kc.stride() != vc.stride()
+    cached, mid, end = ints([37]), ints([0]), ints([0])
+    want, _, tol, _ = ref.attn(q, kn, vn, kc, vc, cached)
+    out, _ = attn(q, kn, vn, kc, vc, cached)
+    assert bool(((out.cpu().double() - want).abs() <= tol).all())
+    w, pos = torch.rand((1, 1, 40), generator=g, device="cuda"), torch.arange(40, device="cuda").int().view(1, 1, 40)
+    edge = rows[0].clone()
+    for call, oracle, length in ((lambda: ds.dep_cache_append(kn, vn, kc, vc, cached, mid, weights=w, pos=pos, start=cached),
+                                  ref.append(kn, vn, kc, vc, cached, w, pos, cached), mid),
+                                 (lambda: ds.dep_cache_evict(kc, vc, w, pos, mid, end, 20, 5), None, end)):
+        oracle = oracle or ref.evict(kc, vc, w, pos, mid, 20, 5)
+        call()
+        torch.cuda.synchronize()
+        for got, x in zip((kc, vc, w, pos, length), oracle):
+            assert torch.equal(got.cpu(), x)
+    assert torch.equal(rows[0], edge)
+    with pytest.raises(ValueError):                         # a stride that is read
+        attn(q, kn, vn, kc, normal(g, (1, 40, 1, 512), BF)[..., :128], cached)
