@@ -102,7 +102,7 @@ def _draw_once(rng):
 
 
 def draw(rng):
-    """One more case of those ranges, no dearer than the largest listed (4.5e11 flops, 2 GB touched, 4e9 scores)."""
+    """One more case of those ranges, no dearer than the largest listed: at most 4.5e11 flops, 1.2e9 bytes, a cache of 2e9 bytes, 1.1e9 scores."""
     while True:
         c = _draw_once(rng)
         del c["name"]
