@@ -312,3 +312,30 @@ def test_keys_and_values_that_differ_in_strides_nothing_reads():
     assert torch.equal(rows[0], edge)
     with pytest.raises(ValueError):                         # a stride that is read
         attn(q, kn, vn, kc, normal(g, (1, 40, 1, 512), BF)[..., :128], cached)
+
+
+# ---- fp16 where the key axis is cut and lengths change ----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("B,T,Hq,Hk,D,lens", [
+    (1, 40, 8, 2, 128, [6000]), (20, 40, 4, 1, 64, [300 * i for i in range(20)]), (64, 3, 2, 1, 128, [0] * 63 + [9000]), (66, 33, 4, 1, 128, [0] * 65 + [3000])])
+def test_fp16_over_caches_that_are_cut(B, T, Hq, Hk, D, lens):
+    print("fp16, cut", B, T, D, flush=True)
+    g = gen(40)
+    q, kn, vn = normal(g, (B, T, Hq, D), FP, 2.0), normal(g, (B, T, Hk, D), FP), normal(g, (B, T, Hk, D), FP)
+    kc, vc, cached = normal(g, (B, max(lens), Hk, D), FP), normal(g, (B, max(lens), Hk, D), FP), ints(lens)
+    assert ds.tree_attn_workspace(q, kn, vn, kc, vc, cached, q) > 0
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:3], device="cuda")
+    ds.dep_tree_attn(q, kn, vn, kc, vc, cached, out, lse=lse)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ds.dep_tree_attn(q, kn, vn, kc, vc, cached, out, lse=lse)
+    for now in (lens, lens[::-1], [n // 3 for n in lens]):
+        cached.copy_(ints(now))
+        out.zero_(), lse.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want, want_l, tol, tol_l = ref.attn(q, kn, vn, kc, vc, cached)
+        assert bool(((out.cpu().double() - want).abs() <= tol).all()) and bool(((lse.cpu().double() - want_l).abs() <= tol_l).all())
+        eager = attn(q, kn, vn, kc, vc, cached)
+        assert torch.equal(out, eager[0]) and torch.equal(lse, eager[1])
