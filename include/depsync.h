@@ -504,7 +504,9 @@ int depsync_copy_chain_plan(const depsync_copy_chain_desc* d, const sync_policy_
 
 /* out = softmax(scale q k^T) v over, for drafted token t of a sequence, all cached rows and those drafted tokens j whose bit is set
  * in row t of `tree`: bit j % 64 of word j / 64.  Masked keys count for nothing, whatever bits (infinities, NaN) they and their values
- * hold.  A token that sees no key gets out = 0 and lse = -infinity.  The same call gives the same bits; how sums are divided depends on
+ * hold.  A token that sees no key, or only scores of -infinity, gets out = 0 and lse = -infinity.  Scores and sums have 32 bits; for the product
+ * with v the softmax weights are rounded to the element type where more than 64 query rows share a key and value head (from 33 on where the caches are large),
+ * and keep twice its bits where fewer do.  The same call gives the same bits; how sums are divided depends on
  * the lengths of all sequences of a call, so those of one differ in their rounding with its neighbours'.                          */
 typedef struct {
     int32_t batch, tokens, heads, kv_heads, head_dim;   /* tokens: drafted ones per sequence, at least 1, at most 65536           */

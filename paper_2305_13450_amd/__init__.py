@@ -773,7 +773,7 @@ def dep_tree_attn(q, k_new, v_new, k_cache, v_cache, cached, out, lse=None, tree
 
     q, out [B, T, Hq, D]; k_new, v_new [B, T, Hk, D]; k_cache, v_cache [B, capacity, Hk, D] (None: no cache) of which sequence b has
     cached[b] rows (int32).  drafted[b] (int32): the tokens that sequence b has; the others' rows of out and lse are left alone.
-    lse [B, T, Hq] (float32) receives the logarithm of each row's sum.  max_cached: the most rows that a sequence has, where the host knows.
+    lse [B, T, Hq] (float32) receives the logarithm of each row's sum.  scale: None or 0 is 1 / sqrt(D).  max_cached: the most rows that a sequence has, where the host knows.
     stream: a torch stream or handle (0: the default stream); None: torch's current stream on the tensors' device."""
     d, device = _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached)
     stream = _current_or(stream, device)
@@ -821,7 +821,8 @@ def dep_cache_append(k_new, v_new, k_cache, v_cache, cached, cached_out, accepte
 def dep_cache_weights(q, lse, k_cache, cached, weights, accepted=None, n_accepted=None, scale: Optional[float] = None,
                       max_cached: Optional[int] = None, stream=None) -> None:
     """Enqueue weights[b, h, k] += the attention weight that cached row k received from the accepted tokens, whose own rows are the last
-    of cached[b] (n_accepted: the append's n_out, where that may have dropped tokens at the capacity).  q [B, T, Hq, D] and lse [B, T, Hq] are dep_tree_attn's; weights is [B, Hk, capacity] (float32).  stream: as there."""
+    of cached[b] (n_accepted: the append's n_out, where that may have dropped tokens at the capacity).  q [B, T, Hq, D] and lse [B, T, Hq] are
+    dep_tree_attn's; weights is [B, Hk, capacity] (float32).  stream: as there."""
     torch = _torch()
     device, dtype = q.get_device(), q.dtype
     code = _dtype_code(q)

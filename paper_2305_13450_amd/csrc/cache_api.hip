@@ -65,7 +65,7 @@ int tree_check(const depsync_tree_attn_desc* d) {
 // up to 28 cuts each (1 to 2048 rows, caches of 0 to 120000; its choice is 4 % behind the best cut in the mean, in the worst case 21 %):
 // a workgroup's start, a block of keys where its workgroup is alone on the CU and where two share it, the keys' way from HBM, the
 // second kernel and the results' way there and back.  5.9 is what a second launch costs a program that waits for the host (one token of 12 heads over 500
-// rows 11.5 us in one launch, 15.1 in two); captured into a graph it is about 4 (11.7 and 11.5).  The lengths are the longest sequence's; the
+// rows 12.4 us in one launch, 15.5 in two); captured into a graph it is about 4 (12.1 and 11.6).  The lengths are the longest sequence's; the
 // kernels then share out the parts by the real ones.
 double tree_cost(int64_t base, int64_t part, int64_t blocks, int64_t pairs, int64_t rows, int64_t row_blocks, int head_dim, int n_cu, bool few) {
     const int64_t parts = cdiv64(blocks, part), groups = base * parts, slots = 2 * (int64_t)n_cu;
@@ -85,8 +85,10 @@ int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t
     if (rows > 1 << 24) return DEPSYNC_ENOTIMPL;
     a.rows = (uint32_t)rows;
     // From 33 to 64 rows two workgroups of 32 walk the same keys, the second from L2; that is ahead of one of 128 rows until the caches are larger than
-    // what L2 and the Infinity Cache keep between the two (16 x 40 rows over 1000 keys of 8 heads, 70 MB: 21 and 26 us; 4 x 52 rows over 8000, 131 MB: 39 and
-    // 35; 16 x 40 over 4000, 268 MB: 64 and 60; 64 x 64 over 1000, 215 MB: 64 and 54).
+    // what L2 and the Infinity Cache keep between the two.  Inputs that change from call to call, us for 32 and for 128 rows: 16 x 40 rows over 1000 keys of 8
+    // heads, 66 MB, 21 and 30; 32 x 40 over 1000, 131 MB, 38 and 35; 64 x 64 over 1000, 262 MB, 73 and 63; 64 x 40 over 4000, 1 GB, 223 and 201; 52 rows of one
+    // head of 64 over 120000, 73 and 62.  Between 100 and 270 MB it depends on how many sequences share them: 8 x 48 over 8000 67 and 64, but 16 x 64
+    // over 4000 64 and 68, 4 x 52 over 8000 40 and 42, 16 x 40 over 2000 36 and 49.
     const int64_t cache_bytes = (int64_t)d->batch * d->kv_heads * rows_hint(d->max_cached, d->capacity) * d->head_dim * 4;
     a.few = rows <= (cache_bytes < 100000000 ? 64 : 32);
     const int64_t keys = a.few ? TREE_FEW_KEYS : TREE_MANY_KEYS, row_blocks = cdiv64(rows, a.few ? TREE_FEW_ROWS : TREE_MANY_ROWS);
@@ -207,14 +209,14 @@ int dep_cache_weights(const depsync_cache_weights_desc* d, void* stream) {
     if (int rc = cu_count(n_cu); rc != DEPSYNC_OK) return rc;
     if (a.few) {
         // Three workgroups share a CU.  Where each would have 8 blocks or more, twice as many even out sequences of different lengths (8 of 500 to
-        // 20000 rows: 36 and 29 us, 2 of 20000 and 39000: 35 and 33); with fewer they cost more than that (4 of 4000 to 8000, 3 blocks: 12.7 and 13.7).
+        // 20000 rows: 36 and 30 us, 2 of 20000 and 39000: 35 and 33); with fewer they cost more than that (4 of 4000 to 8000, 3 blocks: 12.7 and 13.7).
         const int64_t blocks = cdiv64(keys, 128) * pairs, share = cdiv64(blocks, 3 * (int64_t)n_cu);
         a.part_blocks = (uint32_t)std::max<int64_t>(1, share < 8 ? share : cdiv64(blocks, 6 * (int64_t)n_cu));
         a.n_parts = (uint32_t)cdiv64(cdiv64(keys, 128), a.part_blocks);
     } else {
-        // 64 keys to a workgroup read the queries half as often as 32 (4 x 1500 tokens of 32 heads: 71 us, 92 with 32), but the first keys' have all rows to
-        // walk and the last ones' few: where workgroups are not many, twice as many of twice the waves even that out (2048 tokens of 12 heads: 29 us with 64
-        // and 21 with 32; of 32 heads on 4: 77 with 32, 112 with as many waves as for 64).  3 x 1500 tokens of 12 heads, 864 workgroups of 64: 20 us, 24 with 32.
+        // 64 keys to a workgroup read the queries half as often as 32 (4 x 1500 tokens of 32 heads: 69 us, 88 with 32), but the first keys' have all rows to
+        // walk and the last ones' few: where workgroups are not many, twice as many of twice the waves even that out (2048 tokens of 12 heads: 21 us with 64
+        // and 18 with 32; of 32 heads on 4: 133 and 69).  3 x 1500 tokens of 12 heads, 864 workgroups of 64: 27 us, 30 with 32.
         a.keys = pairs * cdiv64(keys, 64) < 2 * (int64_t)n_cu ? 32 : 64;
         a.n_parts = (uint32_t)cdiv64(keys, a.keys);
     }

@@ -81,7 +81,7 @@ __device__ __forceinline__ float rows_weight(const f32x16& st, const float* lse,
 }
 
 // At most 64 rows, those of an accepted path: the time is that of reading K once (16 sequences of 2500 to 4096 rows, 8 heads: 112 MB in
-// 21.5 us, the rate of a copy).  The rows stay in LDS; each wave walks 32 of a block's
+// 21.7 us, the rate of a copy).  The rows stay in LDS; each wave walks 32 of a block's
 // 128 keys, the next ones on their way into registers meanwhile, and no wave waits for another.
 template <typename T, int D>
 __global__ __launch_bounds__(256, 3) void cache_weights_few_kernel(const CacheWeightsArgs a) {

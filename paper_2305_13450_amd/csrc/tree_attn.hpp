@@ -404,7 +404,7 @@ __device__ __forceinline__ void store_row4(const TreeAttnArgs& a, const TreeJob&
 
 // ---- few rows ------------------------------------------------------------------------------------------------------------
 // 32 rows to a workgroup.  Where no more share a head's keys, the time is that of reading the keys and values once (32 sequences of 2000 to 8192 rows,
-// 8 heads, 668 MB: 139 us, 4.8 TB/s).  Each of the four waves walks 32 of a block's 128 keys by itself, with the next step's 16 KB on its way into registers while it works from its own 16 KB of LDS; no wave
+// 8 heads, 668 MB: 142 us, 4.7 TB/s).  Each of the four waves walks 32 of a block's 128 keys by itself, with the next step's 16 KB on its way into registers while it works from its own 16 KB of LDS; no wave
 // waits for another until the end, when their results are joined through LDS.
 template <typename T, int D> constexpr uint32_t tree_wave_bytes() {
     constexpr uint32_t stage = 2 * KeyTile<T, D>::BYTES, join = 32 * (D + 4) * 4;
@@ -766,7 +766,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
 
 // ---- parts joined --------------------------------------------------------------------------------------------------------
 // One wave per query row: D / 4 lanes hold four output values each, and as many such groups as there are walk the parts.  (8 x 63 tokens of 32 heads in
-// 3 parts or so each: 10.5 us for 25 MB; a few rows: 3.8 us, the way through two dependent reads.)
+// 3 parts or so each: 11.5 us for 25 MB; a few rows: 4.7 us, the way through two dependent reads.)
 template <typename T, int D>
 __global__ __launch_bounds__(256) void tree_attn_join(const TreeAttnArgs a) {
     constexpr uint32_t VEC = D / 4, GROUPS = 64 / VEC;
