@@ -589,6 +589,100 @@ typedef struct {
 int dep_cache_evict(const depsync_cache_evict_desc* d, void* workspace, size_t workspace_bytes, void* stream);
 int depsync_cache_evict_workspace(const depsync_cache_evict_desc* d, size_t* bytes);
 
+/* ---- a round of drafts over a cache of 8 bits: norm and rotation, attention, verification, append --------
+ *
+ * The loop above with the steps that stand around its attention, and with half the bytes in its cache:
+ *   1. dep_qk_norm_rope    the drafted tokens' queries and keys are normalised for each head and rotated by their positions;
+ *   2. dep_tree_attn8      the drafted tokens attend to the cache and to one another;
+ *   3. dep_verify_drafts   the target's probabilities decide which path of the tree stays, and which token comes next;
+ *   4. dep_cache_append8   the path's keys and values go behind the cached rows.
+ * Conventions are those of the section above (streams, workspaces, capture, strides, lengths in device memory, rows left alone).
+ *
+ * A cache of 8 bits: rows come in blocks of `block` (32, 64 or 128) tokens.  The rows of a sequence's full blocks, the first cached - cached % block,
+ * are 8-bit floating point numbers (e4m3: sign, 4 bits of exponent, 3 of mantissa, no infinities, largest 448) [batch][capacity][kv_heads][head_dim],
+ * each block and head with a scale: k_scale, v_scale [batch][kv_heads][capacity / block], not negative; a row's value is scale times its number.
+ * The rows behind them, cached % block of them, are held in 16 bits until they fill a block: k_tail, v_tail [batch][block][kv_heads][head_dim], the
+ * first cached % block rows.  So every row is rounded to 8 bits once, with its block's own scale, whichever way appends were divided.
+ * capacity is a positive multiple of block.  The strides of the 8-bit arrays are multiples of 16, bases 16-byte aligned.                            */
+
+/* out as dep_tree_attn's, over the rows of such a cache and the drafted tokens: scores and outputs go by the rows' values, in 32 bits.  In `attn`, k_cache and
+ * v_cache are the 8-bit numbers; max_cached 0 means capacity.  Rows of the last block that is not full and drafted tokens may hold infinities and NaN as
+ * there.  For the product with v weights are two 16-bit numbers each up to 64 query rows to a key and value head, and one (rounded to the element type) beyond; these
+ * carry their block's scale, relative to the largest that the part has met: what falls out of fp16's range then is below 2^-33 of the largest value. */
+typedef struct {
+    depsync_tree_attn_desc attn;
+    int32_t block;
+    const float* k_scale; const float* v_scale;
+    const void* k_tail; const void* v_tail; int64_t tail_batch, tail_token, tail_head;
+} depsync_tree_attn8_desc;
+int dep_tree_attn8(const depsync_tree_attn8_desc* d, void* workspace, size_t workspace_bytes, void* stream);
+/* As depsync_tree_attn_workspace; of `attn` and block only sizes are read.                                                              */
+int depsync_tree_attn8_workspace(const depsync_tree_attn8_desc* d, int n_cu, size_t* bytes);
+
+/* Rows cached[b].. of sequence b become the keys and values of its drafted tokens accepted[b][i], i < n_accepted[b], as for dep_cache_append.  A block that
+ * is full now goes into 8 bits: its scale is the smallest power of two, 2^-126 at least, times which 448 is no less than the largest finite magnitude in it (0 where that
+ * is 0), and its numbers are value / scale to the nearest, ties to even (infinities: +-448, NaN: NaN).  Rows behind the last full block go
+ * into the tails.  Blocks and tail rows that the call does not write are left as they were.                                             */
+typedef struct {
+    int32_t batch, tokens, kv_heads, head_dim, dtype, capacity, block;
+    int32_t n_max;                                      /* as for dep_cache_append                                                 */
+    const void* k_new; const void* v_new; int64_t new_batch, new_token, new_head;
+    void* k_cache; void* v_cache; int64_t cache_batch, cache_token, cache_head;
+    float* k_scale; float* v_scale;
+    void* k_tail; void* v_tail; int64_t tail_batch, tail_token, tail_head;
+    const int32_t* cached;  int32_t* cached_out;        /* [batch]; not the same array                                             */
+    const int32_t* accepted; const int32_t* n_accepted; /* as for dep_cache_append                                                 */
+    int32_t* n_out;                                     /* as for dep_cache_append; may be NULL                                    */
+} depsync_cache_append8_desc;
+int dep_cache_append8(const depsync_cache_append8_desc* d, void* stream);
+
+/* q_out, k_out = the rotated norms of q and k: for every row x of head_dim numbers
+ *   y = x / sqrt(mean(x^2) + eps) * gain          (norm = 0: y = x * gain)
+ * and of y the first rotary_dim numbers in pairs (a, b) -> (a cos - b sin, b cos + a sin), pair i by the angle position * freq[i]: numbers i and
+ * i + rotary_dim / 2 (interleaved = 0), or 2 i and 2 i + 1.  The position of drafted token t is start[b] + depth[t].  All in 32 bits, rounded once; angles
+ * are reduced to a turn in 64-bit whole numbers, so they are as good at position 2^31 as at 1.                                           */
+typedef struct {
+    int32_t batch, tokens, heads, kv_heads, head_dim, dtype;
+    int32_t rotary_dim;                                 /* multiple of 16 up to head_dim; 0: no rotation, freq is not read            */
+    int32_t interleaved, norm;                          /* 0 or 1                                                                  */
+    float eps;                                          /* finite, not negative                                                    */
+    const void* q;     int64_t q_batch, q_token, q_head;
+    const void* k;     int64_t k_batch, k_token, k_head;
+    void* q_out;       int64_t q_out_batch, q_out_token, q_out_head;   /* q and its strides: in place                              */
+    void* k_out;       int64_t k_out_batch, k_out_token, k_out_head;
+    const float* q_gain; const float* k_gain;           /* [head_dim], 16-byte aligned; NULL: ones                                    */
+    const uint64_t* freq;                               /* [rotary_dim / 2] turns per position as fractions: turns * 2^64, modulo 2^64; 16-byte aligned */
+    const int32_t* start;                               /* [batch]; NULL: 0                                                         */
+    const int32_t* depth; int64_t depth_batch;          /* [batch][tokens], depth_batch numbers from one sequence to the next (0: the same for all); NULL: t */
+    const int32_t* drafted;                             /* as for dep_tree_attn: rows of other tokens are left alone; may be NULL           */
+} depsync_qk_norm_rope_desc;
+int dep_qk_norm_rope(const depsync_qk_norm_rope_desc* d, void* stream);
+
+/* Which drafted tokens stay.  Token 0 of a sequence is known (the last one drawn) and always stays; the others hang in a tree: parents[b][t] < t (NULL: t - 1).
+ * p[b][t] are the target's probabilities for what follows token t, q[b][t] those by which the draft drew t's children, independently of one another; without q
+ * the children were not drawn at all (the draft's most likely tokens, say).  From n = 0 on, with w = p[n], R = 1, the children c of the last
+ * token n that stays are looked at in ascending order, x being ids[c]:
+ *   with q:     c stays if u[c] q[n][x] R < w[x]; if not, w becomes max(w - R q[n], 0) and R the sum of w;
+ *   without q:  c stays if u[c] R < w[x]; if not, R becomes max(R - w[x], 0) and w[x] 0.
+ * Where one stays it is n and w and R start anew; where none does, next[b] is the lowest v at which the sum of w up to v exceeds u[0] times the whole
+ * (where nothing is left: of p[n] likewise; where that is nothing either: -1).  With u from [0, 1) at random tokens that stay and the next one follow the target's
+ * distribution.  Sums, products and comparisons have 64 bits.  Probabilities that are negative or not finite count as 0, u below 0 or NaN as 0 and above 1 as 1; a token whose
+ * id is not in 0..vocab-1 never stays.  accepted[b] receives the tokens that stay, 0 first, and n_accepted[b] their number (entries behind it are left
+ * alone): what the appends take.  A sequence with drafted[b] = 0 gets n_accepted 0, and its other outputs are left alone.                 */
+typedef struct {
+    int32_t batch, tokens, vocab;                       /* tokens: 1..65536, vocab: 1..2^24                                        */
+    const float* p;    int64_t p_batch, p_token;        /* [batch][tokens][vocab], strides in numbers (those of dimensions of size 1 are not read) */
+    const float* q;    int64_t q_batch, q_token;        /* likewise, or NULL                                                       */
+    const int32_t* ids;                                 /* [batch][tokens]                                                         */
+    const int32_t* parents; int64_t parents_batch;      /* [batch][tokens], parents_batch numbers from one sequence to the next (0: one tree for all)  */
+    const int32_t* drafted;                             /* [batch], clamped to 0..tokens; NULL: all                                 */
+    const float* u;                                     /* [batch][tokens]                                                         */
+    int32_t* accepted;                                  /* [batch][tokens]                                                         */
+    int32_t* n_accepted; int32_t* next;                 /* [batch]                                                                 */
+} depsync_verify_drafts_desc;
+int dep_verify_drafts(const depsync_verify_drafts_desc* d, void* workspace, size_t workspace_bytes, void* stream);
+int depsync_verify_drafts_workspace(const depsync_verify_drafts_desc* d, size_t* bytes);
+
 /* ---- host mirrors of the device index arithmetic (Fig. 4b; Section II-A) -------------- */
 
 /* Linear position of tile (x,y) in row-major order: y*grid_x + x.                         */

@@ -42,6 +42,7 @@ EXPORTS = [
     "depsync_conv_chain_n_policy", "depsync_gemm_chain_launch_form", "depsync_conv_chain_n_launch_form",
     "dep_tree_attn", "depsync_tree_attn_workspace", "dep_cache_append", "dep_cache_weights", "dep_cache_evict",
     "depsync_cache_evict_workspace",
+    "dep_qk_norm_rope", "dep_tree_attn8", "depsync_tree_attn8_workspace", "dep_cache_append8", "dep_verify_drafts", "depsync_verify_drafts_workspace",
 ]
 
 
@@ -157,6 +158,30 @@ class CacheEvictDesc(ctypes.Structure):
                        k_out="p", v_out="p", out_batch="l", out_token="l", out_head="l", weights_out="p", pos_out="p")
 
 
+class TreeAttn8Desc(ctypes.Structure):
+    _fields_ = [("attn", TreeAttnDesc)] + _fields(block="i", k_scale="p", v_scale="p", k_tail="p", v_tail="p", tail_batch="l", tail_token="l", tail_head="l")
+
+
+class CacheAppend8Desc(ctypes.Structure):
+    _fields_ = _fields(batch="i", tokens="i", kv_heads="i", head_dim="i", dtype="i", capacity="i", block="i", n_max="i",
+                       k_new="p", v_new="p", new_batch="l", new_token="l", new_head="l",
+                       k_cache="p", v_cache="p", cache_batch="l", cache_token="l", cache_head="l", k_scale="p", v_scale="p",
+                       k_tail="p", v_tail="p", tail_batch="l", tail_token="l", tail_head="l",
+                       cached="p", cached_out="p", accepted="p", n_accepted="p", n_out="p")
+
+
+class QkNormRopeDesc(ctypes.Structure):
+    _fields_ = _fields(batch="i", tokens="i", heads="i", kv_heads="i", head_dim="i", dtype="i", rotary_dim="i", interleaved="i", norm="i", eps="f",
+                       q="p", q_batch="l", q_token="l", q_head="l", k="p", k_batch="l", k_token="l", k_head="l",
+                       q_out="p", q_out_batch="l", q_out_token="l", q_out_head="l", k_out="p", k_out_batch="l", k_out_token="l", k_out_head="l",
+                       q_gain="p", k_gain="p", freq="p", start="p", depth="p", depth_batch="l", drafted="p")
+
+
+class VerifyDraftsDesc(ctypes.Structure):
+    _fields_ = _fields(batch="i", tokens="i", vocab="i", p="p", p_batch="l", p_token="l", q="p", q_batch="l", q_token="l",
+                       ids="p", parents="p", parents_batch="l", drafted="p", u="p", accepted="p", n_accepted="p", next="p")
+
+
 _LIB = None
 
 
@@ -210,6 +235,12 @@ def _lib() -> ctypes.CDLL:
         L.dep_cache_weights.argtypes = [vp, vp]
         L.dep_cache_evict.argtypes = [vp, vp, ctypes.c_size_t, vp]
         L.depsync_cache_evict_workspace.argtypes = [vp, szp]
+        L.dep_qk_norm_rope.argtypes = [vp, vp]
+        L.dep_tree_attn8.argtypes = [vp, vp, ctypes.c_size_t, vp]
+        L.depsync_tree_attn8_workspace.argtypes = [vp, i32, szp]
+        L.dep_cache_append8.argtypes = [vp, vp]
+        L.dep_verify_drafts.argtypes = [vp, vp, ctypes.c_size_t, vp]
+        L.depsync_verify_drafts_workspace.argtypes = [vp, szp]
         L.depsync_row_major.argtypes = [i32] * 4
         L.depsync_policy_sem.argtypes = [i32] * 6
         L.depsync_policy_value.argtypes = [i32] * 4
@@ -644,7 +675,7 @@ def _t4(t, name: str, dtype, device: int, shape=None):
     if t.get_device() != device or device < 0 or len(s) != 4 or s[3] != 1:
         raise ValueError(f"{name} must be a 4-D tensor with contiguous rows on the device of the others")
     if t.dtype is not dtype:
-        raise TypeError("all 16-bit tensors of a call must share one element type")
+        raise TypeError(f"{name}: {t.dtype} where {dtype} is needed (all 16-bit tensors of a call share one element type)")
     if shape is not None and t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)} where {tuple(shape)} is needed")
     return t.data_ptr(), s[0], s[1], s[2]
@@ -725,8 +756,8 @@ def tree_mask(parents):
     return torch.tensor(rows, dtype=torch.int64).reshape(*p.shape, -1)
 
 
-def _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached):
-    """(descriptor, device) of a call."""
+def _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached, held=None):
+    """(descriptor, device) of a call.  held: the type of the cache's numbers where it is not the others'."""
     torch = _torch()
     device, dtype = q.get_device(), q.dtype
     code = _dtype_code(q)
@@ -740,7 +771,7 @@ def _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, d
         if v_cache is None or cached is None or k_cache.dim() != 4:
             raise ValueError("a cache is k_cache and v_cache [batch, capacity, kv_heads, head_dim], and cached")
         cap = k_cache.shape[1]
-        cache = _pair(k_cache, v_cache, "cache", dtype, device, (B, cap, Hk, D))
+        cache = _pair(k_cache, v_cache, "cache", held or dtype, device, (B, cap, Hk, D))
         lengths = _arr(cached, "cached", torch.int32, device, (B,))
     tree_ptr, tree_batch = 0, 0
     if tree is not None:
@@ -888,6 +919,182 @@ def cache_evict_workspace(k_cache, v_cache, weights, pos, cached, cached_out, bu
     """Bytes of workspace that dep_cache_evict with these arguments needs."""
     d, device = _cache_evict_desc(k_cache, v_cache, weights, pos, cached, cached_out, budget, recent, max_cached, k_out, v_out, weights_out, pos_out)
     return _bytes("depsync_cache_evict_workspace", device, _lib().depsync_cache_evict_workspace, d)
+
+
+# ---- a round of drafts over a cache of 8 bits ------------------------------------------------
+
+_P_TREE8 = struct.Struct("i4x 4P3q")
+_P_APPEND8 = struct.Struct("8i 2P3q 2P3q 2P 2P3q 5P")
+_P_NORM = struct.Struct("9if P3q P3q P3q P3q 5PqP")
+_P_VERIFY = struct.Struct("3i4x P2q P2q 2PqP P 3P")
+
+
+def _scales(k_scale, v_scale, device: int, shape):
+    f32 = _torch().float32
+    return _arr(k_scale, "k_scale", f32, device, shape), _arr(v_scale, "v_scale", f32, device, shape)
+
+
+def _held8(k_cache, k_scale, v_scale, k_tail, v_tail, dtype, device: int):
+    """(rows of a block, pointers of the scales, pointers and strides of the rows in 16 bits) of a cache of 8 bits."""
+    if k_cache.dim() != 4 or k_tail.dim() != 4:
+        raise ValueError("k_cache must be [batch, capacity, kv_heads, head_dim] and k_tail [batch, block, kv_heads, head_dim]")
+    B, cap, Hk, D = k_cache.shape
+    block = k_tail.shape[1]
+    if block not in (32, 64, 128) or cap < block or cap % block:
+        raise ValueError(f"blocks of {block} rows in a capacity of {cap}: blocks have 32, 64 or 128, and the capacity is a multiple")
+    return block, *_scales(k_scale, v_scale, device, (B, Hk, cap // block)), *_pair(k_tail, v_tail, "tail", dtype, device, (B, block, Hk, D))
+
+
+def _tree_attn8_desc(q, k_new, v_new, k_cache, v_cache, k_scale, v_scale, k_tail, v_tail, cached, out, lse, tree, drafted, scale, max_cached):
+    """(descriptor, device) of a call."""
+    if k_cache is None:
+        raise ValueError("k_cache is missing: without a cache dep_tree_attn does it")
+    d, device = _tree_attn_desc(q, k_new, v_new, k_cache, v_cache, cached, out, lse, tree, drafted, scale, max_cached, _torch().float8_e4m3fn)
+    return d + _P_TREE8.pack(*_held8(k_cache, k_scale, v_scale, k_tail, v_tail, q.dtype, device)), device
+
+
+@functools.lru_cache(maxsize=4096)
+def _tree_attn8_bytes(device: int, sizes: bytes, block: bytes) -> int:
+    """The workspace of dep_tree_attn8, by the descriptor's sizes: all that it depends on beside the device."""
+    d = sizes + bytes(_P_TREE.size - len(sizes)) + block + bytes(_P_TREE8.size - len(block))
+    return _bytes("dep_tree_attn8", device, _lib().depsync_tree_attn8_workspace, d, 0)
+
+
+def dep_tree_attn8(q, k_new, v_new, k_cache, v_cache, k_scale, v_scale, k_tail, v_tail, cached, out, lse=None, tree=None, drafted=None,
+                   scale: Optional[float] = None, max_cached: Optional[int] = None, workspace=None, stream=None) -> None:
+    """Enqueue what dep_tree_attn does over a cache of 8 bits: the rows of full blocks in k_cache, v_cache [B, capacity, Hk, D] (float8_e4m3fn) with
+    k_scale, v_scale [B, Hk, capacity / block] (float32), the rows behind them, cached % block of them, in k_tail, v_tail [B, block, Hk, D] (q's type)."""
+    d, device = _tree_attn8_desc(q, k_new, v_new, k_cache, v_cache, k_scale, v_scale, k_tail, v_tail, cached, out, lse, tree, drafted, scale, max_cached)
+    stream = _current_or(stream, device)
+    need = 0 if workspace is not None else _tree_attn8_bytes(device, d[:32], d[_P_TREE.size:_P_TREE.size + 4])
+    keep, ptr, size = _workspace(need, workspace, device, stream)
+    _call(device, "dep_tree_attn8", _lib().dep_tree_attn8, d, ptr, size, stream)
+
+
+def tree_attn8_workspace(q, k_new, v_new, k_cache, v_cache, k_scale, v_scale, k_tail, v_tail, cached, out, lse=None, tree=None, drafted=None,
+                         scale: Optional[float] = None, max_cached: Optional[int] = None, n_cu: int = 0) -> int:
+    """Bytes of workspace that dep_tree_attn8 with these arguments needs."""
+    d, device = _tree_attn8_desc(q, k_new, v_new, k_cache, v_cache, k_scale, v_scale, k_tail, v_tail, cached, out, lse, tree, drafted, scale, max_cached)
+    return _bytes("depsync_tree_attn8_workspace", device, _lib().depsync_tree_attn8_workspace, d, n_cu)
+
+
+def dep_cache_append8(k_new, v_new, k_cache, v_cache, k_scale, v_scale, k_tail, v_tail, cached, cached_out, accepted=None, n_accepted=None,
+                      n_out=None, stream=None) -> None:
+    """Enqueue: drafted tokens accepted[b, :n_accepted[b]] (int32; None: the first ones) become rows cached[b].. of a cache of 8 bits (see dep_tree_attn8):
+    blocks that are full now go into 8 bits with a scale of their own, the rows behind them into the tails.  cached_out = cached + n; n_out[b] (int32)
+    receives n, which is less than n_accepted[b] where the capacity was reached."""
+    torch = _torch()
+    device, dtype = k_new.get_device(), k_new.dtype
+    code = _dtype_code(k_new)
+    if k_new.dim() != 4:
+        raise ValueError("k_new must be [batch, tokens, kv_heads, head_dim]")
+    B, T, Hk, D = k_new.shape
+    block, ks, vs, *tail = _held8(k_cache, k_scale, v_scale, k_tail, v_tail, dtype, device)
+    cap = k_cache.shape[1]
+    i32 = torch.int32
+    n_max, acc, n_acc = _accepted(B, T, accepted, n_accepted, device)
+    d = _P_APPEND8.pack(B, T, Hk, D, code, cap, block, n_max, *_pair(k_new, v_new, "new", dtype, device, (B, T, Hk, D)),
+                        *_pair(k_cache, v_cache, "cache", torch.float8_e4m3fn, device, (B, cap, Hk, D)), ks, vs, *tail, _arr(cached, "cached", i32, device, (B,)),
+                        _arr(cached_out, "cached_out", i32, device, (B,)), acc, n_acc, _arr(n_out, "n_out", i32, device, (B,)))
+    _call(device, "dep_cache_append8", _lib().dep_cache_append8, d, _current_or(stream, device))
+
+
+def rope_frequencies(angles, device=None):
+    """The `freq` of dep_qk_norm_rope for rotations by angles[i] radians a position (a float64 tensor or list, in host memory or not): int64 [len], turns as
+    fractions of 2^64.  On `device`, by default that of the angles."""
+    from fractions import Fraction
+    torch = _torch()
+    t = torch.as_tensor(angles, dtype=torch.float64)
+    if t.dim() != 1 or not bool(t.isfinite().all()):
+        raise ValueError("angles must be one finite number for each pair")
+    turn = Fraction(2 * 314159265358979323846264338327950288419716939937510, 10 ** 50)   # 2 pi to 50 places
+    words = [round(Fraction(x) / turn * 2 ** 64) % 2 ** 64 for x in t.tolist()]
+    return torch.tensor([w - 2 ** 64 if w >> 63 else w for w in words], dtype=torch.int64, device=t.device if device is None else device)
+
+
+def dep_qk_norm_rope(q, k, freq=None, q_gain=None, k_gain=None, q_out=None, k_out=None, start=None, depth=None, drafted=None, eps: float = 1e-6,
+                     norm: bool = True, interleaved: bool = False, stream=None) -> None:
+    """Enqueue: every row x of q [B, T, Hq, D] and k [B, T, Hk, D] becomes x / sqrt(mean(x^2) + eps) * gain (norm False: x * gain), and the first 2 len(freq)
+    numbers of that are rotated in pairs, pair i by position * freq[i] (see rope_frequencies; None: no rotation): i and i + len(freq), or, interleaved, 2 i and 2 i + 1.
+
+    q_gain, k_gain [D] (float32; None: ones).  q_out, k_out: None is in place.  The position of token t is start[b] + depth[b, t] (int32 [B] and [B, T] or [T]; None: 0, and t).
+    drafted[b] (int32): the tokens that sequence b has; the others' rows are left alone.  stream: as for dep_tree_attn."""
+    torch = _torch()
+    device, dtype = q.get_device(), q.dtype
+    code = _dtype_code(q)
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q and k must be [batch, tokens, heads, head_dim]")
+    B, T, Hq, D = q.shape
+    Hk = k.shape[2]
+    qp, kp = _t4(q, "q", dtype, device), _t4(k, "k", dtype, device, (B, T, Hk, D))
+    R, fp = 0, 0
+    if freq is not None:
+        if freq.dim() != 1:
+            raise ValueError("freq must be one number for each pair")
+        R, fp = 2 * freq.shape[0], _arr(freq, "freq", torch.int64, device, freq.shape)
+    depth_ptr, depth_batch = 0, 0
+    if depth is not None:
+        depth_batch = T if depth.dim() == 2 else 0
+        depth_ptr = _arr(depth, "depth", torch.int32, device, (B, T) if depth_batch else (T,))
+    f32, i32 = torch.float32, torch.int32
+    d = _P_NORM.pack(B, T, Hq, Hk, D, code, R, bool(interleaved), bool(norm), eps, *qp, *kp,
+                     *(qp if q_out is None else _t4(q_out, "q_out", dtype, device, (B, T, Hq, D))),
+                     *(kp if k_out is None else _t4(k_out, "k_out", dtype, device, (B, T, Hk, D))),
+                     _arr(q_gain, "q_gain", f32, device, (D,)), _arr(k_gain, "k_gain", f32, device, (D,)), fp,
+                     _arr(start, "start", i32, device, (B,)), depth_ptr, depth_batch, _arr(drafted, "drafted", i32, device, (B,)))
+    _call(device, "dep_qk_norm_rope", _lib().dep_qk_norm_rope, d, _current_or(stream, device))
+
+
+def _probabilities(t, name: str, device: int, shape):
+    """Pointer and strides of a [batch, tokens, vocab] tensor of 32-bit numbers with contiguous rows; None -> zeros."""
+    if t is None:
+        return 0, 0, 0
+    if t.get_device() != device or t.dtype is not _torch().float32 or t.shape != shape or (t.stride(2) != 1 and shape[2] > 1):
+        raise ValueError(f"{name} must be a float32 tensor of shape {tuple(shape)} with contiguous rows on the device of the others")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _verify_desc(p, ids, u, accepted, n_accepted, next, q, parents, drafted):
+    """(descriptor, device) of a call."""
+    torch = _torch()
+    device = p.get_device()
+    if p.dim() != 3 or device < 0:
+        raise ValueError("p must be a [batch, tokens, vocab] tensor on a GPU")
+    B, T, V = p.shape
+    i32 = torch.int32
+    parents_ptr, parents_batch = 0, 0
+    if parents is not None:
+        parents_batch = T if parents.dim() == 2 else 0
+        parents_ptr = _arr(parents, "parents", i32, device, (B, T) if parents_batch else (T,))
+    return _P_VERIFY.pack(B, T, V, *_probabilities(p, "p", device, p.shape), *_probabilities(q, "q", device, p.shape), _arr(ids, "ids", i32, device, (B, T)),
+                          parents_ptr, parents_batch, _arr(drafted, "drafted", i32, device, (B,)), _arr(u, "u", torch.float32, device, (B, T)),
+                          _arr(accepted, "accepted", i32, device, (B, T)), _arr(n_accepted, "n_accepted", i32, device, (B,)),
+                          _arr(next, "next", i32, device, (B,))), device
+
+
+def dep_verify_drafts(p, ids, u, accepted, n_accepted, next, q=None, parents=None, drafted=None, workspace=None, stream=None) -> None:
+    """Enqueue: which drafted tokens stay, and the token that follows them.  Token 0 of a sequence is known and stays; p [B, T, V] (float32) are the target's probabilities
+    behind each token, q (same shape) those by which the draft drew each token's children (None: they were not drawn), ids [B, T] (int32) the tokens, parents [B, T] or [T]
+    (int32; None: a chain) the tree, u [B, T] (float32) random numbers from [0, 1): u[:, 0] draws the next token, the others decide about theirs.
+
+    accepted [B, T], n_accepted [B] and next [B] (int32) receive the tokens that stay (0 first), their number, and the next token: what the appends take.
+    drafted[b] (int32): the tokens that sequence b has (None: all; 0: nothing to verify).  stream: as for dep_tree_attn."""
+    d, device = _verify_desc(p, ids, u, accepted, n_accepted, next, q, parents, drafted)
+    stream = _current_or(stream, device)
+    need = 0 if workspace is not None else _verify_bytes(d)
+    keep, ptr, size = _workspace(need, workspace, device, stream)
+    _call(device, "dep_verify_drafts", _lib().dep_verify_drafts, d, ptr, size, stream)
+
+
+def _verify_bytes(d: bytes) -> int:
+    need = ctypes.c_size_t(0)
+    _check(_lib().depsync_verify_drafts_workspace(d, ctypes.byref(need)), "dep_verify_drafts")
+    return need.value
+
+
+def verify_drafts_workspace(p, ids, u, accepted, n_accepted, next, q=None, parents=None, drafted=None) -> int:
+    """Bytes of workspace that dep_verify_drafts with these arguments needs."""
+    return _verify_bytes(_verify_desc(p, ids, u, accepted, n_accepted, next, q, parents, drafted)[0])
 
 
 # ---- host mirrors -------------------------------------------------------------------------

@@ -27,6 +27,11 @@ SOURCES = [
     "kern_cache.hip",
     "kern_bf16_tree.hip",
     "kern_f16_tree.hip",
+    "kern_bf16_tree8.hip",
+    "kern_f16_tree8.hip",
+    "kern_append8.hip",
+    "kern_norm.hip",
+    "kern_verify.hip",
 ]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -24,10 +24,10 @@ int64_t cdiv64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Strides of [batch][token][head][head_dim].  Those of dimensions of size one are not read: kernels get what a dense row has.
 // Where rows are written, or read by the bounds of a run of rows, they must not overlap.
-bool strides(Strides& s, int64_t batch, int64_t token, int64_t head, int64_t n_batch, int64_t n_token, int64_t n_head, int dim, bool written, bool run) {
+bool strides(Strides& s, int64_t batch, int64_t token, int64_t head, int64_t n_batch, int64_t n_token, int64_t n_head, int dim, bool written, bool run, int multiple = 8) {
     s = {n_batch > 1 ? batch : dim, n_token > 1 ? token : dim, n_head > 1 ? head : dim};
     for (int64_t x : {s.batch, s.token, s.head})
-        if (x < 0 || x % 8 != 0 || x > (int64_t)1 << 40 || (written && x < dim)) return false;
+        if (x < 0 || x % multiple != 0 || x > (int64_t)1 << 40 || (written && x < dim)) return false;
     return !run || (s.token >= dim && s.token <= MAX_TOKEN_STRIDE);
 }
 
@@ -60,6 +60,26 @@ int tree_check(const depsync_tree_attn_desc* d) {
     return d->max_cached < 0 ? DEPSYNC_EINVAL : DEPSYNC_OK;
 }
 
+// Checks the operands and fills in what does not depend on the division of the work.  multiple: of the cache's strides.
+int tree_operands(const depsync_tree_attn_desc* d, TreeAttnArgs& a, int multiple) {
+    const int D = d->head_dim;
+    if (!operand(d->q) || !operand(d->k_new) || !operand(d->v_new) || !operand(d->out) || !optional(d->drafted) || !optional(d->lse) ||
+        (d->capacity > 0 && (!operand(d->k_cache) || !operand(d->v_cache) || !array(d->cached))) || !aligned(d->tree, 8))
+        return DEPSYNC_EINVAL;
+    if (!strides(a.q_s, d->q_batch, d->q_token, d->q_head, d->batch, d->tokens, d->heads, D, false, false) ||
+        !strides(a.new_s, d->new_batch, d->new_token, d->new_head, d->batch, d->tokens, d->kv_heads, D, false, true) ||
+        !strides(a.out_s, d->out_batch, d->out_token, d->out_head, d->batch, d->tokens, d->heads, D, true, false))
+        return DEPSYNC_EINVAL;
+    if (d->capacity > 0 && !strides(a.cache_s, d->cache_batch, d->cache_token, d->cache_head, d->batch, d->capacity, d->kv_heads, D, false, true, multiple))
+        return DEPSYNC_EINVAL;
+    if (d->tree && d->tree_batch != 0 && d->tree_batch < (int64_t)d->tokens * cdiv64(d->tokens, 64)) return DEPSYNC_EINVAL;
+    if (!base2_scale(d->scale, D, a.scale)) return DEPSYNC_EINVAL;
+    a.q = d->q; a.k_new = d->k_new; a.v_new = d->v_new; a.k_cache = d->k_cache; a.v_cache = d->v_cache;
+    a.cached = d->cached; a.drafted = d->drafted; a.tree = d->tree; a.tree_batch = d->tree_batch;
+    a.out = d->out; a.lse = d->lse;
+    return DEPSYNC_OK;
+}
+
 // How the key axis of dep_tree_attn is cut: few (sequence, head) pairs and row blocks leave CUs idle unless it is, but parts leave results of
 // 4 (head_dim + 2) bytes a row in memory, which a second kernel reads.  The model, in microseconds, fitted to times of 27 shapes under
 // up to 28 cuts each (1 to 2048 rows, caches of 0 to 120000; its choice is 4 % behind the best cut in the mean, in the worst case 21 %):
@@ -76,7 +96,7 @@ double tree_cost(int64_t base, int64_t part, int64_t blocks, int64_t pairs, int6
     return (double)cdiv64(groups, slots) * (3.0 + part * std::cbrt(step * step * step + hbm * hbm * hbm)) + join;   // (between the larger and the sum)
 }
 
-int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t& bytes) {
+int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t& bytes, int held = 0) {   // held: rows of a block of a cache of 8 bits
     if (n_cu <= 0)
         if (int rc = cu_count(n_cu); rc != DEPSYNC_OK) return rc;
     a.batch = d->batch; a.tokens = d->tokens; a.heads = d->heads; a.kv_heads = d->kv_heads; a.capacity = d->capacity;
@@ -90,10 +110,11 @@ int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t
     // head of 64 over 120000, 73 and 62.  Between 100 and 270 MB it depends on how many sequences share them: 8 x 48 over 8000 67 and 64, but 16 x 64
     // over 4000 64 and 68, 4 x 52 over 8000 40 and 42, 16 x 40 over 2000 36 and 49.
     const int64_t cache_bytes = (int64_t)d->batch * d->kv_heads * rows_hint(d->max_cached, d->capacity) * d->head_dim * 4;
-    a.few = rows <= (cache_bytes < 100000000 ? 64 : 32);
+    a.few = held || rows <= (cache_bytes < 100000000 ? 64 : 32);
     const int64_t keys = a.few ? TREE_FEW_KEYS : TREE_MANY_KEYS, row_blocks = cdiv64(rows, a.few ? TREE_FEW_ROWS : TREE_MANY_ROWS);
     const int64_t pairs = (int64_t)d->batch * d->kv_heads, base = pairs * row_blocks;
-    const int64_t blocks = cdiv64(rows_hint(d->max_cached, d->capacity), keys) + cdiv64(d->tokens, keys);
+    const int64_t wide = d->tokens + (held ? held - 1 : 0);        // rows of 16 bits behind those of full blocks
+    const int64_t blocks = cdiv64(rows_hint(d->max_cached, d->capacity), keys) + cdiv64(wide, keys);
     int64_t part = blocks;
     double best = tree_cost(base, part, blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few);
     for (int64_t rounds = 1; rounds <= 4; ++rounds) {             // parts that fill the chip a whole number of times
@@ -107,7 +128,7 @@ int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t
         }
     }
     // (the kernels add up all sequences' blocks in 32 bits)
-    const int64_t parts = d->batch * (cdiv64(d->capacity, keys) + cdiv64(d->tokens, keys)) < 1ll << 32 ? cdiv64(blocks, part) : 1;
+    const int64_t parts = d->batch * (cdiv64(d->capacity, keys) + cdiv64(wide, keys)) < 1ll << 32 ? cdiv64(blocks, part) : 1;
     if (cdiv64(pairs * parts, 8) * 8 * row_blocks > MAX_BLOCKS || cdiv64(pairs * rows, 4) > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;
     a.slots = (uint32_t)(d->batch * parts);
     a.part_slots = (uint32_t)parts;
@@ -128,6 +149,19 @@ int evict_check(const depsync_cache_evict_desc* d) {
     return (int64_t)d->batch * d->kv_heads > MAX_BLOCKS / 4 ? DEPSYNC_ENOTIMPL : DEPSYNC_OK;   // (1024 threads each)
 }
 
+bool cache8_block(int block, int capacity) { return (block == 32 || block == 64 || block == 128) && capacity >= block && capacity % block == 0; }
+
+int verify_check(const depsync_verify_drafts_desc* d) {
+    return d && d->batch >= 1 && d->batch <= 1 << 20 && d->tokens >= 1 && d->tokens <= 65536 && d->vocab >= 1 && d->vocab <= 1 << 24 ? DEPSYNC_OK : DEPSYNC_EINVAL;
+}
+
+// Strides of [batch][tokens][vocab] numbers, those of dimensions of size one not read.
+bool rows(int64_t& batch, int64_t& token, int64_t given_batch, int64_t given_token, const depsync_verify_drafts_desc* d) {
+    batch = d->batch > 1 ? given_batch : 0;
+    token = d->tokens > 1 ? given_token : 0;
+    return batch >= 0 && token >= 0 && batch <= (int64_t)1 << 40 && token <= (int64_t)1 << 40;
+}
+
 }  // namespace
 
 extern "C" {
@@ -144,22 +178,10 @@ int dep_tree_attn(const depsync_tree_attn_desc* d, void* workspace, size_t works
     TreeAttnArgs a = {};
     size_t need = 0;
     const int D = d->head_dim;
-    if (!operand(d->q) || !operand(d->k_new) || !operand(d->v_new) || !operand(d->out) || !optional(d->drafted) || !optional(d->lse) ||
-        (d->capacity > 0 && (!operand(d->k_cache) || !operand(d->v_cache) || !array(d->cached))) || !aligned(d->tree, 8))
-        return DEPSYNC_EINVAL;
-    if (!strides(a.q_s, d->q_batch, d->q_token, d->q_head, d->batch, d->tokens, d->heads, D, false, false) ||
-        !strides(a.new_s, d->new_batch, d->new_token, d->new_head, d->batch, d->tokens, d->kv_heads, D, false, true) ||
-        !strides(a.out_s, d->out_batch, d->out_token, d->out_head, d->batch, d->tokens, d->heads, D, true, false))
-        return DEPSYNC_EINVAL;
-    if (d->capacity > 0 && !strides(a.cache_s, d->cache_batch, d->cache_token, d->cache_head, d->batch, d->capacity, d->kv_heads, D, false, true))
-        return DEPSYNC_EINVAL;
-    if (d->tree && d->tree_batch != 0 && d->tree_batch < (int64_t)d->tokens * cdiv64(d->tokens, 64)) return DEPSYNC_EINVAL;
-    if (!base2_scale(d->scale, D, a.scale)) return DEPSYNC_EINVAL;
+    if (int rc = tree_operands(d, a, 8); rc != DEPSYNC_OK) return rc;
     if (int rc = tree_plan(d, 0, a, need); rc != DEPSYNC_OK) return rc;
     if (need > 0 && (!operand(workspace) || workspace_bytes < need)) return DEPSYNC_EINVAL;
-    a.q = d->q; a.k_new = d->k_new; a.v_new = d->v_new; a.k_cache = d->k_cache; a.v_cache = d->v_cache;
-    a.cached = d->cached; a.drafted = d->drafted; a.tree = d->tree; a.tree_batch = d->tree_batch;
-    a.out = d->out; a.lse = d->lse; a.parts = static_cast<float*>(workspace);
+    a.parts = static_cast<float*>(workspace);
     const hipError_t e = launch_tree_attn(a, d->dtype, D, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);
 }
@@ -259,6 +281,113 @@ int dep_cache_evict(const depsync_cache_evict_desc* d, void* workspace, size_t w
     a.max_moves = (uint32_t)evict_moves(d);
     a.in_place = other ? 0 : 1;
     const hipError_t e = launch_cache_evict(a, D, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);
+}
+
+int depsync_tree_attn8_workspace(const depsync_tree_attn8_desc* d, int n_cu, size_t* bytes) {
+    if (!bytes || !d) return DEPSYNC_EINVAL;
+    if (int rc = tree_check(&d->attn); rc != DEPSYNC_OK) return rc;
+    if (!cache8_block(d->block, d->attn.capacity)) return DEPSYNC_EINVAL;
+    TreeAttn8Args a = {};
+    return tree_plan(&d->attn, n_cu, a, *bytes, d->block);
+}
+
+int dep_tree_attn8(const depsync_tree_attn8_desc* d8, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!d8) return DEPSYNC_EINVAL;
+    const depsync_tree_attn_desc* const d = &d8->attn;
+    if (int rc = tree_check(d); rc != DEPSYNC_OK) return rc;
+    if (!cache8_block(d8->block, d->capacity)) return DEPSYNC_EINVAL;
+    TreeAttn8Args a = {};
+    size_t need = 0;
+    const int D = d->head_dim;
+    if (!operand(d8->k_tail) || !operand(d8->v_tail) || !array(d8->k_scale) || !array(d8->v_scale)) return DEPSYNC_EINVAL;
+    if (int rc = tree_operands(d, a, 16); rc != DEPSYNC_OK) return rc;
+    if (!strides(a.tail_s, d8->tail_batch, d8->tail_token, d8->tail_head, d->batch, d8->block, d->kv_heads, D, false, true)) return DEPSYNC_EINVAL;
+    if (int rc = tree_plan(d, 0, a, need, d8->block); rc != DEPSYNC_OK) return rc;
+    if (need > 0 && (!operand(workspace) || workspace_bytes < need)) return DEPSYNC_EINVAL;
+    a.k_scale = d8->k_scale; a.v_scale = d8->v_scale; a.k_tail = d8->k_tail; a.v_tail = d8->v_tail;
+    a.block_log2 = d8->block == 32 ? 5 : d8->block == 64 ? 6 : 7;
+    a.n_blocks = (uint32_t)(d->capacity / d8->block);
+    a.parts = static_cast<float*>(workspace);
+    const hipError_t e = d->dtype == DEPSYNC_BF16 ? launch_tree_attn8_bf16(a, D, static_cast<hipStream_t>(stream)) : launch_tree_attn8_f16(a, D, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);
+}
+
+int dep_cache_append8(const depsync_cache_append8_desc* d, void* stream) {
+    if (!d) return DEPSYNC_EINVAL;
+    if (int rc = common(d->batch, d->tokens, d->kv_heads, d->kv_heads, d->head_dim, d->dtype, d->capacity); rc != DEPSYNC_OK) return rc;
+    CacheAppend8Args a = {};
+    const int D = d->head_dim;
+    if (!cache8_block(d->block, d->capacity) || d->n_max < 1 || d->n_max > 65536 || (!d->accepted && d->n_max > d->tokens)) return DEPSYNC_EINVAL;
+    if (!operand(d->k_new) || !operand(d->v_new) || !operand(d->k_cache) || !operand(d->v_cache) || !operand(d->k_tail) || !operand(d->v_tail) ||
+        !array(d->k_scale) || !array(d->v_scale) || !array(d->cached) || !array(d->cached_out) || d->cached == d->cached_out || !optional(d->accepted) ||
+        !optional(d->n_accepted) || !optional(d->n_out))
+        return DEPSYNC_EINVAL;
+    if (d->n_out && (d->n_out == d->cached || d->n_out == d->cached_out || d->n_out == d->n_accepted)) return DEPSYNC_EINVAL;
+    if (!strides(a.new_s, d->new_batch, d->new_token, d->new_head, d->batch, d->tokens, d->kv_heads, D, false, false) ||
+        !strides(a.cache_s, d->cache_batch, d->cache_token, d->cache_head, d->batch, d->capacity, d->kv_heads, D, true, true, 16) ||
+        !strides(a.tail_s, d->tail_batch, d->tail_token, d->tail_head, d->batch, d->block, d->kv_heads, D, true, true))
+        return DEPSYNC_EINVAL;
+    a.n_blocks = (uint32_t)(d->capacity / d->block);
+    a.most_full = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(a.n_blocks, ((int64_t)d->block - 1 + d->n_max) / d->block));
+    if ((int64_t)d->batch * d->kv_heads * 2 * a.most_full > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;
+    a.k_new = d->k_new; a.v_new = d->v_new; a.k_cache = d->k_cache; a.v_cache = d->v_cache; a.k_tail = d->k_tail; a.v_tail = d->v_tail;
+    a.k_scale = d->k_scale; a.v_scale = d->v_scale;
+    a.cached = d->cached; a.cached_out = d->cached_out; a.accepted = d->accepted; a.n_accepted = d->n_accepted; a.n_out = d->n_out;
+    a.batch = d->batch; a.tokens = d->tokens; a.kv_heads = d->kv_heads; a.capacity = d->capacity; a.n_max = d->n_max;
+    const hipError_t e = launch_cache_append8(a, d->dtype, D, d->block, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);
+}
+
+int dep_qk_norm_rope(const depsync_qk_norm_rope_desc* d, void* stream) {
+    if (!d) return DEPSYNC_EINVAL;
+    if (int rc = common(d->batch, d->tokens, d->heads, d->kv_heads, d->head_dim, d->dtype, 0); rc != DEPSYNC_OK) return rc;
+    QkNormArgs a = {};
+    const int D = d->head_dim, R = d->rotary_dim;
+    if (R < 0 || R > D || R % 16 != 0 || (d->interleaved & ~1) || (d->norm & ~1) || !std::isfinite(d->eps) || d->eps < 0.0f) return DEPSYNC_EINVAL;
+    if (!operand(d->q) || !operand(d->k) || !operand(d->q_out) || !operand(d->k_out) || !aligned(d->q_gain, 16) || !aligned(d->k_gain, 16) ||
+        (R > 0 && !operand(d->freq)) || !optional(d->start) || !optional(d->depth) || !optional(d->drafted))
+        return DEPSYNC_EINVAL;
+    if (!strides(a.q_s, d->q_batch, d->q_token, d->q_head, d->batch, d->tokens, d->heads, D, false, false) ||
+        !strides(a.k_s, d->k_batch, d->k_token, d->k_head, d->batch, d->tokens, d->kv_heads, D, false, false) ||
+        !strides(a.q_out_s, d->q_out_batch, d->q_out_token, d->q_out_head, d->batch, d->tokens, d->heads, D, true, false) ||
+        !strides(a.k_out_s, d->k_out_batch, d->k_out_token, d->k_out_head, d->batch, d->tokens, d->kv_heads, D, true, false))
+        return DEPSYNC_EINVAL;
+    auto same = [](const Strides& x, const Strides& y) { return x.batch == y.batch && x.token == y.token && x.head == y.head; };
+    if ((d->q == d->q_out && !same(a.q_s, a.q_out_s)) || (d->k == d->k_out && !same(a.k_s, a.k_out_s))) return DEPSYNC_EINVAL;
+    if (d->depth && d->depth_batch != 0 && d->depth_batch < d->tokens) return DEPSYNC_EINVAL;
+    a.q = d->q; a.k = d->k; a.q_out = d->q_out; a.k_out = d->k_out; a.q_gain = d->q_gain; a.k_gain = d->k_gain; a.freq = d->freq;
+    a.start = d->start; a.depth = d->depth; a.depth_batch = d->depth_batch; a.drafted = d->drafted;
+    a.batch = d->batch; a.tokens = d->tokens; a.heads = d->heads; a.kv_heads = d->kv_heads; a.rotary_dim = R; a.eps = d->eps;
+    const int64_t tokens = (int64_t)d->batch * d->tokens, at_once = 64 / (D / 16);
+    a.span = 1;
+    a.q_waves = (uint32_t)cdiv64(d->heads, at_once * a.span);
+    a.k_waves = (uint32_t)cdiv64(d->kv_heads, at_once * a.span);
+    if (cdiv64(tokens * (a.q_waves + a.k_waves), 4) > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;
+    const hipError_t e = launch_qk_norm_rope(a, d->dtype, D, d->interleaved != 0, d->norm != 0, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);
+}
+
+int depsync_verify_drafts_workspace(const depsync_verify_drafts_desc* d, size_t* bytes) {
+    if (!bytes) return DEPSYNC_EINVAL;
+    if (int rc = verify_check(d); rc != DEPSYNC_OK) return rc;
+    *bytes = 0;
+    return DEPSYNC_OK;
+}
+
+int dep_verify_drafts(const depsync_verify_drafts_desc* d, void* workspace, size_t workspace_bytes, void* stream) {
+    size_t need = 0;
+    if (int rc = depsync_verify_drafts_workspace(d, &need); rc != DEPSYNC_OK) return rc;
+    VerifyArgs a = {};
+    if (!array(d->p) || !optional(d->q) || !array(d->ids) || !optional(d->parents) || !optional(d->drafted) || !array(d->u) || !array(d->accepted) ||
+        !array(d->n_accepted) || !array(d->next) || d->n_accepted == d->next || (d->parents && d->parents_batch != 0 && d->parents_batch < d->tokens))
+        return DEPSYNC_EINVAL;
+    if (!rows(a.p_batch, a.p_token, d->p_batch, d->p_token, d) || (d->q && !rows(a.q_batch, a.q_token, d->q_batch, d->q_token, d))) return DEPSYNC_EINVAL;
+    if (need > 0 && (!operand(workspace) || workspace_bytes < need)) return DEPSYNC_EINVAL;
+    a.p = d->p; a.q = d->q; a.ids = d->ids; a.parents = d->parents; a.parents_batch = d->parents_batch; a.drafted = d->drafted; a.u = d->u;
+    a.accepted = d->accepted; a.n_accepted = d->n_accepted; a.next = d->next;
+    a.batch = d->batch; a.tokens = d->tokens; a.vocab = d->vocab;
+    const hipError_t e = launch_verify_drafts(a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);
 }
 

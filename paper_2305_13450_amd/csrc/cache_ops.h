@@ -27,6 +27,49 @@ struct TreeAttnArgs {
     float scale;                          // scores to base-2 exponents
 };
 
+// Attention over a cache of 8 bits: k_cache, v_cache and cache_s are those of the 8-bit numbers.
+struct TreeAttn8Args : TreeAttnArgs {
+    const float *k_scale, *v_scale;
+    const void *k_tail, *v_tail;
+    Strides tail_s;
+    uint32_t block_log2, n_blocks;        // rows of a block, blocks of the capacity
+};
+
+struct CacheAppend8Args {
+    const void *k_new, *v_new;
+    void *k_cache, *v_cache, *k_tail, *v_tail;
+    float *k_scale, *v_scale;
+    const int32_t* cached;
+    int32_t* cached_out;
+    const int32_t *accepted, *n_accepted;
+    int32_t* n_out;                       // may be null
+    Strides new_s, cache_s, tail_s;
+    uint32_t batch, tokens, kv_heads, capacity, n_max;
+    uint32_t n_blocks, most_full;         // blocks of the capacity, blocks that one call can fill (1 at least)
+};
+
+struct QkNormArgs {
+    const void *q, *k;
+    void *q_out, *k_out;
+    const float *q_gain, *k_gain;         // may be null
+    const uint64_t* freq;
+    const int32_t *start, *depth, *drafted;   // may be null
+    Strides q_s, k_s, q_out_s, k_out_s;
+    int64_t depth_batch;
+    uint32_t batch, tokens, heads, kv_heads, rotary_dim;
+    uint32_t span, q_waves, k_waves;      // groups of heads that a wave walks, waves to a token's queries and to its keys
+    float eps;
+};
+
+struct VerifyArgs {
+    const float *p, *q;                   // q may be null
+    const int32_t *ids, *parents, *drafted;   // the last two may be null
+    const float* u;
+    int32_t *accepted, *n_accepted, *next;
+    int64_t p_batch, p_token, q_batch, q_token, parents_batch;
+    uint32_t batch, tokens, vocab;
+};
+
 struct CacheAppendArgs {
     const void *k_new, *v_new;
     void *k_cache, *v_cache;
@@ -76,6 +119,11 @@ hipError_t launch_tree_attn_f16(const TreeAttnArgs& a, int head_dim, hipStream_t
 hipError_t launch_cache_append(const CacheAppendArgs& a, int head_dim, hipStream_t stream);
 hipError_t launch_cache_weights(const CacheWeightsArgs& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t launch_cache_evict(const CacheEvictArgs& a, int head_dim, hipStream_t stream);
+hipError_t launch_tree_attn8_bf16(const TreeAttn8Args& a, int head_dim, hipStream_t stream);
+hipError_t launch_tree_attn8_f16(const TreeAttn8Args& a, int head_dim, hipStream_t stream);
+hipError_t launch_cache_append8(const CacheAppend8Args& a, int dtype, int head_dim, int block, hipStream_t stream);
+hipError_t launch_qk_norm_rope(const QkNormArgs& a, int dtype, int head_dim, bool interleaved, bool norm, hipStream_t stream);
+hipError_t launch_verify_drafts(const VerifyArgs& a, hipStream_t stream);
 
 template <class F, class A>
 inline hipError_t launch_one(F* kernel, uint32_t n_blocks, uint32_t threads, hipStream_t stream, const A& a) {

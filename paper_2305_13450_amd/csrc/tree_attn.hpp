@@ -211,24 +211,31 @@ __device__ __forceinline__ uint32_t wave_prefix(uint32_t x, uint32_t none, F f) 
 __device__ __forceinline__ uint32_t wave_sums_to(uint32_t x) { return wave_prefix(x, 0u, [](uint32_t p, uint32_t q) { return p + q; }); }
 __device__ __forceinline__ uint32_t last_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); }
 
+// A sequence's rows of the cache, and what lies behind them: its drafted tokens.  (A cache held in 8 bits has rows of 16 bits too, see tree_attn8.hpp: they
+// are `held` of the latter.)
+struct TreeLengths { uint32_t cached, drafted, held; };
+__device__ __forceinline__ TreeLengths tree_lengths(const TreeAttnArgs& a, uint32_t b) {
+    return {a.capacity ? clamp_count(a.cached[b], a.capacity) : 0u, a.drafted ? clamp_count(a.drafted[b], a.tokens) : a.tokens, 0u};
+}
+
 // How the key axes of all sequences are cut: the lengths are known here only, so every wave works it out for itself.  Up to 64 sequences, a lane
 // each: all parts have as many blocks as lets them fit `slots`, whichever sequence they belong to, and an uneven batch keeps the chip as busy as an even one
 // (8 x 63 tokens of 32 heads over 500 to 4096 rows: 39 us, and 47 with each sequence cut as the longest one is).  More sequences leave little to cut: there
 // each has as many slots.  All of it stands before the first keys are asked for, so it is kept short (divisions are products: compiled ones, and
 // a walk over any number of sequences, made a call of one token 1.1 us longer).
 struct TreeCut {
-    uint32_t b, cached, drafted;         // a sequence and its lengths
+    uint32_t b, cached, drafted, held;   // a sequence and its lengths
     uint32_t first, n, size;             // its first slot, its parts, blocks in each (the last has what is left)
 };
-template <bool SLOT>                     // of the sequence that slot x belongs to (b = batch: to none), or of sequence x
-__device__ __forceinline__ TreeCut tree_cut(const TreeAttnArgs& a, uint32_t x, uint32_t keys) {
+template <bool SLOT, class Args>         // of the sequence that slot x belongs to (b = batch: to none), or of sequence x
+__device__ __forceinline__ TreeCut tree_cut(const Args& a, uint32_t x, uint32_t keys) {
     TreeCut c;
     const bool wide = a.batch > 64;
     const uint32_t b = !wide ? threadIdx.x & 63u : SLOT ? x / a.part_slots : x;
-    const uint32_t cached = b < a.batch && a.capacity ? clamp_count(a.cached[b], a.capacity) : 0u;
-    const uint32_t drafted = b >= a.batch ? 0u : a.drafted ? clamp_count(a.drafted[b], a.tokens) : a.tokens;
+    const TreeLengths len = b < a.batch ? tree_lengths(a, b) : TreeLengths{0, 0, 0};
+    const uint32_t cached = len.cached, drafted = len.drafted;
     const uint32_t blocks = (cached + keys - 1) / keys + (drafted + keys - 1) / keys;
-    if (wide) return {b, cached, drafted, b * a.part_slots, min(a.part_slots, (blocks + a.part_blocks - 1) / a.part_blocks), a.part_blocks};
+    if (wide) return {b, cached, drafted, len.held, b * a.part_slots, min(a.part_slots, (blocks + a.part_blocks - 1) / a.part_blocks), a.part_blocks};
     const uint32_t all = last_lane(wave_sums_to(blocks));
     // Even sequences fill the slots; of uneven ones the last parts are partly empty, up to nearly one part each, and with so many slots less parts fit in
     // any case (there are at least twice as many as sequences).  q is the quotient or, by rounding, one less, which one block more then makes up for.
@@ -248,6 +255,7 @@ __device__ __forceinline__ TreeCut tree_cut(const TreeAttnArgs& a, uint32_t x, u
     c.b = (uint32_t)__builtin_ctzll(hit);
     c.cached = (uint32_t)__builtin_amdgcn_readlane((int)cached, (int)c.b);
     c.drafted = (uint32_t)__builtin_amdgcn_readlane((int)drafted, (int)c.b);
+    c.held = (uint32_t)__builtin_amdgcn_readlane((int)len.held, (int)c.b);
     c.n = (uint32_t)__builtin_amdgcn_readlane((int)n, (int)c.b);
     c.first = (uint32_t)__builtin_amdgcn_readlane((int)to, (int)c.b) - c.n;
     return c;
@@ -255,21 +263,23 @@ __device__ __forceinline__ TreeCut tree_cut(const TreeAttnArgs& a, uint32_t x, u
 
 // The kernel's arguments, read anew: held from the start on they, and what follows from them, go through more scalar registers than there are (128 of
 // them spilled, a third of the few rows' kernel was moves from and to lanes).
-__device__ __forceinline__ const TreeAttnArgs& tree_args() {
-    typedef const __attribute__((address_space(4))) TreeAttnArgs* Segment;
+template <class Args = TreeAttnArgs>
+__device__ __forceinline__ const Args& tree_args() {
+    typedef const __attribute__((address_space(4))) Args* Segment;
     Segment p = (Segment)__builtin_amdgcn_kernarg_segment_ptr();
     asm volatile("" : "+s"(p));
-    return *(const TreeAttnArgs*)p;
+    return *(const Args*)p;
 }
 
 // What a workgroup works on, the same in every lane.
 struct TreeJob {
     uint32_t b, h;                       // sequence, key and value head
     uint32_t slot, n_parts;              // of all parts, parts of this sequence (0: there is no work)
-    uint32_t cached, drafted;            // of the sequence
+    uint32_t cached, drafted, held;      // of the sequence
     uint32_t cache_blocks, begin, end;   // blocks of cached rows, this part's blocks
 };
-__device__ __forceinline__ TreeJob tree_job(const TreeAttnArgs& a, uint32_t unit, uint32_t block_keys) {
+template <class Args>
+__device__ __forceinline__ TreeJob tree_job(const Args& a, uint32_t unit, uint32_t block_keys) {
     TreeJob j;
     j.h = unit % a.kv_heads;
     j.slot = unit / a.kv_heads;
@@ -280,14 +290,17 @@ __device__ __forceinline__ TreeJob tree_job(const TreeAttnArgs& a, uint32_t unit
         j.b = uni(c.b);
         j.cached = uni(c.cached);
         j.drafted = uni(c.drafted);
+        j.held = uni(c.held);
         j.n_parts = uni(c.n);
         part = uni(j.slot - c.first);
         size = c.size;
         if (j.b >= a.batch || part >= j.n_parts) { j.n_parts = 0; return j; }
     } else {
         j.b = j.slot;
-        j.cached = uni(a.capacity ? clamp_count(a.cached[j.b], a.capacity) : 0u);
-        j.drafted = uni(a.drafted ? clamp_count(a.drafted[j.b], a.tokens) : a.tokens);
+        const TreeLengths len = tree_lengths(a, j.b);
+        j.cached = uni(len.cached);
+        j.drafted = uni(len.drafted);
+        j.held = uni(len.held);
     }
     j.cache_blocks = (j.cached + block_keys - 1) / block_keys;
     const uint32_t blocks = j.cache_blocks + (j.drafted + block_keys - 1) / block_keys;
@@ -767,8 +780,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
 // ---- parts joined --------------------------------------------------------------------------------------------------------
 // One wave per query row: D / 4 lanes hold four output values each, and as many such groups as there are walk the parts.  (8 x 63 tokens of 32 heads in
 // 3 parts or so each: 11.5 us for 25 MB; a few rows: 4.7 us, the way through two dependent reads.)
-template <typename T, int D>
-__global__ __launch_bounds__(256) void tree_attn_join(const TreeAttnArgs a) {
+template <typename T, int D, class Args>
+__global__ __launch_bounds__(256) void tree_attn_join(const Args a) {
     constexpr uint32_t VEC = D / 4, GROUPS = 64 / VEC;
     typedef T T4 __attribute__((ext_vector_type(4)));
     const uint32_t lane = threadIdx.x & 63u;
@@ -823,7 +836,7 @@ hipError_t launch_tree_attn_of(const TreeAttnArgs& a, hipStream_t stream) {
     if (a.few) e = launch_one(tree_attn_few<T, D>, units * ((a.rows + TREE_FEW_ROWS - 1) / TREE_FEW_ROWS), 256, stream, a);
     else e = launch_one(tree_attn_many<T, D>, units * ((a.rows + TREE_MANY_ROWS - 1) / TREE_MANY_ROWS), 256, stream, a);
     if (e != hipSuccess || a.slots == a.batch) return e;
-    return launch_one(tree_attn_join<T, D>, (uint32_t)(((uint64_t)a.batch * a.kv_heads * a.rows + 3) / 4), 256, stream, a);
+    return launch_one(tree_attn_join<T, D, TreeAttnArgs>, (uint32_t)(((uint64_t)a.batch * a.kv_heads * a.rows + 3) / 4), 256, stream, a);
 }
 
 template <typename T>

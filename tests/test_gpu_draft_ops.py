@@ -1,0 +1,315 @@
+"""GPU tests of a round of drafts over a cache of 8 bits (norm and rotation, attention, verification, append) against the 64-bit forms of tests/draft_ref.py."""
+import math
+
+import pytest
+import torch
+
+import cache_ref
+import draft_ref as ref
+import paper_2305_13450_amd as ds
+
+pytestmark = pytest.mark.gpu
+BF, FP = torch.bfloat16, torch.float16
+E4M3 = torch.float8_e4m3fn
+INF, NAN = float("inf"), float("nan")
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def normal(g, shape, dtype, std=1.0):
+    return (torch.randn(shape, generator=g, device="cuda") * std).to(dtype)
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def tree_of(g, B, T):
+    """Parents [B, T] of random trees and dep_tree_attn's words."""
+    parents = (torch.rand((B, T), generator=g, device="cuda") * torch.arange(T, device="cuda")).long()
+    parents[:, 0] = -1
+    return parents, ds.tree_mask(parents.cpu()).cuda()
+
+
+def same(a, b):
+    return torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+
+
+# ---- norm and rotation -------------------------------------------------------------------------------------------------------------
+
+def angles_of(R, base=10000.0):
+    return [base ** (-2 * i / R) for i in range(R // 2)]
+
+
+def check_norm(x, got, want, tol, what):
+    over = ((got.cpu().double() - want).abs() / tol)
+    assert float(over.max()) <= 1.0, f"{what}: {float(over.max()):.3f} of the tolerance"
+
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("B,T,Hq,Hk,D,R,interleaved", [
+    (1, 1, 1, 1, 64, 64, False), (3, 1, 12, 12, 128, 128, False), (2, 63, 32, 8, 128, 128, False), (2, 5, 20, 4, 64, 32, False), (1, 130, 9, 3, 128, 16, False),
+    (4, 7, 64, 8, 128, 128, True), (2, 3, 17, 17, 64, 16, True), (1, 2, 5, 1, 64, 64, True), (2, 2, 3, 3, 128, 96, True), (2, 2, 3, 3, 128, 96, False), (3, 4, 8, 2, 128, 0, False)])
+def test_norm_and_rotation(B, T, Hq, Hk, D, R, interleaved, dtype):
+    print("norm", B, T, Hq, Hk, D, R, interleaved, dtype, flush=True)
+    g = gen(B * T + D + R)
+    qkv = normal(g, (B, T, (Hq + 2 * Hk) * D), dtype, 3.0)
+    q, k = qkv[:, :, : Hq * D].view(B, T, Hq, D), qkv[:, :, Hq * D: (Hq + Hk) * D].view(B, T, Hk, D)
+    qg, kg = (1 + 0.3 * torch.randn(D, generator=g, device="cuda") for _ in range(2))
+    start = torch.randint(-5, 2 ** 31 - 100, (B,), generator=g, device="cuda").int()
+    depth = torch.randint(0, 50, (B, T), generator=g, device="cuda").int()
+    angles = angles_of(R) if R else None
+    freq = ds.rope_frequencies(angles, "cuda") if R else None
+    want = [ref.norm_rope(x, angles, w, start, depth, 1e-5, True, interleaved) for x, w in ((q, qg), (k, kg))]
+    qo, ko = torch.full_like(q, NAN, memory_format=torch.contiguous_format), torch.full_like(k, NAN, memory_format=torch.contiguous_format)
+    ds.dep_qk_norm_rope(q, k, freq, qg, kg, qo, ko, start, depth, eps=1e-5, interleaved=interleaved)
+    torch.cuda.synchronize()
+    check_norm(q, qo, *want[0], "q")
+    check_norm(k, ko, *want[1], "k")
+    before = qkv.clone()                                         # in place: the same numbers, values left as they were
+    ds.dep_qk_norm_rope(q, k, freq, qg, kg, start=start, depth=depth, eps=1e-5, interleaved=interleaved)
+    torch.cuda.synchronize()
+    assert same(q, qo) and same(k, ko) and same(qkv[:, :, (Hq + Hk) * D:], before[:, :, (Hq + Hk) * D:])
+
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+def test_norm_and_rotation_without_their_options(dtype):
+    g = gen(2)
+    B, T, Hq, Hk, D = 3, 6, 10, 2, 128
+    q, k = normal(g, (B, T, Hq, D), dtype), normal(g, (B, T, Hk, D), dtype)
+    angles = angles_of(D, 500000.0)
+    freq = ds.rope_frequencies(angles, "cuda")
+    gain = torch.randn(D, generator=g, device="cuda")
+    start, shared = ints([0, 70000, 12]), ints([0, 1, 1, 2, 2, 2])
+    for kw in (dict(), dict(norm=False), dict(q_gain=gain), dict(k_gain=gain, norm=False), dict(start=start), dict(depth=shared), dict(start=start, depth=shared, eps=0.5)):
+        qo, ko = torch.empty_like(q), torch.empty_like(k)
+        ds.dep_qk_norm_rope(q, k, freq, q_out=qo, k_out=ko, **kw)
+        torch.cuda.synchronize()
+        for x, y, name in ((q, qo, "q_gain"), (k, ko, "k_gain")):
+            want, tol = ref.norm_rope(x, angles, kw.get(name), kw.get("start"), kw.get("depth"), kw.get("eps", 1e-6), kw.get("norm", True))
+            check_norm(x, y, want, tol, (name, kw.keys()))
+    # rows of tokens that are not drafted stay
+    qo, ko = torch.full_like(q, 7.0), torch.full_like(k, 7.0)
+    ds.dep_qk_norm_rope(q, k, freq, q_out=qo, k_out=ko, drafted=ints([0, 9, 4]))
+    torch.cuda.synchronize()
+    assert bool((qo[0] == 7).all()) and bool((ko[2, 4:] == 7).all()) and bool((qo[2, 4:] == 7).all()) and not bool((qo[1] == 7).any())
+
+
+def test_rows_of_zeros_and_of_numbers_that_are_not_finite():
+    q = torch.zeros((1, 4, 2, 64), dtype=BF, device="cuda")
+    q[0, 1, 0, 3], q[0, 2, 1, 60] = INF, NAN
+    k = torch.ones((1, 4, 1, 64), dtype=BF, device="cuda") * 1e-20
+    freq = ds.rope_frequencies(angles_of(64), "cuda")
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    ds.dep_qk_norm_rope(q, k, freq, q_out=qo, k_out=ko)
+    torch.cuda.synchronize()
+    assert bool((qo[0, 0] == 0).all()) and bool((qo[0, 3] == 0).all()) and bool((qo[0, 1, 1] == 0).all()) and bool((qo[0, 2, 0] == 0).all())
+    assert bool(qo[0, 2, 1].isnan().all()) and bool(qo[0, 1, 0].isnan().any())
+    want, tol = ref.norm_rope(k, angles_of(64))
+    check_norm(k, ko, want, tol, "k")
+
+
+def test_far_positions_keep_their_angles():
+    # a turn of 2^-32 a position: 2^31 positions are half a turn, exactly
+    x = torch.randn((1, 1, 1, 64), device="cuda").to(FP)
+    freq = torch.full((32,), 1 << 32, dtype=torch.int64, device="cuda")
+    y, z = torch.empty_like(x), torch.empty_like(x)
+    ds.dep_qk_norm_rope(x, x.clone(), freq, q_out=y, k_out=z, start=ints([2 ** 31 - 1]), depth=ints([1]), norm=False)
+    torch.cuda.synchronize()
+    assert torch.equal(y, -x)
+    ds.dep_qk_norm_rope(x, x.clone(), freq, q_out=y, k_out=z, start=ints([-2 ** 31]), depth=ints([0]), norm=False)
+    torch.cuda.synchronize()
+    assert torch.equal(y, -x)
+
+
+# ---- append ---------------------------------------------------------------------------------------------------------------------------
+
+def check_append(kn, vn, cache, cached, accepted=None, n_accepted=None):
+    want = ref.append8(kn, vn, *cache, cached.cpu(), None if accepted is None else accepted.cpu(), None if n_accepted is None else n_accepted.cpu())
+    out, n = torch.full_like(cached, -7), torch.full_like(cached, -7)
+    ds.dep_cache_append8(kn, vn, *cache, cached, out, accepted=accepted, n_accepted=n_accepted, n_out=n)
+    torch.cuda.synchronize()
+    k, v, ks, vs, kt, vt = (t.cpu() for t in cache)
+    for got, w in ((k, want[0]), (v, want[1])):
+        assert torch.equal(got.double().nan_to_num(9e9), w.nan_to_num(9e9))
+    assert torch.equal(ks, want[2]) and torch.equal(vs, want[3]) and same(kt, want[4]) and same(vt, want[5])
+    assert torch.equal(out.cpu(), want[6]) and torch.equal(n.cpu(), want[7])
+    return out
+
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("B,T,A,Hk,D,block,lens,counts", [
+    (1, 1, None, 1, 64, 32, [0], None), (3, 1, None, 2, 128, 32, [31, 32, 30], None), (4, 16, 6, 3, 128, 64, [60, 0, 63, 64], [5, 6, 1, 0]),
+    (2, 200, None, 2, 128, 64, [10, 100], [200, 117]), (2, 130, None, 1, 64, 128, [0, 127], None), (3, 70, 40, 2, 64, 32, [5, 90, 200], [40, 39, 2]),
+    (2, 300, None, 5, 128, 128, [250, 3], [300, 9]), (2, 64, None, 1, 128, 64, [320, 300], None), (2, 64, None, 2, 64, 32, [384, 383], None)])
+def test_append(B, T, A, Hk, D, block, lens, counts, dtype):
+    print("append8", B, T, A, Hk, D, block, lens, counts, dtype, flush=True)
+    g = gen(B * T + block)
+    cap = 3 * 128 if T <= 130 else 5 * 128
+    cache = ref.make_cache(g, B, cap, Hk, D, block, dtype)
+    kn, vn = normal(g, (B, T, Hk, D), dtype), normal(g, (B, T, Hk, D), dtype, 1e-3)
+    accepted = None if A is None else torch.randint(0, T, (B, A), generator=g, device="cuda").int()
+    check_append(kn, vn, cache, ints(lens), accepted, None if counts is None else ints(counts))
+
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+def test_numbers_of_8_bits(dtype):
+    # one block to a head: zeros, the smallest and largest numbers of the type, halfway cases of every 8-bit number, infinities and NaN
+    block, Hk, D = 32, 8, 64
+    g = gen(5)
+    x = torch.zeros((1, block, Hk, D), dtype=dtype, device="cuda")
+    x[0, :, 1] = normal(g, (block, D), dtype) * 2.0 ** -10
+    half = (ref.POSITIVE[1:] + ref.POSITIVE[:-1]) / 2
+    table = torch.cat([half, -half, ref.POSITIVE, half * (1 + 2.0 ** -7), half * (1 - 2.0 ** -7)]).to(dtype)
+    for h, by in ((2, 1.0), (3, 2.0 ** -8)):
+        x[0, :, h] = torch.cat([table, table.new_zeros(block * D - len(table))]).view(block, D).cuda() * by
+        x[0, 0, h, 0] = 448.0 * by
+    x[0, :, 4] = normal(g, (block, D), dtype)
+    x[0, 3, 4, 5], x[0, 4, 4, 6], x[0, 5, 4, 7] = INF, -INF, NAN
+    x[0, 7, 5, 9] = torch.finfo(dtype).tiny                               # alone: the smallest normal number
+    x[0, 7, 6, 9], x[0, 8, 6, 9] = torch.finfo(dtype).max, -1.0
+    x[0, 7, 7, 9], x[0, 7, 7, 10] = (1e-40, 3e-39) if dtype == BF else (6e-8, 1e-5)   # smaller than that
+    cache = ref.make_cache(g, 1, 64, Hk, D, block, dtype)
+    check_append(x, x.flip(1).contiguous(), cache, ints([32]))
+    # 448 2^e exactly at the border of two scales
+    y = torch.zeros((1, block, 2, D), dtype=dtype, device="cuda")
+    y[0, 0, 0, 0], y[0, 0, 1, 0] = 448.0, 450.0 if dtype == BF else 448.25
+    cache = ref.make_cache(g, 1, 64, 2, D, block, dtype)
+    check_append(y, y, cache, ints([0]))
+    assert cache[2][0, :, 0].tolist() == [1.0, 2.0]
+
+
+def test_append_in_any_division_gives_the_same_cache():
+    g = gen(6)
+    B, Hk, D, block, cap = 2, 2, 128, 32, 256
+    kn, vn = normal(g, (B, 200, Hk, D), BF), normal(g, (B, 200, Hk, D), BF)
+    caches = []
+    for cuts in ([200], [1, 31, 1, 63, 4, 100], [7] * 28 + [4]):
+        cache = ref.make_cache(gen(7), B, cap, Hk, D, block, BF)
+        at = ints([0] * B)
+        done = 0
+        for n in cuts:
+            out = torch.empty_like(at)
+            ds.dep_cache_append8(kn[:, done: done + n], vn[:, done: done + n], *cache, at, out)
+            at, done = out, done + n
+        torch.cuda.synchronize()
+        assert at.tolist() == [200, 200]
+        caches.append(cache)
+    for cache in caches[1:]:
+        for i in range(4):
+            assert same(cache[i], caches[0][i])
+        for i in (4, 5):
+            assert same(cache[i][:, : 200 % block], caches[0][i][:, : 200 % block])
+
+
+# ---- attention -------------------------------------------------------------------------------------------------------------------------
+
+def run_attn(q, kn, vn, cache, cached, **kw):
+    out, lse = torch.full(q.shape, 5.0, dtype=q.dtype, device="cuda"), torch.full(q.shape[:3], 5.0, device="cuda")
+    ds.dep_tree_attn8(q, kn, vn, *cache, cached, out, lse=lse, **kw)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+def check_attn(q, kn, vn, cache, cached, tree=None, drafted=None, scale=None, got=None, **kw):
+    out, lse = got or run_attn(q, kn, vn, cache, cached, tree=tree, drafted=drafted, scale=scale, **kw)
+    want, want_lse, tol, tol_lse = ref.attn8(q, kn, vn, cache, cached.cpu(), tree, None if drafted is None else drafted.cpu(), scale)
+    out, lse = out.cpu().double(), lse.cpu().double()
+    gone = want_lse.isnan()                                                # tokens not drafted: left alone
+    assert bool((out[gone] == 5).all()) and bool((lse[gone] == 5).all())
+    for x, y, t in ((out, want, tol), (lse, want_lse, tol_lse)):
+        x, y, t = x[~gone], y[~gone], t[~gone]
+        fine = y.isfinite()
+        assert torch.equal(x[~fine].nan_to_num(9e9), y[~fine].nan_to_num(9e9))
+        if fine.any():
+            worst = float(((x - y).abs() / t)[fine].max())
+            assert worst <= 1.0, f"{worst:.3f} of the tolerance"
+    return out, lse
+
+
+def spoil(cache, cached):
+    """NaN where no row is: behind the full blocks, in their scales, and behind the rows held in 16 bits."""
+    k, v, ks, vs, kt, vt = cache
+    block = kt.shape[1]
+    for b, n in enumerate(cached.tolist()):
+        n = min(max(n, 0), k.shape[1])
+        for num, scale, tail in ((k, ks, kt), (v, vs, vt)):
+            num.view(torch.uint8)[b, n - n % block:] = 127
+            scale[b, :, n // block:] = NAN
+            tail[b, n % block:] = NAN
+    return cache
+
+
+ATTN = [
+    # B, T, Hq, Hk, D, block, lens
+    (1, 1, 1, 1, 64, 32, [0]), (1, 1, 1, 1, 128, 32, [1]), (2, 1, 12, 12, 128, 64, [500, 63]), (3, 1, 8, 2, 64, 32, [31, 32, 33]), (4, 1, 16, 2, 128, 128, [127, 128, 129, 640]),
+    (2, 5, 8, 2, 128, 64, [200, 64]), (3, 4, 16, 4, 64, 64, [1000, 0, 65]), (2, 7, 10, 2, 128, 32, [96, 321]), (1, 13, 4, 2, 64, 128, [1500]), (2, 9, 16, 2, 128, 32, [700, 5]),
+    (2, 63, 4, 4, 128, 64, [300, 130]), (1, 40, 8, 2, 64, 32, [513]), (70, 2, 4, 2, 64, 32, [3 * i for i in range(70)]), (2, 1, 64, 2, 128, 64, [3000, 17]),
+    (1, 3, 2, 1, 128, 128, [20000]), (2, 70, 8, 1, 64, 64, [190, 700]), (1, 300, 2, 2, 128, 32, [40]), (2, 33, 5, 1, 128, 64, [64, 1000])]
+
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("B,T,Hq,Hk,D,block,lens", ATTN)
+def test_attention(B, T, Hq, Hk, D, block, lens, dtype):
+    print("attn8", B, T, Hq, Hk, D, block, lens, dtype, flush=True)
+    g = gen(B * T + D + block)
+    cap = -(-max(max(lens), 1) // block) * block + block
+    cached = ints(lens)
+    cache = spoil(ref.make_cache(g, B, cap, Hk, D, block, dtype), cached)
+    q, kn, vn = normal(g, (B, T, Hq, D), dtype, 2.0), normal(g, (B, T, Hk, D), dtype), normal(g, (B, T, Hk, D), dtype)
+    check_attn(q, kn, vn, cache, cached)
+    if T > 1:
+        _, tree = tree_of(g, B, T)
+        drafted = ints([T - (T // 3) * (i % 3) // 2 for i in range(B)])
+        first = check_attn(q, kn, vn, cache, cached, tree=tree, drafted=drafted, scale=0.05)
+        again = run_attn(q, kn, vn, cache, cached, tree=tree, drafted=drafted, scale=0.05)
+        assert torch.equal(again[0].cpu().double(), first[0]) and torch.equal(again[1].cpu().double(), first[1])
+
+
+# ---- verification -----------------------------------------------------------------------------------------------------------------------
+
+def check_verify(p, ids, u, q=None, parents=None, drafted=None, **kw):
+    B, T, V = p.shape
+    acc, n, nxt = torch.full((B, T), -9, dtype=torch.int32, device="cuda"), ints([-9] * B), ints([-9] * B)
+    ds.dep_verify_drafts(p, ids, u, acc, n, nxt, q=q, parents=parents, drafted=drafted, **kw)
+    torch.cuda.synchronize()
+    acc, n, nxt = acc.tolist(), n.tolist(), nxt.tolist()
+    want = ref.verify(p, ids, u, q, None if parents is None else parents.cpu(), None if drafted is None else drafted.cpu())
+    for b, w in enumerate(want):
+        if w is None:
+            assert (n[b], nxt[b]) == (0, -9) and acc[b] == [-9] * T
+        else:
+            assert acc[b] == w[0] + [-9] * (T - len(w[0])) and n[b] == len(w[0]) and nxt[b] == w[1], (b, acc[b], w, nxt[b])
+    return want
+
+
+def probabilities(g, B, T, V, spread=3.0, near=1.0):
+    x = torch.randn((B, T, V), generator=g, device="cuda") * spread
+    return torch.softmax(x, -1), torch.softmax(x + near * torch.randn((B, T, V), generator=g, device="cuda"), -1)
+
+
+def drawn_ids(g, q, parents):
+    B, T, V = q.shape
+    rows = q[torch.arange(B, device="cuda")[:, None], parents.clamp(min=0)]
+    return torch.multinomial(rows.reshape(B * T, V), 1, generator=g).view(B, T).int()
+
+
+@pytest.mark.parametrize("B,T,V,shape", [(1, 1, 1, "chain"), (2, 1, 50, "chain"), (3, 6, 1000, "chain"), (5, 4, 50257, "chain"), (4, 16, 333, "tree"), (2, 64, 5000, "tree"),
+                                         (3, 65, 64, "tree"), (2, 200, 7, "tree"), (1, 32, 128000, "tree"), (40, 12, 1025, "tree")])
+@pytest.mark.parametrize("drawn", [True, False], ids=["drawn", "likely"])
+def test_verification(B, T, V, shape, drawn):
+    print("verify", B, T, V, shape, drawn, flush=True)
+    g = gen(B + T + V)
+    p, q = probabilities(g, B, T, V)
+    parents = torch.arange(T, device="cuda").expand(B, T) - 1 if shape == "chain" else tree_of(g, B, T)[0]
+    ids = drawn_ids(g, q, parents)
+    words = None if shape == "chain" else parents.int().contiguous()
+    for seed in range(3):
+        u = torch.rand((B, T), generator=gen(seed), device="cuda")
+        check_verify(p, ids, u, q if drawn else None, words)
+    drafted = ints([T - (i * T) // max(B, 2) for i in range(B)])
+    check_verify(p, ids, u, q if drawn else None, words, drafted)
