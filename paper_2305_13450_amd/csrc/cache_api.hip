@@ -110,7 +110,7 @@ int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t
     // head of 64 over 120000, 73 and 62.  Between 100 and 270 MB it depends on how many sequences share them: 8 x 48 over 8000 67 and 64, but 16 x 64
     // over 4000 64 and 68, 4 x 52 over 8000 40 and 42, 16 x 40 over 2000 36 and 49.
     const int64_t cache_bytes = (int64_t)d->batch * d->kv_heads * rows_hint(d->max_cached, d->capacity) * d->head_dim * 4;
-    a.few = held || rows <= (cache_bytes < 100000000 ? 64 : 32);
+    a.few = rows <= (cache_bytes < 100000000 ? 64 : 32);
     const int64_t keys = a.few ? TREE_FEW_KEYS : TREE_MANY_KEYS, row_blocks = cdiv64(rows, a.few ? TREE_FEW_ROWS : TREE_MANY_ROWS);
     const int64_t pairs = (int64_t)d->batch * d->kv_heads, base = pairs * row_blocks;
     const int64_t wide = d->tokens + (held ? held - 1 : 0);        // rows of 16 bits behind those of full blocks

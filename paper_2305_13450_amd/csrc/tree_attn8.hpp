@@ -6,12 +6,13 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "tree_attn.hpp"
 
 namespace depsync {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4v __attribute__((ext_vector_type(4)));
 
 // The two stretches of a sequence: `cached` rows of full blocks; `drafted` rows of 16 bits, of which `held` are cached ones.
 __device__ __forceinline__ TreeLengths tree_lengths(const TreeAttn8Args& a, uint32_t b) {
@@ -181,7 +182,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
     }
     const float sc = a.scale;
     // Weights of a tile's scores, times `vs`, as two fragments of products with values of U, which hold twice the bits of one.
-    auto weigh = [&]<typename U>(f32x4 (&st)[2], int r, float by, float vs, typename Mma<U>::V8& high, typename Mma<U>::V8& rest) __attribute__((always_inline)) {
+    auto weigh = [&](f32x4 (&st)[2], int r, float by, float vs, auto& high, auto& rest) __attribute__((always_inline)) {
+        using U = std::conditional_t<std::is_same_v<std::remove_reference_t<decltype(high)>, B8>, __bf16, _Float16>;
         float mx = fmaxf(fmaxf(fmaxf(st[0][0], st[0][1]), fmaxf(st[0][2], st[0][3])), fmaxf(fmaxf(st[1][0], st[1][1]), fmaxf(st[1][2], st[1][3]))) * by;
         if (__ballot(mx > m[r] + WEIGHT_SLACK)) {                      // (rarely, after the first steps)
             mx = fmaxf(mx, __shfl_xor(mx, 16));
@@ -220,7 +222,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
         fetch_k(x, t + 2);
         B8 high[NR], rest[NR];
 #pragma unroll
-        for (int r = 0; r < NR; ++r) weigh.template operator()<__bf16>(st[r], r, by, vs, high[r], rest[r]);
+        for (int r = 0; r < NR; ++r) weigh(st[r], r, by, vs, high[r], rest[r]);
 #pragma unroll
         for (int w = 0; w < VW; ++w) {
             B8 vf[4];
@@ -269,7 +271,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
 #pragma unroll
             for (int v = 0; v < 8; ++v)
                 if (!(vis >> (16 * (v >> 2) + 4 * g + (v & 3)) & 1u)) st[r][v >> 2][v & 3] = -INFINITY;
-            weigh.template operator()<T>(st[r], r, sc, 1.0f, high[r], rest[r]);
+            weigh(st[r], r, sc, 1.0f, high[r], rest[r]);
         }
         uint32_t vw[8][NB / 2];                                        // NB numbers of 8 rows each
         bool bad = false;
@@ -345,11 +347,284 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
     }
 }
 
+// ---- many rows -----------------------------------------------------------------------------------------------------------
+// The form for many rows of tree_attn.hpp: 128 rows to a workgroup, tiles of 32 keys in LDS, where they are numbers of T: 8-bit ones are converted on their way from
+// registers into it, once for all four waves (16 conversions and 4 LDS stores a wave and tile, where a wave that converted its fragments would need 64).
+//
+// A weight carries its block's V scale, relative to the largest that the part has met so far (`most`; outputs are in units of it, and are scaled when it grows,
+// which random scales do a few times), so that fp16 weights stay in range: the scale goes into the exponent, and the sum is divided by it again.
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a) {
+    using Tile = KeyTile<T, D>;
+    using Mm = Mma<T>;
+    using V8 = typename Mm::V8;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    using Pad = PaddedTile<D>;
+    constexpr uint32_t SLOT = Pad::BYTES;                              // a tile of K and one of V
+    constexpr int KF = D / 16, NB = D / 32, NV = 2 * NB, AHEAD = 3;    // MFMAs of a tile's scores, of its output (as many), LDS reads ahead of them
+    __shared__ __align__(16) char lds[4 * SLOT];
+    __shared__ uint32_t odd;                                           // a value of the stretch of 16 bits is not finite
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6), h2 = lane >> 5;
+    const TreeUnit u = tree_unit((a.rows + TREE_MANY_ROWS - 1) / TREE_MANY_ROWS);
+    if (u.unit >= a.slots * a.kv_heads) return;
+    const TreeJob j = tree_job(a, u.unit, TREE_MANY_KEYS);
+    const uint32_t r0 = u.row_block * TREE_MANY_ROWS, t_last = (min(r0 + TREE_MANY_ROWS, a.rows) - 1) / a.group;
+    if (j.n_parts == 0 || j.begin >= j.end || r0 / a.group >= j.drafted - j.held) return;
+    // without a tree nothing behind the block's last token is seen
+    const uint32_t end = a.tree ? j.end : min(j.end, max(j.begin, j.cache_blocks + (j.held + t_last) / TREE_MANY_KEYS + 1));
+    constexpr uint32_t NI = Tile::NI / 4;                              // 1 KB copies of a wave: 32 rows of 16 bits over four waves
+    const uint32_t lrow = wave * (Tile::RPI * NI) + lane / Tile::CHUNKS, chunk = lane % Tile::CHUNKS;
+    const uint32_t row8 = tid >> 3, at8 = (tid & 7u) * (D / 8);        // of a tile of 8 bits: a thread's row, and its D / 8 bytes of it
+    const uint32_t pitch = uni((uint32_t)a.cache_s.token);
+    const int64_t base = (int64_t)j.b * a.cache_s.batch + (int64_t)j.h * a.cache_s.head;
+    const char *const kbase = uni_ptr((const char*)a.k_cache + base), *const vbase = uni_ptr((const char*)a.v_cache + base);
+    const size_t scales = ((size_t)j.b * a.kv_heads + j.h) * a.n_blocks;
+    const float *const ksp = (const float*)uni_ptr(a.k_scale + scales), *const vsp = (const float*)uni_ptr(a.v_scale + scales);
+    struct Staged { u32x4 k[NI], v[NI]; } staged[2];
+    auto fetch8 = [&](Staged& f, uint32_t tile) __attribute__((always_inline)) {
+        const uint64_t at = (uint64_t)tile * TREE_MANY_KEYS * pitch;
+        const uint32_t bytes = tile < end ? 31 * pitch + D : 0u;       // (behind the last: zeros)
+        const OperandBuf K(kbase + at, bytes), V(vbase + at, bytes);
+        if constexpr (D == 128) {
+            f.k[0] = K.load16(row8 * pitch + at8, 0);
+            f.v[0] = V.load16(row8 * pitch + at8, 0);
+        } else {
+            const u32x2 k = __builtin_amdgcn_raw_buffer_load_b64(K.rsrc, row8 * pitch + at8, 0, 0), v = __builtin_amdgcn_raw_buffer_load_b64(V.rsrc, row8 * pitch + at8, 0, 0);
+            f.k[0][0] = k[0]; f.k[0][1] = k[1];
+            f.v[0][0] = v[0]; f.v[0][1] = v[1];
+        }
+    };
+    auto put8 = [&](const Staged& f, uint32_t slot) __attribute__((always_inline)) {
+        char* const to = lds + (slot & 3u) * SLOT + at8 * 2;
+#pragma unroll
+        for (uint32_t i = 0; i < D / 64; ++i) {
+            *(V8*)(to + row8 * Pad::K_PITCH + 16 * i) = eight<T>(f.k[0][2 * i], f.k[0][2 * i + 1]);
+            *(V8*)(to + row8 * Pad::V_PITCH + Pad::K_BYTES + 16 * i) = eight<T>(f.v[0][2 * i], f.v[0][2 * i + 1]);
+        }
+    };
+    auto fetch = [&](const TreeAttn8Args& args, Staged& f, uint32_t tile) __attribute__((always_inline)) {
+        Staged x;                                                      // (a copy: stores to f from both branches went through scratch memory)
+        if (tile < j.cache_blocks) {
+            fetch8(x, tile);
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < NI; ++i) {
+                const uint32_t r = tile < end ? (tile - j.cache_blocks) * TREE_MANY_KEYS + lrow + i * Tile::RPI : ~0u;
+                const T *const k = wide_row<T>(args, j, false, r), *const v = wide_row<T>(args, j, true, r);
+                x.k[i] = k ? ((const u32x4*)k)[chunk] : u32x4{0, 0, 0, 0};
+                x.v[i] = v ? ((const u32x4*)v)[chunk] : u32x4{0, 0, 0, 0};
+            }
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < NI; ++i) { f.k[i] = x.k[i]; f.v[i] = x.v[i]; }
+    };
+    auto put = [&](Staged& f, uint32_t tile) __attribute__((always_inline)) {
+        const uint32_t slot = tile - j.begin;
+        if (tile < j.cache_blocks) {
+            put8(f, slot);
+        } else {
+            bool bad = false;
+            char* const to = lds + (slot & 3u) * SLOT + chunk * 16;
+#pragma unroll
+            for (uint32_t i = 0; i < NI; ++i) {
+                u32x4 v = f.v[i];
+                bad |= without_not_finite<T>(v);
+                *(u32x4*)(to + lrow * Pad::K_PITCH + i * Tile::RPI * Pad::K_PITCH) = f.k[i];
+                *(u32x4*)(to + lrow * Pad::V_PITCH + Pad::K_BYTES + i * Tile::RPI * Pad::V_PITCH) = v;
+            }
+            if (bad) odd = 1;
+        }
+    };
+    if (tid == 0) odd = 0;
+    // V of the tile before the first, whose weights are zeros: in slot 3
+    for (uint32_t i = tid; i < 32 * Pad::V_PITCH / 16; i += 256) *(u32x4*)(lds + 3 * SLOT + Pad::K_BYTES + i * 16) = u32x4{0, 0, 0, 0};
+    __syncthreads();
+    fetch(a, staged[0], j.begin);
+    fetch(a, staged[1], j.begin + 1);
+    put(staged[0], j.begin);
+    fetch(a, staged[0], j.begin + 2);
+    put(staged[1], j.begin + 1);
+    fetch(a, staged[1], j.begin + 3);
+    RowState<D> row;
+    clear_row(row);
+    const uint32_t at = r0 + wave * 32 + (lane & 31u), token = min(at, a.rows - 1) / a.group;
+    V8 qf[KF];
+    {
+        const T* const q = query_row<T>(a, j, at);
+        const V8 zero = {};
+#pragma unroll
+        for (int kk = 0; kk < KF; ++kk) qf[kk] = q ? *(const V8*)(q + kk * 16 + h2 * 8) : zero;
+    }
+    const uint32_t koff = (lane & 31u) * Pad::K_PITCH + h2 * 16;
+    const uint32_t voff = Pad::K_BYTES + (4 * h2 + ((lane & 15u) >> 2)) * Pad::V_PITCH + ((lane >> 4) & 1u) * 32 + (lane & 3u) * 8;
+    auto read_k = [&](const char* slot, int i) __attribute__((always_inline)) { return *(const V8*)(slot + koff + i * 32); };
+    auto read_v = [&](const char* slot, int i) __attribute__((always_inline)) {   // slice i / NB of 16 keys, block i % NB of 32 d
+        T4 x[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) x[c] = TrRead<T>::read(slot + voff + ((i / NB) * 16 + c * 8) * Pad::V_PITCH + (i % NB) * 64);
+        return __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    f32x16 st[2];
+    V8 pf[2][2] = {};
+    const float sc = a.scale;
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < 16; ++v) st[0][v] = 0.0f;                      // scores of the first tile
+#pragma unroll
+    for (int i = 0; i < KF; ++i) st[0] = Mm::mma(read_k(lds, i), qf[i], st[0]);
+    auto largest = [&](const f32x16& x) __attribute__((always_inline)) {
+        float m0 = fmaxf(fmaxf(x[0], x[1]), x[2]), m1 = fmaxf(fmaxf(x[3], x[4]), x[5]);
+        m0 = fmaxf(fmaxf(m0, x[6]), x[7]); m1 = fmaxf(fmaxf(m1, x[8]), x[9]);
+        m0 = fmaxf(fmaxf(m0, x[10]), x[11]); m1 = fmaxf(fmaxf(m1, x[12]), x[13]);
+        return fmaxf(fmaxf(fmaxf(m0, x[14]), x[15]), m1);
+    };
+    float top = largest(st[0]);                                        // of this lane's scores of the tile to be weighed
+    // Scales of the tile to be weighed: of its scores, and what its V scale comes to.
+    float ks = 1.0f, vs = 1.0f, most = 0.0f;
+    auto scales_of = [&](uint32_t tile) __attribute__((always_inline)) {
+        const bool held = tile < j.cache_blocks;
+        const uint32_t i = held ? (tile * TREE_MANY_KEYS) >> a.block_log2 : 0u;
+        ks = ksp[i]; vs = vsp[i];
+        if (!held) { ks = 1.0f; vs = 1.0f; }
+    };
+    float of = 0.0f, off = 0.0f, back = 1.0f;                          // the V scale that off and back are of: its logarithm relative to `most`, and the inverse
+    // Weights of the tile whose scores are in `sx`, into `px`; scores of the next tile (in slot `next`) into `sy`, and their largest; output of the
+    // one before (in slot `before`) with `py`.
+    auto segment = [&](f32x16& sx, V8 (&px)[2], f32x16& sy, const V8 (&py)[2], const char* next, const char* before, bool masked, uint32_t vis)
+                       __attribute__((always_inline)) {
+        V8 fr[AHEAD + 1];                                              // fragments on their way
+        auto rd = [&](int i) __attribute__((always_inline)) { fr[i % (AHEAD + 1)] = i < KF ? read_k(next, i) : read_v(before, i - KF); };
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) rd(i);
+        if (masked) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                if (!(vis >> (8 * (v / 4) + 4 * h2 + v % 4) & 1u)) sx[v] = -INFINITY;
+            top = largest(sx);
+        }
+        float alpha = 1.0f, unit = 1.0f;
+        if (vs != of) {                                                // (once a block)
+            of = vs;
+            if (vs > most) { unit = most / vs; most = vs; }
+            const float r = vs / most;
+            off = __builtin_amdgcn_logf(r);
+            back = 1.0f / r;
+        }
+        // What is 2^-60 of the largest scale, or zeros, counts for nothing: fp16 weights would be zeros, and the sum in 32 bits could not be divided.
+        const bool none = vs < most * 0x1p-60f || vs == 0.0f;
+        const float by = sc * ks, mx = max_halves(top) * by;
+        bool grown = __ballot(mx > row.m + WEIGHT_SLACK) != 0;         // (rarely, after the first steps)
+        if (grown) {
+            const float m_new = fmaxf(row.m, mx);
+            alpha = row.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(row.m - m_new);
+            row.m = m_new;
+            row.l *= alpha;
+        }
+        const float ref = (row.m == -INFINITY ? 0.0f : row.m) - WEIGHT_OFF<T> - (none ? 0.0f : off);   // no key seen yet: keep the exponents finite
+        float sum[2] = {0.0f, 0.0f}, x0 = 0.0f, x1 = 0.0f, m0 = -INFINITY, m1 = -INFINITY;
+        auto weigh = [&](int v, int half) __attribute__((always_inline)) {       // scores v and v + 1, in two halves
+            if (half == 0) {
+                x0 = __builtin_fmaf(sx[v], by, -ref);
+                x1 = __builtin_fmaf(sx[v + 1], by, -ref);
+                x0 = __builtin_amdgcn_exp2f(x0);
+            } else {
+                x1 = __builtin_amdgcn_exp2f(x1);
+                sum[0] += x0; sum[1] += x1;                            // summed in 32 bits, rounded to 16 for the product with V alone
+                px[v >> 3][v & 7] = (T)x0; px[v >> 3][(v & 7) + 1] = (T)x1;
+            }
+        };
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sy[v] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < KF + NV; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (i + AHEAD < KF + NV) rd(i + AHEAD);
+            if (i < KF) sy = Mm::mma(fr[i % (AHEAD + 1)], qf[i], sy);
+            else row.o[(i - KF) % NB] = Mm::mma(fr[i % (AHEAD + 1)], py[(i - KF) / NB], row.o[(i - KF) % NB]);
+            if constexpr (KF == 8) weigh(i & ~1, i & 1);
+            else { weigh(2 * i, 0); weigh(2 * i, 1); }
+            constexpr int FIRST = KF + NV - 4;                         // the next scores are there by then: four of them to a slot
+            if (i >= FIRST) {
+                m0 = fmaxf(fmaxf(m0, sy[4 * (i - FIRST)]), sy[4 * (i - FIRST) + 1]);
+                m1 = fmaxf(fmaxf(m1, sy[4 * (i - FIRST) + 2]), sy[4 * (i - FIRST) + 3]);
+            }
+        }
+        asm volatile("" ::"v"(px[0]), "v"(px[1]), "v"(sum[0]), "v"(sum[1]), "v"(m0), "v"(m1));   // (computed here, and not where they are used)
+        __builtin_amdgcn_sched_barrier(0);
+        row.l = __builtin_fmaf(sum[0] + sum[1], none ? 1.0f : back, row.l);
+        top = fmaxf(m0, m1);
+        if (none) px[0] = px[1] = V8{};
+        if (grown || unit != 1.0f) {                                   // what was added so far went by the reference value and unit before
+            alpha *= unit;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) row.o[b][v] *= alpha;
+        }
+    };
+    // One tile: what it copies goes out two tiles before it is put into LDS, and that is a tile before it is read.
+    auto step = [&](const TreeAttn8Args& args, uint32_t tile, int odd_one) __attribute__((always_inline)) {
+        const bool wide = tile >= j.cache_blocks;
+        uint32_t vis = ~0u;
+        if (wide) {
+            const uint32_t first = (tile - j.cache_blocks) * TREE_MANY_KEYS;
+            vis = wide_bits(args, j, token, first, tile < end && first < j.drafted ? min(32u, j.drafted - first) : 0u);
+        }
+        const uint32_t slot = tile - j.begin;
+        scales_of(tile);
+        // (behind the last tile the scores are of whatever the slot holds, and not used)
+        segment(st[odd_one], pf[odd_one], st[odd_one ^ 1], pf[odd_one ^ 1], lds + ((slot + 1) & 3u) * SLOT, lds + ((slot - 1) & 3u) * SLOT, wide || tile >= end, tile >= end ? 0u : vis);
+        put(staged[odd_one], tile + 2);
+        fetch(args, staged[odd_one], tile + 4);
+        __syncthreads();                                               // the tile put is in its slot, the one read is done with
+    };
+    uint32_t tile = j.begin;
+    // The bulk: tiles of 8 bits up to the last one fetched, without the general step's branches.
+    const uint32_t whole = min(end, j.cache_blocks);
+    if (tile + 5 < whole) {
+        scales_of(tile);
+        auto quick = [&](int odd_one, uint32_t slot) __attribute__((always_inline)) {
+            segment(st[odd_one], pf[odd_one], st[odd_one ^ 1], pf[odd_one ^ 1], lds + ((slot + 1) & 3u) * SLOT, lds + ((slot - 1) & 3u) * SLOT, false, ~0u);
+            const uint32_t next = j.begin + slot;
+            put8(staged[odd_one], slot + 2);
+            fetch8(staged[odd_one], next + 4);
+            scales_of(next + 1);
+            __syncthreads();
+        };
+        for (; tile + 5 < whole; tile += 2) {
+            quick(0, tile - j.begin);
+            quick(1, tile - j.begin + 1);
+        }
+    }
+    const TreeAttn8Args& later = tree_args<TreeAttn8Args>();
+    for (; tile < end; tile += 2) {                                    // (a last one without keys where their number is odd)
+        step(later, tile, 0);
+        step(later, tile + 1, 1);
+    }
+    if (j.begin < end) {                                               // the output of the last tile
+        const char* const last = lds + ((((end - j.begin) + 1) & ~1u) - 1 & 3u) * SLOT;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) row.o[i % NB] = Mm::mma(read_v(last, i), pf[1][i / NB], row.o[i % NB]);
+    }
+    const TreeAttn8Args& last_args = tree_args<TreeAttn8Args>();
+    row.l += __shfl_xor(row.l, 32);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            f32x4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = row.o[b][4 * g + e] * most;
+            store8_row4<T, D>(last_args, j, at, 32 * b + 8 * g + 4 * h2, o, row.m, row.l, odd != 0, TREE_MANY_KEYS);
+        }
+}
+
 template <typename T, int D>
 hipError_t launch_tree_attn8_of(const TreeAttn8Args& a, hipStream_t stream) {
     const uint32_t units = (a.slots * a.kv_heads + 7) / 8 * 8;
     hipError_t e;
-    if (a.rows <= 16) e = launch_one(tree_attn8_few<T, D, 1>, units, 256, stream, a);
+    if (!a.few) e = launch_one(tree_attn8_many<T, D>, units * ((a.rows + TREE_MANY_ROWS - 1) / TREE_MANY_ROWS), 256, stream, a);
+    else if (a.rows <= 16) e = launch_one(tree_attn8_few<T, D, 1>, units, 256, stream, a);
     else e = launch_one(tree_attn8_few<T, D, 2>, units * ((a.rows + 31) / 32), 256, stream, a);
     if (e != hipSuccess || a.slots == a.batch) return e;
     return launch_one(tree_attn_join<T, D, TreeAttn8Args>, (uint32_t)(((uint64_t)a.batch * a.kv_heads * a.rows + 3) / 4), 256, stream, a);
