@@ -36,6 +36,10 @@ template <typename T> __device__ __forceinline__ typename Mma<T>::V8 eight(uint3
     return {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// The scales of a sequence's and head's blocks, as scalar loads take them: by vector loads every wait for one was a wait for all keys on their way.
+typedef const __attribute__((address_space(4))) float* Scales;
+__device__ __forceinline__ Scales scales_at(const float* p, size_t at) { return (Scales)(uint64_t)uni_ptr(p + at); }
+
 // 16 x 16 outputs, 32 products each.
 __device__ __forceinline__ f32x4 mma16(Mma<__bf16>::V8 a, Mma<__bf16>::V8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mma16(Mma<_Float16>::V8 a, Mma<_Float16>::V8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -131,8 +135,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
     const char* const kp = uni_ptr((const char*)a.k_cache + base);
     const char* const vp = uni_ptr((const char*)a.v_cache + base);
     const size_t scales = ((size_t)j.b * a.kv_heads + j.h) * a.n_blocks;
-    const float* const ksp = (const float*)uni_ptr(a.k_scale + scales);
-    const float* const vsp = (const float*)uni_ptr(a.v_scale + scales);
+    const Scales ksp = scales_at(a.k_scale, scales), vsp = scales_at(a.v_scale, scales);
     struct Tile8 { u32x4 k[2][NJ]; uint32_t v[8][VW]; float ks, vs; } buf[2];
     const uint32_t kat = n * pitch + 16 * g, vat = 4 * g * pitch + (D / 16) * n, bytes = uni(31 * pitch + D);
     auto fetch_k = [&](Tile8& x, uint32_t t) __attribute__((always_inline)) {
@@ -141,7 +144,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int jj = 0; jj < NJ; ++jj) x.k[kt][jj] = K.load16(kat, kt * 16 * pitch + 64 * jj);
-        const uint32_t at = min((first + t * TREE_FEW_KEYS) >> a.block_log2, a.n_blocks - 1);
+        const uint32_t at = uni(min((first + t * TREE_FEW_KEYS) >> a.block_log2, a.n_blocks - 1));
         x.ks = ksp[at];
         x.vs = vsp[at];
     };
@@ -363,6 +366,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
     constexpr uint32_t SLOT = Pad::BYTES;                              // a tile of K and one of V
     constexpr int KF = D / 16, NB = D / 32, NV = 2 * NB, AHEAD = 3;    // MFMAs of a tile's scores, of its output (as many), LDS reads ahead of them
     __shared__ __align__(16) char lds[4 * SLOT];
+    __shared__ __align__(8) uint32_t tile_scales[4][2];                // of the tile in each slot
     __shared__ uint32_t odd;                                           // a value of the stretch of 16 bits is not finite
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6), h2 = lane >> 5;
     const TreeUnit u = tree_unit((a.rows + TREE_MANY_ROWS - 1) / TREE_MANY_ROWS);
@@ -379,8 +383,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
     const int64_t base = (int64_t)j.b * a.cache_s.batch + (int64_t)j.h * a.cache_s.head;
     const char *const kbase = uni_ptr((const char*)a.k_cache + base), *const vbase = uni_ptr((const char*)a.v_cache + base);
     const size_t scales = ((size_t)j.b * a.kv_heads + j.h) * a.n_blocks;
-    const float *const ksp = (const float*)uni_ptr(a.k_scale + scales), *const vsp = (const float*)uni_ptr(a.v_scale + scales);
-    struct Staged { u32x4 k[NI], v[NI]; } staged[2];
+    const OperandBuf KS(uni_ptr(a.k_scale + scales), a.n_blocks * 4u), VS(uni_ptr(a.v_scale + scales), a.n_blocks * 4u);
+    struct Staged { u32x4 k[NI], v[NI]; uint32_t ks, vs; } staged[2];
     auto fetch8 = [&](Staged& f, uint32_t tile) __attribute__((always_inline)) {
         const uint64_t at = (uint64_t)tile * TREE_MANY_KEYS * pitch;
         const uint32_t bytes = tile < end ? 31 * pitch + D : 0u;       // (behind the last: zeros)
@@ -393,6 +397,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
             f.k[0][0] = k[0]; f.k[0][1] = k[1];
             f.v[0][0] = v[0]; f.v[0][1] = v[1];
         }
+        const uint32_t block = (tile * TREE_MANY_KEYS >> a.block_log2) * 4;
+        f.ks = __builtin_amdgcn_raw_buffer_load_b32(KS.rsrc, 0, block, 0);
+        f.vs = __builtin_amdgcn_raw_buffer_load_b32(VS.rsrc, 0, block, 0);
     };
     auto put8 = [&](const Staged& f, uint32_t slot) __attribute__((always_inline)) {
         char* const to = lds + (slot & 3u) * SLOT + at8 * 2;
@@ -401,6 +408,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
             *(V8*)(to + row8 * Pad::K_PITCH + 16 * i) = eight<T>(f.k[0][2 * i], f.k[0][2 * i + 1]);
             *(V8*)(to + row8 * Pad::V_PITCH + Pad::K_BYTES + 16 * i) = eight<T>(f.v[0][2 * i], f.v[0][2 * i + 1]);
         }
+        if (tid < 1) *(u32x2*)tile_scales[slot & 3u] = u32x2{f.ks, f.vs};
     };
     auto fetch = [&](const TreeAttn8Args& args, Staged& f, uint32_t tile) __attribute__((always_inline)) {
         Staged x;                                                      // (a copy: stores to f from both branches went through scratch memory)
@@ -414,9 +422,11 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
                 x.k[i] = k ? ((const u32x4*)k)[chunk] : u32x4{0, 0, 0, 0};
                 x.v[i] = v ? ((const u32x4*)v)[chunk] : u32x4{0, 0, 0, 0};
             }
+            x.ks = x.vs = __builtin_bit_cast(uint32_t, 1.0f);
         }
 #pragma unroll
         for (uint32_t i = 0; i < NI; ++i) { f.k[i] = x.k[i]; f.v[i] = x.v[i]; }
+        f.ks = x.ks; f.vs = x.vs;
     };
     auto put = [&](Staged& f, uint32_t tile) __attribute__((always_inline)) {
         const uint32_t slot = tile - j.begin;
@@ -433,6 +443,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
                 *(u32x4*)(to + lrow * Pad::V_PITCH + Pad::K_BYTES + i * Tile::RPI * Pad::V_PITCH) = v;
             }
             if (bad) odd = 1;
+            if (tid < 1) *(u32x2*)tile_scales[slot & 3u] = u32x2{f.ks, f.vs};
         }
     };
     if (tid == 0) odd = 0;
@@ -479,15 +490,19 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
         return fmaxf(fmaxf(fmaxf(m0, x[14]), x[15]), m1);
     };
     float top = largest(st[0]);                                        // of this lane's scores of the tile to be weighed
-    // Scales of the tile to be weighed: of its scores, and what its V scale comes to.
-    float ks = 1.0f, vs = 1.0f, most = 0.0f;
-    auto scales_of = [&](uint32_t tile) __attribute__((always_inline)) {
-        const bool held = tile < j.cache_blocks;
-        const uint32_t i = held ? (tile * TREE_MANY_KEYS) >> a.block_log2 : 0u;
-        ks = ksp[i]; vs = vsp[i];
-        if (!held) { ks = 1.0f; vs = 1.0f; }
+    // Scales of the tile to be weighed, read from LDS while the one before is.
+    float ks, vs, most = 0.0f;
+    auto scales_of = [&](uint32_t slot) __attribute__((always_inline)) {
+        const u32x2 x = *(const u32x2*)tile_scales[slot & 3u];
+        const uint32_t k = x[0], v = x[1];
+        ks = __builtin_bit_cast(float, k);
+        vs = __builtin_bit_cast(float, v);
     };
-    float of = 0.0f, off = 0.0f, back = 1.0f;                          // the V scale that off and back are of: its logarithm relative to `most`, and the inverse
+    scales_of(0);
+    // Of the V scale `of` (its bits): the logarithm of what it is of `most`, and the inverse.  What is below 2^-60 of that counts for nothing: fp16
+    // weights would be zeros, and a sum in 32 bits could not be divided.
+    uint32_t of = ~0u, none = 0;
+    float off = 0.0f, back = 1.0f;
     // Weights of the tile whose scores are in `sx`, into `px`; scores of the next tile (in slot `next`) into `sy`, and their largest; output of the
     // one before (in slot `before`) with `py`.
     auto segment = [&](f32x16& sx, V8 (&px)[2], f32x16& sy, const V8 (&py)[2], const char* next, const char* before, bool masked, uint32_t vis)
@@ -503,24 +518,25 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
             top = largest(sx);
         }
         float alpha = 1.0f, unit = 1.0f;
-        if (vs != of) {                                                // (once a block)
-            of = vs;
-            if (vs > most) { unit = most / vs; most = vs; }
-            const float r = vs / most;
-            off = __builtin_amdgcn_logf(r);
-            back = 1.0f / r;
+        uint32_t larger = 0;
+        if (uni(__builtin_bit_cast(uint32_t, vs)) != of) {             // (once a block)
+            of = uni(__builtin_bit_cast(uint32_t, vs));
+            larger = uni(vs > most ? 1u : 0u);
+            const float inverse = __builtin_amdgcn_rcpf(vs);
+            if (larger) { unit = most * inverse; most = vs; }
+            none = uni(vs == 0.0f || vs < most * 0x1p-60f ? 1u : 0u);
+            back = none ? 1.0f : most * inverse;                       // (off by the reciprocal's rounding, as off then is)
+            off = none ? 0.0f : -__builtin_amdgcn_logf(back);
         }
-        // What is 2^-60 of the largest scale, or zeros, counts for nothing: fp16 weights would be zeros, and the sum in 32 bits could not be divided.
-        const bool none = vs < most * 0x1p-60f || vs == 0.0f;
         const float by = sc * ks, mx = max_halves(top) * by;
-        bool grown = __ballot(mx > row.m + WEIGHT_SLACK) != 0;         // (rarely, after the first steps)
+        const bool grown = __ballot(mx > row.m + WEIGHT_SLACK) != 0;         // (rarely, after the first steps)
         if (grown) {
             const float m_new = fmaxf(row.m, mx);
             alpha = row.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(row.m - m_new);
             row.m = m_new;
             row.l *= alpha;
         }
-        const float ref = (row.m == -INFINITY ? 0.0f : row.m) - WEIGHT_OFF<T> - (none ? 0.0f : off);   // no key seen yet: keep the exponents finite
+        const float ref = (row.m == -INFINITY ? 0.0f : row.m) - WEIGHT_OFF<T> - off;   // no key seen yet: keep the exponents finite
         float sum[2] = {0.0f, 0.0f}, x0 = 0.0f, x1 = 0.0f, m0 = -INFINITY, m1 = -INFINITY;
         auto weigh = [&](int v, int half) __attribute__((always_inline)) {       // scores v and v + 1, in two halves
             if (half == 0) {
@@ -551,10 +567,10 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
         }
         asm volatile("" ::"v"(px[0]), "v"(px[1]), "v"(sum[0]), "v"(sum[1]), "v"(m0), "v"(m1));   // (computed here, and not where they are used)
         __builtin_amdgcn_sched_barrier(0);
-        row.l = __builtin_fmaf(sum[0] + sum[1], none ? 1.0f : back, row.l);
+        row.l = __builtin_fmaf(sum[0] + sum[1], back, row.l);
         top = fmaxf(m0, m1);
-        if (none) px[0] = px[1] = V8{};
-        if (grown || unit != 1.0f) {                                   // what was added so far went by the reference value and unit before
+        if (__builtin_expect(none, 0)) px[0] = px[1] = V8{};
+        if (grown || larger) {                                         // what was added so far went by the reference value and unit before
             alpha *= unit;
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -571,9 +587,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
             vis = wide_bits(args, j, token, first, tile < end && first < j.drafted ? min(32u, j.drafted - first) : 0u);
         }
         const uint32_t slot = tile - j.begin;
-        scales_of(tile);
         // (behind the last tile the scores are of whatever the slot holds, and not used)
         segment(st[odd_one], pf[odd_one], st[odd_one ^ 1], pf[odd_one ^ 1], lds + ((slot + 1) & 3u) * SLOT, lds + ((slot - 1) & 3u) * SLOT, wide || tile >= end, tile >= end ? 0u : vis);
+        scales_of(slot + 1);
         put(staged[odd_one], tile + 2);
         fetch(args, staged[odd_one], tile + 4);
         __syncthreads();                                               // the tile put is in its slot, the one read is done with
@@ -582,13 +598,11 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
     // The bulk: tiles of 8 bits up to the last one fetched, without the general step's branches.
     const uint32_t whole = min(end, j.cache_blocks);
     if (tile + 5 < whole) {
-        scales_of(tile);
         auto quick = [&](int odd_one, uint32_t slot) __attribute__((always_inline)) {
             segment(st[odd_one], pf[odd_one], st[odd_one ^ 1], pf[odd_one ^ 1], lds + ((slot + 1) & 3u) * SLOT, lds + ((slot - 1) & 3u) * SLOT, false, ~0u);
-            const uint32_t next = j.begin + slot;
+            scales_of(slot + 1);
             put8(staged[odd_one], slot + 2);
-            fetch8(staged[odd_one], next + 4);
-            scales_of(next + 1);
+            fetch8(staged[odd_one], j.begin + slot + 4);
             __syncthreads();
         };
         for (; tile + 5 < whole; tile += 2) {
