@@ -681,6 +681,7 @@ typedef struct {
     int32_t* n_accepted; int32_t* next;                 /* [batch]                                                                 */
 } depsync_verify_drafts_desc;
 int dep_verify_drafts(const depsync_verify_drafts_desc* d, void* workspace, size_t workspace_bytes, void* stream);
+/* Goes by the sizes, and by whether q and parents are given.                                                                             */
 int depsync_verify_drafts_workspace(const depsync_verify_drafts_desc* d, size_t* bytes);
 
 /* ---- host mirrors of the device index arithmetic (Fig. 4b; Section II-A) -------------- */

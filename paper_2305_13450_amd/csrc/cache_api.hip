@@ -155,6 +155,16 @@ int verify_check(const depsync_verify_drafts_desc* d) {
     return d && d->batch >= 1 && d->batch <= 1 << 20 && d->tokens >= 1 && d->tokens <= 65536 && d->vocab >= 1 && d->vocab <= 1 << 24 ? DEPSYNC_OK : DEPSYNC_EINVAL;
 }
 
+// How dep_verify_drafts spreads its rows.
+void verify_plan(const depsync_verify_drafts_desc* d, VerifyArgs& a, size_t& bytes) {
+    a.launches = 0;
+    a.pieces = (uint32_t)std::min<int64_t>(VERIFY_PIECES, std::min<int64_t>(cdiv64(d->vocab, 1024), 1024 / d->batch));
+    if (a.pieces >= 2 && d->vocab >= 16384) a.launches = d->q && d->parents ? 1 + (uint32_t)std::min(std::max(d->tokens - 2, 0), 6) : 1;
+    if (!a.launches) a.pieces = 1;
+    a.piece = (uint32_t)cdiv64(cdiv64(d->vocab, a.pieces), 256) * 256;
+    bytes = (size_t)a.launches * d->batch * (sizeof(VerifyState) + a.pieces * sizeof(double));
+}
+
 // Strides of [batch][tokens][vocab] numbers, those of dimensions of size one not read.
 bool rows(int64_t& batch, int64_t& token, int64_t given_batch, int64_t given_token, const depsync_verify_drafts_desc* d) {
     batch = d->batch > 1 ? given_batch : 0;
@@ -371,7 +381,8 @@ int dep_qk_norm_rope(const depsync_qk_norm_rope_desc* d, void* stream) {
 int depsync_verify_drafts_workspace(const depsync_verify_drafts_desc* d, size_t* bytes) {
     if (!bytes) return DEPSYNC_EINVAL;
     if (int rc = verify_check(d); rc != DEPSYNC_OK) return rc;
-    *bytes = 0;
+    VerifyArgs a = {};
+    verify_plan(d, a, *bytes);
     return DEPSYNC_OK;
 }
 
@@ -387,6 +398,9 @@ int dep_verify_drafts(const depsync_verify_drafts_desc* d, void* workspace, size
     a.p = d->p; a.q = d->q; a.ids = d->ids; a.parents = d->parents; a.parents_batch = d->parents_batch; a.drafted = d->drafted; a.u = d->u;
     a.accepted = d->accepted; a.n_accepted = d->n_accepted; a.next = d->next;
     a.batch = d->batch; a.tokens = d->tokens; a.vocab = d->vocab;
+    verify_plan(d, a, need);
+    a.sums = static_cast<double*>(workspace);
+    a.states = reinterpret_cast<VerifyState*>(a.sums + (size_t)a.launches * d->batch * a.pieces);
     const hipError_t e = launch_verify_drafts(a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);
 }

@@ -61,14 +61,27 @@ struct QkNormArgs {
     float eps;
 };
 
+// How far a sequence has come: what is left of the last token's probabilities, that token, how many stay, and the token to be looked at next.
+struct VerifyState {
+    double C, R;
+    uint32_t last, n, at;
+    uint32_t stale;                       // R is of before the last refusal
+    uint32_t sums, unused;                // one more than the launch whose sums the next token is drawn by; 0: none yet
+};
+
 struct VerifyArgs {
     const float *p, *q;                   // q may be null
     const int32_t *ids, *parents, *drafted;   // the last two may be null
     const float* u;
     int32_t *accepted, *n_accepted, *next;
     int64_t p_batch, p_token, q_batch, q_token, parents_batch;
+    VerifyState* states;                  // workspace: [launches][batch], and [launches][batch][pieces] sums
+    double* sums;
     uint32_t batch, tokens, vocab;
+    uint32_t launches, launch;            // that spread rows over several workgroups, before the last one (0: none); the present one
+    uint32_t pieces, piece;               // workgroups to a row, numbers that each sums
 };
+constexpr uint32_t VERIFY_PIECES = 64;    // at most
 
 struct CacheAppendArgs {
     const void *k_new, *v_new;

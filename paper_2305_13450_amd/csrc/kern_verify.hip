@@ -1,4 +1,11 @@
 // Verification of drafted tokens against the target's probabilities.
+//
+// Whether a token stays is decided in 64 bits: the products are then exact or nearly so, and a sum of 2^17 probabilities is off by 2^-50 or so, where
+// one in 32 bits is off by more than a rare token has, and a token next to a border would depend on the order of the sum.
+//
+// The refusals at a node add up: max(max(p - R0 q, 0) - R1 q, 0) = max(p - (R0 + R1) q, 0), so the weights left after any number of them are known from one
+// number C, and R, their sum, is asked for only where another child is looked at: a pass over the row (p and q).  What a sequence reads is a few numbers a
+// token, those passes, and the row that the next token is drawn from.
 #include <hip/hip_runtime.h>
 
 #include "cache_ops.h"
@@ -18,197 +25,334 @@ __device__ __forceinline__ double lane_value(double x, uint32_t lane) {
     return __builtin_bit_cast(double, lo | hi << 32);
 }
 __device__ __forceinline__ uint32_t lane_word(uint32_t x, uint32_t lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, (int)lane); }
-
-constexpr uint32_t VERIFY_WAVES = 16, FILTER = 1 << 15, LISTED = 256;
-
-// One workgroup to a sequence.
-//
-// Whether a token stays is decided in 64 bits: the products are then exact or nearly so, and a sum of 2^17 probabilities is off by 2^-50 or so, where
-// one in 32 bits is off by more than a rare token has, and a token next to a border would depend on the order of the sum.
-//
-// The refusals at a node add up: max(max(p - R0 q, 0) - R1 q, 0) = max(p - (R0 + R1) q, 0), so the weights left after any number of them are known from one
-// number C, and R, their sum, is asked for only where another child is looked at: a pass over the row (p and q), by the whole workgroup.
-// Tokens are taken up in lots of 64, a lane each (in every wave alike): children of the last token that stays are found by a ballot.
-template <bool DRAWN>
-__global__ __launch_bounds__(64 * VERIFY_WAVES) void verify_drafts_kernel(const VerifyArgs a) {
-    __shared__ double sums[VERIFY_WAVES];
-    __shared__ uint32_t filter[FILTER / 32], refused_ids[LISTED], n_refused;
-    const uint32_t b = blockIdx.x, lane = threadIdx.x & 63u, wave = uni(threadIdx.x >> 6);
-    const uint32_t drafted = uni(a.drafted ? clamp_count(a.drafted[b], a.tokens) : a.tokens);
-    if (drafted == 0) {
-        if (threadIdx.x == 0) a.n_accepted[b] = 0;
-        return;
+// Sums up to each lane, by DPP: rows of 16 lanes, then each row's last lane to the next row, and lane 31 to the upper half.
+__device__ __forceinline__ double sums_to(double x) {
+#define DS_DPP(ctrl, rows) { \
+        const uint64_t bits = __builtin_bit_cast(uint64_t, x); \
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)bits, ctrl, rows, 0xf, false), \
+                       hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(bits >> 32), ctrl, rows, 0xf, false); \
+        x += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo); \
     }
-    const float* const P = a.p + (int64_t)b * a.p_batch;
-    const float* const Q = DRAWN ? a.q + (int64_t)b * a.q_batch : nullptr;
-    const int32_t* const ids = a.ids + (size_t)b * a.tokens;
-    const int32_t* const parents = a.parents ? a.parents + (int64_t)b * a.parents_batch : nullptr;
-    auto parent_of = [&](uint32_t t) __attribute__((always_inline)) { return parents ? parents[t] : (int32_t)t - 1; };
-    // the sum of x over the workgroup, the same in every thread
-    auto everywhere = [&](double x) __attribute__((always_inline)) {
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
-        __syncthreads();                                                 // (the sums of the call before are read)
-        if (lane == 0) sums[wave] = x;
-        __syncthreads();
-        double s = 0.0;
-#pragma unroll
-        for (uint32_t w = 0; w < VERIFY_WAVES; ++w) s += sums[w];
-        return s;
-    };
-    uint32_t last = 0, n = 1;
-    double C = 0.0, R = 1.0;
-    bool stale = false;                                                  // R is of before the last refusal
-    if (threadIdx.x == 0) a.accepted[(size_t)b * a.tokens] = 0;
-    for (uint32_t t0 = 0; t0 < drafted; t0 += 64) {
+    DS_DPP(0x111, 0xf) DS_DPP(0x112, 0xf) DS_DPP(0x114, 0xf) DS_DPP(0x118, 0xf)   // row_shr 1, 2, 4, 8
+    DS_DPP(0x142, 0xa) DS_DPP(0x143, 0xc)                                        // row_bcast 15, 31
+#undef DS_DPP
+    return x;
+}
+__device__ __forceinline__ double wave_sum(double x) { return lane_value(sums_to(x), 63); }
+
+// A sequence's arrays.
+struct Drafts {
+    const float *p, *q;
+    const int32_t *ids, *parents;
+    uint32_t drafted;
+    __device__ __forceinline__ Drafts(const VerifyArgs& a, uint32_t b)
+        : p(a.p + (int64_t)b * a.p_batch), q(a.q ? a.q + (int64_t)b * a.q_batch : nullptr), ids(a.ids + (size_t)b * a.tokens),
+          parents(a.parents ? a.parents + (int64_t)b * a.parents_batch : nullptr), drafted(uni(a.drafted ? clamp_count(a.drafted[b], a.tokens) : a.tokens)) {}
+    __device__ __forceinline__ int32_t parent(uint32_t t) const { return parents ? parents[t] : (int32_t)t - 1; }
+};
+
+// From s.at on; every wave that calls this does the same.  Tokens are taken up in lots of 64, a lane each: the children of the last one that stays are found by a ballot.
+// Where R is needed and stale: pass(s) renews it, or returns false, and so does this then.
+template <bool DRAWN, class Pass>
+__device__ __forceinline__ bool verify_walk(const VerifyArgs& a, uint32_t b, const Drafts& d, VerifyState& s, bool write, Pass pass) {
+    const uint32_t lane = threadIdx.x & 63u;
+    if (write && s.at == 1) a.accepted[(size_t)b * a.tokens] = 0;
+    for (uint32_t t0 = s.at & ~63u; t0 < d.drafted; t0 += 64) {
         const uint32_t t = t0 + lane;
         int32_t parent = -1, id = -1;
         double u = 0.0, px = 0.0, qx = 0.0;
-        if (t < drafted && t > 0) {
-            parent = parent_of(t);
-            id = ids[t];
+        if (t < d.drafted && t > 0) {
+            parent = d.parent(t);
+            id = d.ids[t];
             u = unit(a.u[(size_t)b * a.tokens + t]);
             if (parent >= 0 && (uint32_t)parent < t && id >= 0 && (uint32_t)id < a.vocab) {
-                px = mass(P[(int64_t)parent * a.p_token + id]);
-                if (DRAWN) qx = mass(Q[(int64_t)parent * a.q_token + id]);
+                px = mass(d.p[(int64_t)parent * a.p_token + id]);
+                if (DRAWN) qx = mass(d.q[(int64_t)parent * a.q_token + id]);
             } else {
                 id = -1;
             }
         }
         uint64_t refused = 0;                                            // of this lot, at this node
-        uint64_t open = __ballot(t > last && parent == (int32_t)last);
+        uint64_t open = __ballot(t > s.last && t >= s.at && parent == (int32_t)s.last);
         while (open) {
             const uint32_t i = (uint32_t)__builtin_ctzll(open);
-            open &= open - 1;
             const uint32_t x = lane_word((uint32_t)id, i);
             const double ux = lane_value(u, i);
             double w = lane_value(px, i), test;
             if (DRAWN) {
-                if (stale) {
-                    const float *p = P + (int64_t)last * a.p_token, *q = Q + (int64_t)last * a.q_token;
-                    double s = 0.0;
-                    for (uint32_t v = threadIdx.x; v < a.vocab; v += 64 * VERIFY_WAVES) s += fmax(mass(p[v]) - C * mass(q[v]), 0.0);
-                    R = everywhere(s);
-                    stale = false;
+                if (s.stale) {
+                    s.at = t0 + i;
+                    if (!pass(s)) return false;
+                    s.stale = 0;
                 }
                 const double qv = lane_value(qx, i);
-                w = fmax(w - C * qv, 0.0);
-                test = ux * qv * R;
+                w = fmax(w - s.C * qv, 0.0);
+                test = ux * qv * s.R;
             } else {
                 // a token refused here before has nothing left
                 bool again = (__ballot((uint32_t)id == x) & refused) != 0;
                 for (uint32_t e0 = 0; e0 < t0 && !again; e0 += 64) {
                     const uint32_t e = e0 + lane;
-                    again = __ballot(e > last && parent_of(e) == (int32_t)last && (uint32_t)ids[e] == x) != 0;
+                    again = __ballot(e > s.last && d.parent(e) == (int32_t)s.last && (uint32_t)d.ids[e] == x) != 0;
                 }
                 if (again) w = 0.0;
-                test = ux * R;
+                test = ux * s.R;
             }
+            open &= open - 1;
             if ((int32_t)x >= 0 && test < w) {
-                last = t0 + i;
-                if (threadIdx.x == 0) a.accepted[(size_t)b * a.tokens + n] = (int32_t)last;
-                ++n;
-                C = 0.0; R = 1.0; stale = false;
+                s.last = t0 + i;
+                if (write) a.accepted[(size_t)b * a.tokens + s.n] = (int32_t)s.last;
+                ++s.n;
+                s.C = 0.0; s.R = 1.0; s.stale = 0;
                 refused = 0;
-                open = __ballot(t > last && parent == (int32_t)last);
+                open = __ballot(t > s.last && parent == (int32_t)s.last);
             } else if ((int32_t)x >= 0) {
                 refused |= 1ull << i;
-                if (DRAWN) { C += R; stale = true; }
-                else R = fmax(R - w, 0.0);
+                if (DRAWN) { s.C += s.R; s.stale = 1; }
+                else s.R = fmax(s.R - w, 0.0);
             }
         }
     }
-    // ---- the next token ----
-    if (threadIdx.x == 0) a.n_accepted[b] = (int32_t)n;
-    const float *p = P + (int64_t)last * a.p_token, *q = DRAWN ? Q + (int64_t)last * a.q_token : nullptr;
-    if (!DRAWN) {
-        // The children refused, whose probabilities count for nothing: their numbers, and a filter of 2^15 bits by which hardly any other token is compared with them.
-        for (uint32_t w = threadIdx.x; w < FILTER / 32; w += 64 * VERIFY_WAVES) filter[w] = 0;
-        __syncthreads();
-        if (wave == 0) {
-            uint32_t count = 0;
-            for (uint32_t t0 = last & ~63u; t0 < drafted; t0 += 64) {
-                const uint32_t t = t0 + lane;
-                const bool child = t > last && t < drafted && parent_of(t) == (int32_t)last;
-                const uint32_t id = child ? (uint32_t)ids[t] : 0u;
-                const uint64_t children = __ballot(child);
-                const uint32_t at = count + (uint32_t)__builtin_popcountll(children & ((1ull << lane) - 1));
-                if (child) atomicOr(&filter[id % FILTER / 32], 1u << (id % 32));
-                if (child && at < LISTED) refused_ids[at] = id;
-                count += (uint32_t)__builtin_popcountll(children);
-            }
-            if (lane == 0) n_refused = count;
+    s.at = d.drafted;
+    return true;
+}
+
+// The children refused at the last token that stays, without q: their probabilities count for nothing.  Their numbers, and a filter of 2^15 bits by which
+// hardly any other token is compared with them.
+constexpr uint32_t FILTER = 1 << 15, LISTED = 256;
+struct Refused { uint32_t filter[FILTER / 32], ids[LISTED], n; };
+template <uint32_t THREADS>
+__device__ __forceinline__ void list_refused(Refused& r, const Drafts& d, uint32_t last) {
+    const uint32_t lane = threadIdx.x & 63u;
+    for (uint32_t w = threadIdx.x; w < FILTER / 32; w += THREADS) r.filter[w] = 0;
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        uint32_t count = 0;
+        for (uint32_t t0 = last & ~63u; t0 < d.drafted; t0 += 64) {
+            const uint32_t t = t0 + lane;
+            const bool child = t > last && t < d.drafted && d.parent(t) == (int32_t)last;
+            const uint32_t id = child ? (uint32_t)d.ids[t] : 0u;
+            const uint64_t children = __ballot(child);
+            const uint32_t at = count + (uint32_t)__builtin_popcountll(children & ((1ull << lane) - 1));
+            if (child) atomicOr(&r.filter[id % FILTER / 32], 1u << (id % 32));
+            if (child && at < LISTED) r.ids[at] = id;
+            count += (uint32_t)__builtin_popcountll(children);
         }
-        __syncthreads();
+        if (lane == 0) r.n = count;
     }
-    bool whole = false;                                                  // p as it is
-    auto refused_here = [&](uint32_t v) __attribute__((always_inline)) {
-        if (n_refused <= LISTED) {
-            for (uint32_t e = 0; e < n_refused; ++e)
-                if (refused_ids[e] == v) return true;
-        } else {
-            for (uint32_t t = last + 1; t < drafted; ++t)
-                if (parent_of(t) == (int32_t)last && (uint32_t)ids[t] == v) return true;
-        }
-        return false;
-    };
-    auto weight = [&](uint32_t v) __attribute__((always_inline)) {
+    __syncthreads();
+}
+__device__ __noinline__ bool is_refused(const Refused& r, const Drafts& d, uint32_t last, uint32_t v) {
+    if (r.n <= LISTED) {
+        for (uint32_t e = 0; e < r.n; ++e)
+            if (r.ids[e] == v) return true;
+    } else {
+        for (uint32_t t = last + 1; t < d.drafted; ++t)
+            if (d.parent(t) == (int32_t)last && (uint32_t)d.ids[t] == v) return true;
+    }
+    return false;
+}
+
+// The weight of a token in a row.
+template <bool DRAWN> struct Weights {
+    const float *p, *q;
+    double C;
+    const Refused& refused;
+    const Drafts& d;
+    uint32_t last;
+    bool whole;                          // p as it is
+    __device__ __forceinline__ Weights(const VerifyArgs& a, const Drafts& drafts, const VerifyState& s, const Refused& r)
+        : p(drafts.p + (int64_t)s.last * a.p_token), q(DRAWN ? drafts.q + (int64_t)s.last * a.q_token : nullptr), C(s.C), refused(r), d(drafts), last(s.last), whole(false) {}
+    __device__ __forceinline__ double operator()(uint32_t v) const {
         const double w = mass(p[v]);
         if (whole) return w;
         if (DRAWN) return fmax(w - C * mass(q[v]), 0.0);
-        if ((filter[v % FILTER / 32] >> (v % 32) & 1u) && refused_here(v)) return 0.0;
+        if ((refused.filter[v % FILTER / 32] >> (v % 32) & 1u) && is_refused(refused, d, last, v)) return 0.0;
         return w;
-    };
-    // Where the sum passes the target: a run is cut into 16 pieces, a wave sums each, and the piece that the target lies in is the next run.  Where rounding
-    // leaves none, it is the last one that has any weight.
+    }
+};
+
+constexpr uint32_t VERIFY_WAVES = 16;
+
+// The sum of x over a workgroup of `WAVES` waves, the same in every thread; sums[w] stays the sum of wave w until the next call.
+template <uint32_t WAVES> __device__ __forceinline__ double everywhere(double x, double* sums) {
+    x = wave_sum(x);
+    __syncthreads();                                                     // (the sums of the call before are read)
+    if ((threadIdx.x & 63u) == 0) sums[threadIdx.x >> 6] = x;
+    __syncthreads();
+    double s = 0.0;
+#pragma unroll
+    for (uint32_t w = 0; w < WAVES; ++w) s += sums[w];
+    return s;
+}
+
+// The piece whose sum, added to `before` and those in front of it, passes the target: `before` becomes the sum in front of it.  A lane holds each (64 at most, others
+// 0).  Where rounding leaves none it is the last that has any weight, and the target infinity.
+__device__ __forceinline__ uint32_t find_piece(double mine, double& before, double& target) {
+    const double upto = sums_to(mine);
+    const uint64_t over = __ballot(before + upto > target && mine > 0.0), some = __ballot(mine > 0.0);
+    if (!over) target = INFINITY;
+    const uint32_t hit = over ? (uint32_t)__builtin_ctzll(over) : some ? 63u - (uint32_t)__builtin_clzll(some) : 0u;
+    if (hit) before += lane_value(upto, hit - 1);
+    return hit;
+}
+
+// The rest of a sequence in one workgroup: the walk with its passes, and the next token.
+// Where the sum passes the target: a run is cut into 16 pieces, a wave sums each, and the piece that the target lies in is the next run, until that is short enough for registers.
+// piece_sum: of an earlier launch, of the row's pieces of `size` numbers, one a lane (size 0: there are none).
+template <bool DRAWN>
+__device__ __forceinline__ void verify_rest(const VerifyArgs& a, uint32_t b, const Drafts& d, VerifyState& s, double piece_sum, uint32_t size, double* sums, Refused& refused) {
+    constexpr uint32_t SHORT = VERIFY_WAVES * 256;
+    const uint32_t lane = threadIdx.x & 63u, wave = uni(threadIdx.x >> 6);
+    if (size == 0)
+        verify_walk<DRAWN>(a, b, d, s, threadIdx.x == 0, [&](VerifyState& st) __attribute__((always_inline)) {
+            const Weights<DRAWN> weight(a, d, st, refused);
+            double x = 0.0;
+            if constexpr (DRAWN) {
+#pragma unroll 8
+                for (uint32_t v = threadIdx.x; v < a.vocab; v += 64 * VERIFY_WAVES) x += weight(v);
+            }
+            st.R = everywhere<VERIFY_WAVES>(x, sums);
+            return true;
+        });
+    if (threadIdx.x == 0) a.n_accepted[b] = (int32_t)s.n;
+    if (!DRAWN) list_refused<64 * VERIFY_WAVES>(refused, d, s.last);
+    Weights<DRAWN> weight(a, d, s, refused);
     uint32_t begin = 0, end = a.vocab;
     double before = 0.0, target = -1.0;                                  // the sum in front of the run
+    const double u = unit(a.u[(size_t)b * a.tokens]);
     int32_t next = -1;
-    for (;;) {
+    if (size) {
+        const double all = wave_sum(piece_sum);
+        if (all > 0.0) {
+            target = u * all;
+            begin = find_piece(piece_sum, before, target) * size;
+            end = min(end, begin + size);
+        } else {
+            weight.whole = true;
+        }
+    }
+    bool done = false;
+    while (end - begin > SHORT || target < 0.0) {
         const uint32_t piece = ((end - begin + VERIFY_WAVES - 1) / VERIFY_WAVES + 63) & ~63u;
         const uint32_t from = begin + wave * piece, to = min(end, from + piece);
-        double s = 0.0;
-#pragma unroll 4
-        for (uint32_t v = from + lane; v < to; v += 64) s += weight(v);
-        const double all = everywhere(s);
+        double x = 0.0;
+#pragma unroll 8
+        for (uint32_t v = from + lane; v < to; v += 64) x += weight(v);
+        const double all = everywhere<VERIFY_WAVES>(x, sums);
         if (target < 0.0) {                                              // the first run is the row
             if (!(all > 0.0)) {
-                if (whole) break;
-                whole = true;
+                done = weight.whole;                                     // nothing at all: -1
+                if (done) break;
+                weight.whole = true;
                 continue;
             }
-            target = unit(a.u[(size_t)b * a.tokens]) * all;
+            target = u * all;
         }
-        uint32_t hit = VERIFY_WAVES, some = 0;
-        double sum = before, in_front = before, in_front_of_some = before;
-        for (uint32_t w = 0; w < VERIFY_WAVES; ++w) {
-            if (sums[w] > 0.0) { some = w; in_front_of_some = sum; }
-            if (hit == VERIFY_WAVES && sum + sums[w] > target) { hit = w; in_front = sum; }
-            sum += sums[w];
-        }
-        if (hit == VERIFY_WAVES) { hit = some; in_front = in_front_of_some; target = INFINITY; }
-        before = in_front;
-        begin += hit * piece;
+        begin += find_piece(lane < VERIFY_WAVES ? sums[lane] : 0.0, before, target) * piece;
         end = min(end, begin + piece);
-        if (piece == 64) {
-            const double w = begin + lane < end ? weight(begin + lane) : 0.0;
-            double upto = w;
+    }
+    if (!done) {
+        // 256 numbers to a wave, four to a lane, in order from 64 to 64
+        double upto[4], w[4], x = 0.0;
 #pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const double y = __shfl_up(upto, d);
-                if (lane >= (uint32_t)d) upto += y;
-            }
-            const uint64_t over = __ballot(before + upto > target && w > 0.0), any = __ballot(w > 0.0);
-            next = (int32_t)(begin + (over ? (uint32_t)__builtin_ctzll(over) : 63u - (uint32_t)__builtin_clzll(any | 1u)));
-            break;
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t v = begin + wave * 256 + k * 64 + lane;
+            w[k] = v < end ? weight(v) : 0.0;
         }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            upto[k] = sums_to(w[k]) + x;
+            x = lane_value(upto[k], 63);
+        }
+        __syncthreads();
+        if (lane == 0) sums[wave] = x;
+        __syncthreads();
+        const uint32_t hit = find_piece(lane < VERIFY_WAVES ? sums[lane] : 0.0, before, target);
+        if (wave != hit) return;
+        uint32_t last_some = 0;
+        bool found = false;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint64_t over = __ballot(before + upto[k] > target && w[k] > 0.0), any = __ballot(w[k] > 0.0);
+            if (over && !found) { found = true; next = (int32_t)(begin + hit * 256 + k * 64 + (uint32_t)__builtin_ctzll(over)); }
+            if (any) last_some = k * 64 + 63u - (uint32_t)__builtin_clzll(any);
+        }
+        if (!found) next = (int32_t)(begin + hit * 256 + last_some);
+        if (lane == 0) a.next[b] = next;
+        return;
     }
     if (threadIdx.x == 0) a.next[b] = next;
 }
 
+// One workgroup to a sequence.
+template <bool DRAWN>
+__global__ __launch_bounds__(64 * VERIFY_WAVES) void verify_drafts_kernel(const VerifyArgs a) {
+    __shared__ double sums[VERIFY_WAVES];
+    __shared__ Refused refused;
+    const uint32_t b = blockIdx.x;
+    const Drafts d(a, b);
+    if (d.drafted == 0) {
+        if (threadIdx.x == 0) a.n_accepted[b] = 0;
+        return;
+    }
+    VerifyState s = {0.0, 1.0, 0, 1, 1, 0, 0, 0};
+    double piece_sum = 0.0;
+    if (a.launches) {                                                    // what earlier launches found out
+        s = a.states[(size_t)(a.launches - 1) * a.batch + b];
+        const uint32_t lane = threadIdx.x & 63u;
+        if (lane < a.pieces) piece_sum = a.sums[((size_t)((s.sums ? s.sums : a.launches) - 1) * a.batch + b) * a.pieces + lane];
+        if (!s.sums) {
+            s.R = wave_sum(piece_sum);
+            s.stale = 0;
+        }
+    }
+    verify_rest<DRAWN>(a, b, d, s, piece_sum, s.sums ? a.piece : 0u, sums, refused);
+}
+
+// A row over several workgroups: each goes as far as it can without a pass (all of a sequence's do the same), leaves the sum of its piece of the
+// row that it came to, and the next launch goes on from there.
+template <bool DRAWN>
+__global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyArgs a) {
+    __shared__ double sums[4];
+    __shared__ Refused refused;
+    const uint32_t b = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces, lane = threadIdx.x & 63u;
+    const Drafts d(a, b);
+    if (d.drafted == 0) return;
+    VerifyState s = {0.0, 1.0, 0, 1, 1, 0, 0, 0};
+    VerifyState* const to = a.states + (size_t)a.launch * a.batch + b;
+    if (a.launch) {
+        s = a.states[(size_t)(a.launch - 1) * a.batch + b];
+        if (s.sums) {
+            if (piece == 0 && threadIdx.x == 0) *to = s;
+            return;
+        }
+        const double* const from = a.sums + ((size_t)(a.launch - 1) * a.batch + b) * a.pieces;
+        s.R = wave_sum(lane < a.pieces ? from[lane] : 0.0);
+        s.stale = 0;
+    }
+    if (verify_walk<DRAWN>(a, b, d, s, piece == 0 && threadIdx.x == 0, [](VerifyState&) { return false; })) s.sums = a.launch + 1;
+    if (!DRAWN) list_refused<256>(refused, d, s.last);
+    const Weights<DRAWN> weight(a, d, s, refused);
+    const uint32_t end = min(a.vocab, (piece + 1) * a.piece);
+    double x = 0.0;
+#pragma unroll 8
+    for (uint32_t v = piece * a.piece + threadIdx.x; v < end; v += 256) x += weight(v);
+    x = everywhere<4>(x, sums);
+    if (threadIdx.x == 0) {
+        a.sums[((size_t)a.launch * a.batch + b) * a.pieces + piece] = x;
+        if (piece == 0) *to = s;
+    }
+}
+
 }  // namespace
 
-hipError_t launch_verify_drafts(const VerifyArgs& a, hipStream_t stream) {
+hipError_t launch_verify_drafts(const VerifyArgs& args, hipStream_t stream) {
+    VerifyArgs a = args;
+    for (a.launch = 0; a.launch < a.launches; ++a.launch) {
+        const hipError_t e = a.q ? launch_one(verify_sums_kernel<true>, a.batch * a.pieces, 256, stream, a) : launch_one(verify_sums_kernel<false>, a.batch * a.pieces, 256, stream, a);
+        if (e != hipSuccess) return e;
+    }
     return a.q ? launch_one(verify_drafts_kernel<true>, a.batch, 64 * VERIFY_WAVES, stream, a) : launch_one(verify_drafts_kernel<false>, a.batch, 64 * VERIFY_WAVES, stream, a);
 }
 

@@ -524,7 +524,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
             larger = uni(vs > most ? 1u : 0u);
             const float inverse = __builtin_amdgcn_rcpf(vs);
             if (larger) { unit = most * inverse; most = vs; }
-            none = uni(vs == 0.0f || vs < most * 0x1p-60f ? 1u : 0u);
+            none = uni(vs < 0x1p-126f || vs < most * 0x1p-60f ? 1u : 0u);
             back = none ? 1.0f : most * inverse;                       // (off by the reciprocal's rounding, as off then is)
             off = none ? 0.0f : -__builtin_amdgcn_logf(back);
         }

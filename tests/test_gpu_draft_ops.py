@@ -299,13 +299,17 @@ def drawn_ids(g, q, parents):
 
 
 @pytest.mark.parametrize("B,T,V,shape", [(1, 1, 1, "chain"), (2, 1, 50, "chain"), (3, 6, 1000, "chain"), (5, 4, 50257, "chain"), (4, 16, 333, "tree"), (2, 64, 5000, "tree"),
-                                         (3, 65, 64, "tree"), (2, 200, 7, "tree"), (1, 32, 128000, "tree"), (40, 12, 1025, "tree")])
+                                         (3, 65, 64, "tree"), (2, 200, 7, "tree"), (1, 32, 128000, "tree"), (40, 12, 1025, "tree"), (3, 40, 16384, "star"), (2, 130, 20001, "star"),
+                                         (600, 3, 16500, "chain"), (2, 5, 300000, "star")])
 @pytest.mark.parametrize("drawn", [True, False], ids=["drawn", "likely"])
 def test_verification(B, T, V, shape, drawn):
     print("verify", B, T, V, shape, drawn, flush=True)
     g = gen(B + T + V)
     p, q = probabilities(g, B, T, V)
     parents = torch.arange(T, device="cuda").expand(B, T) - 1 if shape == "chain" else tree_of(g, B, T)[0]
+    if shape == "star":                                            # nearly all hang from the root: many refusals at one node
+        parents = torch.where(torch.arange(T, device="cuda") % 7 == 6, parents, 0)
+        parents[:, 0] = -1
     ids = drawn_ids(g, q, parents)
     words = None if shape == "chain" else parents.int().contiguous()
     for seed in range(3):
