@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 
@@ -48,10 +49,14 @@ bool base2_scale(float given, int head_dim, float& out) {
 int rows_hint(int max_cached, int capacity) { return max_cached == 0 ? capacity : std::min(max_cached, capacity); }
 
 int cu_count(int& n_cu) {
+    static std::atomic<int> known[64];               // of a device, once asked for (0: not yet)
     int dev = 0;
     if (hipError_t e = hipGetDevice(&dev); e != hipSuccess) return hip_fail(e);
+    if (dev >= 0 && dev < 64 && (n_cu = known[dev].load(std::memory_order_relaxed)) > 0) return DEPSYNC_OK;
     const hipError_t e = hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, dev);
-    return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);
+    if (e != hipSuccess) return hip_fail(e);
+    if (dev >= 0 && dev < 64) known[dev].store(n_cu, std::memory_order_relaxed);
+    return DEPSYNC_OK;
 }
 
 int tree_check(const depsync_tree_attn_desc* d) {
@@ -87,11 +92,15 @@ int tree_operands(const depsync_tree_attn_desc* d, TreeAttnArgs& a, int multiple
 // second kernel and the results' way there and back.  5.9 is what a second launch costs a program that waits for the host (one token of 12 heads over 500
 // rows 12.4 us in one launch, 15.5 in two); captured into a graph it is about 4 (12.1 and 11.6).  The lengths are the longest sequence's; the
 // kernels then share out the parts by the real ones.
-double tree_cost(int64_t base, int64_t part, int64_t blocks, int64_t pairs, int64_t rows, int64_t row_blocks, int head_dim, int n_cu, bool few) {
+// Over a cache of 8 bits (fitted to 31 shapes, 1 to 128 rows): a block takes the form for few rows 0.8 us for up to 16 rows of 128 and 1.1 for 32 (0.6 and 0.8 of 64) while its
+// workgroup is alone on a CU, 1.7 times as long where two share it; and HBM, which one workgroup a CU saturates, gives a tenth less to two.
+double tree_cost(int64_t base, int64_t part, int64_t blocks, int64_t pairs, int64_t rows, int64_t row_blocks, int head_dim, int n_cu, bool few, bool held) {
     const int64_t parts = cdiv64(blocks, part), groups = base * parts, slots = 2 * (int64_t)n_cu;
     const double at_once = (double)std::min(groups, slots), wide = head_dim / 128.0;
-    const double step = few ? 0.13 + 1.32 * wide : (at_once > n_cu ? 1.0 : at_once > n_cu / 2 ? 0.8 : 0.55) * (0.3 + 0.7 * wide);
-    const double hbm = at_once / row_blocks * (few ? TREE_FEW_KEYS : TREE_MANY_KEYS) * 4.0 * head_dim / 5.2e6;
+    double step = few ? 0.13 + 1.32 * wide : (at_once > n_cu ? 1.0 : at_once > n_cu / 2 ? 0.8 : 0.55) * (0.3 + 0.7 * wide);
+    if (few && held) step = (0.2 + 0.3 * wide + (rows <= 16 ? 0.15 : 0.3) * (1.0 + wide)) * (at_once > n_cu ? 1.7 : 1.0);
+    const double rate = held ? (at_once > n_cu ? 9.4e6 : 10.4e6) : 5.2e6;   // of a cached row's 4 bytes a dimension
+    const double hbm = at_once / row_blocks * (few ? TREE_FEW_KEYS : TREE_MANY_KEYS) * 4.0 * head_dim / rate;
     const double join = parts > 1 ? 5.9 + (double)parts * pairs * rows * (head_dim + 2) * 8.0 / 4e6 : 0.0;
     return (double)cdiv64(groups, slots) * (3.0 + part * std::cbrt(step * step * step + hbm * hbm * hbm)) + join;   // (between the larger and the sum)
 }
@@ -110,20 +119,20 @@ int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t
     // head of 64 over 120000, 73 and 62.  Between 100 and 270 MB it depends on how many sequences share them: 8 x 48 over 8000 67 and 64, but 16 x 64
     // over 4000 64 and 68, 4 x 52 over 8000 40 and 42, 16 x 40 over 2000 36 and 49.
     const int64_t cache_bytes = (int64_t)d->batch * d->kv_heads * rows_hint(d->max_cached, d->capacity) * d->head_dim * 4;
-    a.few = rows <= (cache_bytes < 100000000 ? 64 : 32);
+    a.few = rows <= (held || cache_bytes < 100000000 ? 64 : 32);
     const int64_t keys = a.few ? TREE_FEW_KEYS : TREE_MANY_KEYS, row_blocks = cdiv64(rows, a.few ? TREE_FEW_ROWS : TREE_MANY_ROWS);
     const int64_t pairs = (int64_t)d->batch * d->kv_heads, base = pairs * row_blocks;
     const int64_t wide = d->tokens + (held ? held - 1 : 0);        // rows of 16 bits behind those of full blocks
     const int64_t blocks = cdiv64(rows_hint(d->max_cached, d->capacity), keys) + cdiv64(wide, keys);
     int64_t part = blocks;
-    double best = tree_cost(base, part, blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few);
+    double best = tree_cost(base, part, blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few, held != 0);
     for (int64_t rounds = 1; rounds <= 4; ++rounds) {             // parts that fill the chip a whole number of times
         const int64_t parts = std::min(blocks, std::max<int64_t>(1, rounds * 2 * n_cu / base)), p = cdiv64(blocks, parts);
-        const double t = tree_cost(base, p, blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few);
+        const double t = tree_cost(base, p, blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few, held != 0);
         if (t < best) { best = t; part = p; }
         if (p + 1 > blocks) continue;
         for (int64_t q : {2 * p, 4 * p}) {                         // or fewer, where their results cost more
-            const double u = tree_cost(base, std::min(q, blocks), blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few);
+            const double u = tree_cost(base, std::min(q, blocks), blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few, held != 0);
             if (u < best) { best = u; part = std::min(q, blocks); }
         }
     }

@@ -256,17 +256,32 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
         const uint32_t at = (blk - j.cache_blocks) * TREE_FEW_KEYS + wave * 32;
         if (at >= j.drafted) break;
         const uint32_t there = min(32u, j.drafted - at);
-        f32x4 st[NR][2] = {};
+        V8 kf[2][2 * NJ];                                              // everything is asked for before anything is waited for
+        uint32_t vw[8][NB / 2];                                        // NB numbers of 8 rows each
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
             const T* const k = wide_row<T>(a, j, false, at + 16 * kt + n);
 #pragma unroll
-            for (int f = 0; f < 2 * NJ; ++f) {
-                const V8 kf = k ? *(const V8*)(k + 64 * (f / 2) + 16 * g + 8 * (f % 2)) : V8{};
-#pragma unroll
-                for (int r = 0; r < NR; ++r) st[r][kt] = mma16(kf, qf[r][f], st[r][kt]);
-            }
+            for (int f = 0; f < 2 * NJ; ++f) kf[kt][f] = k ? *(const V8*)(k + 64 * (f / 2) + 16 * g + 8 * (f % 2)) : V8{};
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const T* const v = wide_row<T>(a, j, true, at + 4 * g + (i < 4 ? i : 12 + i));
+            u32x4 x = {0, 0, 0, 0};
+            if (v) {
+                if constexpr (NB == 8) x = *(const u32x4*)(v + NB * n);
+                else { const u32x2 y = *(const u32x2*)(v + NB * n); x[0] = y[0]; x[1] = y[1]; }
+            }
+#pragma unroll
+            for (int w = 0; w < NB / 2; ++w) vw[i][w] = x[w];
+        }
+        f32x4 st[NR][2] = {};
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int f = 0; f < 2 * NJ; ++f)
+#pragma unroll
+                for (int r = 0; r < NR; ++r) st[r][kt] = mma16(kf[kt][f], qf[r][f], st[r][kt]);
         V8 high[NR], rest[NR];
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
@@ -276,16 +291,12 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
                 if (!(vis >> (16 * (v >> 2) + 4 * g + (v & 3)) & 1u)) st[r][v >> 2][v & 3] = -INFINITY;
             weigh(st[r], r, sc, 1.0f, high[r], rest[r]);
         }
-        uint32_t vw[8][NB / 2];                                        // NB numbers of 8 rows each
         bool bad = false;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const T* const v = wide_row<T>(a, j, true, at + 4 * g + (i < 4 ? i : 12 + i));
             u32x4 x = {0, 0, 0, 0};
-            if (v) {
-                if constexpr (NB == 8) x = *(const u32x4*)(v + NB * n);
-                else { const u32x2 y = *(const u32x2*)(v + NB * n); x[0] = y[0]; x[1] = y[1]; }
-            }
+#pragma unroll
+            for (int w = 0; w < NB / 2; ++w) x[w] = vw[i][w];
             bad |= without_not_finite<T>(x);
 #pragma unroll
             for (int w = 0; w < NB / 2; ++w) vw[i][w] = x[w];
