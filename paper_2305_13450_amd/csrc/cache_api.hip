@@ -327,6 +327,7 @@ int dep_tree_attn8(const depsync_tree_attn8_desc* d8, void* workspace, size_t wo
     a.k_scale = d8->k_scale; a.v_scale = d8->v_scale; a.k_tail = d8->k_tail; a.v_tail = d8->v_tail;
     a.block_log2 = d8->block == 32 ? 5 : d8->block == 64 ? 6 : 7;
     a.n_blocks = (uint32_t)(d->capacity / d8->block);
+    a.together = d->kv_heads > 1 && a.cache_s.head < 128 ? 1 : 0;
     a.parts = static_cast<float*>(workspace);
     const hipError_t e = d->dtype == DEPSYNC_BF16 ? launch_tree_attn8_bf16(a, D, static_cast<hipStream_t>(stream)) : launch_tree_attn8_f16(a, D, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);

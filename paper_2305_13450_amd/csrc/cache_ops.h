@@ -33,6 +33,7 @@ struct TreeAttn8Args : TreeAttnArgs {
     const void *k_tail, *v_tail;
     Strides tail_s;
     uint32_t block_log2, n_blocks;        // rows of a block, blocks of the capacity
+    uint32_t together;                    // 2^together units that follow one another run on one XCD
 };
 
 struct CacheAppend8Args {

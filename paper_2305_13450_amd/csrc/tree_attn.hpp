@@ -83,7 +83,8 @@ template <typename T> struct WeightPair {
     typedef T T2 __attribute__((ext_vector_type(2)));
     typedef uint16_t Bits __attribute__((ext_vector_type(2)));
     T2 high, rest;
-    __device__ __forceinline__ WeightPair(float a, float b) {
+    // infinite: values may be, so `rest` keeps to that least.
+    __device__ __forceinline__ WeightPair(float a, float b, bool infinite = true) {
         Bits least;
         if constexpr (__is_same(T, __bf16)) {
             const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
@@ -97,7 +98,7 @@ template <typename T> struct WeightPair {
             rest[1] = (T)(b - (float)high[1]);
             least = __builtin_elementwise_min(__builtin_bit_cast(Bits, high), Bits{1, 1});
         }
-        rest = __builtin_bit_cast(T2, __builtin_elementwise_max(__builtin_bit_cast(Bits, rest), least));
+        if (infinite) rest = __builtin_bit_cast(T2, __builtin_elementwise_max(__builtin_bit_cast(Bits, rest), least));
     }
 };
 

@@ -20,6 +20,14 @@ __device__ __forceinline__ TreeLengths tree_lengths(const TreeAttn8Args& a, uint
     return {n - held, held + (a.drafted ? clamp_count(a.drafted[b], a.tokens) : a.tokens), held};
 }
 
+// As tree_unit, but 2^together units that follow one another, heads of one sequence, run on one XCD: rows of 64 bytes share cache lines of 128 with their
+// neighbours' (4 tokens of 8 heads of 64 over 120001 rows: 47 us, and 36 so; where rows fill their lines it makes no difference to few rows, and 4 x 256 tokens
+// took 620 us for 518, the heads of the longest sequence being on fewer XCDs).
+__device__ __forceinline__ TreeUnit tree_unit8(uint32_t row_blocks, uint32_t together) {
+    const uint32_t slot = blockIdx.x >> 3, n = slot / row_blocks;
+    return {(((n >> together) * 8 + (blockIdx.x & 7u)) << together) + (n & ((1u << together) - 1u)), slot % row_blocks};
+}
+
 // Two of four 8-bit numbers as numbers of T.
 template <typename T> struct Held8;
 template <> struct Held8<__bf16> {
@@ -120,7 +128,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
     __shared__ float ml[4][ROWS][2];
     __shared__ uint32_t odd;                                           // a value of the stretch of 16 bits is not finite
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6), n = lane & 15u, g = lane >> 4;
-    const TreeUnit u = tree_unit((a.rows + ROWS - 1) / ROWS);
+    const TreeUnit u = tree_unit8((a.rows + ROWS - 1) / ROWS, a.together);
     if (u.unit >= a.slots * a.kv_heads) return;
     const TreeJob j = tree_job(a, u.unit, TREE_FEW_KEYS);
     const uint32_t r0 = u.row_block * ROWS;
@@ -184,9 +192,11 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
         for (int b = 0; b < NB; ++b) o[r][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
     const float sc = a.scale;
-    // Weights of a tile's scores, times `vs`, as two fragments of products with values of U, which hold twice the bits of one.
-    auto weigh = [&](f32x4 (&st)[2], int r, float by, float vs, auto& high, auto& rest) __attribute__((always_inline)) {
+    // Weights of a tile's scores, times its V scale, as two fragments of products with values of U, which hold twice the bits of one.  The scale goes into the exponent, and
+    // the sum is divided by it again (both off by the same rounding); but a scale so small that weights would fall out of 32 bits is multiplied afterwards.
+    auto weigh = [&](f32x4 (&st)[2], int r, float by, float vs, auto held, auto& high, auto& rest) __attribute__((always_inline)) {
         using U = std::conditional_t<std::is_same_v<std::remove_reference_t<decltype(high)>, B8>, __bf16, _Float16>;
+        constexpr bool HELD = decltype(held)::value;                   // a tile of 8 bits: with a scale, and without infinities
         float mx = fmaxf(fmaxf(fmaxf(st[0][0], st[0][1]), fmaxf(st[0][2], st[0][3])), fmaxf(fmaxf(st[1][0], st[1][1]), fmaxf(st[1][2], st[1][3]))) * by;
         if (__ballot(mx > m[r] + WEIGHT_SLACK)) {                      // (rarely, after the first steps)
             mx = fmaxf(mx, __shfl_xor(mx, 16));
@@ -200,13 +210,26 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
 #pragma unroll
                 for (int v = 0; v < 4; ++v) o[r][b][v] *= alpha;
         }
-        const float ref = (m[r] == -INFINITY ? 0.0f : m[r]) - WEIGHT_OFF<T>;   // no key seen yet: keep the exponents finite
+        float ref = (m[r] == -INFINITY ? 0.0f : m[r]) - WEIGHT_OFF<T>;   // no key seen yet: keep the exponents finite
+        const bool small = HELD && uni(vs < 0x1p-60f ? 1u : 0u);
+        float back = 1.0f;
+        if (HELD && !small) {
+            back = __builtin_amdgcn_rcpf(vs);
+            ref += __builtin_amdgcn_logf(back);
+        }
+        float p[8], sum[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+            p[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[v >> 2][v & 3], by, -ref));
+            sum[v & 1] += p[v];
+        }
+        l[r] = __builtin_fmaf(sum[0] + sum[1], back, l[r]);
+        if (__builtin_expect(small, 0))
+#pragma unroll
+            for (int v = 0; v < 8; ++v) p[v] *= vs;
 #pragma unroll
         for (int v = 0; v < 8; v += 2) {
-            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(st[v >> 2][v & 3], by, -ref));
-            const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(st[v >> 2][(v & 3) + 1], by, -ref));
-            l[r] += p0 + p1;
-            const WeightPair<U> w(p0 * vs, p1 * vs);
+            const WeightPair<U> w(p[v], p[v + 1], !HELD);
             high[v] = w.high[0]; high[v + 1] = w.high[1];
             rest[v] = w.rest[0]; rest[v + 1] = w.rest[1];
         }
@@ -225,7 +248,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
         fetch_k(x, t + 2);
         B8 high[NR], rest[NR];
 #pragma unroll
-        for (int r = 0; r < NR; ++r) weigh(st[r], r, by, vs, high[r], rest[r]);
+        for (int r = 0; r < NR; ++r) weigh(st[r], r, by, vs, std::true_type{}, high[r], rest[r]);
 #pragma unroll
         for (int w = 0; w < VW; ++w) {
             B8 vf[4];
@@ -289,7 +312,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
 #pragma unroll
             for (int v = 0; v < 8; ++v)
                 if (!(vis >> (16 * (v >> 2) + 4 * g + (v & 3)) & 1u)) st[r][v >> 2][v & 3] = -INFINITY;
-            weigh(st[r], r, sc, 1.0f, high[r], rest[r]);
+            weigh(st[r], r, sc, 1.0f, std::false_type{}, high[r], rest[r]);
         }
         bool bad = false;
 #pragma unroll
@@ -380,7 +403,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
     __shared__ __align__(8) uint32_t tile_scales[4][2];                // of the tile in each slot
     __shared__ uint32_t odd;                                           // a value of the stretch of 16 bits is not finite
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6), h2 = lane >> 5;
-    const TreeUnit u = tree_unit((a.rows + TREE_MANY_ROWS - 1) / TREE_MANY_ROWS);
+    const TreeUnit u = tree_unit8((a.rows + TREE_MANY_ROWS - 1) / TREE_MANY_ROWS, a.together);
     if (u.unit >= a.slots * a.kv_heads) return;
     const TreeJob j = tree_job(a, u.unit, TREE_MANY_KEYS);
     const uint32_t r0 = u.row_block * TREE_MANY_ROWS, t_last = (min(r0 + TREE_MANY_ROWS, a.rows) - 1) / a.group;
@@ -646,7 +669,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
 
 template <typename T, int D>
 hipError_t launch_tree_attn8_of(const TreeAttn8Args& a, hipStream_t stream) {
-    const uint32_t units = (a.slots * a.kv_heads + 7) / 8 * 8;
+    const uint32_t at_once = 8u << a.together, units = (a.slots * a.kv_heads + at_once - 1) / at_once * at_once;
     hipError_t e;
     if (!a.few) e = launch_one(tree_attn8_many<T, D>, units * ((a.rows + TREE_MANY_ROWS - 1) / TREE_MANY_ROWS), 256, stream, a);
     else if (a.rows <= 16) e = launch_one(tree_attn8_few<T, D, 1>, units, 256, stream, a);
