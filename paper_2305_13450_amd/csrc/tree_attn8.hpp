@@ -388,6 +388,10 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
 // The form for many rows of tree_attn.hpp: 128 rows to a workgroup, tiles of 32 keys in LDS, where they are numbers of T: 8-bit ones are converted on their way from
 // registers into it, once for all four waves (16 conversions and 4 LDS stores a wave and tile, where a wave that converted its fragments would need 64).
 //
+// Weights of these tiles and their values go into the products as fp16 numbers whatever T is: 8-bit values are exact in it, and its three bits more than bf16 has leave outputs
+// as near to 64 bits as with 32-bit weights (4 x 256 tokens in bf16: 1.7e-3 of their norm, the output's own rounding; 2.1e-3 with bf16 weights), in the same
+// time.  Tiles of 16 bits keep to T.
+//
 // A weight carries its block's V scale, relative to the largest that the part has met so far (`most`; outputs are in units of it, and are scaled when it grows,
 // which random scales do a few times), so that fp16 weights stay in range: the scale goes into the exponent, and the sum is divided by it again.
 template <typename T, int D>
@@ -395,7 +399,11 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
     using Tile = KeyTile<T, D>;
     using Mm = Mma<T>;
     using V8 = typename Mm::V8;
-    typedef T T4 __attribute__((ext_vector_type(4)));
+    using H = Mma<_Float16>;
+    using H8 = H::V8;
+    typedef _Float16 T4 __attribute__((ext_vector_type(4)));
+    constexpr bool MIXED = !std::is_same_v<T, _Float16>;               // tiles of 16 bits are of another type
+    constexpr float OFF = WEIGHT_OFF<_Float16>;
     using Pad = PaddedTile<D>;
     constexpr uint32_t SLOT = Pad::BYTES;                              // a tile of K and one of V
     constexpr int KF = D / 16, NB = D / 32, NV = 2 * NB, AHEAD = 3;    // MFMAs of a tile's scores, of its output (as many), LDS reads ahead of them
@@ -440,7 +448,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
 #pragma unroll
         for (uint32_t i = 0; i < D / 64; ++i) {
             *(V8*)(to + row8 * Pad::K_PITCH + 16 * i) = eight<T>(f.k[0][2 * i], f.k[0][2 * i + 1]);
-            *(V8*)(to + row8 * Pad::V_PITCH + Pad::K_BYTES + 16 * i) = eight<T>(f.v[0][2 * i], f.v[0][2 * i + 1]);
+            *(H8*)(to + row8 * Pad::V_PITCH + Pad::K_BYTES + 16 * i) = eight<_Float16>(f.v[0][2 * i], f.v[0][2 * i + 1]);
         }
         if (tid < 1) *(u32x2*)tile_scales[slot & 3u] = u32x2{f.ks, f.vs};
     };
@@ -502,21 +510,26 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
     }
     const uint32_t koff = (lane & 31u) * Pad::K_PITCH + h2 * 16;
     const uint32_t voff = Pad::K_BYTES + (4 * h2 + ((lane & 15u) >> 2)) * Pad::V_PITCH + ((lane >> 4) & 1u) * 32 + (lane & 3u) * 8;
-    auto read_k = [&](const char* slot, int i) __attribute__((always_inline)) { return *(const V8*)(slot + koff + i * 32); };
+    auto read_k = [&](const char* slot, int i) __attribute__((always_inline)) { return *(const u32x4*)(slot + koff + i * 32); };
     auto read_v = [&](const char* slot, int i) __attribute__((always_inline)) {   // slice i / NB of 16 keys, block i % NB of 32 d
         T4 x[2];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) x[c] = TrRead<T>::read(slot + voff + ((i / NB) * 16 + c * 8) * Pad::V_PITCH + (i % NB) * 64);
-        return __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        for (int c = 0; c < 2; ++c) x[c] = TrRead<_Float16>::read(slot + voff + ((i / NB) * 16 + c * 8) * Pad::V_PITCH + (i % NB) * 64);
+        return __builtin_bit_cast(u32x4, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    // a product of weights and values, of T where both are of a tile of 16 bits
+    auto weighted = [&](auto wide, const u32x4& v, const u32x4& p, const f32x16& o) __attribute__((always_inline)) {
+        if constexpr (MIXED && decltype(wide)::value) return Mm::mma(__builtin_bit_cast(V8, v), __builtin_bit_cast(V8, p), o);
+        else return H::mma(__builtin_bit_cast(H8, v), __builtin_bit_cast(H8, p), o);
     };
     f32x16 st[2];
-    V8 pf[2][2] = {};
+    u32x4 pf[2][2] = {};
     const float sc = a.scale;
     __syncthreads();
 #pragma unroll
     for (int v = 0; v < 16; ++v) st[0][v] = 0.0f;                      // scores of the first tile
 #pragma unroll
-    for (int i = 0; i < KF; ++i) st[0] = Mm::mma(read_k(lds, i), qf[i], st[0]);
+    for (int i = 0; i < KF; ++i) st[0] = Mm::mma(__builtin_bit_cast(V8, read_k(lds, i)), qf[i], st[0]);
     auto largest = [&](const f32x16& x) __attribute__((always_inline)) {
         float m0 = fmaxf(fmaxf(x[0], x[1]), x[2]), m1 = fmaxf(fmaxf(x[3], x[4]), x[5]);
         m0 = fmaxf(fmaxf(m0, x[6]), x[7]); m1 = fmaxf(fmaxf(m1, x[8]), x[9]);
@@ -539,9 +552,13 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
     float off = 0.0f, back = 1.0f;
     // Weights of the tile whose scores are in `sx`, into `px`; scores of the next tile (in slot `next`) into `sy`, and their largest; output of the
     // one before (in slot `before`) with `py`.
-    auto segment = [&](f32x16& sx, V8 (&px)[2], f32x16& sy, const V8 (&py)[2], const char* next, const char* before, bool masked, uint32_t vis)
+    // wide: whether these tiles are of 16 bits.
+    auto segment = [&](auto wide, f32x16& sx, u32x4 (&px)[2], f32x16& sy, const u32x4 (&py)[2], const char* next, const char* before, bool masked, uint32_t vis)
                        __attribute__((always_inline)) {
-        V8 fr[AHEAD + 1];                                              // fragments on their way
+        using W = std::conditional_t<MIXED && decltype(wide)::value, T, _Float16>;
+        typedef W W8 __attribute__((ext_vector_type(8)));
+        W8 weights[2];
+        u32x4 fr[AHEAD + 1];                                              // fragments on their way
         auto rd = [&](int i) __attribute__((always_inline)) { fr[i % (AHEAD + 1)] = i < KF ? read_k(next, i) : read_v(before, i - KF); };
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) rd(i);
@@ -570,7 +587,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
             row.m = m_new;
             row.l *= alpha;
         }
-        const float ref = (row.m == -INFINITY ? 0.0f : row.m) - WEIGHT_OFF<T> - off;   // no key seen yet: keep the exponents finite
+        const float ref = (row.m == -INFINITY ? 0.0f : row.m) - OFF - off;   // no key seen yet: keep the exponents finite
         float sum[2] = {0.0f, 0.0f}, x0 = 0.0f, x1 = 0.0f, m0 = -INFINITY, m1 = -INFINITY;
         auto weigh = [&](int v, int half) __attribute__((always_inline)) {       // scores v and v + 1, in two halves
             if (half == 0) {
@@ -580,7 +597,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
             } else {
                 x1 = __builtin_amdgcn_exp2f(x1);
                 sum[0] += x0; sum[1] += x1;                            // summed in 32 bits, rounded to 16 for the product with V alone
-                px[v >> 3][v & 7] = (T)x0; px[v >> 3][(v & 7) + 1] = (T)x1;
+                weights[v >> 3][v & 7] = (W)x0; weights[v >> 3][(v & 7) + 1] = (W)x1;
             }
         };
 #pragma unroll
@@ -589,8 +606,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
         for (int i = 0; i < KF + NV; ++i) {
             __builtin_amdgcn_sched_barrier(0);
             if (i + AHEAD < KF + NV) rd(i + AHEAD);
-            if (i < KF) sy = Mm::mma(fr[i % (AHEAD + 1)], qf[i], sy);
-            else row.o[(i - KF) % NB] = Mm::mma(fr[i % (AHEAD + 1)], py[(i - KF) / NB], row.o[(i - KF) % NB]);
+            if (i < KF) sy = Mm::mma(__builtin_bit_cast(V8, fr[i % (AHEAD + 1)]), qf[i], sy);
+            else row.o[(i - KF) % NB] = weighted(wide, fr[i % (AHEAD + 1)], py[(i - KF) / NB], row.o[(i - KF) % NB]);
             if constexpr (KF == 8) weigh(i & ~1, i & 1);
             else { weigh(2 * i, 0); weigh(2 * i, 1); }
             constexpr int FIRST = KF + NV - 4;                         // the next scores are there by then: four of them to a slot
@@ -599,11 +616,13 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
                 m1 = fmaxf(fmaxf(m1, sy[4 * (i - FIRST) + 2]), sy[4 * (i - FIRST) + 3]);
             }
         }
+        px[0] = __builtin_bit_cast(u32x4, weights[0]);
+        px[1] = __builtin_bit_cast(u32x4, weights[1]);
         asm volatile("" ::"v"(px[0]), "v"(px[1]), "v"(sum[0]), "v"(sum[1]), "v"(m0), "v"(m1));   // (computed here, and not where they are used)
         __builtin_amdgcn_sched_barrier(0);
         row.l = __builtin_fmaf(sum[0] + sum[1], back, row.l);
         top = fmaxf(m0, m1);
-        if (__builtin_expect(none, 0)) px[0] = px[1] = V8{};
+        if (__builtin_expect(none, 0)) px[0] = px[1] = u32x4{0, 0, 0, 0};
         if (grown || larger) {                                         // what was added so far went by the reference value and unit before
             alpha *= unit;
 #pragma unroll
@@ -613,27 +632,33 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
         }
     };
     // One tile: what it copies goes out two tiles before it is put into LDS, and that is a tile before it is read.
-    auto step = [&](const TreeAttn8Args& args, uint32_t tile, int odd_one) __attribute__((always_inline)) {
-        const bool wide = tile >= j.cache_blocks;
+    auto step = [&](auto wide, const TreeAttn8Args& args, uint32_t tile, int odd_one) __attribute__((always_inline)) {
+        constexpr bool WIDE = decltype(wide)::value;
         uint32_t vis = ~0u;
-        if (wide) {
+        if constexpr (WIDE) {
             const uint32_t first = (tile - j.cache_blocks) * TREE_MANY_KEYS;
             vis = wide_bits(args, j, token, first, tile < end && first < j.drafted ? min(32u, j.drafted - first) : 0u);
         }
         const uint32_t slot = tile - j.begin;
         // (behind the last tile the scores are of whatever the slot holds, and not used)
-        segment(st[odd_one], pf[odd_one], st[odd_one ^ 1], pf[odd_one ^ 1], lds + ((slot + 1) & 3u) * SLOT, lds + ((slot - 1) & 3u) * SLOT, wide || tile >= end, tile >= end ? 0u : vis);
+        segment(wide, st[odd_one], pf[odd_one], st[odd_one ^ 1], pf[odd_one ^ 1], lds + ((slot + 1) & 3u) * SLOT, lds + ((slot - 1) & 3u) * SLOT, WIDE, vis);
         scales_of(slot + 1);
         put(staged[odd_one], tile + 2);
         fetch(args, staged[odd_one], tile + 4);
         __syncthreads();                                               // the tile put is in its slot, the one read is done with
+    };
+    // The output of a tile whose weights are in pf[1].
+    auto flush = [&](auto wide, uint32_t tile) __attribute__((always_inline)) {
+        const char* const slot = lds + ((tile - j.begin) & 3u) * SLOT;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) row.o[i % NB] = weighted(wide, read_v(slot, i), pf[1][i / NB], row.o[i % NB]);
     };
     uint32_t tile = j.begin;
     // The bulk: tiles of 8 bits up to the last one fetched, without the general step's branches.
     const uint32_t whole = min(end, j.cache_blocks);
     if (tile + 5 < whole) {
         auto quick = [&](int odd_one, uint32_t slot) __attribute__((always_inline)) {
-            segment(st[odd_one], pf[odd_one], st[odd_one ^ 1], pf[odd_one ^ 1], lds + ((slot + 1) & 3u) * SLOT, lds + ((slot - 1) & 3u) * SLOT, false, ~0u);
+            segment(std::false_type{}, st[odd_one], pf[odd_one], st[odd_one ^ 1], pf[odd_one ^ 1], lds + ((slot + 1) & 3u) * SLOT, lds + ((slot - 1) & 3u) * SLOT, false, ~0u);
             scales_of(slot + 1);
             put8(staged[odd_one], slot + 2);
             fetch8(staged[odd_one], j.begin + slot + 4);
@@ -645,17 +670,33 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
         }
     }
     const TreeAttn8Args& later = tree_args<TreeAttn8Args>();
-    for (; tile < end; tile += 2) {                                    // (a last one without keys where their number is odd)
-        step(later, tile, 0);
-        step(later, tile + 1, 1);
+    for (; tile + 1 < whole; tile += 2) {
+        step(std::false_type{}, later, tile, 0);
+        step(std::false_type{}, later, tile + 1, 1);
     }
-    if (j.begin < end) {                                               // the output of the last tile
-        const char* const last = lds + ((((end - j.begin) + 1) & ~1u) - 1 & 3u) * SLOT;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) row.o[i % NB] = Mm::mma(read_v(last, i), pf[1][i / NB], row.o[i % NB]);
+    if (tile < whole) {                                                // (an odd one: what follows begins with the registers of the first of two)
+        step(std::false_type{}, later, tile, 0);
+        ++tile;
+        st[0] = st[1];
+        pf[1][0] = pf[0][0]; pf[1][1] = pf[0][1];
+        const Staged x = staged[0];
+        staged[0] = staged[1];
+        staged[1] = x;
+    }
+    if (tile > j.begin) flush(std::false_type{}, tile - 1);
+    if (tile < end) {
+        pf[1][0] = pf[1][1] = u32x4{0, 0, 0, 0};
+        for (; tile < end; tile += 2) {                                // (a last one without keys where their number is odd)
+            step(std::true_type{}, later, tile, 0);
+            step(std::true_type{}, later, tile + 1, 1);
+        }
+        flush(std::true_type{}, tile - 1);
     }
     const TreeAttn8Args& last_args = tree_args<TreeAttn8Args>();
-    row.l += __shfl_xor(row.l, 32);
+    static_assert(OFF - (MIXED ? 0.0f : OFF) == (MIXED ? 9.0f : 0.0f), "as LESS has it");
+    constexpr float LESS = MIXED ? 0x1p-9f : 1.0f;               // (weights carry 2^OFF, and in T 2^WEIGHT_OFF<T>)
+    row.l = (row.l + __shfl_xor(row.l, 32)) * LESS;
+    most *= LESS;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
