@@ -122,7 +122,7 @@ int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t
     a.few = rows <= (held || cache_bytes < 100000000 ? 64 : 32);
     const int64_t keys = a.few ? TREE_FEW_KEYS : TREE_MANY_KEYS, row_blocks = cdiv64(rows, a.few ? TREE_FEW_ROWS : TREE_MANY_ROWS);
     const int64_t pairs = (int64_t)d->batch * d->kv_heads, base = pairs * row_blocks;
-    const int64_t wide = d->tokens + (held ? held - 1 : 0);        // rows of 16 bits behind those of full blocks
+    const int64_t wide = d->tokens + held;                         // rows of 16 bits behind those of full blocks (and room up to a tile)
     const int64_t blocks = cdiv64(rows_hint(d->max_cached, d->capacity), keys) + cdiv64(wide, keys);
     int64_t part = blocks;
     double best = tree_cost(base, part, blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few, held != 0);

@@ -14,11 +14,16 @@ namespace depsync {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// The two stretches of a sequence: `cached` rows of full blocks; `drafted` rows of 16 bits, of which `held` are cached ones.
+// The two stretches of a sequence: `cached` rows of full blocks; `drafted` rows of 16 bits, of which the first are `held` cached ones and room up to a multiple of
+// 32, so that a tile of 32 keys is of one array.
+__device__ __forceinline__ uint32_t held_room(uint32_t held) { return (held + 31u) & ~31u; }
 __device__ __forceinline__ TreeLengths tree_lengths(const TreeAttn8Args& a, uint32_t b) {
     const uint32_t n = clamp_count(a.cached[b], a.capacity), held = n & ((1u << a.block_log2) - 1u);
-    return {n - held, held + (a.drafted ? clamp_count(a.drafted[b], a.tokens) : a.tokens), held};
+    return {n - held, held_room(held) + (a.drafted ? clamp_count(a.drafted[b], a.tokens) : a.tokens), held};
 }
+__device__ __forceinline__ uint32_t tokens_of(const TreeJob& j) { return j.drafted - held_room(j.held); }
+
+template <typename V> __device__ __forceinline__ void swapped(V& a, V& b) { const V x = a; a = b; b = x; }
 
 // As tree_unit, but 2^together units that follow one another, heads of one sequence, run on one XCD: rows of 64 bytes share cache lines of 128 with their
 // neighbours' (4 tokens of 8 heads of 64 over 120001 rows: 47 us, and 36 so; where rows fill their lines it makes no difference to few rows, and 4 x 256 tokens
@@ -52,51 +57,53 @@ __device__ __forceinline__ Scales scales_at(const float* p, size_t at) { return 
 __device__ __forceinline__ f32x4 mma16(Mma<__bf16>::V8 a, Mma<__bf16>::V8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mma16(Mma<_Float16>::V8 a, Mma<_Float16>::V8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// Row r of the stretch of 16 bits (null: there is none).
-template <typename T>
-__device__ __forceinline__ const T* wide_row(const TreeAttn8Args& a, const TreeJob& j, bool values, uint32_t r) {
-    if (r >= j.drafted) return nullptr;
-    if (r < j.held)
-        return (const T*)(values ? a.v_tail : a.k_tail) + (int64_t)j.b * a.tail_s.batch + (int64_t)r * a.tail_s.token + (int64_t)j.h * a.tail_s.head;
-    return (const T*)(values ? a.v_new : a.k_new) + (int64_t)j.b * a.new_s.batch + (int64_t)(r - j.held) * a.new_s.token + (int64_t)j.h * a.new_s.head;
+// The tile of 32 keys at `at` of the stretch of 16 bits: where its rows lie, how far apart, and how many there are.
+struct WideRun {
+    const char *k, *v;
+    uint32_t step;       // bytes
+    uint32_t first, n;   // among the rows held or the drafted tokens
+    bool held;
+};
+template <int D>
+__device__ __forceinline__ WideRun wide_run(const TreeAttn8Args& a, const TreeJob& j, uint32_t at) {
+    WideRun x;
+    const uint32_t room = held_room(j.held);
+    x.held = at < room;
+    x.first = at - (x.held ? 0u : room);
+    const uint32_t have = x.held ? j.held : j.drafted - room;
+    x.n = x.first < have ? min(32u, have - x.first) : 0u;
+    const Strides& s = x.held ? a.tail_s : a.new_s;
+    const int64_t off = ((int64_t)j.b * s.batch + (int64_t)x.first * s.token + (int64_t)j.h * s.head) * 2;
+    x.k = (const char*)(x.held ? a.k_tail : a.k_new) + off;
+    x.v = (const char*)(x.held ? a.v_tail : a.v_new) + off;
+    x.step = (uint32_t)s.token * 2u;
+    return x;
 }
+template <int D> __device__ __forceinline__ uint32_t wide_bytes(const WideRun& x) { return x.n ? (x.n - 1) * x.step + D * 2u : 0u; }
 
-// The keys of a run of up to 32 in that stretch, from `first` on, that token t sees.
-__device__ __forceinline__ uint32_t wide_bits(const TreeAttn8Args& a, const TreeJob& j, uint32_t t, uint32_t first, uint32_t n) {
-    if (n == 0) return 0u;
-    const uint32_t there = n >= 32 ? ~0u : (1u << n) - 1u;
-    const uint32_t held = first < j.held ? min(32u, j.held - first) : 0u;      // of the run's: seen by all
-    const uint32_t all = held >= 32 ? ~0u : (1u << held) - 1u;
-    if (held >= n) return there;
-    const uint32_t d0 = first + held - j.held, left = n - held;               // the run's first drafted token, and how many
-    uint32_t bits;
-    if (!a.tree) {
-        bits = t < d0 ? 0u : t - d0 >= 31 ? ~0u : (2u << (t - d0)) - 1u;
-    } else {
-        const uint32_t words = (a.tokens + 63) / 64;
-        const uint32_t* const w = (const uint32_t*)(a.tree + (int64_t)j.b * a.tree_batch + (int64_t)t * words);
-        const uint32_t at = d0 >> 5, by = d0 & 31u;
-        const uint32_t lo = w[at], hi = by + left > 32 ? w[at + 1] : 0u;      // (the words end behind the last token)
-        bits = (uint32_t)(((uint64_t)hi << 32 | lo) >> by);
-    }
-    return there & (all | (held < 32 ? bits << held : 0u));
+// The keys of such a tile that token t sees: rows held are seen by all.
+__device__ __forceinline__ uint32_t wide_bits(const TreeAttn8Args& a, const TreeJob& j, const WideRun& x, uint32_t t) {
+    if (x.held) return x.n >= 32 ? ~0u : (1u << x.n) - 1u;
+    return tree_bits(a, j.b, t, x.first, x.n);
 }
 
 // Values of that stretch that are not finite were multiplied as zeros; they are added to the sums of the rows that see them.
-template <typename T>
+template <typename T, int D>
 __device__ __forceinline__ f32x4 add_wide_not_finite(const TreeAttn8Args& a, const TreeJob& j, uint32_t block_keys, uint32_t t, uint32_t d, f32x4 o) {
     typedef T T4 __attribute__((ext_vector_type(4)));
     if (j.end <= j.cache_blocks) return o;
     const uint32_t first = (max(j.begin, j.cache_blocks) - j.cache_blocks) * block_keys, last = min(j.drafted, (j.end - j.cache_blocks) * block_keys);
-    for (uint32_t k0 = first; k0 < last; k0 += 32)
-        for (uint32_t bits = wide_bits(a, j, t, k0, min(32u, last - k0)); bits; bits &= bits - 1) {
-            const T4 x = *(const T4*)(wide_row<T>(a, j, true, k0 + (uint32_t)__builtin_ctz(bits)) + d);
+    for (uint32_t k0 = first; k0 < last; k0 += 32) {
+        const WideRun run = wide_run<D>(a, j, k0);
+        for (uint32_t bits = wide_bits(a, j, run, t); bits; bits &= bits - 1) {
+            const T4 x = *(const T4*)(run.v + (uint64_t)__builtin_ctz(bits) * run.step + d * 2);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float v = (float)x[e];
                 if (!(fabsf(v) < INFINITY)) o[e] += v;
             }
         }
+    }
     return o;
 }
 
@@ -105,8 +112,8 @@ template <typename T, int D>
 __device__ __forceinline__ void store8_row4(const TreeAttn8Args& a, const TreeJob& j, uint32_t r, uint32_t d, f32x4 o, float m, float l, bool odd, uint32_t block_keys) {
     if (r >= a.rows) return;
     const uint32_t t = r / a.group;
-    if (t >= j.drafted - j.held) return;
-    if (__builtin_expect(odd, 0)) o = add_wide_not_finite<T>(a, j, block_keys, t, d, o);
+    if (t >= tokens_of(j)) return;
+    if (__builtin_expect(odd, 0)) o = add_wide_not_finite<T, D>(a, j, block_keys, t, d, o);
     store_row4<T, D>(a, j, r, d, o, m, l, false, block_keys);
 }
 
@@ -132,7 +139,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
     if (u.unit >= a.slots * a.kv_heads) return;
     const TreeJob j = tree_job(a, u.unit, TREE_FEW_KEYS);
     const uint32_t r0 = u.row_block * ROWS;
-    if (j.n_parts == 0 || j.begin >= j.end || r0 / a.group >= j.drafted - j.held) return;
+    if (j.n_parts == 0 || j.begin >= j.end || r0 / a.group >= tokens_of(j)) return;
     if (tid == 0) odd = 0;
     // ---- the rows of full blocks ----
     const uint32_t pitch = uni((uint32_t)a.cache_s.token);             // bytes
@@ -278,25 +285,25 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
     for (uint32_t blk = max(j.begin, j.cache_blocks); blk < j.end; ++blk) {
         const uint32_t at = (blk - j.cache_blocks) * TREE_FEW_KEYS + wave * 32;
         if (at >= j.drafted) break;
-        const uint32_t there = min(32u, j.drafted - at);
-        V8 kf[2][2 * NJ];                                              // everything is asked for before anything is waited for
+        const WideRun run = wide_run<D>(a, j, at);
+        const OperandBuf K(uni_ptr(run.k), uni(wide_bytes<D>(run))), V(uni_ptr(run.v), uni(wide_bytes<D>(run)));   // rows that are not there: zeros
+        u32x4 kf[2][2 * NJ];                                           // everything is asked for before anything is waited for
         uint32_t vw[8][NB / 2];                                        // NB numbers of 8 rows each
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-            const T* const k = wide_row<T>(a, j, false, at + 16 * kt + n);
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-            for (int f = 0; f < 2 * NJ; ++f) kf[kt][f] = k ? *(const V8*)(k + 64 * (f / 2) + 16 * g + 8 * (f % 2)) : V8{};
-        }
+            for (int f = 0; f < 2 * NJ; ++f) kf[kt][f] = K.load16(n * run.step + 32 * g + 128 * (f / 2) + 16 * (f % 2), 16 * kt * run.step);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const T* const v = wide_row<T>(a, j, true, at + 4 * g + (i < 4 ? i : 12 + i));
-            u32x4 x = {0, 0, 0, 0};
-            if (v) {
-                if constexpr (NB == 8) x = *(const u32x4*)(v + NB * n);
-                else { const u32x2 y = *(const u32x2*)(v + NB * n); x[0] = y[0]; x[1] = y[1]; }
-            }
+            const uint32_t off = 4 * g * run.step + 2 * NB * n, row = (i < 4 ? i : 12 + i) * run.step;
+            if constexpr (NB == 8) {
+                const u32x4 x = V.load16(off, row);
 #pragma unroll
-            for (int w = 0; w < NB / 2; ++w) vw[i][w] = x[w];
+                for (int w = 0; w < 4; ++w) vw[i][w] = x[w];
+            } else {
+                const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(V.rsrc, off, row, 0);
+                vw[i][0] = x[0]; vw[i][1] = x[1];
+            }
         }
         f32x4 st[NR][2] = {};
 #pragma unroll
@@ -304,11 +311,11 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
 #pragma unroll
             for (int f = 0; f < 2 * NJ; ++f)
 #pragma unroll
-                for (int r = 0; r < NR; ++r) st[r][kt] = mma16(kf[kt][f], qf[r][f], st[r][kt]);
+                for (int r = 0; r < NR; ++r) st[r][kt] = mma16(__builtin_bit_cast(V8, kf[kt][f]), qf[r][f], st[r][kt]);
         V8 high[NR], rest[NR];
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-            const uint32_t vis = wide_bits(a, j, token[r], at, there);
+            const uint32_t vis = wide_bits(a, j, run, token[r]);
 #pragma unroll
             for (int v = 0; v < 8; ++v)
                 if (!(vis >> (16 * (v >> 2) + 4 * g + (v & 3)) & 1u)) st[r][v >> 2][v & 3] = -INFINITY;
@@ -415,9 +422,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
     if (u.unit >= a.slots * a.kv_heads) return;
     const TreeJob j = tree_job(a, u.unit, TREE_MANY_KEYS);
     const uint32_t r0 = u.row_block * TREE_MANY_ROWS, t_last = (min(r0 + TREE_MANY_ROWS, a.rows) - 1) / a.group;
-    if (j.n_parts == 0 || j.begin >= j.end || r0 / a.group >= j.drafted - j.held) return;
+    if (j.n_parts == 0 || j.begin >= j.end || r0 / a.group >= tokens_of(j)) return;
     // without a tree nothing behind the block's last token is seen
-    const uint32_t end = a.tree ? j.end : min(j.end, max(j.begin, j.cache_blocks + (j.held + t_last) / TREE_MANY_KEYS + 1));
+    const uint32_t end = a.tree ? j.end : min(j.end, max(j.begin, j.cache_blocks + (held_room(j.held) + t_last) / TREE_MANY_KEYS + 1));
     constexpr uint32_t NI = Tile::NI / 4;                              // 1 KB copies of a wave: 32 rows of 16 bits over four waves
     const uint32_t lrow = wave * (Tile::RPI * NI) + lane / Tile::CHUNKS, chunk = lane % Tile::CHUNKS;
     const uint32_t row8 = tid >> 3, at8 = (tid & 7u) * (D / 8);        // of a tile of 8 bits: a thread's row, and its D / 8 bytes of it
@@ -426,49 +433,51 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
     const char *const kbase = uni_ptr((const char*)a.k_cache + base), *const vbase = uni_ptr((const char*)a.v_cache + base);
     const size_t scales = ((size_t)j.b * a.kv_heads + j.h) * a.n_blocks;
     const OperandBuf KS(uni_ptr(a.k_scale + scales), a.n_blocks * 4u), VS(uni_ptr(a.v_scale + scales), a.n_blocks * 4u);
-    struct Staged { u32x4 k[NI], v[NI]; uint32_t ks, vs; } staged[2];
+    // A tile on its way: of 8 bits the first D / 8 bytes of k[0] and v[0] (D = 64: of h), else all of k and v.
+    struct Staged { u32x4 k[NI], v[NI]; u32x2 h[2]; uint32_t ks, vs; } staged[2];
+    constexpr uint32_t NOWHERE = 1u << 31;                             // an offset behind the end of any tile: nothing is read, and zeros come
+    auto load8 = [&](Staged& f, const OperandBuf& K, const OperandBuf& V, uint32_t off, uint32_t scale) __attribute__((always_inline)) {
+        if constexpr (D == 128) {
+            f.k[0] = K.load16(off, 0);
+            f.v[0] = V.load16(off, 0);
+        } else {
+            f.h[0] = __builtin_amdgcn_raw_buffer_load_b64(K.rsrc, off, 0, 0);
+            f.h[1] = __builtin_amdgcn_raw_buffer_load_b64(V.rsrc, off, 0, 0);
+        }
+        f.ks = __builtin_amdgcn_raw_buffer_load_b32(KS.rsrc, scale, 0, 0);
+        f.vs = __builtin_amdgcn_raw_buffer_load_b32(VS.rsrc, scale, 0, 0);
+    };
     auto fetch8 = [&](Staged& f, uint32_t tile) __attribute__((always_inline)) {
         const uint64_t at = (uint64_t)tile * TREE_MANY_KEYS * pitch;
         const uint32_t bytes = tile < end ? 31 * pitch + D : 0u;       // (behind the last: zeros)
-        const OperandBuf K(kbase + at, bytes), V(vbase + at, bytes);
-        if constexpr (D == 128) {
-            f.k[0] = K.load16(row8 * pitch + at8, 0);
-            f.v[0] = V.load16(row8 * pitch + at8, 0);
-        } else {
-            const u32x2 k = __builtin_amdgcn_raw_buffer_load_b64(K.rsrc, row8 * pitch + at8, 0, 0), v = __builtin_amdgcn_raw_buffer_load_b64(V.rsrc, row8 * pitch + at8, 0, 0);
-            f.k[0][0] = k[0]; f.k[0][1] = k[1];
-            f.v[0][0] = v[0]; f.v[0][1] = v[1];
+        load8(f, OperandBuf(kbase + at, bytes), OperandBuf(vbase + at, bytes), row8 * pitch + at8, (tile * TREE_MANY_KEYS >> a.block_log2) * 4);
+    };
+    // Of either kind, without a branch around loads: behind one each of the first four tiles was waited for before the next was asked for (3 us).
+    auto fetch = [&](const TreeAttn8Args& args, Staged& f, uint32_t tile) __attribute__((always_inline)) {
+        const bool wide = tile >= j.cache_blocks;
+        const WideRun run = wide_run<D>(args, j, (tile - j.cache_blocks) * TREE_MANY_KEYS);
+        const uint64_t at = (uint64_t)tile * TREE_MANY_KEYS * pitch;
+        const uint32_t bytes = uni(tile >= end ? 0u : wide ? wide_bytes<D>(run) : 31 * pitch + D);
+        const OperandBuf K(uni_ptr(wide ? run.k : kbase + at), bytes), V(uni_ptr(wide ? run.v : vbase + at), bytes);
+        const uint32_t off8 = row8 * pitch + at8, off16 = wide ? lrow * run.step + chunk * 16 : NOWHERE;
+        load8(f, K, V, D == 128 && wide ? off16 : wide ? NOWHERE : off8, wide ? NOWHERE : (tile * TREE_MANY_KEYS >> a.block_log2) * 4);
+#pragma unroll
+        for (uint32_t i = D == 128 ? 1 : 0; i < NI; ++i) {
+            f.k[i] = K.load16(off16, wide ? i * Tile::RPI * run.step : 0u);
+            f.v[i] = V.load16(off16, wide ? i * Tile::RPI * run.step : 0u);
         }
-        const uint32_t block = (tile * TREE_MANY_KEYS >> a.block_log2) * 4;
-        f.ks = __builtin_amdgcn_raw_buffer_load_b32(KS.rsrc, 0, block, 0);
-        f.vs = __builtin_amdgcn_raw_buffer_load_b32(VS.rsrc, 0, block, 0);
     };
     auto put8 = [&](const Staged& f, uint32_t slot) __attribute__((always_inline)) {
         char* const to = lds + (slot & 3u) * SLOT + at8 * 2;
 #pragma unroll
         for (uint32_t i = 0; i < D / 64; ++i) {
-            *(V8*)(to + row8 * Pad::K_PITCH + 16 * i) = eight<T>(f.k[0][2 * i], f.k[0][2 * i + 1]);
-            *(H8*)(to + row8 * Pad::V_PITCH + Pad::K_BYTES + 16 * i) = eight<_Float16>(f.v[0][2 * i], f.v[0][2 * i + 1]);
+            u32x2 k, v;
+            if constexpr (D == 128) { k = u32x2{f.k[0][2 * i], f.k[0][2 * i + 1]}; v = u32x2{f.v[0][2 * i], f.v[0][2 * i + 1]}; }
+            else { k = f.h[0]; v = f.h[1]; }
+            *(V8*)(to + row8 * Pad::K_PITCH + 16 * i) = eight<T>(k[0], k[1]);
+            *(H8*)(to + row8 * Pad::V_PITCH + Pad::K_BYTES + 16 * i) = eight<_Float16>(v[0], v[1]);
         }
         if (tid < 1) *(u32x2*)tile_scales[slot & 3u] = u32x2{f.ks, f.vs};
-    };
-    auto fetch = [&](const TreeAttn8Args& args, Staged& f, uint32_t tile) __attribute__((always_inline)) {
-        Staged x;                                                      // (a copy: stores to f from both branches went through scratch memory)
-        if (tile < j.cache_blocks) {
-            fetch8(x, tile);
-        } else {
-#pragma unroll
-            for (uint32_t i = 0; i < NI; ++i) {
-                const uint32_t r = tile < end ? (tile - j.cache_blocks) * TREE_MANY_KEYS + lrow + i * Tile::RPI : ~0u;
-                const T *const k = wide_row<T>(args, j, false, r), *const v = wide_row<T>(args, j, true, r);
-                x.k[i] = k ? ((const u32x4*)k)[chunk] : u32x4{0, 0, 0, 0};
-                x.v[i] = v ? ((const u32x4*)v)[chunk] : u32x4{0, 0, 0, 0};
-            }
-            x.ks = x.vs = __builtin_bit_cast(uint32_t, 1.0f);
-        }
-#pragma unroll
-        for (uint32_t i = 0; i < NI; ++i) { f.k[i] = x.k[i]; f.v[i] = x.v[i]; }
-        f.ks = x.ks; f.vs = x.vs;
     };
     auto put = [&](Staged& f, uint32_t tile) __attribute__((always_inline)) {
         const uint32_t slot = tile - j.begin;
@@ -485,7 +494,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
                 *(u32x4*)(to + lrow * Pad::V_PITCH + Pad::K_BYTES + i * Tile::RPI * Pad::V_PITCH) = v;
             }
             if (bad) odd = 1;
-            if (tid < 1) *(u32x2*)tile_scales[slot & 3u] = u32x2{f.ks, f.vs};
+            const uint32_t one = __builtin_bit_cast(uint32_t, 1.0f);
+            if (tid < 1) *(u32x2*)tile_scales[slot & 3u] = u32x2{one, one};
         }
     };
     if (tid == 0) odd = 0;
@@ -636,8 +646,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
         constexpr bool WIDE = decltype(wide)::value;
         uint32_t vis = ~0u;
         if constexpr (WIDE) {
-            const uint32_t first = (tile - j.cache_blocks) * TREE_MANY_KEYS;
-            vis = wide_bits(args, j, token, first, tile < end && first < j.drafted ? min(32u, j.drafted - first) : 0u);
+            const WideRun run = wide_run<D>(args, j, (tile - j.cache_blocks) * TREE_MANY_KEYS);
+            vis = tile < end ? wide_bits(args, j, run, token) : 0u;
         }
         const uint32_t slot = tile - j.begin;
         // (behind the last tile the scores are of whatever the slot holds, and not used)
@@ -679,9 +689,11 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
         ++tile;
         st[0] = st[1];
         pf[1][0] = pf[0][0]; pf[1][1] = pf[0][1];
-        const Staged x = staged[0];
-        staged[0] = staged[1];
-        staged[1] = x;
+#pragma unroll
+        for (uint32_t i = 0; i < NI; ++i) { swapped(staged[0].k[i], staged[1].k[i]); swapped(staged[0].v[i], staged[1].v[i]); }
+        if constexpr (D == 64) { swapped(staged[0].h[0], staged[1].h[0]); swapped(staged[0].h[1], staged[1].h[1]); }
+        swapped(staged[0].ks, staged[1].ks);
+        swapped(staged[0].vs, staged[1].vs);
     }
     if (tile > j.begin) flush(std::false_type{}, tile - 1);
     if (tile < end) {
