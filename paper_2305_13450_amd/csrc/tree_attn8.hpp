@@ -118,20 +118,21 @@ __device__ __forceinline__ void store8_row4(const TreeAttn8Args& a, const TreeJo
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------------------------
-// 16 NR rows to a workgroup, the keys in blocks of 128 of which each of the four waves walks 32 by itself.  Keys and values go from memory into the registers that the matrix
-// cores read, without LDS: which 8 of a row's numbers a lane holds for a product of 32, and which d an output row is, is free as long as both operands
-// agree, so that
-//   K: a lane holds 16 consecutive bytes of one row, two fragments of the scores' products (queries are read in the same order);
-//   V: a lane holds D / 16 consecutive bytes of each of 8 rows, a fragment of as many 16-row blocks of the output (block b's row m is d = D / 16 m + b);
+// 16 NR rows to a workgroup, the keys in blocks of 128 of which each of the four waves walks 32 by itself, with the next one or two tiles on their way into registers.  They come in runs
+// that fill cache lines (a load of a wave is 1 KB of whole rows): a CU that is nearly alone reads 90 GB/s so, where rows fetched as the matrix cores take them, 64 and 128 bytes
+// a row and load, came at 45.  Through LDS of its own a wave then reads them in fragments.  Which 8 of a row's numbers a lane holds for a product of 32,
+// and which d an output row is, is free as long as both operands agree, so that
+//   K: a lane reads 16 consecutive bytes of one row, two fragments of the scores' products (queries are held in the same order);
+//   V: a lane reads D / 16 consecutive bytes of each of 8 rows, a fragment of as many 16-row blocks of the output (block b's row m is d = D / 16 m + b);
 //      pairs of rows are brought together byte by byte, and converted.
-// The next two tiles are on their way meanwhile.
 template <typename T, int D, int NR>
 __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) {
     using V8 = typename Mma<T>::V8;
     using B8 = Mma<__bf16>::V8;
     constexpr uint32_t ROWS = 16 * NR, PITCH = D + 4;
     constexpr int NJ = D / 64, NB = D / 16, VW = D / 64;               // 16-byte runs of a K row, blocks of 16 d, words of a V row that a lane holds
-    __shared__ __align__(16) float join[4][ROWS][PITCH];
+    constexpr uint32_t WAVE = 64 * D > ROWS * PITCH * 4 ? 64 * D : ROWS * PITCH * 4;
+    __shared__ __align__(16) char lds[4 * WAVE];                       // a wave's tile, and its results at the end
     __shared__ float ml[4][ROWS][2];
     __shared__ uint32_t odd;                                           // a value of the stretch of 16 bits is not finite
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uni(tid >> 6), n = lane & 15u, g = lane >> 4;
@@ -151,34 +152,30 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
     const char* const vp = uni_ptr((const char*)a.v_cache + base);
     const size_t scales = ((size_t)j.b * a.kv_heads + j.h) * a.n_blocks;
     const Scales ksp = scales_at(a.k_scale, scales), vsp = scales_at(a.v_scale, scales);
-    struct Tile8 { u32x4 k[2][NJ]; uint32_t v[8][VW]; float ks, vs; } buf[2];
-    const uint32_t kat = n * pitch + 16 * g, vat = 4 * g * pitch + (D / 16) * n, bytes = uni(31 * pitch + D);
-    auto fetch_k = [&](Tile8& x, uint32_t t) __attribute__((always_inline)) {
-        const OperandBuf K(kp + (uint64_t)t * TREE_FEW_KEYS * pitch, t < tiles ? bytes : 0u);   // (behind the last: zeros)
+    constexpr uint32_t CHUNKS = D / 16, RPI = 64 / CHUNKS, NI = 32 / RPI;   // 16-byte chunks of a row, rows of a load, loads of a tile
+    constexpr uint32_t AHEAD = NR == 2 && D == 128 ? 1 : 2;            // tiles on their way (two spill registers there)
+    struct Tile8 { u32x4 k[NI], v[NI]; float ks, vs; } buf[AHEAD];
+    const uint32_t lrow = lane / CHUNKS, chunk = lane % CHUNKS, bytes = uni(31 * pitch + D);
+    auto fetch = [&](Tile8& x, uint32_t t) __attribute__((always_inline)) {
+        const uint64_t at = (uint64_t)t * TREE_FEW_KEYS * pitch;
+        const OperandBuf K(kp + at, t < tiles ? bytes : 0u), V(vp + at, t < tiles ? bytes : 0u);   // (behind the last: zeros)
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+        for (uint32_t i = 0; i < NI; ++i) x.k[i] = K.load16(lrow * pitch + chunk * 16, i * RPI * pitch);
 #pragma unroll
-            for (int jj = 0; jj < NJ; ++jj) x.k[kt][jj] = K.load16(kat, kt * 16 * pitch + 64 * jj);
-        const uint32_t at = uni(min((first + t * TREE_FEW_KEYS) >> a.block_log2, a.n_blocks - 1));
-        x.ks = ksp[at];
-        x.vs = vsp[at];
+        for (uint32_t i = 0; i < NI; ++i) x.v[i] = V.load16(lrow * pitch + chunk * 16, i * RPI * pitch);
+        const uint32_t block = uni(min((first + t * TREE_FEW_KEYS) >> a.block_log2, a.n_blocks - 1));
+        x.ks = ksp[block];
+        x.vs = vsp[block];
     };
-    auto fetch_v = [&](Tile8& x, uint32_t t) __attribute__((always_inline)) {
-        const OperandBuf V(vp + (uint64_t)t * TREE_FEW_KEYS * pitch, t < tiles ? bytes : 0u);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t row = (i < 4 ? i : 12 + i) * pitch;
-            if constexpr (VW == 2) {
-                const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(V.rsrc, vat, row, 0);
-                x.v[i][0] = w[0]; x.v[i][1] = w[1];
-            } else {
-                x.v[i][0] = __builtin_amdgcn_raw_buffer_load_b32(V.rsrc, vat, row, 0);
-            }
-        }
-    };
+    // A row's chunks lie in LDS at exclusive-ors of their number and the row's, by which the lanes that read or write together find different banks.
+    auto swz8 = [](uint32_t row) __attribute__((always_inline)) { return D == 128 ? row & 7u : (row >> 1) & 3u; };
+    char* const ldsK = lds + wave * WAVE;
+    char* const ldsV = ldsK + 32 * D;
+    const uint32_t put = lrow * D + ((chunk ^ swz8(lrow)) << 4), kat = n * D + ((g ^ swz8(n)) << 4);
+    const uint32_t vat = 4 * g * D + (((n * D / 256) ^ swz8(4 * g)) << 4) + (n * (D / 16) & 15u);
     if (tiles) {
-        fetch_k(buf[0], 0); fetch_v(buf[0], 0);
-        fetch_k(buf[1], 1); fetch_v(buf[1], 1);
+#pragma unroll
+        for (uint32_t i = 0; i < AHEAD; ++i) fetch(buf[i], i);
     }
     V8 qf[NR][2 * NJ];
     uint32_t token[NR];
@@ -242,17 +239,40 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
         }
     };
     auto step = [&](Tile8& x, uint32_t t) __attribute__((always_inline)) {
+#pragma unroll
+        for (uint32_t i = 0; i < NI; ++i) *(u32x4*)(ldsK + put + i * 1024) = x.k[i];
+#pragma unroll
+        for (uint32_t i = 0; i < NI; ++i) *(u32x4*)(ldsV + put + i * 1024) = x.v[i];
+        const float by = sc * x.ks, vs = x.vs;
+        fetch(x, t + AHEAD);
+        asm volatile("" ::: "memory");                                 // (a wave's LDS accesses keep their order)
+        __builtin_amdgcn_wave_barrier();
+        u32x4 kr[2][NJ];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int jj = 0; jj < NJ; ++jj) kr[kt][jj] = *(const u32x4*)(ldsK + (kat ^ (64 * jj)) + kt * 16 * D);
+        uint32_t vr[8][VW];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t row = i < 4 ? i : 12 + i;                   // behind 4 g, whose low bits it leaves alone
+            const char* const p = ldsV + (vat ^ (swz8(row) << 4)) + row * D;
+            if constexpr (VW == 2) {
+                const u32x2 w = *(const u32x2*)p;
+                vr[i][0] = w[0]; vr[i][1] = w[1];
+            } else {
+                vr[i][0] = *(const uint32_t*)p;
+            }
+        }
         f32x4 st[NR][2] = {};
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int f = 0; f < 2 * NJ; ++f) {
-                const V8 k = eight<T>(x.k[kt][f / 2][2 * (f % 2)], x.k[kt][f / 2][2 * (f % 2) + 1]);
+                const V8 k = eight<T>(kr[kt][f / 2][2 * (f % 2)], kr[kt][f / 2][2 * (f % 2) + 1]);
 #pragma unroll
                 for (int r = 0; r < NR; ++r) st[r][kt] = mma16(k, qf[r][f], st[r][kt]);
             }
-        const float by = sc * x.ks, vs = x.vs;
-        fetch_k(x, t + 2);
         B8 high[NR], rest[NR];
 #pragma unroll
         for (int r = 0; r < NR; ++r) weigh(st[r], r, by, vs, std::true_type{}, high[r], rest[r]);
@@ -261,7 +281,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
             B8 vf[4];
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
-                const uint32_t lo = __builtin_amdgcn_perm(x.v[i + 1][w], x.v[i][w], 0x05010400u), hi = __builtin_amdgcn_perm(x.v[i + 1][w], x.v[i][w], 0x07030602u);
+                const uint32_t lo = __builtin_amdgcn_perm(vr[i + 1][w], vr[i][w], 0x05010400u), hi = __builtin_amdgcn_perm(vr[i + 1][w], vr[i][w], 0x07030602u);
                 const auto y0 = Held8<__bf16>::two<false>(lo), y1 = Held8<__bf16>::two<true>(lo), y2 = Held8<__bf16>::two<false>(hi), y3 = Held8<__bf16>::two<true>(hi);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) { vf[0][i + e] = y0[e]; vf[1][i + e] = y1[e]; vf[2][i + e] = y2[e]; vf[3][i + e] = y3[e]; }
@@ -274,11 +294,13 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
                     o[r][4 * w + b] = mma16(vf[b], rest[r], o[r][4 * w + b]);
                 }
         }
-        fetch_v(x, t + 2);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
     };
-    for (uint32_t t = 0; t < tiles; t += 2) {
+    for (uint32_t t = 0; t < tiles; t += AHEAD) {
         step(buf[0], t);
-        if (t + 1 < tiles) step(buf[1], t + 1);
+        if constexpr (AHEAD == 2)
+            if (t + 1 < tiles) step(buf[1], t + 1);
     }
     // ---- the rows of 16 bits ----
     __syncthreads();                                                   // (odd is 0)
@@ -367,7 +389,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
                 f32x4 x;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[e] = none ? 0.0f : o[r][b + e][v] * f;
-                *(f32x4*)&join[wave][16 * r + n][NB * (4 * g + v) + b] = x;
+                *(f32x4*)((float*)(lds + wave * WAVE) + (16 * r + n) * PITCH + NB * (4 * g + v) + b) = x;
             }
     }
     __syncthreads();
@@ -386,7 +408,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
     for (uint32_t d = (tid % TPR) * 4; d < D; d += TPR * 4) {
         f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) x += *(const f32x4*)&join[w][rr][d];
+        for (int w = 0; w < 4; ++w) x += *(const f32x4*)((const float*)(lds + w * WAVE) + rr * PITCH + d);
         store8_row4<T, D>(late, j, r0 + rr, d, x, mm, L, odd != 0, TREE_FEW_KEYS);
     }
 }
