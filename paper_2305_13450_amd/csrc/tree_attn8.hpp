@@ -314,16 +314,16 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-            for (int f = 0; f < 2 * NJ; ++f) kf[kt][f] = K.load16(n * run.step + 32 * g + 128 * (f / 2) + 16 * (f % 2), 16 * kt * run.step);
+            for (int f = 0; f < 2 * NJ; ++f) kf[kt][f] = K.load16((16 * kt + n) * run.step + 32 * g + 128 * (f / 2) + 16 * (f % 2), 0);   // (rows' ends count offsets of lanes)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t off = 4 * g * run.step + 2 * NB * n, row = (i < 4 ? i : 12 + i) * run.step;
+            const uint32_t off = (4 * g + (i < 4 ? i : 12 + i)) * run.step + 2 * NB * n;
             if constexpr (NB == 8) {
-                const u32x4 x = V.load16(off, row);
+                const u32x4 x = V.load16(off, 0);
 #pragma unroll
                 for (int w = 0; w < 4; ++w) vw[i][w] = x[w];
             } else {
-                const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(V.rsrc, off, row, 0);
+                const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(V.rsrc, off, 0, 0);
                 vw[i][0] = x[0]; vw[i][1] = x[1];
             }
         }
@@ -485,8 +485,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
         load8(f, K, V, D == 128 && wide ? off16 : wide ? NOWHERE : off8, wide ? NOWHERE : (tile * TREE_MANY_KEYS >> a.block_log2) * 4);
 #pragma unroll
         for (uint32_t i = D == 128 ? 1 : 0; i < NI; ++i) {
-            f.k[i] = K.load16(off16, wide ? i * Tile::RPI * run.step : 0u);
-            f.v[i] = V.load16(off16, wide ? i * Tile::RPI * run.step : 0u);
+            const uint32_t off = wide ? off16 + i * Tile::RPI * run.step : NOWHERE;   // (rows' ends count offsets of lanes)
+            f.k[i] = K.load16(off, 0);
+            f.v[i] = V.load16(off, 0);
         }
     };
     auto put8 = [&](const Staged& f, uint32_t slot) __attribute__((always_inline)) {
