@@ -640,7 +640,7 @@ int dep_cache_append8(const depsync_cache_append8_desc* d, void* stream);
 /* q_out, k_out = the rotated norms of q and k: for every row x of head_dim numbers
  *   y = x / sqrt(mean(x^2) + eps) * gain          (norm = 0: y = x * gain)
  * and of y the first rotary_dim numbers in pairs (a, b) -> (a cos - b sin, b cos + a sin), pair i by the angle position * freq[i]: numbers i and
- * i + rotary_dim / 2 (interleaved = 0), or 2 i and 2 i + 1.  The position of drafted token t is start[b] + depth[t].  All in 32 bits, rounded once; angles
+ * i + rotary_dim / 2 (interleaved = 0), or 2 i and 2 i + 1.  The position of drafted token t is start[b] + depth[t].  All in 32 bits (in which the squares have to fit), rounded once; angles
  * are reduced to a turn in 64-bit whole numbers, so they are as good at position 2^31 as at 1.                                           */
 typedef struct {
     int32_t batch, tokens, heads, kv_heads, head_dim, dtype;
@@ -671,7 +671,7 @@ int dep_qk_norm_rope(const depsync_qk_norm_rope_desc* d, void* stream);
  * id is not in 0..vocab-1 never stays.  accepted[b] receives the tokens that stay, 0 first, and n_accepted[b] their number (entries behind it are left
  * alone): what the appends take.  A sequence with drafted[b] = 0 gets n_accepted 0, and its other outputs are left alone.                 */
 typedef struct {
-    int32_t batch, tokens, vocab;                       /* tokens: 1..65536, vocab: 1..2^24                                        */
+    int32_t batch, tokens, vocab;                       /* tokens: 1..4096 (up to 65536: DEPSYNC_ENOTIMPL), vocab: 1..2^24             */
     const float* p;    int64_t p_batch, p_token;        /* [batch][tokens][vocab], strides in numbers (those of dimensions of size 1 are not read) */
     const float* q;    int64_t q_batch, q_token;        /* likewise, or NULL                                                       */
     const int32_t* ids;                                 /* [batch][tokens]                                                         */

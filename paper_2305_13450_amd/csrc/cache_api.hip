@@ -160,11 +160,16 @@ int evict_check(const depsync_cache_evict_desc* d) {
 
 bool cache8_block(int block, int capacity) { return (block == 32 || block == 64 || block == 128) && capacity >= block && capacity % block == 0; }
 
+// Hundreds of children of one node are compared with one another, so tokens are limited to what a draft may have.
 int verify_check(const depsync_verify_drafts_desc* d) {
-    return d && d->batch >= 1 && d->batch <= 1 << 20 && d->tokens >= 1 && d->tokens <= 65536 && d->vocab >= 1 && d->vocab <= 1 << 24 ? DEPSYNC_OK : DEPSYNC_EINVAL;
+    if (!d || d->batch < 1 || d->batch > 1 << 20 || d->tokens < 1 || d->tokens > 65536 || d->vocab < 1 || d->vocab > 1 << 24) return DEPSYNC_EINVAL;
+    return d->tokens > 4096 ? DEPSYNC_ENOTIMPL : DEPSYNC_OK;
 }
 
-// How dep_verify_drafts spreads its rows.
+// How dep_verify_drafts spreads its rows.  One workgroup to a sequence reads some 80 GB/s (32 chains of 6 over 50257 tokens: 43 us, 18 with rows over 32
+// workgroups each; 16 trees of 32 over 32000 without draft probabilities: 17.6 and 16.3, each before the sums went by DPP); below 16384 numbers a second launch costs what it saves.
+// A tree whose tokens were drawn needs a pass over a row for each refusal that another child follows: so many launches go on where the one before stopped, and
+// most sequences are done after a few (8 trees of 64 over 128000: 162 us without, 39 with six); the last does the rest itself.
 void verify_plan(const depsync_verify_drafts_desc* d, VerifyArgs& a, size_t& bytes) {
     a.launches = 0;
     a.pieces = (uint32_t)std::min<int64_t>(VERIFY_PIECES, std::min<int64_t>(cdiv64(d->vocab, 1024), 1024 / d->batch));
@@ -380,9 +385,8 @@ int dep_qk_norm_rope(const depsync_qk_norm_rope_desc* d, void* stream) {
     a.start = d->start; a.depth = d->depth; a.depth_batch = d->depth_batch; a.drafted = d->drafted;
     a.batch = d->batch; a.tokens = d->tokens; a.heads = d->heads; a.kv_heads = d->kv_heads; a.rotary_dim = R; a.eps = d->eps;
     const int64_t tokens = (int64_t)d->batch * d->tokens, at_once = 64 / (D / 16);
-    a.span = 1;
-    a.q_waves = (uint32_t)cdiv64(d->heads, at_once * a.span);
-    a.k_waves = (uint32_t)cdiv64(d->kv_heads, at_once * a.span);
+    a.q_waves = (uint32_t)cdiv64(d->heads, at_once);
+    a.k_waves = (uint32_t)cdiv64(d->kv_heads, at_once);
     if (cdiv64(tokens * (a.q_waves + a.k_waves), 4) > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;
     const hipError_t e = launch_qk_norm_rope(a, d->dtype, D, d->interleaved != 0, d->norm != 0, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);

@@ -58,7 +58,7 @@ struct QkNormArgs {
     Strides q_s, k_s, q_out_s, k_out_s;
     int64_t depth_batch;
     uint32_t batch, tokens, heads, kv_heads, rotary_dim;
-    uint32_t span, q_waves, k_waves;      // groups of heads that a wave walks, waves to a token's queries and to its keys
+    uint32_t q_waves, k_waves;            // waves to a token's queries and to its keys
     float eps;
 };
 

@@ -29,7 +29,8 @@ __device__ __forceinline__ uint32_t e4m3_of(float a, float b, float c, float d) 
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(within(c), within(d), x, true);
 }
 
-// A workgroup to a sequence, head, K or V, and a block that the call can fill.  Its rows stay in registers between the search for the largest magnitude
+// A workgroup to a sequence, head, K or V, and a block that the call can fill.  Bound by latency: lengths, the row's number, the row and the search are behind one another (one to
+// six accepted rows of 32 sequences: 4.6 us; 4 x 1024 tokens of 8 heads in blocks of 32, 26 MB: 8.3, 3.1 TB/s, 2048 workgroups that all start at once).  Its rows stay in registers between the search for the largest magnitude
 // and the conversion, so they are read once.  The workgroup of the first block reads the rows held in 16 bits, which the rows behind the last full block
 // overwrite: that workgroup writes these too, afterwards.
 template <typename T, int D, int BLOCK>

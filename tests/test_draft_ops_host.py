@@ -93,6 +93,7 @@ def test_refusals(name):
 def test_launches_too_large_are_refused():
     assert call("dep_cache_append8", append8(batch=1 << 20, kv_heads=64, n_max=8)) == ds.ENOTIMPL
     assert call("dep_qk_norm_rope", norm(batch=1 << 20, tokens=64)) == ds.ENOTIMPL
+    assert call("dep_verify_drafts", verify(tokens=4097)) == ds.ENOTIMPL
     n = ctypes.c_size_t(0)
     f = ds._lib().depsync_tree_attn8_workspace
     assert f(ctypes.byref(attn8(batch=1 << 20, capacity=1 << 20, heads=64, kv_heads=64)), 256, ctypes.byref(n)) == ds.ENOTIMPL

@@ -342,7 +342,7 @@ def test_norm_of_rows_past_32_bits():
 
 @BOTH
 def test_norm_of_many_tokens(dtype):
-    # several groups of heads to a wave
+    # several waves to a token, the last with heads that are not there
     g = gen(42)
     for B, T, Hq, Hk, D in ((2, 2000, 39, 3, 128), (1, 5000, 34, 17, 64)):
         q, k = normal(g, (B, T, Hq, D), dtype), normal(g, (B, T, Hk, D), dtype)
@@ -352,6 +352,18 @@ def test_norm_of_many_tokens(dtype):
         torch.cuda.synchronize()
         for x, y, w in ((q, qo, gain), (k, ko, None)):
             check_norm(x, y, *ref.norm_rope(x, angles_of(D), w, start), (B, T))
+
+
+@BOTH
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_numbers_behind_the_rotated_ones_are_no_pairs(interleaved, dtype):
+    g = gen(43)
+    x = normal(g, (1, 2, 3, 64), dtype)
+    x[0, 1, 1, 40], x[0, 1, 2, 63], x[0, 0, 0, 33] = INF, NAN, -INF
+    y, z = torch.empty_like(x), torch.empty_like(x)
+    ds.dep_qk_norm_rope(x, x.clone(), ds.rope_frequencies(angles_of(32), "cuda"), q_out=y, k_out=z, norm=False, interleaved=interleaved)
+    torch.cuda.synchronize()
+    assert same(y[..., 32:], x[..., 32:]) and same(y, z) and bool(y[..., :32].isfinite().all())
 
 
 # ---- streams, graphs, whole rounds --------------------------------------------------------------------------------------------------
