@@ -59,6 +59,7 @@ struct QkNormArgs {
     int64_t depth_batch;
     uint32_t batch, tokens, heads, kv_heads, rotary_dim;
     uint32_t q_waves, k_waves;            // waves to a token's queries and to its keys
+    uint32_t streams;                     // 1: the outputs are larger than the L2 caches
     float eps;
 };
 

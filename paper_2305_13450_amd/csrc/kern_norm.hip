@@ -36,7 +36,7 @@ template <int LANES> __device__ __forceinline__ float row_sum(float x) {
 // A wave takes 8 heads of 128 numbers (16 of 64) of one token, queries or keys.  A lane holds two runs of 8 numbers of a head that are each other's partners
 // (8 u and 8 u + rotary_dim / 2; interleaved, and behind rotary_dim: 16 u and 16 u + 8), D / 16 lanes to a head, so no number crosses lanes but the sum of
 // squares.  Bound by HBM, read and written once: 4 x 2048 tokens of 64 + 8 heads of 128, 302 MB, in 60 us, 5.0 TB/s where a copy has 5.1; the eight angles of a lane are worked
-// out anew by each of a token's 9 waves meanwhile.  One token of 32 sequences: 4.4 us, four loads behind one another.
+// out anew by each of a token's 9 waves meanwhile.  What L2 cannot hold for the next kernel is stored past it (inputs that change, 302 MB: 68 and 66 us, 84 MB: 22 and 20).  One token of 32 sequences: 4.4 us, four loads behind one another.
 template <typename T, int D, bool INTERLEAVED, bool NORM>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkNormArgs a) {
     constexpr uint32_t LANES = D / 16, HEADS = 64 / LANES;
@@ -54,12 +54,6 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkNormArgs a) {
     T* const to = (T*)(keys ? a.k_out : a.q_out) + (int64_t)b * to_s.batch + (int64_t)t * to_s.token;
     const bool rotated = unit < a.rotary_dim / 16;
     const uint32_t e0 = !INTERLEAVED && rotated ? 8 * unit : 16 * unit, e1 = !INTERLEAVED && rotated ? e0 + a.rotary_dim / 2 : e0 + 8;
-    const uint32_t h = (keys ? part - a.q_waves : part) * HEADS + lane / LANES;
-    T8 in[2] = {};
-    if (h < heads) {
-        in[0] = *(const T8*)(from + (int64_t)h * from_s.head + e0);
-        in[1] = *(const T8*)(from + (int64_t)h * from_s.head + e1);
-    }
     float cs[8], sn[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) { cs[i] = 1.0f; sn[i] = 0.0f; }
@@ -78,6 +72,12 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkNormArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) gain[c][4 * v + i] = x[i];
         }
+    const uint32_t h = (keys ? part - a.q_waves : part) * HEADS + lane / LANES;
+    T8 in[2] = {};
+    if (h < heads) {
+        in[0] = *(const T8*)(from + (int64_t)h * from_s.head + e0);
+        in[1] = *(const T8*)(from + (int64_t)h * from_s.head + e1);
+    }
     float x[2][8], sum = 0.0f;
 #pragma unroll
     for (int c = 0; c < 2; ++c)
@@ -100,9 +100,14 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkNormArgs a) {
         out[ca][ia] = (T)__builtin_fmaf(u, cs[i], rotated ? -v * sn[i] : 0.0f);   // (numbers behind rotary_dim are no pairs: one that is not finite stays alone)
         out[cb][ib] = (T)__builtin_fmaf(v, cs[i], rotated ? u * sn[i] : 0.0f);
     }
-    if (h < heads) {
-        *(T8*)(to + (int64_t)h * to_s.head + e0) = out[0];
-        *(T8*)(to + (int64_t)h * to_s.head + e1) = out[1];
+    if (h >= heads) return;
+    T8 *const to0 = (T8*)(to + (int64_t)h * to_s.head + e0), *const to1 = (T8*)(to + (int64_t)h * to_s.head + e1);
+    if (a.streams) {
+        __builtin_nontemporal_store(out[0], to0);
+        __builtin_nontemporal_store(out[1], to1);
+    } else {
+        *to0 = out[0];
+        *to1 = out[1];
     }
 }
 
