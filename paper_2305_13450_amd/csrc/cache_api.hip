@@ -388,9 +388,9 @@ int dep_qk_norm_rope(const depsync_qk_norm_rope_desc* d, void* stream) {
     const int64_t tokens = (int64_t)d->batch * d->tokens, at_once = 64 / (D / 16);
     a.q_waves = (uint32_t)cdiv64(d->heads, at_once);
     a.k_waves = (uint32_t)cdiv64(d->kv_heads, at_once);
-    a.streams = tokens * (d->heads + d->kv_heads) * D * 2 > L2_BYTES ? 1 : 0;
+    const bool streams = tokens * (d->heads + d->kv_heads) * D * 2 > L2_BYTES;
     if (cdiv64(tokens * (a.q_waves + a.k_waves), 4) > MAX_BLOCKS) return DEPSYNC_ENOTIMPL;
-    const hipError_t e = launch_qk_norm_rope(a, d->dtype, D, d->interleaved != 0, d->norm != 0, static_cast<hipStream_t>(stream));
+    const hipError_t e = launch_qk_norm_rope(a, d->dtype, D, d->interleaved != 0, d->norm != 0, streams, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);
 }
 

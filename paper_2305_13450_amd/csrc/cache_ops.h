@@ -59,7 +59,6 @@ struct QkNormArgs {
     int64_t depth_batch;
     uint32_t batch, tokens, heads, kv_heads, rotary_dim;
     uint32_t q_waves, k_waves;            // waves to a token's queries and to its keys
-    uint32_t streams;                     // 1: the outputs are larger than the L2 caches
     float eps;
 };
 
@@ -137,7 +136,8 @@ hipError_t launch_cache_evict(const CacheEvictArgs& a, int head_dim, hipStream_t
 hipError_t launch_tree_attn8_bf16(const TreeAttn8Args& a, int head_dim, hipStream_t stream);
 hipError_t launch_tree_attn8_f16(const TreeAttn8Args& a, int head_dim, hipStream_t stream);
 hipError_t launch_cache_append8(const CacheAppend8Args& a, int dtype, int head_dim, int block, hipStream_t stream);
-hipError_t launch_qk_norm_rope(const QkNormArgs& a, int dtype, int head_dim, bool interleaved, bool norm, hipStream_t stream);
+// streams: the outputs are larger than the L2 caches.
+hipError_t launch_qk_norm_rope(const QkNormArgs& a, int dtype, int head_dim, bool interleaved, bool norm, bool streams, hipStream_t stream);
 hipError_t launch_verify_drafts(const VerifyArgs& a, hipStream_t stream);
 
 template <class F, class A>

@@ -37,7 +37,7 @@ template <int LANES> __device__ __forceinline__ float row_sum(float x) {
 // (8 u and 8 u + rotary_dim / 2; interleaved, and behind rotary_dim: 16 u and 16 u + 8), D / 16 lanes to a head, so no number crosses lanes but the sum of
 // squares.  Bound by HBM, read and written once: 4 x 2048 tokens of 64 + 8 heads of 128, 302 MB, in 60 us, 5.0 TB/s where a copy has 5.1; the eight angles of a lane are worked
 // out anew by each of a token's 9 waves meanwhile.  What L2 cannot hold for the next kernel is stored past it (inputs that change, 302 MB: 68 and 66 us, 84 MB: 22 and 20).  One token of 32 sequences: 4.4 us, four loads behind one another.
-template <typename T, int D, bool INTERLEAVED, bool NORM>
+template <typename T, int D, bool INTERLEAVED, bool NORM, bool STREAMS>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkNormArgs a) {
     constexpr uint32_t LANES = D / 16, HEADS = 64 / LANES;
     typedef T T8 __attribute__((ext_vector_type(8)));
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkNormArgs a) {
     }
     if (h >= heads) return;
     T8 *const to0 = (T8*)(to + (int64_t)h * to_s.head + e0), *const to1 = (T8*)(to + (int64_t)h * to_s.head + e1);
-    if (a.streams) {
+    if constexpr (STREAMS) {                                           // (two branches' stores, alike but for their way, would become one)
         __builtin_nontemporal_store(out[0], to0);
         __builtin_nontemporal_store(out[1], to1);
     } else {
@@ -111,19 +111,23 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkNormArgs a) {
     }
 }
 
-template <typename T, int D>
-hipError_t launch_norm_of(const QkNormArgs& a, bool interleaved, bool norm, hipStream_t stream) {
+template <typename T, int D, bool INTERLEAVED, bool NORM>
+hipError_t launch_norm_with(const QkNormArgs& a, bool streams, hipStream_t stream) {
     const uint64_t waves = (uint64_t)a.batch * a.tokens * (a.q_waves + a.k_waves);
     const uint32_t n = (uint32_t)((waves + 3) / 4);
-    if (interleaved) return norm ? launch_one(qk_norm_rope_kernel<T, D, true, true>, n, 256, stream, a) : launch_one(qk_norm_rope_kernel<T, D, true, false>, n, 256, stream, a);
-    return norm ? launch_one(qk_norm_rope_kernel<T, D, false, true>, n, 256, stream, a) : launch_one(qk_norm_rope_kernel<T, D, false, false>, n, 256, stream, a);
+    return streams ? launch_one(qk_norm_rope_kernel<T, D, INTERLEAVED, NORM, true>, n, 256, stream, a) : launch_one(qk_norm_rope_kernel<T, D, INTERLEAVED, NORM, false>, n, 256, stream, a);
+}
+template <typename T, int D>
+hipError_t launch_norm_of(const QkNormArgs& a, bool interleaved, bool norm, bool streams, hipStream_t stream) {
+    if (interleaved) return norm ? launch_norm_with<T, D, true, true>(a, streams, stream) : launch_norm_with<T, D, true, false>(a, streams, stream);
+    return norm ? launch_norm_with<T, D, false, true>(a, streams, stream) : launch_norm_with<T, D, false, false>(a, streams, stream);
 }
 
 }  // namespace
 
-hipError_t launch_qk_norm_rope(const QkNormArgs& a, int dtype, int head_dim, bool interleaved, bool norm, hipStream_t stream) {
-    if (dtype == 0) return head_dim == 128 ? launch_norm_of<__bf16, 128>(a, interleaved, norm, stream) : launch_norm_of<__bf16, 64>(a, interleaved, norm, stream);
-    return head_dim == 128 ? launch_norm_of<_Float16, 128>(a, interleaved, norm, stream) : launch_norm_of<_Float16, 64>(a, interleaved, norm, stream);
+hipError_t launch_qk_norm_rope(const QkNormArgs& a, int dtype, int head_dim, bool interleaved, bool norm, bool streams, hipStream_t stream) {
+    if (dtype == 0) return head_dim == 128 ? launch_norm_of<__bf16, 128>(a, interleaved, norm, streams, stream) : launch_norm_of<__bf16, 64>(a, interleaved, norm, streams, stream);
+    return head_dim == 128 ? launch_norm_of<_Float16, 128>(a, interleaved, norm, streams, stream) : launch_norm_of<_Float16, 64>(a, interleaved, norm, streams, stream);
 }
 
 }  // namespace depsync
