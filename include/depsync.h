@@ -607,8 +607,8 @@ int depsync_cache_evict_workspace(const depsync_cache_evict_desc* d, size_t* byt
 
 /* out as dep_tree_attn's, over the rows of such a cache and the drafted tokens: scores and outputs go by the rows' values, in 32 bits.  In `attn`, k_cache and
  * v_cache are the 8-bit numbers; max_cached 0 means capacity.  Rows of the last block that is not full and drafted tokens may hold infinities and NaN as
- * there.  For the product with v weights are two 16-bit numbers each up to 64 query rows to a key and value head, and one beyond, fp16 for rows of 8 bits and of the
- * element type for the others; these carry their block's scale, relative to the largest that the part has met: what falls out of fp16's range then is below 2^-33
+ * there.  For the product with v weights are two 16-bit numbers each up to 64 query rows to a key and value head, and one beyond, of the element type for rows of 16 bits
+ * and fp16 for those of 8, which carry their block's scale, relative to the largest that the part has met: what falls out of fp16's range then is below 2^-33
  * of the largest value.                                                                                                                  */
 typedef struct {
     depsync_tree_attn_desc attn;

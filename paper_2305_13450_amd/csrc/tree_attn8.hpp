@@ -581,6 +581,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
     scales_of(0);
     // Of the V scale `of` (its bits): the logarithm of what it is of `most`, and the inverse.  What is below 2^-60 of that counts for nothing: fp16
     // weights would be zeros, and a sum in 32 bits could not be divided.
+    // Rows of 16 bits have no scale that says how large they are, so `most` is 1 for them (2^-60 of what it was if that is more, so that outputs so far stay in 32 bits).
     uint32_t of = ~0u, none = 0;
     float off = 0.0f, back = 1.0f;
     // Weights of the tile whose scores are in `sx`, into `px`; scores of the next tile (in slot `next`) into `sy`, and their largest; output of the
@@ -605,10 +606,11 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
         uint32_t larger = 0;
         if (uni(__builtin_bit_cast(uint32_t, vs)) != of) {             // (once a block)
             of = uni(__builtin_bit_cast(uint32_t, vs));
-            larger = uni(vs > most ? 1u : 0u);
+            const float u = wide ? fmaxf(1.0f, most * 0x1p-60f) : vs;
+            larger = uni((wide ? u != most : u > most) ? 1u : 0u);
             const float inverse = __builtin_amdgcn_rcpf(vs);
-            if (larger) { unit = most * inverse; most = vs; }
-            none = uni(vs < 0x1p-126f || vs < most * 0x1p-60f ? 1u : 0u);
+            if (larger) { unit = most * __builtin_amdgcn_rcpf(u); most = u; }
+            none = uni(!wide && (vs < 0x1p-126f || vs < most * 0x1p-60f) ? 1u : 0u);
             back = none ? 1.0f : most * inverse;                       // (off by the reciprocal's rounding, as off then is)
             off = none ? 0.0f : -__builtin_amdgcn_logf(back);
         }
@@ -721,6 +723,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
     if (tile > j.begin) flush(std::false_type{}, tile - 1);
     if (tile < end) {
         pf[1][0] = pf[1][1] = u32x4{0, 0, 0, 0};
+        of = ~0u;
         for (; tile < end; tile += 2) {                                // (a last one without keys where their number is odd)
             step(std::true_type{}, later, tile, 0);
             step(std::true_type{}, later, tile + 1, 1);

@@ -92,6 +92,22 @@ def test_scales_of_every_size(T, Hq, Hk, D, block, lens, dtype):
 
 
 @BOTH
+@FORMS
+def test_large_values_before_rows_of_16_bits(T, Hq, Hk, D, block, lens, dtype):
+    # rows of 16 bits have no scale, so theirs says nothing about their values beside those of blocks
+    print("large values", T, Hq, Hk, D, block, lens, dtype, flush=True)
+    g = gen(23)
+    for by in (2.0 ** 70, 2.0 ** 100) if dtype == BF else (2.0 ** 9,):
+        q, kn, vn, cache, cached = setup(g, 2, T, Hq, Hk, D, block, [4 * block + 11, 2 * block], dtype, cap=5 * block)
+        cache[3][:] *= by
+        cache[5][:] *= by
+        check_attn(q, kn, vn * by, cache, cached)
+        cache[3][:, :, 1] = by                                        # with the last block's scale, and one that a row of 16 bits has by itself
+        cache[3][:, :, 2:] = 1.0
+        check_attn(q, kn, vn * by, cache, cached)
+
+
+@BOTH
 @pytest.mark.parametrize("T,Hq,Hk,D", [(3, 4, 2, 64), (20, 4, 2, 128), (100, 2, 1, 128)])
 def test_rows_that_see_nothing(T, Hq, Hk, D, dtype):
     g = gen(14)
