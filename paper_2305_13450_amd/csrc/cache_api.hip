@@ -93,7 +93,7 @@ int tree_operands(const depsync_tree_attn_desc* d, TreeAttnArgs& a, int multiple
 // second kernel and the results' way there and back.  5.9 is what a second launch costs a program that waits for the host (one token of 12 heads over 500
 // rows 12.4 us in one launch, 15.5 in two); captured into a graph it is about 4 (12.1 and 11.6).  The lengths are the longest sequence's; the
 // kernels then share out the parts by the real ones.
-// Over a cache of 8 bits (fitted to 31 shapes, 1 to 128 rows): a block takes the form for few rows 0.8 us for up to 16 rows of 128 and 1.1 for 32 (0.6 and 0.8 of 64) while its
+// Over a cache of 8 bits (fitted to measured times of 1 to 128 rows): a block takes the form for few rows 0.8 us for up to 16 rows of 128 and 1.1 for 32 (0.6 and 0.8 of 64) while its
 // workgroup is alone on a CU, 1.7 times as long where two share it; and HBM, which one workgroup a CU saturates, gives a tenth less to two.
 double tree_cost(int64_t base, int64_t part, int64_t blocks, int64_t pairs, int64_t rows, int64_t row_blocks, int head_dim, int n_cu, bool few, bool held) {
     const int64_t parts = cdiv64(blocks, part), groups = base * parts, slots = 2 * (int64_t)n_cu;
@@ -167,17 +167,19 @@ int verify_check(const depsync_verify_drafts_desc* d) {
     return d->tokens > 4096 ? DEPSYNC_ENOTIMPL : DEPSYNC_OK;
 }
 
-// How dep_verify_drafts spreads its rows.  One workgroup to a sequence reads some 80 GB/s (32 chains of 6 over 50257 tokens: 43 us, 18 with rows over 32
-// workgroups each; 16 trees of 32 over 32000 without draft probabilities: 17.6 and 16.3, each before the sums went by DPP); below 16384 numbers a second launch costs what it saves.
+// How dep_verify_drafts spreads its rows.  One workgroup to a sequence has some 32 KB of reads on their way, 30 to 80 GB/s (32 chains of 6 over 50257 tokens: 43 us, 18 with
+// rows over 32 workgroups each; 16 trees of 32 over 32000 without draft probabilities: 17.6 and 16.3, each before the sums went by DPP); below 16384 numbers a second launch
+// costs what it saves.
 // A tree whose tokens were drawn needs a pass over a row for each refusal that another child follows: so many launches go on where the one before stopped, and
-// most sequences are done after a few (8 trees of 64 over 128000: 162 us without, 39 with six); the last does the rest itself.
+// the last does the rest itself, 25 us a pass over 128000 numbers.  A launch that finds everything done costs 2.7.  Trees of 64 tokens, 8 at a time, need 3 to 6 passes mostly and 11 at
+// times: 162 us without further launches, and on average over their inputs 58 with four, 38 with six, 41 with nine (one tree of 16: 24, 28 and 36).
 void verify_plan(const depsync_verify_drafts_desc* d, VerifyArgs& a, size_t& bytes) {
     a.launches = 0;
     a.pieces = (uint32_t)std::min<int64_t>(VERIFY_PIECES, std::min<int64_t>(cdiv64(d->vocab, 1024), 1024 / d->batch));
-    if (a.pieces >= 2 && d->vocab >= 16384) a.launches = d->q && d->parents ? 1 + (uint32_t)std::min(std::max(d->tokens - 2, 0), 6) : 1;
+    if (a.pieces >= 2 && d->vocab >= 16384) a.launches = d->q && d->parents ? std::min(1 + (uint32_t)std::max(d->tokens - 2, 0), VERIFY_LAUNCHES) : 1;
     if (!a.launches) a.pieces = 1;
     a.piece = (uint32_t)cdiv64(cdiv64(d->vocab, a.pieces), 256) * 256;
-    bytes = (size_t)a.launches * d->batch * (sizeof(VerifyState) + a.pieces * sizeof(double));
+    bytes = (size_t)a.launches * d->batch * (sizeof(VerifyState) + a.pieces * sizeof(double)) + (a.launches > 1 ? (size_t)d->batch * d->tokens * 8 : 0);
 }
 
 // Strides of [batch][tokens][vocab] numbers, those of dimensions of size one not read.
@@ -417,6 +419,7 @@ int dep_verify_drafts(const depsync_verify_drafts_desc* d, void* workspace, size
     verify_plan(d, a, need);
     a.sums = static_cast<double*>(workspace);
     a.states = reinterpret_cast<VerifyState*>(a.sums + (size_t)a.launches * d->batch * a.pieces);
+    a.kept = reinterpret_cast<VerifyToken*>(a.states + (size_t)a.launches * d->batch);
     const hipError_t e = launch_verify_drafts(a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? DEPSYNC_OK : hip_fail(e);
 }

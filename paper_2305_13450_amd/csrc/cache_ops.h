@@ -67,8 +67,10 @@ struct VerifyState {
     double C, R;
     uint32_t last, n, at;
     uint32_t stale;                       // R is of before the last refusal
-    uint32_t sums, unused;                // one more than the launch whose sums the next token is drawn by; 0: none yet
+    uint32_t done;                        // one more than the launch whose sums the next token is drawn by; 0: none yet
 };
+
+struct VerifyToken { float p, q; };       // a token's own probabilities
 
 struct VerifyArgs {
     const float *p, *q;                   // q may be null
@@ -76,13 +78,14 @@ struct VerifyArgs {
     const float* u;
     int32_t *accepted, *n_accepted, *next;
     int64_t p_batch, p_token, q_batch, q_token, parents_batch;
-    VerifyState* states;                  // workspace: [launches][batch], and [launches][batch][pieces] sums
+    VerifyState* states;                  // workspace: [launches][batch], [launches][batch][pieces] sums, and where launches are more than one [batch][tokens]
+    VerifyToken* kept;
     double* sums;
     uint32_t batch, tokens, vocab;
     uint32_t launches, launch;            // that spread rows over several workgroups, before the last one (0: none); the present one
     uint32_t pieces, piece;               // workgroups to a row, numbers that each sums
 };
-constexpr uint32_t VERIFY_PIECES = 64;    // at most
+constexpr uint32_t VERIFY_PIECES = 64, VERIFY_LAUNCHES = 7;   // at most
 
 struct CacheAppendArgs {
     const void *k_new, *v_new;

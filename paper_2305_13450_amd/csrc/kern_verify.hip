@@ -51,27 +51,50 @@ struct Drafts {
     __device__ __forceinline__ int32_t parent(uint32_t t) const { return parents ? parents[t] : (int32_t)t - 1; }
 };
 
-// From s.at on; every wave that calls this does the same.  Tokens are taken up in lots of 64, a lane each: the children of the last one that stays are found by a ballot.
+// 64 tokens from t0 on, a lane each.  Their probabilities are gathered from rows far apart once: where launches follow one another the first keeps them.
+struct Lot {
+    int32_t parent = -1, id = -1;        // -1: none, or not in the vocabulary
+    double u = 0.0, px = 0.0, qx = 0.0;
+};
+__device__ __forceinline__ Lot tokens_of(const VerifyArgs& a, uint32_t b, const Drafts& d, uint32_t t0) {
+    const uint32_t t = t0 + (threadIdx.x & 63u);
+    Lot x;
+    if (t > 0 && t < a.tokens) {
+        x.parent = d.parent(t);
+        x.id = d.ids[t];
+        x.u = unit(a.u[(size_t)b * a.tokens + t]);
+    }
+    return x;
+}
+template <bool DRAWN> __device__ __forceinline__ Lot lot_of(const VerifyArgs& a, uint32_t b, const Drafts& d, uint32_t t0, bool kept) {
+    const uint32_t t = t0 + (threadIdx.x & 63u);
+    Lot x = tokens_of(a, b, d, t0);
+    VerifyToken w = {0.0f, 0.0f};
+    if (DRAWN && kept && t < a.tokens) w = a.kept[(size_t)b * a.tokens + t];
+    if (x.parent >= 0 && (uint32_t)x.parent < t && x.id >= 0 && (uint32_t)x.id < a.vocab) {
+        if (!DRAWN || !kept) {
+            w.p = d.p[(int64_t)x.parent * a.p_token + x.id];
+            if (DRAWN) w.q = d.q[(int64_t)x.parent * a.q_token + x.id];
+        }
+        x.px = mass(w.p);
+        if (DRAWN) x.qx = mass(w.q);
+    } else {
+        x.id = -1;
+    }
+    return x;
+}
+
+// From s.at on; every wave that calls this does the same.  The children of the last one that stays are found by a ballot.  first: the lot from 0 on.
 // Where R is needed and stale: pass(s) renews it, or returns false, and so does this then.
 template <bool DRAWN, class Pass>
-__device__ __forceinline__ bool verify_walk(const VerifyArgs& a, uint32_t b, const Drafts& d, VerifyState& s, bool write, Pass pass) {
+__device__ __forceinline__ bool verify_walk(const VerifyArgs& a, uint32_t b, const Drafts& d, const Lot& first, bool kept, VerifyState& s, bool write, Pass pass) {
     const uint32_t lane = threadIdx.x & 63u;
     if (write && s.at == 1) a.accepted[(size_t)b * a.tokens] = 0;
     for (uint32_t t0 = s.at & ~63u; t0 < d.drafted; t0 += 64) {
         const uint32_t t = t0 + lane;
-        int32_t parent = -1, id = -1;
-        double u = 0.0, px = 0.0, qx = 0.0;
-        if (t < d.drafted && t > 0) {
-            parent = d.parent(t);
-            id = d.ids[t];
-            u = unit(a.u[(size_t)b * a.tokens + t]);
-            if (parent >= 0 && (uint32_t)parent < t && id >= 0 && (uint32_t)id < a.vocab) {
-                px = mass(d.p[(int64_t)parent * a.p_token + id]);
-                if (DRAWN) qx = mass(d.q[(int64_t)parent * a.q_token + id]);
-            } else {
-                id = -1;
-            }
-        }
+        const Lot x0 = t0 ? lot_of<DRAWN>(a, b, d, t0, kept) : first;
+        const int32_t parent = t < d.drafted ? x0.parent : -1, id = x0.id;
+        const double u = x0.u, px = x0.px, qx = x0.qx;
         uint64_t refused = 0;                                            // of this lot, at this node
         uint64_t open = __ballot(t > s.last && t >= s.at && parent == (int32_t)s.last);
         while (open) {
@@ -122,7 +145,7 @@ __device__ __forceinline__ bool verify_walk(const VerifyArgs& a, uint32_t b, con
 constexpr uint32_t FILTER = 1 << 15, LISTED = 256;
 struct Refused { uint32_t filter[FILTER / 32], ids[LISTED], n; };
 template <uint32_t THREADS>
-__device__ __forceinline__ void list_refused(Refused& r, const Drafts& d, uint32_t last) {
+__device__ __forceinline__ void list_refused(Refused& r, const Drafts& d, const Lot& first, uint32_t last) {
     const uint32_t lane = threadIdx.x & 63u;
     for (uint32_t w = threadIdx.x; w < FILTER / 32; w += THREADS) r.filter[w] = 0;
     __syncthreads();
@@ -130,8 +153,9 @@ __device__ __forceinline__ void list_refused(Refused& r, const Drafts& d, uint32
         uint32_t count = 0;
         for (uint32_t t0 = last & ~63u; t0 < d.drafted; t0 += 64) {
             const uint32_t t = t0 + lane;
-            const bool child = t > last && t < d.drafted && d.parent(t) == (int32_t)last;
-            const uint32_t id = child ? (uint32_t)d.ids[t] : 0u;
+            bool child = t > last && t < d.drafted;
+            child = child && (t0 ? d.parent(t) : first.parent) == (int32_t)last;
+            const uint32_t id = !child ? 0u : t0 ? (uint32_t)d.ids[t] : (uint32_t)first.id;
             const uint64_t children = __ballot(child);
             const uint32_t at = count + (uint32_t)__builtin_popcountll(children & ((1ull << lane) - 1));
             if (child) atomicOr(&r.filter[id % FILTER / 32], 1u << (id % 32));
@@ -163,12 +187,28 @@ template <bool DRAWN> struct Weights {
     bool whole;                          // p as it is
     __device__ __forceinline__ Weights(const VerifyArgs& a, const Drafts& drafts, const VerifyState& s, const Refused& r)
         : p(drafts.p + (int64_t)s.last * a.p_token), q(DRAWN ? drafts.q + (int64_t)s.last * a.q_token : nullptr), C(s.C), refused(r), d(drafts), last(s.last), whole(false) {}
-    __device__ __forceinline__ double operator()(uint32_t v) const {
-        const double w = mass(p[v]);
+    __device__ __forceinline__ double of(uint32_t v, float pv, float qv) const {
+        const double w = mass(pv);
         if (whole) return w;
-        if (DRAWN) return fmax(w - C * mass(q[v]), 0.0);
+        if (DRAWN) return fmax(w - C * mass(qv), 0.0);
         if ((refused.filter[v % FILTER / 32] >> (v % 32) & 1u) && is_refused(refused, d, last, v)) return 0.0;
         return w;
+    }
+    // The sum over v, v + step, .. below `end`, eight numbers on their way at a time, also where fewer are left.
+    __device__ __forceinline__ double sum(uint32_t v, uint32_t step, uint32_t end) const {
+        double x = 0.0;
+        for (; v < end; v += 8 * step) {
+            float pv[8], qv[8] = {};
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k) pv[k] = p[min(v + k * step, end - 1)];
+            if (DRAWN)
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k) qv[k] = q[min(v + k * step, end - 1)];
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k)
+                if (v + k * step < end) x += of(v + k * step, pv[k], qv[k]);
+        }
+        return x;
     }
 };
 
@@ -201,26 +241,21 @@ __device__ __forceinline__ uint32_t find_piece(double mine, double& before, doub
 // Where the sum passes the target: a run is cut into 16 pieces, a wave sums each, and the piece that the target lies in is the next run, until that is short enough for registers.
 // piece_sum: of an earlier launch, of the row's pieces of `size` numbers, one a lane (size 0: there are none).
 template <bool DRAWN>
-__device__ __forceinline__ void verify_rest(const VerifyArgs& a, uint32_t b, const Drafts& d, VerifyState& s, double piece_sum, uint32_t size, double* sums, Refused& refused) {
+__device__ __forceinline__ void verify_rest(const VerifyArgs& a, uint32_t b, const Drafts& d, const Lot& first, float u0, VerifyState& s, double piece_sum, uint32_t size, double* sums, Refused& refused) {
     constexpr uint32_t SHORT = VERIFY_WAVES * 256;
     const uint32_t lane = threadIdx.x & 63u, wave = uni(threadIdx.x >> 6);
     if (size == 0)
-        verify_walk<DRAWN>(a, b, d, s, threadIdx.x == 0, [&](VerifyState& st) __attribute__((always_inline)) {
+        verify_walk<DRAWN>(a, b, d, lot_of<DRAWN>(a, b, d, 0, a.launches > 1), a.launches > 1, s, threadIdx.x == 0, [&](VerifyState& st) __attribute__((always_inline)) {
             const Weights<DRAWN> weight(a, d, st, refused);
-            double x = 0.0;
-            if constexpr (DRAWN) {
-#pragma unroll 8
-                for (uint32_t v = threadIdx.x; v < a.vocab; v += 64 * VERIFY_WAVES) x += weight(v);
-            }
-            st.R = everywhere<VERIFY_WAVES>(x, sums);
+            if constexpr (DRAWN) st.R = everywhere<VERIFY_WAVES>(weight.sum(threadIdx.x, 64 * VERIFY_WAVES, a.vocab), sums);
             return true;
         });
     if (threadIdx.x == 0) a.n_accepted[b] = (int32_t)s.n;
-    if (!DRAWN) list_refused<64 * VERIFY_WAVES>(refused, d, s.last);
+    if (!DRAWN) list_refused<64 * VERIFY_WAVES>(refused, d, first, s.last);
     Weights<DRAWN> weight(a, d, s, refused);
     uint32_t begin = 0, end = a.vocab;
     double before = 0.0, target = -1.0;                                  // the sum in front of the run
-    const double u = unit(a.u[(size_t)b * a.tokens]);
+    const double u = unit(u0);
     int32_t next = -1;
     if (size) {
         const double all = wave_sum(piece_sum);
@@ -236,10 +271,7 @@ __device__ __forceinline__ void verify_rest(const VerifyArgs& a, uint32_t b, con
     while (end - begin > SHORT || target < 0.0) {
         const uint32_t piece = ((end - begin + VERIFY_WAVES - 1) / VERIFY_WAVES + 63) & ~63u;
         const uint32_t from = begin + wave * piece, to = min(end, from + piece);
-        double x = 0.0;
-#pragma unroll 8
-        for (uint32_t v = from + lane; v < to; v += 64) x += weight(v);
-        const double all = everywhere<VERIFY_WAVES>(x, sums);
+        const double all = everywhere<VERIFY_WAVES>(weight.sum(from + lane, 64, to), sums);
         if (target < 0.0) {                                              // the first run is the row
             if (!(all > 0.0)) {
                 done = weight.whole;                                     // nothing at all: -1
@@ -255,10 +287,17 @@ __device__ __forceinline__ void verify_rest(const VerifyArgs& a, uint32_t b, con
     if (!done) {
         // 256 numbers to a wave, four to a lane, in order from 64 to 64
         double upto[4], w[4], x = 0.0;
+        float pv[4], qv[4] = {};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const uint32_t v = begin + wave * 256 + k * 64 + lane;
-            w[k] = v < end ? weight(v) : 0.0;
+            pv[k] = weight.p[min(v, end - 1)];
+            if (DRAWN) qv[k] = weight.q[min(v, end - 1)];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t v = begin + wave * 256 + k * 64 + lane;
+            w[k] = v < end ? weight.of(v, pv[k], qv[k]) : 0.0;
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -290,54 +329,81 @@ template <bool DRAWN>
 __global__ __launch_bounds__(64 * VERIFY_WAVES) void verify_drafts_kernel(const VerifyArgs a) {
     __shared__ double sums[VERIFY_WAVES];
     __shared__ Refused refused;
-    const uint32_t b = blockIdx.x;
+    const uint32_t b = blockIdx.x, lane = threadIdx.x & 63u;
     const Drafts d(a, b);
+    VerifyState s = {0.0, 1.0, 0, 1, 1, 0, 0};
+    double found[VERIFY_LAUNCHES] = {}, piece_sum = 0.0;
+    if (a.launches) {                                                    // what earlier launches found out: all of it is asked for at once
+        s = a.states[(size_t)(a.launches - 1) * a.batch + b];
+#pragma unroll
+        for (uint32_t l = 0; l < VERIFY_LAUNCHES; ++l)
+            if (l < a.launches && lane < a.pieces) found[l] = a.sums[((size_t)l * a.batch + b) * a.pieces + lane];
+    }
+    const Lot first = tokens_of(a, b, d, 0);
+    const float u0 = a.u[(size_t)b * a.tokens];
     if (d.drafted == 0) {
         if (threadIdx.x == 0) a.n_accepted[b] = 0;
         return;
     }
-    VerifyState s = {0.0, 1.0, 0, 1, 1, 0, 0, 0};
-    double piece_sum = 0.0;
-    if (a.launches) {                                                    // what earlier launches found out
-        s = a.states[(size_t)(a.launches - 1) * a.batch + b];
-        const uint32_t lane = threadIdx.x & 63u;
-        if (lane < a.pieces) piece_sum = a.sums[((size_t)((s.sums ? s.sums : a.launches) - 1) * a.batch + b) * a.pieces + lane];
-        if (!s.sums) {
-            s.R = wave_sum(piece_sum);
-            s.stale = 0;
-        }
+#pragma unroll
+    for (uint32_t l = 0; l < VERIFY_LAUNCHES; ++l)
+        if (l + 1 == (s.done ? s.done : a.launches)) piece_sum = found[l];
+    if (a.launches && !s.done) {
+        s.R = wave_sum(piece_sum);
+        s.stale = 0;
     }
-    verify_rest<DRAWN>(a, b, d, s, piece_sum, s.sums ? a.piece : 0u, sums, refused);
+    verify_rest<DRAWN>(a, b, d, first, u0, s, piece_sum, s.done ? a.piece : 0u, sums, refused);
 }
 
-// A row over several workgroups: each goes as far as it can without a pass (all of a sequence's do the same), leaves the sum of its piece of the
+// A row over several workgroups: the first wave of each goes as far as it can without a pass (all of a sequence's do the same), each leaves the sum of its piece of the
 // row that it came to, and the next launch goes on from there.
+// Latency bounds it, some 5 us a launch: its loads wait for one another (state, tokens, their probabilities, the row), so as many as can go together do, and the gathered ones are kept (32
+// trees of 16 over 50000 tokens, on average over their inputs: 41 us before that, and 37).
 template <bool DRAWN>
 __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyArgs a) {
     __shared__ double sums[4];
+    __shared__ VerifyState come;
     __shared__ Refused refused;
-    const uint32_t b = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces, lane = threadIdx.x & 63u;
-    const Drafts d(a, b);
-    if (d.drafted == 0) return;
-    VerifyState s = {0.0, 1.0, 0, 1, 1, 0, 0, 0};
+    const uint32_t b = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces, wave = uni(threadIdx.x >> 6);
     VerifyState* const to = a.states + (size_t)a.launch * a.batch + b;
+    VerifyState s = {0.0, 1.0, 0, 1, 1, 0, 0};
     if (a.launch) {
         s = a.states[(size_t)(a.launch - 1) * a.batch + b];
-        if (s.sums) {
+        if (s.done) {
             if (piece == 0 && threadIdx.x == 0) *to = s;
             return;
         }
-        const double* const from = a.sums + ((size_t)(a.launch - 1) * a.batch + b) * a.pieces;
-        s.R = wave_sum(lane < a.pieces ? from[lane] : 0.0);
-        s.stale = 0;
     }
-    if (verify_walk<DRAWN>(a, b, d, s, piece == 0 && threadIdx.x == 0, [](VerifyState&) { return false; })) s.sums = a.launch + 1;
-    if (!DRAWN) list_refused<256>(refused, d, s.last);
+    const Drafts d(a, b);
+    if (d.drafted == 0) {
+        s.done = 1;
+        if (piece == 0 && threadIdx.x == 0) *to = s;
+        return;
+    }
+    Lot first;
+    if (wave == 0) {
+        const uint32_t lane = threadIdx.x;
+        double piece_sum = 0.0;
+        if (a.launch && lane < a.pieces) piece_sum = a.sums[((size_t)(a.launch - 1) * a.batch + b) * a.pieces + lane];
+        first = lot_of<DRAWN>(a, b, d, 0, a.launch > 0);
+        if (a.launch) {
+            s.R = wave_sum(piece_sum);
+            s.stale = 0;
+        }
+        if (verify_walk<DRAWN>(a, b, d, first, a.launch > 0, s, piece == 0 && lane == 0, [](VerifyState&) { return false; })) s.done = a.launch + 1;
+        if (lane == 0) come = s;
+    }
+    if (DRAWN && a.launch == 0 && a.launches > 1)
+        for (uint32_t t0 = (piece * 4 + wave) * 64; t0 < a.tokens; t0 += a.pieces * 256) {
+            const Lot x = t0 ? lot_of<DRAWN>(a, b, d, t0, false) : first;
+            const uint32_t t = t0 + (threadIdx.x & 63u);
+            if (t < a.tokens) a.kept[(size_t)b * a.tokens + t] = VerifyToken{(float)x.px, (float)x.qx};
+        }
+    __syncthreads();
+    s = {lane_value(come.C, 0), lane_value(come.R, 0), uni(come.last), uni(come.n), uni(come.at), uni(come.stale), uni(come.done)};   // (the same in every lane: 12 us longer where the compiler was not told)
+    if (!DRAWN) list_refused<256>(refused, d, first, s.last);
     const Weights<DRAWN> weight(a, d, s, refused);
-    const uint32_t end = min(a.vocab, (piece + 1) * a.piece);
-    double x = 0.0;
-#pragma unroll 8
-    for (uint32_t v = piece * a.piece + threadIdx.x; v < end; v += 256) x += weight(v);
+    double x = weight.sum(piece * a.piece + threadIdx.x, 256, min(a.vocab, (piece + 1) * a.piece));
     x = everywhere<4>(x, sums);
     if (threadIdx.x == 0) {
         a.sums[((size_t)a.launch * a.batch + b) * a.pieces + piece] = x;

@@ -320,3 +320,6 @@ def test_verification(B, T, V, shape, drawn):
         check_verify(p, ids, u, q if drawn else None, words)
     drafted = ints([T - (i * T) // max(B, 2) for i in range(B)])
     check_verify(p, ids, u, q if drawn else None, words, drafted)
+    # sequences without drafts, and a workspace that holds something
+    room = ds.verify_drafts_workspace(p, ids, u, torch.empty_like(ids), ints([0] * B), ints([0] * B), q=q if drawn else None, parents=words)
+    check_verify(p, ids, u, q if drawn else None, words, ints([T * (i % 2) for i in range(B)]), workspace=torch.full((room + 16,), 255, dtype=torch.uint8, device="cuda"))
