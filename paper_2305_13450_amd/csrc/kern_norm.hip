@@ -35,7 +35,7 @@ template <int LANES> __device__ __forceinline__ float row_sum(float x) {
 
 // A wave takes 8 heads of 128 numbers (16 of 64) of one token, queries or keys.  A lane holds two runs of 8 numbers of a head that are each other's partners
 // (8 u and 8 u + rotary_dim / 2; interleaved, and behind rotary_dim: 16 u and 16 u + 8), D / 16 lanes to a head, so no number crosses lanes but the sum of
-// squares.  Bound by HBM, read and written once: 4 x 2048 tokens of 64 + 8 heads of 128, 302 MB, in 60 us, 5.0 TB/s where a copy has 5.1; the eight angles of a lane are worked
+// squares.  Bound by HBM, read and written once: 4 x 2048 tokens of 64 + 8 heads of 128, 302 MB, in 53 us warm and 57 to 62 in turn with others, 5 TB/s as a copy; the eight angles of a lane are worked
 // out anew by each of a token's 9 waves meanwhile.  What L2 cannot hold for the next kernel is stored past it (inputs that change, 302 MB: 68 and 66 us, 84 MB: 22 and 20).  One token of 32 sequences: 4.4 us, four loads behind one another.
 template <typename T, int D, bool INTERLEAVED, bool NORM, bool STREAMS>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkNormArgs a) {
