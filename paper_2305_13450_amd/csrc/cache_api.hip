@@ -93,17 +93,25 @@ int tree_operands(const depsync_tree_attn_desc* d, TreeAttnArgs& a, int multiple
 // second kernel and the results' way there and back.  5.9 is what a second launch costs a program that waits for the host (one token of 12 heads over 500
 // rows 12.4 us in one launch, 15.5 in two); captured into a graph it is about 4 (12.1 and 11.6).  The lengths are the longest sequence's; the
 // kernels then share out the parts by the real ones.
-// Over a cache of 8 bits (fitted to measured times of 1 to 128 rows): a block takes the form for few rows 0.8 us for up to 16 rows of 128 and 1.1 for 32 (0.6 and 0.8 of 64) while its
-// workgroup is alone on a CU, 1.7 times as long where two share it; and HBM, which one workgroup a CU saturates, gives a tenth less to two.
-double tree_cost(int64_t base, int64_t part, int64_t blocks, int64_t pairs, int64_t rows, int64_t row_blocks, int head_dim, int n_cu, bool few, bool held) {
+// Over a cache of 8 bits the form for few rows has constants of its own, fitted to 46 shapes of 1 to 64 rows and both head sizes, cut in up to 128 parts: a block takes 0.75 us for up to 16 rows of 128 and
+// 1.3 for 32 (0.62 and 1.0 with 64) while its workgroup is alone on a CU, 1.4 times as long where two share it, or what HBM lets through, a quarter less to two. Several
+// sequences count as three quarters of the longest: parts divide the real lengths between them, so cutting evens them out, and uncut ones leave HBM to the longest in the end (12 sequences of 1000 to
+// 4000 rows, 25 query rows: 46 us uncut, as taking all for the longest has it, and 35; 8 of 500 to 4096, 64 rows: 30 and 26). The cut taken is on average 2.7 % behind the best, 4.3 % without that.
+double tree_cost(int64_t base, int64_t part, int64_t blocks, int64_t pairs, int64_t rows, int64_t row_blocks, int head_dim, int n_cu, bool few, bool held, int64_t batch) {
     const int64_t parts = cdiv64(blocks, part), groups = base * parts, slots = 2 * (int64_t)n_cu;
     const double at_once = (double)std::min(groups, slots), wide = head_dim / 128.0;
     double step = few ? 0.13 + 1.32 * wide : (at_once > n_cu ? 1.0 : at_once > n_cu / 2 ? 0.8 : 0.55) * (0.3 + 0.7 * wide);
-    if (few && held) step = (0.2 + 0.3 * wide + (rows <= 16 ? 0.15 : 0.3) * (1.0 + wide)) * (at_once > n_cu ? 1.7 : 1.0);
-    const double rate = held ? (at_once > n_cu ? 9.4e6 : 10.4e6) : 5.2e6;   // of a cached row's 4 bytes a dimension
-    const double hbm = at_once / row_blocks * (few ? TREE_FEW_KEYS : TREE_MANY_KEYS) * 4.0 * head_dim / rate;
-    const double join = parts > 1 ? 5.9 + (double)parts * pairs * rows * (head_dim + 2) * 8.0 / 4e6 : 0.0;
-    return (double)cdiv64(groups, slots) * (3.0 + part * std::cbrt(step * step * step + hbm * hbm * hbm)) + join;   // (between the larger and the sum)
+    double rate = held ? (at_once > n_cu ? 9.4e6 : 10.4e6) : 5.2e6, start = 5.9;   // of a cached row's 4 bytes a dimension; of a second launch
+    double mean = 1.0, late = 1.0;                                 // of the longest sequence: what a part has, and what HBM has to bring while that is walked
+    if (few && held) {
+        step = (0.25 + 0.25 * wide + (rows <= 16 ? 0.25 : 0.4) * (1.0 + wide)) * (at_once > n_cu ? 1.4 : 1.0);
+        rate = at_once > n_cu ? 9.8e6 : 13e6;
+        start = 5.5;
+        if (batch > 1) (parts > 1 ? mean : late) = 0.75;
+    }
+    const double hbm = at_once / row_blocks * (few ? TREE_FEW_KEYS : TREE_MANY_KEYS) * 4.0 * head_dim / rate * late;
+    const double join = parts > 1 ? start + (double)parts * pairs * rows * (head_dim + 2) * 8.0 / 4e6 : 0.0;
+    return (double)cdiv64(groups, slots) * (3.0 + mean * part * std::cbrt(step * step * step + hbm * hbm * hbm)) + join;   // (between the larger and the sum)
 }
 
 int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t& bytes, int held = 0) {   // held: rows of a block of a cache of 8 bits
@@ -126,14 +134,14 @@ int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t
     const int64_t wide = d->tokens + held;                         // rows of 16 bits behind those of full blocks (and room up to a tile)
     const int64_t blocks = cdiv64(rows_hint(d->max_cached, d->capacity), keys) + cdiv64(wide, keys);
     int64_t part = blocks;
-    double best = tree_cost(base, part, blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few, held != 0);
+    double best = tree_cost(base, part, blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few, held != 0, d->batch);
     for (int64_t rounds = 1; rounds <= 4; ++rounds) {             // parts that fill the chip a whole number of times
         const int64_t parts = std::min(blocks, std::max<int64_t>(1, rounds * 2 * n_cu / base)), p = cdiv64(blocks, parts);
-        const double t = tree_cost(base, p, blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few, held != 0);
+        const double t = tree_cost(base, p, blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few, held != 0, d->batch);
         if (t < best) { best = t; part = p; }
         if (p + 1 > blocks) continue;
         for (int64_t q : {2 * p, 4 * p}) {                         // or fewer, where their results cost more
-            const double u = tree_cost(base, std::min(q, blocks), blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few, held != 0);
+            const double u = tree_cost(base, std::min(q, blocks), blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few, held != 0, d->batch);
             if (u < best) { best = u; part = std::min(q, blocks); }
         }
     }
