@@ -93,24 +93,30 @@ int tree_operands(const depsync_tree_attn_desc* d, TreeAttnArgs& a, int multiple
 // second kernel and the results' way there and back.  5.9 is what a second launch costs a program that waits for the host (one token of 12 heads over 500
 // rows 12.4 us in one launch, 15.5 in two); captured into a graph it is about 4 (12.1 and 11.6).  The lengths are the longest sequence's; the
 // kernels then share out the parts by the real ones.
-// Over a cache of 8 bits the form for few rows has constants of its own, fitted to 46 shapes of 1 to 64 rows and both head sizes, cut in up to 128 parts: a block takes 0.75 us for up to 16 rows of 128 and
+// Over a cache of 8 bits the form for few rows has constants of its own, fitted to 46 shapes of 1 to 64 rows and both head sizes: a block takes 0.75 us for up to 16 rows of 128 and
 // 1.3 for 32 (0.62 and 1.0 with 64) while its workgroup is alone on a CU, 1.4 times as long where two share it, or what HBM lets through, a quarter less to two. Several
 // sequences count as three quarters of the longest: parts divide the real lengths between them, so cutting evens them out, and uncut ones leave HBM to the longest in the end (12 sequences of 1000 to
 // 4000 rows, 25 query rows: 46 us uncut, as taking all for the longest has it, and 35; 8 of 500 to 4096, 64 rows: 30 and 26). The cut taken is on average 2.7 % behind the best, 4.3 % without that.
+// The form for many rows (28 shapes): a block as below, never HBM; 0.5 % behind the best cut, 3 % with the constants over 16 bits (8 sequences of 2300 rows, 252 query rows: 66 us uncut, and 48).
 double tree_cost(int64_t base, int64_t part, int64_t blocks, int64_t pairs, int64_t rows, int64_t row_blocks, int head_dim, int n_cu, bool few, bool held, int64_t batch) {
     const int64_t parts = cdiv64(blocks, part), groups = base * parts, slots = 2 * (int64_t)n_cu;
     const double at_once = (double)std::min(groups, slots), wide = head_dim / 128.0;
     double step = few ? 0.13 + 1.32 * wide : (at_once > n_cu ? 1.0 : at_once > n_cu / 2 ? 0.8 : 0.55) * (0.3 + 0.7 * wide);
-    double rate = held ? (at_once > n_cu ? 9.4e6 : 10.4e6) : 5.2e6, start = 5.9;   // of a cached row's 4 bytes a dimension; of a second launch
+    double rate = 5.2e6, start = 5.9, results = 4e6;               // of a cached row's 4 bytes a dimension; of a second launch, and of what it reads
     double mean = 1.0, late = 1.0;                                 // of the longest sequence: what a part has, and what HBM has to bring while that is walked
     if (few && held) {
         step = (0.25 + 0.25 * wide + (rows <= 16 ? 0.25 : 0.4) * (1.0 + wide)) * (at_once > n_cu ? 1.4 : 1.0);
         rate = at_once > n_cu ? 9.8e6 : 13e6;
         start = 5.5;
         if (batch > 1) (parts > 1 ? mean : late) = 0.75;
+    } else if (held) {
+        step = (at_once > n_cu ? 1.07 : at_once > n_cu / 2 ? 0.82 : 0.76) * (0.5 + 0.5 * wide);
+        late = 0.0;
+        start = 8.0;
+        results = 6e6;
     }
     const double hbm = at_once / row_blocks * (few ? TREE_FEW_KEYS : TREE_MANY_KEYS) * 4.0 * head_dim / rate * late;
-    const double join = parts > 1 ? start + (double)parts * pairs * rows * (head_dim + 2) * 8.0 / 4e6 : 0.0;
+    const double join = parts > 1 ? start + (double)parts * pairs * rows * (head_dim + 2) * 8.0 / results : 0.0;
     return (double)cdiv64(groups, slots) * (3.0 + mean * part * std::cbrt(step * step * step + hbm * hbm * hbm)) + join;   // (between the larger and the sum)
 }
 
