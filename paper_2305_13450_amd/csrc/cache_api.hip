@@ -141,8 +141,10 @@ int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t
     const int64_t blocks = cdiv64(rows_hint(d->max_cached, d->capacity), keys) + cdiv64(wide, keys);
     int64_t part = blocks;
     double best = tree_cost(base, part, blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few, held != 0, d->batch);
-    for (int64_t rounds = 1; rounds <= 4; ++rounds) {             // parts that fill the chip a whole number of times
-        const int64_t parts = std::min(blocks, std::max<int64_t>(1, rounds * 2 * n_cu / base)), p = cdiv64(blocks, parts);
+    for (int64_t rounds = 1, before = 0, p; rounds <= 4; ++rounds, before = p) {   // parts that fill the chip a whole number of times
+        const int64_t parts = std::min(blocks, std::max<int64_t>(1, rounds * 2 * n_cu / base));
+        p = cdiv64(blocks, parts);
+        if (p == before) continue;
         const double t = tree_cost(base, p, blocks, pairs, rows, row_blocks, d->head_dim, n_cu, a.few, held != 0, d->batch);
         if (t < best) { best = t; part = p; }
         if (p + 1 > blocks) continue;

@@ -276,7 +276,7 @@ def test_verification_of_odd_numbers(V, drawn):
         check_verify(p, ids, v, q if drawn else None)
 
 
-@pytest.mark.parametrize("T,V", [(400, 700), (320, 17000), (1000, 300)])
+@pytest.mark.parametrize("T,V", [(400, 700), (320, 17000), (1000, 300), (4096, 16400)])
 @pytest.mark.parametrize("drawn", [True, False], ids=["drawn", "likely"])
 def test_verification_of_hundreds_of_children(T, V, drawn):
     g = gen(32)
