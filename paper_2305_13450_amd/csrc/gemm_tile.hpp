@@ -76,7 +76,8 @@ typedef __attribute__((address_space(3))) void* lptr_t;
 // counts it exactly.  global_load_lds is a FLAT instruction that touches LDS; with one in flight every wait for an
 // LDS read became a wait for all of them (2048 tokens of the 12288 x 6144 x 12288 chain 507 -> 499 us, one token of
 // 1024 x 1024 x 1024 14.1 -> 13.1).  (An operand is smaller than 4 GiB; `bytes` is where it ends: reads at
-// and past that offset, 0xfffffff0 at the latest, give zeros.)
+// and past that offset, 0xfffffff0 at the latest, give zeros.  The builtin is documented to leave `uniform_off` out of that check, so
+// where reads may lie past the end `off` alone has to reach it: a row that may not be there is counted in `off`.)
 struct OperandBuf {
     __amdgpu_buffer_rsrc_t rsrc;
     __device__ __forceinline__ explicit OperandBuf(const char* uniform_base, uint32_t bytes = 0xffffffffu)

@@ -448,9 +448,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn_few(const TreeAttnArgs a) {
         const uint32_t bytes = uni(run_bytes<D>(x)), first = lrow * x.pitch + chunk * 16;
         const OperandBuf K(uni_ptr(x.k), bytes), V(uni_ptr(x.v), bytes);   // rows that are not there: zeros
 #pragma unroll
-        for (uint32_t i = 0; i < Tile::NI; ++i) kreg[i] = K.load16(first, i * Tile::RPI * x.pitch);
+        for (uint32_t i = 0; i < Tile::NI; ++i) kreg[i] = K.load16(first + i * Tile::RPI * x.pitch, 0);
 #pragma unroll
-        for (uint32_t i = 0; i < Tile::NI; ++i) vreg[i] = V.load16(first, i * Tile::RPI * x.pitch);
+        for (uint32_t i = 0; i < Tile::NI; ++i) vreg[i] = V.load16(first + i * Tile::RPI * x.pitch, 0);
     };
     KeyRun x = key_run<D>(a, j, j.begin, TREE_FEW_KEYS, wave * 32, 32);
     fetch(x);
@@ -588,9 +588,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn_many(const TreeAttnArgs a) {
         const OperandBuf K(uni_ptr(x.k), bytes), V(uni_ptr(x.v), bytes);
         f.drafted = x.drafted;
 #pragma unroll
-        for (uint32_t i = 0; i < NI; ++i) f.k[i] = K.load16(first, i * Tile::RPI * x.pitch);
+        for (uint32_t i = 0; i < NI; ++i) f.k[i] = K.load16(first + i * Tile::RPI * x.pitch, 0);
 #pragma unroll
-        for (uint32_t i = 0; i < NI; ++i) f.v[i] = V.load16(first, i * Tile::RPI * x.pitch);
+        for (uint32_t i = 0; i < NI; ++i) f.v[i] = V.load16(first + i * Tile::RPI * x.pitch, 0);
     };
     auto finite = [&](Staged& f) __attribute__((always_inline)) {
         bool bad = false;

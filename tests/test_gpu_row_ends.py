@@ -1,0 +1,41 @@
+"""GPU tests that nothing behind a sequence's last row is read: what lies there, NaN and infinities, changes no bit of a result."""
+import pytest
+import torch
+
+import paper_2305_13450_amd as ds
+from test_gpu_draft_ops import BF, FP, INF, NAN, gen, ints, normal, same, tree_of
+
+pytestmark = pytest.mark.gpu
+BOTH = pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+
+
+def behind(x, lens, value):
+    """A copy of x [B, rows, H, D] with `value` in every row from lens[b] on."""
+    y = x.clone()
+    for b, n in enumerate(lens):
+        y[b, n:] = value
+    return y
+
+
+# up to 32 rows to a head and more than 64: both forms; every number of rows in a last tile, of cached rows and of drafted tokens
+@BOTH
+@pytest.mark.parametrize("B,T,Hq,Hk,D", [(64, 7, 4, 2, 128), (100, 4, 4, 1, 64), (40, 40, 4, 1, 128), (36, 70, 2, 1, 64)])
+def test_attention_reads_nothing_behind_the_ends(B, T, Hq, Hk, D, dtype):
+    print("ends", B, T, Hq, Hk, D, dtype, flush=True)
+    g = gen(91)
+    lens, drafted = [1 + (5 * b) % 97 for b in range(B)], [1 + b % T for b in range(B)]
+    cap = 97
+    q, kn, vn = normal(g, (B, T, Hq, D), dtype, 2.0), normal(g, (B, T, Hk, D), dtype), normal(g, (B, T, Hk, D), dtype)
+    kc, vc = normal(g, (B, cap, Hk, D), dtype), normal(g, (B, cap, Hk, D), dtype)
+    _, tree = tree_of(g, B, T)
+    for words in (None, tree):
+        got = []
+        for value in (0.0, NAN, INF):
+            out, lse = torch.zeros_like(q), torch.zeros((B, T, Hq), device="cuda")
+            ds.dep_tree_attn(q, behind(kn, drafted, value), behind(vn, drafted, value), behind(kc, lens, value), behind(vc, lens, value), ints(lens), out, lse=lse,
+                             tree=words, drafted=ints(drafted))
+            torch.cuda.synchronize()
+            got.append((out, lse))
+        assert bool(got[0][0].isfinite().all())
+        for out, lse in got[1:]:
+            assert same(out, got[0][0]) and same(lse, got[0][1])
