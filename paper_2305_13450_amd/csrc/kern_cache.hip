@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256, 3) void cache_weights_few_kernel(const CacheWe
         const OperandBuf K(uni_ptr(keys + (int64_t)first * pitch), uni(have ? (have - 1) * pitch + D * 2u : 0u));   // (rows that are not there: zeros)
         const uint32_t off = lrow * pitch + chunk * 16;
 #pragma unroll
-        for (uint32_t i = 0; i < Tile::NI; ++i) kreg[i] = K.load16(off, i * Tile::RPI * pitch);
+        for (uint32_t i = 0; i < Tile::NI; ++i) kreg[i] = K.load16(off + i * Tile::RPI * pitch, 0);
         if (lane < have) old = weights[first + lane];
     };
     fetch(begin);
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 2) void cache_weights_many_kern
             const OperandBuf K(uni_ptr(p), uni((have - 1) * pitch + D * 2u));   // (rows that are not there: zeros)
             u32x4 reg[NK];                                         // (tiles of 32 keys behind one another)
 #pragma unroll
-            for (uint32_t i = 0; i < NK; ++i) reg[i] = K.load16(lrow * pitch + chunk * 16, (wave * NK + i) * Tile::RPI * pitch);
+            for (uint32_t i = 0; i < NK; ++i) reg[i] = K.load16(((wave * NK + i) * Tile::RPI + lrow) * pitch + chunk * 16, 0);
             __syncthreads();                                       // (the rows of the keys before are done with)
 #pragma unroll
             for (uint32_t i = 0; i < NK; ++i) {
@@ -220,7 +220,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES / 2) void cache_weights_many_kern
             if (!a.accepted) {                                     // (rows that are not there: zeros)
                 const OperandBuf Q(uni_ptr(q + (int64_t)at.i * a.q_s.token), uni((min(32u, n - at.i) - 1) * q_pitch + D * 2u));
 #pragma unroll
-                for (uint32_t i = 0; i < Tile::NI; ++i) qreg[i] = Q.load16(lrow * q_pitch + chunk * 16, i * Tile::RPI * q_pitch);
+                for (uint32_t i = 0; i < Tile::NI; ++i) qreg[i] = Q.load16((i * Tile::RPI + lrow) * q_pitch + chunk * 16, 0);
             } else {                                               // (the last one)
 #pragma unroll
                 for (uint32_t i = 0; i < Tile::NI; ++i)

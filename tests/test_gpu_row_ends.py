@@ -39,3 +39,24 @@ def test_attention_reads_nothing_behind_the_ends(B, T, Hq, Hk, D, dtype):
         assert bool(got[0][0].isfinite().all())
         for out, lse in got[1:]:
             assert same(out, got[0][0]) and same(lse, got[0][1])
+
+
+# accepted paths (up to 64 rows to a head) and prompts: the keys' ends, and with rows taken in order the queries'
+@BOTH
+@pytest.mark.parametrize("B,T,Hq,Hk,D", [(97, 6, 4, 2, 128), (97, 9, 4, 1, 64), (3, 97, 4, 1, 128), (3, 97, 4, 2, 64), (97, 33, 8, 2, 128), (97, 70, 2, 1, 64)])
+def test_weights_read_nothing_behind_the_ends(B, T, Hq, Hk, D, dtype):
+    print("weights' ends", B, T, Hq, Hk, D, dtype, flush=True)
+    g = gen(92)
+    cap = 200
+    n = [1 + (7 * b) % T for b in range(B)]
+    lens = [n[b] + (11 * b) % (cap - T) for b in range(B)]
+    q, kc, lse = normal(g, (B, T, Hq, D), dtype, 2.0), normal(g, (B, cap, Hk, D), dtype), 8 + torch.randn((B, T, Hq), generator=g, device="cuda")
+    got = []
+    for value in (0.0, NAN, INF):
+        w = torch.zeros((B, Hk, cap), device="cuda")
+        ds.dep_cache_weights(behind(q, n, value), behind(lse.unsqueeze(-1), n, 0.0).squeeze(-1).contiguous(), behind(kc, lens, value), ints(lens), w, n_accepted=ints(n))
+        torch.cuda.synchronize()
+        got.append(w)
+    assert bool(got[0].isfinite().all()) and all(same(w, got[0]) for w in got[1:])
+    for b in range(B):
+        assert bool((got[0][b, :, lens[b]:] == 0).all()) and bool((got[0][b, :, : lens[b] - n[b] + 1] > 0).all())
