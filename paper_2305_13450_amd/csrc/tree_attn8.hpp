@@ -33,6 +33,8 @@ __device__ __forceinline__ TreeUnit tree_unit8(uint32_t row_blocks, uint32_t tog
     return {(((n >> together) * 8 + (blockIdx.x & 7u)) << together) + (n & ((1u << together) - 1u)), slot % row_blocks};
 }
 
+constexpr uint32_t NOWHERE = 1u << 31;   // an offset behind the end of any tile: nothing is read, and zeros come
+
 // Two of four 8-bit numbers as numbers of T.
 template <typename T> struct Held8;
 template <> struct Held8<__bf16> {
@@ -158,11 +160,12 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
     const uint32_t lrow = lane / CHUNKS, chunk = lane % CHUNKS, bytes = uni(31 * pitch + D);
     auto fetch = [&](Tile8& x, uint32_t t) __attribute__((always_inline)) {
         const uint64_t at = (uint64_t)t * TREE_FEW_KEYS * pitch;
-        const OperandBuf K(kp + at, t < tiles ? bytes : 0u), V(vp + at, t < tiles ? bytes : 0u);   // (behind the last: zeros)
+        const OperandBuf K(kp + at, bytes), V(vp + at, bytes);
+        const uint32_t off = t < tiles ? lrow * pitch + chunk * 16 : NOWHERE;
 #pragma unroll
-        for (uint32_t i = 0; i < NI; ++i) x.k[i] = K.load16(lrow * pitch + chunk * 16, i * RPI * pitch);
+        for (uint32_t i = 0; i < NI; ++i) x.k[i] = K.load16(off, i * RPI * pitch);
 #pragma unroll
-        for (uint32_t i = 0; i < NI; ++i) x.v[i] = V.load16(lrow * pitch + chunk * 16, i * RPI * pitch);
+        for (uint32_t i = 0; i < NI; ++i) x.v[i] = V.load16(off, i * RPI * pitch);
         const uint32_t block = uni(min((first + t * TREE_FEW_KEYS) >> a.block_log2, a.n_blocks - 1));
         x.ks = ksp[block];
         x.vs = vsp[block];
@@ -457,7 +460,6 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
     const OperandBuf KS(uni_ptr(a.k_scale + scales), a.n_blocks * 4u), VS(uni_ptr(a.v_scale + scales), a.n_blocks * 4u);
     // A tile on its way: of 8 bits the first D / 8 bytes of k[0] and v[0] (D = 64: of h), else all of k and v.
     struct Staged { u32x4 k[NI], v[NI]; u32x2 h[2]; uint32_t ks, vs; } staged[2];
-    constexpr uint32_t NOWHERE = 1u << 31;                             // an offset behind the end of any tile: nothing is read, and zeros come
     auto load8 = [&](Staged& f, const OperandBuf& K, const OperandBuf& V, uint32_t off, uint32_t scale) __attribute__((always_inline)) {
         if constexpr (D == 128) {
             f.k[0] = K.load16(off, 0);

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import draft_ref
 import paper_2305_13450_amd as ds
 from test_gpu_draft_ops import BF, FP, INF, NAN, gen, ints, normal, same, tree_of
 
@@ -60,3 +61,29 @@ def test_weights_read_nothing_behind_the_ends(B, T, Hq, Hk, D, dtype):
     assert bool(got[0].isfinite().all()) and all(same(w, got[0]) for w in got[1:])
     for b in range(B):
         assert bool((got[0][b, :, lens[b]:] == 0).all()) and bool((got[0][b, :, : lens[b] - n[b] + 1] > 0).all())
+
+
+@BOTH
+@pytest.mark.parametrize("B,T,Hq,Hk,D,block", [(64, 7, 4, 2, 128, 32), (100, 4, 4, 1, 64, 64), (40, 40, 4, 1, 128, 128), (36, 70, 2, 1, 64, 32), (48, 14, 4, 2, 128, 64)])
+def test_attention_over_8_bits_reads_nothing_behind_the_ends(B, T, Hq, Hk, D, block, dtype):
+    print("8-bit ends", B, T, Hq, Hk, D, block, dtype, flush=True)
+    g = gen(93)
+    cap = 4 * block
+    lens, drafted = [(29 * b) % (cap + 1) for b in range(B)], [1 + b % T for b in range(B)]
+    full, held = [n // block * block for n in lens], [n % block for n in lens]
+    q, kn, vn = normal(g, (B, T, Hq, D), dtype, 2.0), normal(g, (B, T, Hk, D), dtype), normal(g, (B, T, Hk, D), dtype)
+    k, v, ks, vs, kt, vt = draft_ref.make_cache(g, B, cap, Hk, D, block, dtype)
+    eight = lambda x, byte: behind(x.view(torch.uint8), full, byte).view(x.dtype)
+    ends = lambda s, value: behind(s.transpose(1, 2), [n // block for n in full], value).transpose(1, 2).contiguous()   # (full blocks have scales)
+    _, tree = tree_of(g, B, T)
+    for words in (None, tree):
+        got = []
+        for value, byte in ((0.0, 0), (NAN, 127), (INF, 126)):
+            out, lse = torch.zeros_like(q), torch.zeros((B, T, Hq), device="cuda")
+            ds.dep_tree_attn8(q, behind(kn, drafted, value), behind(vn, drafted, value), eight(k, byte), eight(v, byte), ends(ks, value), ends(vs, value),
+                              behind(kt, held, value), behind(vt, held, value), ints(lens), out, lse=lse, tree=words, drafted=ints(drafted))
+            torch.cuda.synchronize()
+            got.append((out, lse))
+        assert bool(got[0][0].isfinite().all())
+        for out, lse in got[1:]:
+            assert same(out, got[0][0]) and same(lse, got[0][1])
