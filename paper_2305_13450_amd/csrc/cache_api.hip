@@ -177,10 +177,10 @@ int evict_check(const depsync_cache_evict_desc* d) {
 
 bool cache8_block(int block, int capacity) { return (block == 32 || block == 64 || block == 128) && capacity >= block && capacity % block == 0; }
 
-// Hundreds of children of one node are compared with one another, so tokens are limited to what a draft may have.
+// The children refused at one node are listed in LDS, so tokens are limited to what a draft may have.
 int verify_check(const depsync_verify_drafts_desc* d) {
     if (!d || d->batch < 1 || d->batch > 1 << 20 || d->tokens < 1 || d->tokens > 65536 || d->vocab < 1 || d->vocab > 1 << 24) return DEPSYNC_EINVAL;
-    return d->tokens > 4096 ? DEPSYNC_ENOTIMPL : DEPSYNC_OK;
+    return d->tokens > (int32_t)VERIFY_TOKENS ? DEPSYNC_ENOTIMPL : DEPSYNC_OK;
 }
 
 // How dep_verify_drafts spreads its rows.  One workgroup to a sequence has some 32 KB of reads on their way, 30 to 80 GB/s (32 chains of 6 over 50257 tokens: 43 us, 18 with

@@ -86,6 +86,7 @@ struct VerifyArgs {
     uint32_t pieces, piece;               // workgroups to a row, numbers that each sums
 };
 constexpr uint32_t VERIFY_PIECES = 64, VERIFY_LAUNCHES = 7;   // at most
+constexpr uint32_t VERIFY_TOKENS = 4096, VERIFY_FEW = 512;    // of a sequence at most; up to which the refused ones take less LDS
 
 struct CacheAppendArgs {
     const void *k_new, *v_new;

@@ -51,6 +51,12 @@ struct Drafts {
     __device__ __forceinline__ int32_t parent(uint32_t t) const { return parents ? parents[t] : (int32_t)t - 1; }
 };
 
+// A wave's LDS accesses keep their order.
+__device__ __forceinline__ void in_order() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // 64 tokens from t0 on, a lane each.  Their probabilities are gathered from rows far apart once: where launches follow one another the first keeps them.
 struct Lot {
     int32_t parent = -1, id = -1;        // -1: none, or not in the vocabulary
@@ -84,19 +90,53 @@ template <bool DRAWN> __device__ __forceinline__ Lot lot_of(const VerifyArgs& a,
     return x;
 }
 
+// The children refused at the last token that stays, without q: their probabilities count for nothing.  Their numbers in a table of twice as many places (from a
+// number's own on, the first that is free), and a filter of 2^15 bits by which hardly any other token of the vocabulary is looked for in it.  Up to 512 tokens: 8 KB, which cost no
+// launch a place on a CU; up to 4096: 36 KB.  (2 stars of 200 refused children over 32000 numbers: 33 us; of 4096: 0.48 ms, nearly all of it the walk from child to child, 0.11 us each.)
+constexpr uint32_t FILTER = 1 << 15;
+template <uint32_t LISTED> struct Refused {
+    static constexpr uint32_t PLACES = 2 * LISTED, FREE = ~0u;
+    uint32_t filter[FILTER / 32], table[PLACES];
+    static __device__ __forceinline__ uint32_t place(uint32_t id) { return id * 0x9e3779b1u >> (32 - __builtin_ctz(PLACES)); }
+    template <uint32_t THREADS> __device__ __forceinline__ void clear(uint32_t thread) {
+        for (uint32_t i = thread; i < FILTER / 128; i += THREADS) ((u32x4*)filter)[i] = u32x4{0, 0, 0, 0};
+        for (uint32_t i = thread; i < PLACES / 4; i += THREADS) ((u32x4*)table)[i] = u32x4{FREE, FREE, FREE, FREE};
+    }
+    // (LISTED different ones at most, so a place is free)
+    __device__ __forceinline__ void add(uint32_t id) {
+        for (uint32_t i = place(id);; i = (i + 1) % PLACES) {
+            const uint32_t there = atomicCAS(&table[i], FREE, id);
+            if (there == FREE || there == id) break;
+        }
+        atomicOr(&filter[id % FILTER / 32], 1u << (id % 32));
+    }
+    __device__ __forceinline__ bool listed(uint32_t id) const {
+        for (uint32_t i = place(id);; i = (i + 1) % PLACES) {
+            const uint32_t there = table[i];
+            if (there == id) return true;
+            if (there == FREE) return false;
+        }
+    }
+    __device__ __forceinline__ bool has(uint32_t id) const { return (filter[id % FILTER / 32] >> (id % 32) & 1u) && listed(id); }
+};
+
 // From s.at on; every wave that calls this does the same.  The children of the last one that stays are found by a ballot.  first: the lot from 0 on.
 // Where R is needed and stale: pass(s) renews it, or returns false, and so does this then.
-template <bool DRAWN, class Pass>
-__device__ __forceinline__ bool verify_walk(const VerifyArgs& a, uint32_t b, const Drafts& d, const Lot& first, bool kept, VerifyState& s, bool write, Pass pass) {
+// Without q one wave of a workgroup calls this, from the first token on, and `refused`, empty before, holds the children of s.last afterwards.
+template <bool DRAWN, class Set, class Pass>
+__device__ __forceinline__ bool verify_walk(const VerifyArgs& a, uint32_t b, const Drafts& d, const Lot& first, bool kept, VerifyState& s, bool write, Set& refused, Pass pass) {
     const uint32_t lane = threadIdx.x & 63u;
+    bool some = false;                                                   // `refused` is not empty: children of earlier lots
     if (write && s.at == 1) a.accepted[(size_t)b * a.tokens] = 0;
     for (uint32_t t0 = s.at & ~63u; t0 < d.drafted; t0 += 64) {
         const uint32_t t = t0 + lane;
         const Lot x0 = t0 ? lot_of<DRAWN>(a, b, d, t0, kept) : first;
         const int32_t parent = t < d.drafted ? x0.parent : -1, id = x0.id;
         const double u = x0.u, px = x0.px, qx = x0.qx;
-        uint64_t refused = 0;                                            // of this lot, at this node
+        uint64_t gone = 0;                                               // refused, of this lot, at this node
         uint64_t open = __ballot(t > s.last && t >= s.at && parent == (int32_t)s.last);
+        uint64_t before = 0;                                             // whose token was refused at this node in an earlier lot
+        if (!DRAWN && some && open) before = __ballot((open >> lane & 1u) && id >= 0 && refused.listed((uint32_t)id));
         while (open) {
             const uint32_t i = (uint32_t)__builtin_ctzll(open);
             const uint32_t x = lane_word((uint32_t)id, i);
@@ -113,12 +153,7 @@ __device__ __forceinline__ bool verify_walk(const VerifyArgs& a, uint32_t b, con
                 test = ux * qv * s.R;
             } else {
                 // a token refused here before has nothing left
-                bool again = (__ballot((uint32_t)id == x) & refused) != 0;
-                for (uint32_t e0 = 0; e0 < t0 && !again; e0 += 64) {
-                    const uint32_t e = e0 + lane;
-                    again = __ballot(e > s.last && d.parent(e) == (int32_t)s.last && (uint32_t)d.ids[e] == x) != 0;
-                }
-                if (again) w = 0.0;
+                if ((__ballot((uint32_t)id == x) & gone) | (before >> i & 1u)) w = 0.0;
                 test = ux * s.R;
             }
             open &= open - 1;
@@ -127,72 +162,42 @@ __device__ __forceinline__ bool verify_walk(const VerifyArgs& a, uint32_t b, con
                 if (write) a.accepted[(size_t)b * a.tokens + s.n] = (int32_t)s.last;
                 ++s.n;
                 s.C = 0.0; s.R = 1.0; s.stale = 0;
-                refused = 0;
+                gone = before = 0;
+                if (!DRAWN && some) {                                    // (once a lot at most)
+                    refused.template clear<64>(lane);
+                    in_order();
+                    some = false;
+                }
                 open = __ballot(t > s.last && parent == (int32_t)s.last);
             } else if ((int32_t)x >= 0) {
-                refused |= 1ull << i;
+                gone |= 1ull << i;
                 if (DRAWN) { s.C += s.R; s.stale = 1; }
                 else s.R = fmax(s.R - w, 0.0);
             }
+        }
+        if (!DRAWN && gone) {
+            if (gone >> lane & 1u) refused.add((uint32_t)id);
+            in_order();
+            some = true;
         }
     }
     s.at = d.drafted;
     return true;
 }
 
-// The children refused at the last token that stays, without q: their probabilities count for nothing.  Their numbers, and a filter of 2^15 bits by which
-// hardly any other token is compared with them.
-constexpr uint32_t FILTER = 1 << 15, LISTED = 256;
-struct Refused { uint32_t filter[FILTER / 32], ids[LISTED], n; };
-template <uint32_t THREADS>
-__device__ __forceinline__ void list_refused(Refused& r, const Drafts& d, const Lot& first, uint32_t last) {
-    const uint32_t lane = threadIdx.x & 63u;
-    for (uint32_t w = threadIdx.x; w < FILTER / 32; w += THREADS) r.filter[w] = 0;
-    __syncthreads();
-    if (threadIdx.x < 64) {
-        uint32_t count = 0;
-        for (uint32_t t0 = last & ~63u; t0 < d.drafted; t0 += 64) {
-            const uint32_t t = t0 + lane;
-            bool child = t > last && t < d.drafted;
-            child = child && (t0 ? d.parent(t) : first.parent) == (int32_t)last;
-            const uint32_t id = !child ? 0u : t0 ? (uint32_t)d.ids[t] : (uint32_t)first.id;
-            const uint64_t children = __ballot(child);
-            const uint32_t at = count + (uint32_t)__builtin_popcountll(children & ((1ull << lane) - 1));
-            if (child) atomicOr(&r.filter[id % FILTER / 32], 1u << (id % 32));
-            if (child && at < LISTED) r.ids[at] = id;
-            count += (uint32_t)__builtin_popcountll(children);
-        }
-        if (lane == 0) r.n = count;
-    }
-    __syncthreads();
-}
-__device__ __noinline__ bool is_refused(const Refused& r, const Drafts& d, uint32_t last, uint32_t v) {
-    if (r.n <= LISTED) {
-        for (uint32_t e = 0; e < r.n; ++e)
-            if (r.ids[e] == v) return true;
-    } else {
-        for (uint32_t t = last + 1; t < d.drafted; ++t)
-            if (d.parent(t) == (int32_t)last && (uint32_t)d.ids[t] == v) return true;
-    }
-    return false;
-}
-
 // The weight of a token in a row.
-template <bool DRAWN> struct Weights {
+template <bool DRAWN, class Set> struct Weights {
     const float *p, *q;
     double C;
-    const Refused& refused;
-    const Drafts& d;
-    uint32_t last;
+    const Set& refused;
     bool whole;                          // p as it is
-    __device__ __forceinline__ Weights(const VerifyArgs& a, const Drafts& drafts, const VerifyState& s, const Refused& r)
-        : p(drafts.p + (int64_t)s.last * a.p_token), q(DRAWN ? drafts.q + (int64_t)s.last * a.q_token : nullptr), C(s.C), refused(r), d(drafts), last(s.last), whole(false) {}
+    __device__ __forceinline__ Weights(const VerifyArgs& a, const Drafts& drafts, const VerifyState& s, const Set& r)
+        : p(drafts.p + (int64_t)s.last * a.p_token), q(DRAWN ? drafts.q + (int64_t)s.last * a.q_token : nullptr), C(s.C), refused(r), whole(false) {}
     __device__ __forceinline__ double of(uint32_t v, float pv, float qv) const {
         const double w = mass(pv);
         if (whole) return w;
         if (DRAWN) return fmax(w - C * mass(qv), 0.0);
-        if ((refused.filter[v % FILTER / 32] >> (v % 32) & 1u) && is_refused(refused, d, last, v)) return 0.0;
-        return w;
+        return refused.has(v) ? 0.0 : w;
     }
     // The sum over v, v + step, .. below `end`, eight numbers on their way at a time, also where fewer are left.
     __device__ __forceinline__ double sum(uint32_t v, uint32_t step, uint32_t end) const {
@@ -211,6 +216,11 @@ template <bool DRAWN> struct Weights {
         return x;
     }
 };
+
+// (the same in every lane: 12 us longer where the compiler was not told)
+__device__ __forceinline__ VerifyState uniform(const VerifyState& x) {
+    return {lane_value(x.C, 0), lane_value(x.R, 0), uni(x.last), uni(x.n), uni(x.at), uni(x.stale), uni(x.done)};
+}
 
 constexpr uint32_t VERIFY_WAVES = 16;
 
@@ -240,19 +250,35 @@ __device__ __forceinline__ uint32_t find_piece(double mine, double& before, doub
 // The rest of a sequence in one workgroup: the walk with its passes, and the next token.
 // Where the sum passes the target: a run is cut into 16 pieces, a wave sums each, and the piece that the target lies in is the next run, until that is short enough for registers.
 // piece_sum: of an earlier launch, of the row's pieces of `size` numbers, one a lane (size 0: there are none).
-template <bool DRAWN>
-__device__ __forceinline__ void verify_rest(const VerifyArgs& a, uint32_t b, const Drafts& d, const Lot& first, float u0, VerifyState& s, double piece_sum, uint32_t size, double* sums, Refused& refused) {
+// tokens: of this wave's lot of the first ones.
+template <bool DRAWN, class Set>
+__device__ __forceinline__ void verify_rest(const VerifyArgs& a, uint32_t b, const Drafts& d, const Lot& tokens, float u0, VerifyState& s, double piece_sum, uint32_t size, double* sums, VerifyState& come, Set& refused) {
     constexpr uint32_t SHORT = VERIFY_WAVES * 256;
     const uint32_t lane = threadIdx.x & 63u, wave = uni(threadIdx.x >> 6);
-    if (size == 0)
-        verify_walk<DRAWN>(a, b, d, lot_of<DRAWN>(a, b, d, 0, a.launches > 1), a.launches > 1, s, threadIdx.x == 0, [&](VerifyState& st) __attribute__((always_inline)) {
-            const Weights<DRAWN> weight(a, d, st, refused);
-            if constexpr (DRAWN) st.R = everywhere<VERIFY_WAVES>(weight.sum(threadIdx.x, 64 * VERIFY_WAVES, a.vocab), sums);
+    if (!DRAWN) {
+        refused.template clear<64 * VERIFY_WAVES>(threadIdx.x);
+        __syncthreads();
+        if (size) {
+            for (uint32_t t0 = wave * 64; t0 < d.drafted; t0 += 64 * VERIFY_WAVES) {
+                const Lot x = t0 == wave * 64 ? tokens : tokens_of(a, b, d, t0);
+                const uint32_t t = t0 + lane;
+                if (t > s.last && t < d.drafted && x.parent == (int32_t)s.last && (uint32_t)x.id < a.vocab) refused.add((uint32_t)x.id);
+            }
+        } else if (wave == 0) {
+            verify_walk<DRAWN>(a, b, d, lot_of<DRAWN>(a, b, d, 0, false), false, s, lane == 0, refused, [](VerifyState&) { return true; });
+            if (lane == 0) come = s;
+        }
+        __syncthreads();
+        if (size == 0) s = uniform(come);
+    } else if (size == 0) {
+        verify_walk<DRAWN>(a, b, d, lot_of<DRAWN>(a, b, d, 0, a.launches > 1), a.launches > 1, s, threadIdx.x == 0, refused, [&](VerifyState& st) __attribute__((always_inline)) {
+            const Weights<DRAWN, Set> weight(a, d, st, refused);
+            st.R = everywhere<VERIFY_WAVES>(weight.sum(threadIdx.x, 64 * VERIFY_WAVES, a.vocab), sums);
             return true;
         });
+    }
     if (threadIdx.x == 0) a.n_accepted[b] = (int32_t)s.n;
-    if (!DRAWN) list_refused<64 * VERIFY_WAVES>(refused, d, first, s.last);
-    Weights<DRAWN> weight(a, d, s, refused);
+    Weights<DRAWN, Set> weight(a, d, s, refused);
     uint32_t begin = 0, end = a.vocab;
     double before = 0.0, target = -1.0;                                  // the sum in front of the run
     const double u = unit(u0);
@@ -325,10 +351,11 @@ __device__ __forceinline__ void verify_rest(const VerifyArgs& a, uint32_t b, con
 }
 
 // One workgroup to a sequence.
-template <bool DRAWN>
+template <bool DRAWN, uint32_t LISTED>
 __global__ __launch_bounds__(64 * VERIFY_WAVES) void verify_drafts_kernel(const VerifyArgs a) {
     __shared__ double sums[VERIFY_WAVES];
-    __shared__ Refused refused;
+    __shared__ VerifyState come;
+    __shared__ __align__(16) Refused<LISTED> refused;
     const uint32_t b = blockIdx.x, lane = threadIdx.x & 63u;
     const Drafts d(a, b);
     VerifyState s = {0.0, 1.0, 0, 1, 1, 0, 0};
@@ -339,7 +366,7 @@ __global__ __launch_bounds__(64 * VERIFY_WAVES) void verify_drafts_kernel(const 
         for (uint32_t l = 0; l < VERIFY_LAUNCHES; ++l)
             if (l < a.launches && lane < a.pieces) found[l] = a.sums[((size_t)l * a.batch + b) * a.pieces + lane];
     }
-    const Lot first = tokens_of(a, b, d, 0);
+    const Lot tokens = tokens_of(a, b, d, uni(threadIdx.x >> 6) * 64);
     const float u0 = a.u[(size_t)b * a.tokens];
     if (d.drafted == 0) {
         if (threadIdx.x == 0) a.n_accepted[b] = 0;
@@ -352,18 +379,18 @@ __global__ __launch_bounds__(64 * VERIFY_WAVES) void verify_drafts_kernel(const 
         s.R = wave_sum(piece_sum);
         s.stale = 0;
     }
-    verify_rest<DRAWN>(a, b, d, first, u0, s, piece_sum, s.done ? a.piece : 0u, sums, refused);
+    verify_rest<DRAWN>(a, b, d, tokens, u0, s, piece_sum, s.done ? a.piece : 0u, sums, come, refused);
 }
 
 // A row over several workgroups: the first wave of each goes as far as it can without a pass (all of a sequence's do the same), each leaves the sum of its piece of the
 // row that it came to, and the next launch goes on from there.
 // Latency bounds it, some 5 us a launch: its loads wait for one another (state, tokens, their probabilities, the row), so as many as can go together do, and the gathered ones are kept (32
 // trees of 16 over 50000 tokens, on average over their inputs: 41 us before that, and 37).
-template <bool DRAWN>
+template <bool DRAWN, uint32_t LISTED>
 __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyArgs a) {
     __shared__ double sums[4];
     __shared__ VerifyState come;
-    __shared__ Refused refused;
+    __shared__ __align__(16) Refused<LISTED> refused;
     const uint32_t b = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces, wave = uni(threadIdx.x >> 6);
     VerifyState* const to = a.states + (size_t)a.launch * a.batch + b;
     VerifyState s = {0.0, 1.0, 0, 1, 1, 0, 0};
@@ -381,16 +408,20 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyArgs a) {
         return;
     }
     Lot first;
+    if (wave == 0) first = lot_of<DRAWN>(a, b, d, 0, a.launch > 0);
+    if (!DRAWN) {
+        refused.template clear<256>(threadIdx.x);
+        __syncthreads();
+    }
     if (wave == 0) {
         const uint32_t lane = threadIdx.x;
         double piece_sum = 0.0;
         if (a.launch && lane < a.pieces) piece_sum = a.sums[((size_t)(a.launch - 1) * a.batch + b) * a.pieces + lane];
-        first = lot_of<DRAWN>(a, b, d, 0, a.launch > 0);
         if (a.launch) {
             s.R = wave_sum(piece_sum);
             s.stale = 0;
         }
-        if (verify_walk<DRAWN>(a, b, d, first, a.launch > 0, s, piece == 0 && lane == 0, [](VerifyState&) { return false; })) s.done = a.launch + 1;
+        if (verify_walk<DRAWN>(a, b, d, first, a.launch > 0, s, piece == 0 && lane == 0, refused, [](VerifyState&) { return false; })) s.done = a.launch + 1;
         if (lane == 0) come = s;
     }
     if (DRAWN && a.launch == 0 && a.launches > 1)
@@ -400,9 +431,8 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyArgs a) {
             if (t < a.tokens) a.kept[(size_t)b * a.tokens + t] = VerifyToken{(float)x.px, (float)x.qx};
         }
     __syncthreads();
-    s = {lane_value(come.C, 0), lane_value(come.R, 0), uni(come.last), uni(come.n), uni(come.at), uni(come.stale), uni(come.done)};   // (the same in every lane: 12 us longer where the compiler was not told)
-    if (!DRAWN) list_refused<256>(refused, d, first, s.last);
-    const Weights<DRAWN> weight(a, d, s, refused);
+    s = uniform(come);
+    const Weights<DRAWN, Refused<LISTED>> weight(a, d, s, refused);
     double x = weight.sum(piece * a.piece + threadIdx.x, 256, min(a.vocab, (piece + 1) * a.piece));
     x = everywhere<4>(x, sums);
     if (threadIdx.x == 0) {
@@ -411,15 +441,18 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyArgs a) {
     }
 }
 
+template <bool DRAWN, uint32_t LISTED>
+hipError_t launch_verify_with(VerifyArgs a, hipStream_t stream) {
+    for (a.launch = 0; a.launch < a.launches; ++a.launch)
+        if (hipError_t e = launch_one(verify_sums_kernel<DRAWN, LISTED>, a.batch * a.pieces, 256, stream, a); e != hipSuccess) return e;
+    return launch_one(verify_drafts_kernel<DRAWN, LISTED>, a.batch, 64 * VERIFY_WAVES, stream, a);
+}
+
 }  // namespace
 
-hipError_t launch_verify_drafts(const VerifyArgs& args, hipStream_t stream) {
-    VerifyArgs a = args;
-    for (a.launch = 0; a.launch < a.launches; ++a.launch) {
-        const hipError_t e = a.q ? launch_one(verify_sums_kernel<true>, a.batch * a.pieces, 256, stream, a) : launch_one(verify_sums_kernel<false>, a.batch * a.pieces, 256, stream, a);
-        if (e != hipSuccess) return e;
-    }
-    return a.q ? launch_one(verify_drafts_kernel<true>, a.batch, 64 * VERIFY_WAVES, stream, a) : launch_one(verify_drafts_kernel<false>, a.batch, 64 * VERIFY_WAVES, stream, a);
+hipError_t launch_verify_drafts(const VerifyArgs& a, hipStream_t stream) {
+    if (a.q) return launch_verify_with<true, VERIFY_FEW>(a, stream);   // (which list nothing)
+    return a.tokens <= VERIFY_FEW ? launch_verify_with<false, VERIFY_FEW>(a, stream) : launch_verify_with<false, VERIFY_TOKENS>(a, stream);
 }
 
 }  // namespace depsync
