@@ -669,7 +669,8 @@ int dep_qk_norm_rope(const depsync_qk_norm_rope_desc* d, void* stream);
  * (where nothing is left: of p[n] likewise; where that is nothing either: -1).  With u from [0, 1) at random tokens that stay and the next one follow the target's
  * distribution.  Sums, products and comparisons have 64 bits.  Probabilities that are negative or not finite count as 0, u below 0 or NaN as 0 and above 1 as 1; a token whose
  * id is not in 0..vocab-1 never stays.  accepted[b] receives the tokens that stay, 0 first, and n_accepted[b] their number (entries behind it are left
- * alone): what the appends take.  A sequence with drafted[b] = 0 gets n_accepted 0, and its other outputs are left alone.                 */
+ * alone): what the appends take.  A sequence with drafted[b] = 0 gets n_accepted 0, and its other outputs are left alone.  No output is the array of
+ * another or of an input: drafted cannot be counted down in place (DEPSYNC_EINVAL).                                                          */
 typedef struct {
     int32_t batch, tokens, vocab;                       /* tokens: 1..4096 (up to 65536: DEPSYNC_ENOTIMPL), vocab: 1..2^24             */
     const float* p;    int64_t p_batch, p_token;        /* [batch][tokens][vocab], strides in numbers (those of dimensions of size 1 are not read) */

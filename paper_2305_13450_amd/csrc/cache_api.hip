@@ -5,6 +5,7 @@
 #include <atomic>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 
 #include "../../include/depsync.h"
 #include "cache_ops.h"
@@ -22,6 +23,12 @@ bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(
 bool operand(const void* p) { return p && aligned(p, 16); }
 bool array(const void* p) { return p && aligned(p, 4); }
 bool optional(const void* p) { return aligned(p, 4); }
+// Arrays that a call writes are neither one another nor any that it reads (some workgroups read while others write).
+bool apart(std::initializer_list<const void*> written, std::initializer_list<const void*> read) {
+    for (auto w = written.begin(); w != written.end(); ++w)
+        if (*w && (std::count(written.begin(), w, *w) || std::count(read.begin(), read.end(), *w))) return false;
+    return true;
+}
 int64_t cdiv64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Strides of [batch][token][head][head_dim].  Those of dimensions of size one are not read: kernels get what a dense row has.
@@ -425,7 +432,7 @@ int dep_verify_drafts(const depsync_verify_drafts_desc* d, void* workspace, size
     if (int rc = depsync_verify_drafts_workspace(d, &need); rc != DEPSYNC_OK) return rc;
     VerifyArgs a = {};
     if (!array(d->p) || !optional(d->q) || !array(d->ids) || !optional(d->parents) || !optional(d->drafted) || !array(d->u) || !array(d->accepted) ||
-        !array(d->n_accepted) || !array(d->next) || d->n_accepted == d->next || (d->parents && d->parents_batch != 0 && d->parents_batch < d->tokens))
+        !array(d->n_accepted) || !array(d->next) || !apart({d->accepted, d->n_accepted, d->next}, {d->p, d->q, d->ids, d->parents, d->drafted, d->u}) || (d->parents && d->parents_batch != 0 && d->parents_batch < d->tokens))
         return DEPSYNC_EINVAL;
     if (!rows(a.p_batch, a.p_token, d->p_batch, d->p_token, d) || (d->q && !rows(a.q_batch, a.q_token, d->q_batch, d->q_token, d))) return DEPSYNC_EINVAL;
     if (need > 0 && (!operand(workspace) || workspace_bytes < need)) return DEPSYNC_EINVAL;

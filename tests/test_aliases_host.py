@@ -1,0 +1,30 @@
+"""CPU tests that arrays which a call writes while it reads others may not be those others: refused before anything reaches a device."""
+import ctypes
+
+import pytest
+
+import paper_2305_13450_amd as ds
+from test_draft_ops_host import BAD, verify
+
+P = 0x10000          # aligned addresses that nothing reads are its multiples
+
+
+def call(name, d):
+    f = getattr(ds._lib(), name)
+    return f(ctypes.byref(d), P, 1 << 40, None) if name == "dep_verify_drafts" else f(ctypes.byref(d), None)
+
+
+def verify_apart(**kw):
+    return verify(**{**dict(p=P, q=2 * P, ids=3 * P, parents=4 * P, drafted=5 * P, u=6 * P, accepted=7 * P, n_accepted=8 * P, next=9 * P, q_batch=8000, q_token=1000), **kw})
+
+
+@pytest.mark.parametrize("written", ["accepted", "n_accepted", "next"])
+def test_verification_writes_arrays_of_its_own(written):
+    for other in ("p", "q", "ids", "parents", "drafted", "u", "accepted", "n_accepted", "next"):
+        if other != written:
+            assert call("dep_verify_drafts", verify_apart(**{written: getattr(verify_apart(), other)})) == ds.EINVAL, other
+
+
+def test_refusals_of_verification_with_arrays_apart():
+    for kw in BAD["dep_verify_drafts"][1]:
+        assert call("dep_verify_drafts", verify_apart(**kw)) == ds.EINVAL, kw
