@@ -631,7 +631,7 @@ typedef struct {
     void* k_cache; void* v_cache; int64_t cache_batch, cache_token, cache_head;
     float* k_scale; float* v_scale;
     void* k_tail; void* v_tail; int64_t tail_batch, tail_token, tail_head;
-    const int32_t* cached;  int32_t* cached_out;        /* [batch]; not the same array                                             */
+    const int32_t* cached;  int32_t* cached_out;        /* [batch]; cached_out is none of the arrays read, nor is n_out             */
     const int32_t* accepted; const int32_t* n_accepted; /* as for dep_cache_append                                                 */
     int32_t* n_out;                                     /* as for dep_cache_append; may be NULL                                    */
 } depsync_cache_append8_desc;

@@ -4,7 +4,7 @@ import ctypes
 import pytest
 
 import paper_2305_13450_amd as ds
-from test_draft_ops_host import BAD, verify
+from test_draft_ops_host import BAD, append8, verify
 
 P = 0x10000          # aligned addresses that nothing reads are its multiples
 
@@ -28,3 +28,11 @@ def test_verification_writes_arrays_of_its_own(written):
 def test_refusals_of_verification_with_arrays_apart():
     for kw in BAD["dep_verify_drafts"][1]:
         assert call("dep_verify_drafts", verify_apart(**kw)) == ds.EINVAL, kw
+
+
+@pytest.mark.parametrize("written", ["cached_out", "n_out"])
+def test_the_append_to_8_bits_writes_lengths_of_its_own(written):
+    apart = dict(cached=P, cached_out=2 * P, accepted=3 * P, n_accepted=4 * P, n_out=5 * P)
+    for other in apart:
+        if other != written:
+            assert call("dep_cache_append8", append8(**{**apart, written: apart[other]})) == ds.EINVAL, other
