@@ -540,7 +540,7 @@ typedef struct {
     int32_t n_max;                                      /* entries of `accepted` per sequence (without it: 0..tokens, the first n are taken) */
     const void* k_new; const void* v_new; int64_t new_batch, new_token, new_head;
     void* k_cache; void* v_cache; int64_t cache_batch, cache_token, cache_head;
-    const int32_t* cached;  int32_t* cached_out;        /* [batch]; not the same array                                             */
+    const int32_t* cached;  int32_t* cached_out;        /* [batch]; no array written is another or one that is read                */
     const int32_t* accepted;                            /* [batch][n_max], clamped to 0..tokens-1; NULL: token i                    */
     const int32_t* n_accepted;                          /* [batch], clamped to 0..n_max; NULL: n_max                                */
     float* weights; int32_t* pos;                       /* [batch][kv_heads][capacity]; either may be NULL                          */

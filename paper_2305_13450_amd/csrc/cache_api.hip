@@ -243,10 +243,9 @@ int dep_cache_append(const depsync_cache_append_desc* d, void* stream) {
     const int D = d->head_dim;
     if (d->capacity < 1 || d->n_max < 1 || d->n_max > 65536 || (!d->accepted && d->n_max > d->tokens)) return DEPSYNC_EINVAL;
     if (!operand(d->k_new) || !operand(d->v_new) || !operand(d->k_cache) || !operand(d->v_cache) || !array(d->cached) || !array(d->cached_out) ||
-        d->cached == d->cached_out || !optional(d->accepted) || !optional(d->n_accepted) || !optional(d->weights) || !optional(d->pos) ||
-        (d->pos && !array(d->start)) || !optional(d->n_out))
+        !optional(d->accepted) || !optional(d->n_accepted) || !optional(d->weights) || !optional(d->pos) || (d->pos && !array(d->start)) || !optional(d->n_out) ||
+        !apart({d->cached_out, d->n_out, d->weights, d->pos}, {d->cached, d->accepted, d->n_accepted, d->pos ? d->start : nullptr}))
         return DEPSYNC_EINVAL;
-    if (d->n_out && (d->n_out == d->cached || d->n_out == d->cached_out || d->n_out == d->n_accepted)) return DEPSYNC_EINVAL;
     if (!strides(a.new_s, d->new_batch, d->new_token, d->new_head, d->batch, d->tokens, d->kv_heads, D, false, false) ||
         !strides(a.cache_s, d->cache_batch, d->cache_token, d->cache_head, d->batch, d->capacity, d->kv_heads, D, true, true))
         return DEPSYNC_EINVAL;

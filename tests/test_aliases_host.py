@@ -4,6 +4,7 @@ import ctypes
 import pytest
 
 import paper_2305_13450_amd as ds
+from test_cache_ops_host import append
 from test_draft_ops_host import BAD, append8, verify
 
 P = 0x10000          # aligned addresses that nothing reads are its multiples
@@ -36,3 +37,11 @@ def test_the_append_to_8_bits_writes_lengths_of_its_own(written):
     for other in apart:
         if other != written:
             assert call("dep_cache_append8", append8(**{**apart, written: apart[other]})) == ds.EINVAL, other
+
+
+@pytest.mark.parametrize("written", ["cached_out", "n_out", "weights", "pos"])
+def test_the_append_writes_arrays_of_its_own(written):
+    apart = dict(cached=P, cached_out=2 * P, accepted=3 * P, n_accepted=4 * P, n_out=5 * P, start=6 * P, weights=7 * P, pos=8 * P)
+    for other in apart:
+        if other != written:
+            assert call("dep_cache_append", append(**{**apart, written: apart[other]})) == ds.EINVAL, other
