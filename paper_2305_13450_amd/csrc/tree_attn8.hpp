@@ -200,7 +200,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
     }
     const float sc = a.scale;
     // Weights of a tile's scores, times its V scale, as two fragments of products with values of U, which hold twice the bits of one.  The scale goes into the exponent, and
-    // the sum is divided by it again (both off by the same rounding); but a scale so small that weights would fall out of 32 bits is multiplied afterwards.
+    // the sum is divided by it again (both off by the same rounding); but a scale so small or large that weights or their sum would fall out of 32 bits is multiplied afterwards.
     auto weigh = [&](f32x4 (&st)[2], int r, float by, float vs, auto held, auto& high, auto& rest) __attribute__((always_inline)) {
         using U = std::conditional_t<std::is_same_v<std::remove_reference_t<decltype(high)>, B8>, __bf16, _Float16>;
         constexpr bool HELD = decltype(held)::value;                   // a tile of 8 bits: with a scale, and without infinities
@@ -218,9 +218,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
                 for (int v = 0; v < 4; ++v) o[r][b][v] *= alpha;
         }
         float ref = (m[r] == -INFINITY ? 0.0f : m[r]) - WEIGHT_OFF<T>;   // no key seen yet: keep the exponents finite
-        const bool small = HELD && uni(vs < 0x1p-60f ? 1u : 0u);
+        const bool far = HELD && uni(vs < 0x1p-60f || vs > 0x1p60f ? 1u : 0u);
         float back = 1.0f;
-        if (HELD && !small) {
+        if (HELD && !far) {
             back = __builtin_amdgcn_rcpf(vs);
             ref += __builtin_amdgcn_logf(back);
         }
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
             sum[v & 1] += p[v];
         }
         l[r] = __builtin_fmaf(sum[0] + sum[1], back, l[r]);
-        if (__builtin_expect(small, 0))
+        if (__builtin_expect(far, 0))
 #pragma unroll
             for (int v = 0; v < 8; ++v) p[v] *= vs;
 #pragma unroll
