@@ -55,6 +55,12 @@ template <typename T> __device__ __forceinline__ typename Mma<T>::V8 eight(uint3
 typedef const __attribute__((address_space(4))) float* Scales;
 __device__ __forceinline__ Scales scales_at(const float* p, size_t at) { return (Scales)(uint64_t)uni_ptr(p + at); }
 
+// a / b, of scales.  (The inverse of one beyond 2^126 is no normal number, and would come out as 0.)
+__device__ __forceinline__ float quotient(float a, float b) {
+    const float k = b > 0x1p64f ? 0x1p-64f : 1.0f;
+    return a * k * __builtin_amdgcn_rcpf(b * k);
+}
+
 // 16 x 16 outputs, 32 products each.
 __device__ __forceinline__ f32x4 mma16(Mma<__bf16>::V8 a, Mma<__bf16>::V8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mma16(Mma<_Float16>::V8 a, Mma<_Float16>::V8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -610,10 +616,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
             of = uni(__builtin_bit_cast(uint32_t, vs));
             const float u = wide ? fmaxf(1.0f, most * 0x1p-60f) : vs;
             larger = uni((wide ? u != most : u > most) ? 1u : 0u);
-            const float inverse = __builtin_amdgcn_rcpf(vs);
-            if (larger) { unit = most * __builtin_amdgcn_rcpf(u); most = u; }
+            if (larger) { unit = quotient(most, u); most = u; }
             none = uni(!wide && (vs < 0x1p-126f || vs < most * 0x1p-60f) ? 1u : 0u);
-            back = none ? 1.0f : most * inverse;                       // (off by the reciprocal's rounding, as off then is)
+            back = none ? 1.0f : quotient(most, vs);                     // (off by the reciprocal's rounding, as off then is)
             off = none ? 0.0f : -__builtin_amdgcn_logf(back);
         }
         const float by = sc * ks, mx = max_halves(top) * by;

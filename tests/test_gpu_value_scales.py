@@ -39,7 +39,7 @@ def check(q, kn, vn, cache, cached):
 SHAPES = pytest.mark.parametrize("T,Hq,Hk,D,block", [(1, 4, 2, 128, 64), (9, 4, 2, 64, 32), (90, 4, 1, 128, 32), (40, 6, 2, 64, 64)])
 
 
-@pytest.mark.parametrize("T,Hq,Hk,D,block", [(1, 4, 2, 128, 64), (9, 4, 2, 64, 32)])
+@SHAPES
 def test_scales_up_to_the_largest_finite_one(T, Hq, Hk, D, block):
     # all weights alike, and numbers so small that their sums fit 32 bits
     g = gen(98)
