@@ -600,16 +600,16 @@ int depsync_cache_evict_workspace(const depsync_cache_evict_desc* d, size_t* byt
  *
  * A cache of 8 bits: rows come in blocks of `block` (32, 64 or 128) tokens.  The rows of a sequence's full blocks, the first cached - cached % block,
  * are 8-bit floating point numbers (e4m3: sign, 4 bits of exponent, 3 of mantissa, no infinities, largest 448) [batch][capacity][kv_heads][head_dim],
- * each block and head with a scale: k_scale, v_scale [batch][kv_heads][capacity / block], not negative; a row's value is scale times its number.
+ * each block and head with a scale: k_scale, v_scale [batch][kv_heads][capacity / block], finite and not negative; a row's value is scale times its number.
  * The rows behind them, cached % block of them, are held in 16 bits until they fill a block: k_tail, v_tail [batch][block][kv_heads][head_dim], the
  * first cached % block rows.  So every row is rounded to 8 bits once, with its block's own scale, whichever way appends were divided.
  * capacity is a positive multiple of block.  The strides of the 8-bit arrays are multiples of 16, bases 16-byte aligned.                            */
 
 /* out as dep_tree_attn's, over the rows of such a cache and the drafted tokens: scores and outputs go by the rows' values, in 32 bits.  In `attn`, k_cache and
  * v_cache are the 8-bit numbers; max_cached 0 means capacity.  Rows of the last block that is not full and drafted tokens may hold infinities and NaN as
- * there.  For the product with v weights are two 16-bit numbers each up to 64 query rows to a key and value head, and one beyond, of the element type for rows of 16 bits
- * and fp16 for those of 8, which carry their block's scale, relative to the largest that the part has met: what falls out of fp16's range then is below 2^-33
- * of the largest value.                                                                                                                  */
+ * there.  For the product with v weights are two 16-bit numbers each up to 64 query rows to a key and value head, and one beyond: of the element type for rows of 16 bits
+ * (in bf16 a prompt's outputs are 2.1e-3 of their norm from 64 bits, 1.7e-3 with weights of 32 bits), and fp16 for those of 8, which carry their block's scale. There weights below
+ * 2^-25 of the row's largest, and blocks whose v_scale is below 2^-60 of another's, may count for nothing.                                  */
 typedef struct {
     depsync_tree_attn_desc attn;
     int32_t block;

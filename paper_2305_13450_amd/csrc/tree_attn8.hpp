@@ -430,8 +430,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_few(const TreeAttn8Args a) 
 // as near to 64 bits as with 32-bit weights (4 x 256 tokens in bf16: 1.7e-3 of their norm, the output's own rounding; 2.1e-3 with bf16 weights), in the same
 // time.  Tiles of 16 bits keep to T.
 //
-// A weight carries its block's V scale, relative to the largest that the part has met so far (`most`; outputs are in units of it, and are scaled when it grows,
-// which random scales do a few times), so that fp16 weights stay in range: the scale goes into the exponent, and the sum is divided by it again.
+// A weight carries its block's V scale, relative to one that the part has met (`most`; outputs are in units of it, and are scaled when it changes), so that fp16 weights
+// stay in range: the scale goes into the exponent, and the sum is divided by it again.  `most` follows where a block's scale is larger, or less than 2^-8 of it, which random scales
+// come to a few times.  (With the largest one kept as the unit, a row that saw blocks of small values alone had weights of few bits: a V scale of 2^-29 of it left 4.)
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a) {
     using Tile = KeyTile<T, D>;
@@ -579,7 +580,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
     };
     float top = largest(st[0]);                                        // of this lane's scores of the tile to be weighed
     // Scales of the tile to be weighed, read from LDS while the one before is.
-    float ks, vs, most = 0.0f;
+    float ks, vs, most = 0.0f, peak = 0.0f;                             // (the unit, and the largest V scale so far)
     auto scales_of = [&](uint32_t slot) __attribute__((always_inline)) {
         const u32x2 x = *(const u32x2*)tile_scales[slot & 3u];
         const uint32_t k = x[0], v = x[1];
@@ -587,9 +588,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
         vs = __builtin_bit_cast(float, v);
     };
     scales_of(0);
-    // Of the V scale `of` (its bits): the logarithm of what it is of `most`, and the inverse.  What is below 2^-60 of that counts for nothing: fp16
-    // weights would be zeros, and a sum in 32 bits could not be divided.
-    // Rows of 16 bits have no scale that says how large they are, so `most` is 1 for them (2^-60 of what it was if that is more, so that outputs so far stay in 32 bits).
+    // Of the V scale `of` (its bits): the logarithm of what it is of `most`, and the inverse.  What is below 2^-60 of the largest counts for nothing, so outputs stay in 32 bits
+    // in whatever unit.
+    // Rows of 16 bits have no scale that says how large they are, so `most` is 1 for them (2^-60 of the largest if that is more, for the same reason).
     uint32_t of = ~0u, none = 0;
     float off = 0.0f, back = 1.0f;
     // Weights of the tile whose scores are in `sx`, into `px`; scores of the next tile (in slot `next`) into `sy`, and their largest; output of the
@@ -611,13 +612,14 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
             top = largest(sx);
         }
         float alpha = 1.0f, unit = 1.0f;
-        uint32_t larger = 0;
+        uint32_t moved = 0;
         if (uni(__builtin_bit_cast(uint32_t, vs)) != of) {             // (once a block)
             of = uni(__builtin_bit_cast(uint32_t, vs));
-            const float u = wide ? fmaxf(1.0f, most * 0x1p-60f) : vs;
-            larger = uni((wide ? u != most : u > most) ? 1u : 0u);
-            if (larger) { unit = quotient(most, u); most = u; }
-            none = uni(!wide && (vs < 0x1p-126f || vs < most * 0x1p-60f) ? 1u : 0u);
+            if (!wide) peak = fmaxf(peak, vs);
+            const float u = wide ? fmaxf(1.0f, peak * 0x1p-60f) : vs;
+            none = uni(!wide && (vs < 0x1p-126f || vs < peak * 0x1p-60f) ? 1u : 0u);
+            moved = uni((wide ? u != most : !none && (u > most || u < most * 0x1p-8f)) ? 1u : 0u);
+            if (moved) { unit = quotient(most, u); most = u; }
             back = none ? 1.0f : quotient(most, vs);                     // (off by the reciprocal's rounding, as off then is)
             off = none ? 0.0f : -__builtin_amdgcn_logf(back);
         }
@@ -665,7 +667,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn8_many(const TreeAttn8Args a)
         row.l = __builtin_fmaf(sum[0] + sum[1], back, row.l);
         top = fmaxf(m0, m1);
         if (__builtin_expect(none, 0)) px[0] = px[1] = u32x4{0, 0, 0, 0};
-        if (grown || larger) {                                         // what was added so far went by the reference value and unit before
+        if (grown || moved) {                                          // what was added so far went by the reference value and unit before
             alpha *= unit;
 #pragma unroll
             for (int b = 0; b < NB; ++b)

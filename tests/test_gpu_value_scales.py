@@ -36,6 +36,29 @@ def check(q, kn, vn, cache, cached):
     assert float(over.max()) <= 1.0, f"{float(over.max()):.3f} of the tolerance"
 
 
+# Query rows look either at blocks with large values or at blocks with small ones: scores of the others are e^-70 and less of theirs.  up to 64 rows to a head,
+# and more; the latter's weights are fp16 numbers
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("order", ["LS", "SL", "LSL", "SLS", "LLSSLS", "SSSSLLLL"])
+@pytest.mark.parametrize("T,Hq,Hk,D,block", [(2, 4, 2, 128, 32), (20, 4, 2, 64, 32), (90, 4, 1, 128, 32), (40, 6, 2, 64, 64), (80, 2, 1, 128, 128)])
+def test_rows_that_see_small_values_alone_are_as_good(T, Hq, Hk, D, block, order, dtype):
+    print("small values", T, Hq, Hk, D, block, order, dtype, flush=True)
+    g = gen(97)
+    n = len(order) * block
+    large, small = (2.0 ** 10, 2.0 ** -20) if dtype == BF else (2.0 ** 7, 2.0 ** -22)
+    q, kn, vn = normal(g, (2, T, Hq, D), dtype, 0.1), normal(g, (2, T, Hk, D), dtype, 0.1), normal(g, (2, T, Hk, D), dtype)
+    q[..., 0] = torch.where(torch.arange(T, device="cuda") % 2 == 0, 16.0, -16.0)[None, :, None].to(dtype)
+    kn[..., 0] = 0.0
+    k, v = ((8 * torch.randn((2, n, Hk, D), generator=g, device="cuda")).to(E4M3).float() for _ in range(2))
+    v = 224 + 224 * torch.rand(v.shape, generator=g, device="cuda")
+    ks, vs = torch.full((2, Hk, len(order)), 2.0 ** -4, device="cuda"), torch.zeros((2, Hk, len(order)), device="cuda")
+    for i, c in enumerate(order):
+        k[:, i * block: (i + 1) * block, :, 0] = 448.0 if c == "L" else -448.0
+        vs[:, :, i] = large if c == "L" else small
+    tails = torch.zeros((2, block, Hk, D), dtype=dtype, device="cuda")
+    check(q, kn, vn, (k.to(E4M3), v.to(E4M3), ks, vs, tails, tails.clone()), ints([n, n]))
+
+
 SHAPES = pytest.mark.parametrize("T,Hq,Hk,D,block", [(1, 4, 2, 128, 64), (9, 4, 2, 64, 32), (90, 4, 1, 128, 32), (40, 6, 2, 64, 64)])
 
 
