@@ -1008,14 +1008,14 @@ def dep_cache_append8(k_new, v_new, k_cache, v_cache, k_scale, v_scale, k_tail, 
 
 
 def rope_frequencies(angles, device=None):
-    """The `freq` of dep_qk_norm_rope for rotations by angles[i] radians a position (a float64 tensor or list, in host memory or not): int64 [len], turns as
-    fractions of 2^64.  On `device`, by default that of the angles."""
+    """The `freq` of dep_qk_norm_rope for rotations by angles[i] radians a position (a float64 tensor or list of numbers below 2^100 in magnitude, in host memory or not): int64 [len],
+    turns as fractions of 2^64.  On `device`, by default that of the angles.  Worked out exactly on the host, once for a model: angles in device memory are waited for."""
     from fractions import Fraction
     torch = _torch()
     t = torch.as_tensor(angles, dtype=torch.float64)
-    if t.dim() != 1 or not bool(t.isfinite().all()):
-        raise ValueError("angles must be one finite number for each pair")
-    turn = Fraction(2 * 314159265358979323846264338327950288419716939937510, 10 ** 50)   # 2 pi to 50 places
+    if t.dim() != 1 or not bool((t.abs() < 2.0 ** 100).all()):
+        raise ValueError("angles must be one finite number below 2^100 for each pair")
+    turn = Fraction(2 * 314159265358979323846264338327950288419716939937510, 10 ** 50)   # 2 pi to 50 places: a turn is off by 2^-66 at most
     words = [round(Fraction(x) / turn * 2 ** 64) % 2 ** 64 for x in t.tolist()]
     return torch.tensor([w - 2 ** 64 if w >> 63 else w for w in words], dtype=torch.int64, device=t.device if device is None else device)
 
