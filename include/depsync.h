@@ -608,8 +608,8 @@ int depsync_cache_evict_workspace(const depsync_cache_evict_desc* d, size_t* byt
 /* out as dep_tree_attn's, over the rows of such a cache and the drafted tokens: scores and outputs go by the rows' values, in 32 bits.  In `attn`, k_cache and
  * v_cache are the 8-bit numbers; max_cached 0 means capacity.  Rows of the last block that is not full and drafted tokens may hold infinities and NaN as
  * there.  For the product with v weights are two 16-bit numbers each up to 64 query rows to a key and value head, and one beyond: of the element type for rows of 16 bits
- * (in bf16 a prompt's outputs are 2.1e-3 of their norm from 64 bits, 1.7e-3 with weights of 32 bits), and fp16 for those of 8, which carry their block's scale. There weights below
- * 2^-25 of the row's largest, and blocks whose v_scale is below 2^-60 of another's, may count for nothing.                                  */
+ * (a prompt's outputs in bf16, with nothing cached, are 2.1e-3 of their norm from 64 bits, 1.6e-3 with weights of 32 bits), and fp16 for those of 8, which carry their block's
+ * scale. There weights below 2^-25 of the row's largest, and blocks whose v_scale is below 2^-60 of another's, may count for nothing.         */
 typedef struct {
     depsync_tree_attn_desc attn;
     int32_t block;

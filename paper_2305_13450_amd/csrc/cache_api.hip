@@ -140,6 +140,10 @@ int tree_plan(const depsync_tree_attn_desc* d, int n_cu, TreeAttnArgs& a, size_t
     // heads, 66 MB, 21 and 30; 32 x 40 over 1000, 131 MB, 38 and 35; 64 x 64 over 1000, 262 MB, 73 and 63; 64 x 40 over 4000, 1 GB, 223 and 201; 52 rows of one
     // head of 64 over 120000, 73 and 62.  Between 100 and 270 MB it depends on how many sequences share them: 8 x 48 over 8000 67 and 64, but 16 x 64
     // over 4000 64 and 68, 4 x 52 over 8000 40 and 42, 16 x 40 over 2000 36 and 49.
+    // Over a cache of 8 bits the form for few rows is ahead up to 64 rows at all sizes but one of 30 measured: its tiles are converted in each of two workgroups of 32 rows, but in
+    // step with what HBM brings, and those of one of 128 rows behind barriers.  In us: 64 x 64 rows over 4000 keys of 8 heads, 524 MB, 147 and 169 us; 32 x 64 over 4000,
+    // 262 MB, 76 and 96; 64 x 40 over 1000, 131 MB, 51 and 54; 52 rows of 8 heads of 64 over 120001 51 and 62; 16 x 33 over 2000 27 and 38; many short sequences last: 128 x 48 over
+    // 500 67 and 71, 256 x 64 over 300 (4 heads) 57 and 54.
     const int64_t cache_bytes = (int64_t)d->batch * d->kv_heads * rows_hint(d->max_cached, d->capacity) * d->head_dim * 4;
     a.few = rows <= (held || cache_bytes < 100000000 ? 64 : 32);
     const int64_t keys = a.few ? TREE_FEW_KEYS : TREE_MANY_KEYS, row_blocks = cdiv64(rows, a.few ? TREE_FEW_ROWS : TREE_MANY_ROWS);
